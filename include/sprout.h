@@ -296,6 +296,205 @@ typedef struct {
 spr_status spr_serve(spr_model* m, int32_t n, const spr_request* reqs, int32_t max_active, int32_t eos_id,
                      int32_t* tok, int32_t* out, int32_t* lengths, spr_serve_stats* stats);
 
+/* ---------------------------------------------------------------------------
+ * Speculative decoding: several drafted tokens of a request are run through
+ * the model in one pass, the ones that the target model's distribution
+ * accepts are kept, and the rest leave no trace.  The loop is Section II-A's;
+ * the accepted tokens are distributed as its own (equal to them where greedy).
+ *
+ * A request's drafted tokens form a tree of n_nodes nodes.  Node 0, the root,
+ * is the request's last token (not yet cached); node j > 0 is a drafted token
+ * that continues node parents[j] < j.  Node j's keys and values sit at cache
+ * position len + j while the tree is open, whatever its depth; its rotary
+ * position is len + depth(j).  Calls take the nodes of all requests as token
+ * rows, request after request.
+ *
+ * The three operators (spr_tree_attention, spr_tree_verify, spr_tree_keep)
+ * run on caller-owned tensors through an operator handle; spr_tree_step runs
+ * them inside a whole model pass.
+ * ------------------------------------------------------------------------ */
+
+#define SPR_MAX_TREE_REQUESTS 64 /* requests of one call */
+#define SPR_MAX_TREE_NODES 64    /* nodes of one request's tree */
+#define SPR_MAX_TREE_ROWS 128    /* nodes of one call, over all requests */
+
+/*
+ * A paged KV cache.  Block b of layer l holds 16 positions of every KV head:
+ * n_kv_heads tiles of 16 * head_dim elements from element
+ * ((l * n_blocks + b) * n_kv_heads) * 16 * head_dim of k and of v.  Position t
+ * of request i is position t % 16 of block block_table[slots[i]][t / 16].
+ * With P = 16 / element size, element (t, d) of a tile (position t < 16,
+ * dimension d) is at
+ *   keys:   ((d / 4P) * 64 + (d % 4P) / P * 16 + t) * P + d % P
+ *   values: fp32  (((d / 16) * 4 + t / 4) * 16 + d % 16) * 4 + t % 4
+ *           bf16  ((((d / 32) * 4 + t / 4) * 16 + d % 16) * 2 + (d / 16) % 2) * 4 + t % 4
+ * (keys as the matrix unit's operand of K q^T, values of V^T p).
+ * Constraints: head_dim 64 or 128; n_kv_heads 1..512; n_layers, n_blocks,
+ * n_slots, max_blocks >= 1; k and v 16-byte aligned.  A block id outside
+ * [0, n_blocks) that a call meets in the table is read as block 0 and fails
+ * the handle's next call (SPR_ERR_DEVICE_CHECK); spr_tree_keep then moves
+ * nothing for that request and layer.
+ */
+typedef struct {
+  void* k; /* device */
+  void* v; /* device */
+  int32_t kv_dtype; /* spr_dtype */
+  int32_t n_layers, n_blocks, n_kv_heads, head_dim;
+  const int32_t* block_table; /* device [n_slots][max_blocks] */
+  int32_t n_slots, max_blocks;
+} spr_kv_view;
+
+/*
+ * The drafted trees of one call (host memory, read during the call).
+ *   n        1..SPR_MAX_TREE_REQUESTS
+ *   slots    [n]: distinct rows of the block table
+ *   lens     [n]: cached positions before the tree, 0..2^30
+ *   n_nodes  [n]: 1..SPR_MAX_TREE_NODES each, at most SPR_MAX_TREE_ROWS in all
+ *   parents  [sum(n_nodes)]: -1 for each root (its first entry), else in
+ *            [0, j) for node j
+ * spr_tree_verify does not read slots and lens, which may then be NULL.
+ */
+typedef struct {
+  int32_t n;
+  const int32_t *slots, *lens, *n_nodes, *parents;
+} spr_tree_batch;
+
+typedef struct spr_tree_ops spr_tree_ops; /* opaque, library-owned host state */
+
+/* Device bytes the caller must provide to spr_tree_ops_init. */
+size_t spr_tree_ops_workspace_bytes(void);
+
+/*
+ * Creates an operator handle on the current device, in the caller's device
+ * workspace (256-byte aligned, kept alive until the release) and on the given
+ * HIP stream.  The library allocates no device memory of its own.  The
+ * conventions at the top of this file hold, with the handle in the model's
+ * place: status codes, sticky HIP errors, device checks (a block id or a
+ * drafted token out of range, a logits row with a NaN or no finite maximum,
+ * a malformed path), and one thread at a time.  Operators enqueue kernels
+ * only and may be captured into a graph; a captured call keeps the host
+ * arguments it was given.  Calls of one handle share its workspace: run its
+ * graphs and its eager calls one after the other, and give concurrent streams
+ * a handle each.  Calls may come while another device is current.
+ */
+spr_status spr_tree_ops_init(void* dev_ws, size_t ws_bytes, void* hip_stream, spr_tree_ops** out);
+
+/*
+ * Later calls enqueue on hip_stream.  The caller orders it after the work that
+ * the handle's earlier calls put on another stream.
+ */
+spr_status spr_tree_ops_set_stream(spr_tree_ops* ops, void* hip_stream);
+
+/* Releases the host state.  The workspace is the caller's to free afterwards. */
+spr_status spr_tree_ops_release(spr_tree_ops* ops);
+
+/*
+ * Attention of drafted trees over the cache, for layer `layer` of the view:
+ * row r = (request i, node j) and head h attend to positions 0..lens[i]-1 and
+ * to positions lens[i] + a for a = j and every ancestor a of j,
+ *   out[r][h] = softmax(q[r][h] . K^T / sqrt(head_dim)) V
+ * (head h reads KV head h / (n_heads / n_kv_heads)).  The nodes' keys and
+ * values are in the cache already.  One-node trees are ordinary decode
+ * attention.  What lies in the cache behind a request's nodes, or at nodes
+ * that a row does not see, does not reach its output, whatever it holds.
+ *   n_heads    a multiple of n_kv_heads, n_heads / n_kv_heads <= 16
+ *   io_dtype   of q and out; scores, sums and products are held in fp32
+ *   q          device [rows] x [n_heads * head_dim], row r at q + r * q_stride
+ *              elements; out likewise.  16-byte aligned, strides a multiple of
+ *              16 bytes and >= n_heads * head_dim.  out must not overlap q.
+ * SPR_ERR_INVALID_ARG also where lens[i] + n_nodes[i] exceeds max_blocks * 16.
+ */
+spr_status spr_tree_attention(spr_tree_ops* ops, const spr_kv_view* kv, int32_t layer, const spr_tree_batch* batch,
+                              int32_t n_heads, int32_t io_dtype, const void* q, int64_t q_stride, void* out,
+                              int64_t out_stride);
+
+/*
+ * Verification of drafted tokens against the target's distribution, from the
+ * caller's random numbers (speculative sampling).  logits row r = (request i,
+ * node u) are the target's logits after node u; p = softmax(logits / T), T the
+ * request's temperature.  From the root on, the children x_1, x_2, ... of the
+ * node reached are tried in node order, with r_0 = p:
+ *   child x_k is accepted, and becomes the node reached, if
+ *     accept[its row] * q(x_k) < r_{k-1}(x_k);
+ *   else r_k = max(r_{k-1} - q, 0) / sum.
+ * q is the node's row of draft_probs (the distribution its children were drawn
+ * from; entries that are negative or NaN count as 0) or, with draft_probs
+ * NULL, a point mass at x_k.  Where no child is left, the next token is the
+ * lowest t whose cumulative weight sum_{s <= t} r(s) exceeds
+ * sample[i] * sum r (the last t of positive weight if none does), and the walk
+ * ends; a node all of whose r is gone (possible only where draft_probs do not
+ * sum to 1) draws from p.  T = 0 is greedy: a child is accepted if it is the
+ * row's argmax (lowest index on ties), and the argmax is the next token.
+ * Probabilities and their sums are held in fp64.
+ *   vocab         1..1048576
+ *   dtype         of logits and draft_probs; row r at r * stride elements
+ *   tokens        device int32 [rows]: the drafted tokens (roots' are not read);
+ *                 one outside [0, vocab) is never accepted and fails the
+ *                 handle's next call
+ *   temperature   host [n], >= 0 and finite, or NULL: 1
+ *   accept        device fp32 [rows]: uniform in [0, 1) (roots' are not read)
+ *   sample        device fp32 [n]: uniform in [0, 1)
+ *   emitted       device int32 [rows]: request i's accepted tokens and the next
+ *                 token, from its root's row on, -1 behind them
+ *   path          device int32 [rows]: the nodes walked, 0 first, likewise
+ *   count         device int32 [n]: tokens emitted = nodes walked (accepted + 1);
+ *                 0 (and -1 in every entry) where the walk met a logits row
+ *                 with a NaN or no finite maximum
+ */
+spr_status spr_tree_verify(spr_tree_ops* ops, const spr_tree_batch* batch, int32_t vocab, int32_t dtype,
+                           const int32_t* tokens, const void* logits, int64_t logits_stride, const void* draft_probs,
+                           int64_t draft_stride, const float* temperature, const float* accept, const float* sample,
+                           int32_t* emitted, int32_t* path, int32_t* count);
+
+/*
+ * Closes trees in the cache: in every layer, the keys and values of node
+ * path[root row of i + k] move to position lens[i] + k for k < count[i].
+ * Positions from lens[i] + count[i] on are left as they were or hold what
+ * rejected nodes left there.  Per request, nodes 0 <= path[0] < path[1] < ...
+ * < n_nodes[i] and count[i] <= n_nodes[i]; one that breaks this is left as it
+ * is and fails the handle's next call.  count[i] < 1 moves nothing.
+ *   path    device int32 [rows], count device int32 [n]: as spr_tree_verify
+ *           writes them
+ */
+spr_status spr_tree_keep(spr_tree_ops* ops, const spr_kv_view* kv, const spr_tree_batch* batch, const int32_t* path,
+                         const int32_t* count);
+
+/*
+ * The model's own cache as a view (keys, values and block table in its
+ * workspace; slots are its slot ids), for the operators above or for reading.
+ */
+spr_status spr_model_kv_view(spr_model* m, spr_kv_view* out);
+
+/*
+ * One decode step over drafted trees: every node runs through the model in
+ * one pass (spr_tree_attention in each layer), spr_tree_verify picks each
+ * request's path, and spr_tree_keep closes the trees in all layers.  With
+ * one-node trees and temperature 0 it is a decode step.
+ *   batch         slots: distinct active slots; lens: as in spr_decode_step.
+ *                 The tree takes positions of the slot's reserved blocks:
+ *                 lens[i] + n_nodes[i] must not exceed 16 * their number
+ *                 (SPR_ERR_KV_FULL), and a tree has at most as many levels as
+ *                 the slot still has tokens to generate (SPR_ERR_INVALID_ARG).
+ *   tok           device int32 [max_slots], indexed by slot: the roots' tokens
+ *                 are read from it, and each request's last emitted token is
+ *                 written to it, so tree steps and decode steps alternate
+ *                 freely
+ *   tokens        device int32 [rows]: the drafted tokens (roots' are not read)
+ *   draft_probs   device fp32 [rows, vocab] or NULL
+ *   temperature, accept, sample, emitted: as in spr_tree_verify (accept and
+ *                 sample may be NULL where every temperature is 0)
+ *   logits        device fp32 [rows, vocab]: each node's logits
+ *   count         host int32 [n]: tokens emitted, 1..levels of the tree
+ *   retired       host int32 [n] or NULL: 1 where the slot reached its stop_len
+ * Each slot advances by count[i] positions and tokens; spr_rewind_slot drops
+ * them again.  Synchronous: the counts are the host's.  A drafted token
+ * outside [0, vocab) or a bad logits row on the way fails this call
+ * (SPR_ERR_DEVICE_CHECK), not the next.
+ */
+spr_status spr_tree_step(spr_model* m, const spr_tree_batch* batch, int32_t* tok, const int32_t* tokens,
+                         const float* draft_probs, const float* temperature, const float* accept, const float* sample,
+                         float* logits, int32_t* emitted, int32_t* count, int32_t* retired);
+
 /* Releases the host state.  The workspace is the caller's to free afterwards. */
 spr_status spr_release(spr_model* m);
 

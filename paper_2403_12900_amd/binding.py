@@ -57,6 +57,17 @@ class SprServeStats(ctypes.Structure):
                 ("level_tokens", ctypes.c_double * MAX_LEVELS), ("level_seconds", ctypes.c_double * MAX_LEVELS)]
 
 
+class SprKvView(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("kv_dtype", ctypes.c_int32),
+                ("n_layers", ctypes.c_int32), ("n_blocks", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("block_table", ctypes.c_void_p), ("n_slots", ctypes.c_int32),
+                ("max_blocks", ctypes.c_int32)]
+
+
+class SprTreeBatch(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("slots", _I32P), ("lens", _I32P), ("n_nodes", _I32P), ("parents", _I32P)]
+
+
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     global _lib
     if _lib is not None:
@@ -101,6 +112,20 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     L.spr_serve.restype = ctypes.c_int
     L.spr_serve.argtypes = [vp, ctypes.c_int32, ctypes.POINTER(SprRequest), ctypes.c_int32, ctypes.c_int32, vp, vp,
                             _I32P, ctypes.POINTER(SprServeStats)]
+    batch, view, f32p = ctypes.POINTER(SprTreeBatch), ctypes.POINTER(SprKvView), ctypes.POINTER(ctypes.c_float)
+    i32, i64 = ctypes.c_int32, ctypes.c_int64
+    L.spr_tree_ops_workspace_bytes.restype = ctypes.c_size_t
+    L.spr_tree_ops_workspace_bytes.argtypes = []
+    for name, args in (("spr_tree_ops_init", [vp, ctypes.c_size_t, vp, ctypes.POINTER(vp)]),
+                       ("spr_tree_ops_set_stream", [vp, vp]),
+                       ("spr_tree_ops_release", [vp]),
+                       ("spr_tree_attention", [vp, view, i32, batch, i32, i32, vp, i64, vp, i64]),
+                       ("spr_tree_verify", [vp, batch, i32, i32, vp, vp, i64, vp, i64, f32p, vp, vp, vp, vp, vp]),
+                       ("spr_tree_keep", [vp, view, batch, vp, vp]),
+                       ("spr_model_kv_view", [vp, view]),
+                       ("spr_tree_step", [vp, batch, vp, vp, vp, f32p, vp, vp, vp, vp, _I32P, _I32P])):
+        getattr(L, name).restype = ctypes.c_int
+        getattr(L, name).argtypes = args
     L.spr_release.restype = ctypes.c_int
     L.spr_release.argtypes = [vp]
     L.spr_last_error.restype = ctypes.c_char_p
@@ -196,6 +221,47 @@ class DecodeModel:
                                                        ctypes.c_void_p(logits.data_ptr() if want_logits else 0),
                                                        _ptr(retired)))
         return logits, retired
+
+    def kv_view(self):
+        """The model's cache as a KVView (spr_model_kv_view); its tensors alias the workspace."""
+        from .tree import KVView
+        v = SprKvView()
+        _check(self.lib.spr_model_kv_view(self.h, ctypes.byref(v)))
+        torch = self.torch
+        dt = torch.bfloat16 if v.kv_dtype == SPR_BF16 else torch.float32
+
+        def part(ptr, dtype, *shape):
+            n = int(np.prod(shape)) * dtype.itemsize
+            at = ptr - self.ws.data_ptr()
+            return self.ws[at:at + n].view(dtype).view(*shape)
+
+        pool = (v.n_layers, v.n_blocks, v.n_kv_heads, 16 * v.head_dim)
+        return KVView(part(v.k, dt, *pool), part(v.v, dt, *pool),
+                      part(v.block_table, torch.int32, v.n_slots, v.max_blocks))
+
+    def tree_step(self, batch, tokens, tok, temperature=None, accept=None, sample=None, draft_probs=None):
+        """One decode step over drafted trees (spr_tree_step).
+
+        batch: a TreeBatch; tokens: device int32 [rows]; tok: the slots' token buffer; accept [rows] and sample [n]:
+        device fp32 uniforms, needed where a temperature (per request, default all 1) is above 0; draft_probs: device
+        fp32 [rows, vocab] or None.  Returns (tokens emitted per request, device int32 [rows] of them, logits
+        [rows, vocab], retired)."""
+        torch = self.torch
+        n, rows = batch.n, batch.rows
+        for name, t, dt, shape in (("tokens", tokens, torch.int32, (rows,)), ("tok", tok, torch.int32, (self.max_slots,)),
+                                   ("accept", accept, torch.float32, (rows,)), ("sample", sample, torch.float32, (n,)),
+                                   ("draft_probs", draft_probs, torch.float32, (rows, self.vocab))):
+            if t is not None and (t.device != self.device or t.dtype != dt or tuple(t.shape) != shape or not t.is_contiguous()):
+                raise SproutError(SPR_ERR_INVALID_ARG, f"tree_step: {name} must be a contiguous {dt} tensor of shape {shape} "
+                                                       f"on {self.device}")
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        logits = torch.empty((rows, self.vocab), dtype=torch.float32, device=self.device)
+        emitted = torch.empty(rows, dtype=torch.int32, device=self.device)
+        count, retired = np.zeros(n, dtype=np.int32), np.zeros(n, dtype=np.int32)
+        _check(self.lib.spr_tree_step(self.h, batch.ref, ptr(tok), ptr(tokens), ptr(draft_probs),
+                                      batch.temperatures(temperature), ptr(accept), ptr(sample), ptr(logits), ptr(emitted),
+                                      _ptr(count), _ptr(retired)))
+        return count, emitted, logits, retired
 
     def rewind(self, slot: int, length: int, produced: int):
         _check(self.lib.spr_rewind_slot(self.h, slot, length, produced))

@@ -220,6 +220,30 @@ __device__ __forceinline__ typename P::elem weight_elem(uint64_t stream, uint64_
   return P::from_f32(weight_draw(stream, e));
 }
 
+// Bits of the device check flag (mapped host memory; the host reports a
+// nonzero flag at the next call).
+constexpr int kErrTokenRange = 1;  // a fed token id outside [0, V)
+constexpr int kErrLogits = 2;      // a logits row with a NaN or no finite maximum
+constexpr int kErrBlockId = 4;     // a block id outside the pool
+constexpr int kErrPath = 8;        // a malformed path of tree nodes
+
+// Sets bit `bit` of the flag.  The flag lives in host memory, so this is a
+// plain load and store (no read-modify-write atomic over the host link); two
+// kernels racing to set different bits may leave only one, and the flag is
+// still nonzero.  Runs only on the error path.
+__device__ __forceinline__ void raise_check(int* err, int bit) {
+  const int v = __hip_atomic_load(err, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+  __hip_atomic_store(err, v | bit, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+}
+
+// The larger of two candidates, the lower index where they are equal.
+__device__ __forceinline__ void better_of(float& v, int& i, float ov, int oi) {
+  if (ov > v || (ov == v && oi < i)) {
+    v = ov;
+    i = oi;
+  }
+}
+
 __device__ __forceinline__ float wave_max(float v) {
   for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
   return v;

@@ -375,6 +375,7 @@ struct EpiQKV {
   const int32_t* bt;            // [slots][mb]
   const float2* rope;           // [positions][hd / 2] (cos, sin)
   RowSlotPos rows;
+  int at[kRows];                // cache index of the row: its position, or len + node inside a drafted tree
 
   // Per row tile of a lane: the rotary (cos, sin) pairs of its four features
   // (q and k rows), the KV block its position falls in (k and v rows) and, if
@@ -393,13 +394,13 @@ struct EpiQKV {
     for (int j = 0; j < JT; ++j) {
       const int b = 16 * j + (lane & 15);
       const int bb = b < n_rows ? b : 0;
-      const int p = rows.pos[bb];
+      const int p = rows.pos[bb], c = at[bb];
       if constexpr (kRowScale) pr.s[j] = rs[bb];
       if (n0 < qr + kr) {
         const int dd = (n0 < qr ? n0 : n0 - qr) % hd;
         pr.cs[j] = *reinterpret_cast<const float4*>(rope + static_cast<size_t>(p) * (hd / 2) + dd / 2);
       }
-      if (n0 >= qr) pr.blk[j] = bt[static_cast<size_t>(rows.slot[bb]) * mb + (p >> 4)];
+      if (n0 >= qr) pr.blk[j] = bt[static_cast<size_t>(rows.slot[bb]) * mb + (c >> 4)];
     }
     return pr;
   }
@@ -414,7 +415,6 @@ struct EpiQKV {
       if (b >= n_rows) continue;
       const float s = kRowScale ? pr.s[kRowScale ? j : 0] : rsqrtf(ssq[j] / static_cast<float>(dnorm) + eps);
       float v0 = acc[j][0] * s, v1 = acc[j][1] * s, v2 = acc[j][2] * s, v3 = acc[j][3] * s;
-      const int p = rows.pos[b];
       if (n0 < qr + kr) {
         const float2 c0 = make_float2(pr.cs[j].x, pr.cs[j].y), c1 = make_float2(pr.cs[j].z, pr.cs[j].w);
         const float a0 = v0 * c0.x - v1 * c0.y, a1 = v0 * c0.y + v1 * c0.x;
@@ -429,7 +429,7 @@ struct EpiQKV {
         continue;
       }
       const int blk = pr.blk[j];
-      const int off = p & 15;
+      const int off = at[b] & 15;
       if (n0 < qr + kr) {
         const int m = n0 - qr, kvh = m / hd, dd = m % hd;
         typename KP::elem* dst = kc + (static_cast<size_t>(blk) * Hkv + kvh) * 16 * hd + ktile_offset<KP>(off, dd);

@@ -210,35 +210,41 @@ void SlotTable::commit_prefill(int n, const int32_t* slots, const int32_t* seq_l
   }
 }
 
-spr_status SlotTable::check_decode(int n, const int32_t* slots, const int32_t* lens, std::string* err) const {
-  if (n < 1 || n > d_.S) {
-    *err = "decode_step: n_active must be in [1, max_slots]";
-    return SPR_ERR_INVALID_ARG;
-  }
+// Active slots, listed once each, at their cached lengths.
+spr_status SlotTable::check_active(const char* what, int n, const int32_t* slots, const int32_t* lens,
+                                   std::string* err) const {
   std::vector<char> seen(d_.S, 0);
   for (int i = 0; i < n; ++i) {
     const int s = slots[i];
     if (s < 0 || s >= d_.S) {
-      *err = "decode_step: slot id out of range";
+      *err = std::string(what) + ": slot id out of range";
       return SPR_ERR_INVALID_ARG;
     }
     if (seen[s]) {
-      *err = "decode_step: slot listed twice";
+      *err = std::string(what) + ": slot listed twice";
       return SPR_ERR_INVALID_ARG;
     }
     seen[s] = 1;
     const Slot& sl = slots_[s];
     if (sl.state != kActive) {
-      *err = "decode_step: slot " + std::to_string(s) + (sl.state == kFree ? " is free" : " has finished");
+      *err = std::string(what) + ": slot " + std::to_string(s) + (sl.state == kFree ? " is free" : " has finished");
       return SPR_ERR_STATE;
     }
     if (lens[i] != sl.len) {
-      *err = "decode_step: slot " + std::to_string(s) + " has " + std::to_string(sl.len) + " cached positions, " +
-             std::to_string(lens[i]) + " given";
+      *err = std::string(what) + ": slot " + std::to_string(s) + " has " + std::to_string(sl.len) +
+             " cached positions, " + std::to_string(lens[i]) + " given";
       return SPR_ERR_STATE;
     }
   }
   return SPR_OK;
+}
+
+spr_status SlotTable::check_decode(int n, const int32_t* slots, const int32_t* lens, std::string* err) const {
+  if (n < 1 || n > d_.S) {
+    *err = "decode_step: n_active must be in [1, max_slots]";
+    return SPR_ERR_INVALID_ARG;
+  }
+  return check_active("decode_step", n, slots, lens, err);
 }
 
 void SlotTable::commit_decode(int n, const int32_t* slots, int32_t* retired) {
@@ -246,6 +252,38 @@ void SlotTable::commit_decode(int n, const int32_t* slots, int32_t* retired) {
     Slot& sl = slots_[slots[i]];
     sl.len += 1;
     sl.produced += 1;
+    const bool done = sl.produced >= sl.stop;
+    if (done) sl.state = kFinished;
+    if (retired) retired[i] = done ? 1 : 0;
+  }
+}
+
+spr_status SlotTable::check_tree(int n, const int32_t* slots, const int32_t* lens, const int32_t* nodes,
+                                 const int32_t* levels, std::string* err) const {
+  const spr_status st = check_active("tree_step", n, slots, lens, err);
+  if (st != SPR_OK) return st;
+  for (int i = 0; i < n; ++i) {
+    const Slot& sl = slots_[slots[i]];
+    if (levels[i] > sl.stop - sl.produced) {
+      *err = "tree_step: slot " + std::to_string(slots[i]) + " has " + std::to_string(sl.stop - sl.produced) +
+             " tokens left to generate, fewer than its tree has levels";
+      return SPR_ERR_INVALID_ARG;
+    }
+    const size_t room = sl.blocks.size() * kKvBlock;
+    if (static_cast<size_t>(lens[i]) + nodes[i] > room) {
+      *err = "tree_step: slot " + std::to_string(slots[i]) + " has room for " + std::to_string(room) +
+             " positions, " + std::to_string(lens[i] + nodes[i]) + " needed while its tree is open";
+      return SPR_ERR_KV_FULL;
+    }
+  }
+  return SPR_OK;
+}
+
+void SlotTable::commit_tree(int n, const int32_t* slots, const int32_t* count, int32_t* retired) {
+  for (int i = 0; i < n; ++i) {
+    Slot& sl = slots_[slots[i]];
+    sl.len += count[i];
+    sl.produced += count[i];
     const bool done = sl.produced >= sl.stop;
     if (done) sl.state = kFinished;
     if (retired) retired[i] = done ? 1 : 0;

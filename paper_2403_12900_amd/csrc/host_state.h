@@ -83,6 +83,9 @@ class SlotTable {
   spr_status check_prefill(int n, const int32_t* slots, const int32_t* seq_lens, const int32_t* stop_lens,
                            std::string* err) const;
   spr_status check_decode(int n, const int32_t* slots, const int32_t* lens, std::string* err) const;
+  // A tree step of n slots: nodes and levels of each one's tree.
+  spr_status check_tree(int n, const int32_t* slots, const int32_t* lens, const int32_t* nodes, const int32_t* levels,
+                        std::string* err) const;
   spr_status check_rewind(int slot, int len, int produced, std::string* err) const;
   spr_status check_free(int slot, std::string* err) const;
 
@@ -91,6 +94,7 @@ class SlotTable {
   void commit_prefill(int n, const int32_t* slots, const int32_t* seq_lens, const int32_t* stop_lens,
                       int32_t* retired);
   void commit_decode(int n, const int32_t* slots, int32_t* retired);
+  void commit_tree(int n, const int32_t* slots, const int32_t* count, int32_t* retired);  // count: tokens emitted
   void commit_rewind(int slot, int len, int produced);
   void commit_free(int slot);
 
@@ -101,6 +105,8 @@ class SlotTable {
   static int blocks_for(int seq_len, int stop_len) { return (seq_len + stop_len - 1 + kKvBlock - 1) / kKvBlock; }
 
  private:
+  spr_status check_active(const char* what, int n, const int32_t* slots, const int32_t* lens, std::string* err) const;
+
   Dims d_{};
   std::vector<Slot> slots_;
   std::vector<int32_t> free_;   // stack of free block ids

@@ -24,6 +24,9 @@
 //   then k_gather_rows of the rows that end a prompt, and the decode LM head
 //   (bf16 chunks of at most 128 rows run a decode pass's projections instead,
 //   with the row scales of k_row_rscale).
+// A tree step runs every request's drafted tokens as rows of one decode pass,
+// with k_tree_attn (tree_attn.hip) in k_attn_decode's place, then verifies them
+// and closes the trees in the cache (tree.hip).
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -40,6 +43,7 @@
 #include "prefill_kernels.h"
 #include "step_kernels.h"
 #include "tile_launch.h"
+#include "tree_launch.h"
 #include "wgen_kernels.h"
 
 using namespace sprk;
@@ -73,8 +77,8 @@ struct spr_model {
   spr_status sticky = SPR_OK;
   std::string sticky_msg;
   uint64_t seed = 0;
-  // Decode attention work-groups resident at once (CUs x occupancy).
-  int attn_slots = 1024;
+  // Decode attention work-groups resident at once (CUs x occupancy); CUs.
+  int attn_slots = 1024, n_cu = 256;
   // Device-side error flag in mapped pinned host memory (host and device
   // views): kernels set a bit when a step met an input they cannot honour (a
   // token id outside the vocabulary, a logits row with no finite maximum);
@@ -273,6 +277,13 @@ spr_status init_weights(spr_model* m) {
   return SPR_OK;
 }
 
+// The model's cache as the drafted-tree operators take it.
+spr_kv_view model_view(const spr_model* m) {
+  Ptrs p{m->ws, &m->lay};
+  const spr::Dims& d = m->d;
+  return spr_kv_view{p.kc(0), p.vc(0), d.kv_dtype, d.L, d.nb, d.Hkv, d.hd, p.bt(), d.S, d.mb};
+}
+
 // Rows of one forward pass.
 struct RowSet {
   int n = 0;
@@ -406,9 +417,10 @@ void launch_row_rscale(spr_model* m, int C) {
 
 // QKV projection of layer l over n rows: a decode pass, or (kPrefill) a
 // prefill chunk of as many rows, whose norms take their scales from the fp32
-// residual.
+// residual.  at: the rows' cache indices (null: their positions).
 template <class P, class KP, bool kPrefill>
-spr_status qkv_projection(spr_model* m, int l, int n, const RowSlotPos& rows, const SplitRoom& room) {
+spr_status qkv_projection(spr_model* m, int l, int n, const RowSlotPos& rows, const SplitRoom& room,
+                          const int* at = nullptr) {
   const spr::Dims& d = m->d;
   Ptrs p{m->ws, &m->lay};
   if constexpr (kPrefill) launch_row_rscale(m, n);
@@ -427,6 +439,7 @@ spr_status qkv_projection(spr_model* m, int l, int n, const RowSlotPos& rows, co
   e.bt = p.bt();
   e.rope = p.rope();
   e.rows = rows;
+  std::memcpy(e.at, at != nullptr ? at : rows.pos, sizeof(e.at));
   return launch_gemm<QKVIn<P>>(m, d.nt_qkv, p.wqkv(l), p.act(0), d.kb_d, e, room);
 }
 
@@ -457,6 +470,46 @@ spr_status mlp_projections(spr_model* m, int l, int n, bool qkv_next, const Spli
   return launch_gemm<P>(m, d.nt_2, p.w2(l), p.act(1), d.kb_f, e, room);
 }
 
+// Embeddings of n rows into the residual and the first QKV input; tok_in !=
+// null: row b's token is tok_in[index[b]], otherwise tok[b].
+template <class P>
+spr_status embed_rows(spr_model* m, int n, const int32_t* tok_in, const int* index, const int* tok) {
+  const spr::Dims& d = m->d;
+  Ptrs p{m->ws, &m->lay};
+  EmbedArgs ea{};
+  ea.emb = p.emb();
+  ea.tok_dev = tok_in;
+  ea.x = p.x();
+  ea.act = p.act(0);
+  ea.err = m->err_dev;
+  ea.n_rows = n;
+  ea.d = d.d;
+  ea.V = d.V;
+  ea.rec = act_rec(16 * row_tiles(n));
+  std::memcpy(ea.slot, index, sizeof(ea.slot));
+  std::memcpy(ea.tok, tok, sizeof(ea.tok));
+  k_embed<QKVIn<P>><<<dim3(ceil_div(d.d / 4, 64), n), 64, 0, m->st>>>(ea);
+  SPR_LAUNCHED(m, "k_embed");
+  return SPR_OK;
+}
+
+// LM head of n rows: row b's logits go to row out_row[b] of `logits` (if non-
+// null), its greedy candidates to sc.amax.
+template <class P>
+spr_status lm_head(spr_model* m, int n, const int* out_row, float* logits, const DecodeScratch& sc) {
+  const spr::Dims& d = m->d;
+  Ptrs p{m->ws, &m->lay};
+  EpiLogits<P> e{};
+  e.n_rows = n;
+  e.V = d.V;
+  e.dnorm = d.d;
+  e.eps = d.eps;
+  e.logits = logits;
+  e.part = sc.amax;
+  std::memcpy(e.out_row, out_row, sizeof(e.out_row));
+  return launch_gemm<P>(m, d.nt_lm, p.wlm(), p.act(0), d.kb_d, e, split_room(sc));
+}
+
 // One forward pass over rs (rows: slot, position, emitted logits row).
 // tok_in != null: the inputs are tok_in[slot]; otherwise rs.tok.  Emitting
 // rows write their greedy token to tok_out[slot].
@@ -467,27 +520,12 @@ spr_status forward(spr_model* m, const RowSet& rs, const int32_t* tok_in, int32_
   Ptrs p{m->ws, &m->lay};
   const int n = rs.n;
   const ActRec rec = act_rec(16 * row_tiles(n));
-  using E = typename P::elem;
   RowSlotPos sp;
   std::memcpy(sp.slot, rs.slot, sizeof(sp.slot));
   std::memcpy(sp.pos, rs.pos, sizeof(sp.pos));
 
-  {
-    EmbedArgs ea{};
-    ea.emb = p.emb();
-    ea.tok_dev = tok_in;
-    ea.x = p.x();
-    ea.act = p.act(0);
-    ea.err = m->err_dev;
-    ea.n_rows = n;
-    ea.d = d.d;
-    ea.V = d.V;
-    ea.rec = rec;
-    std::memcpy(ea.slot, rs.slot, sizeof(ea.slot));
-    std::memcpy(ea.tok, rs.tok, sizeof(ea.tok));
-    k_embed<QKVIn<P>><<<dim3(ceil_div(d.d / 4, 64), n), 64, 0, m->st>>>(ea);
-    SPR_LAUNCHED(m, "k_embed");
-  }
+  spr_status st = embed_rows<P>(m, n, tok_in, rs.slot, rs.tok);
+  if (st != SPR_OK) return st;
 
   // KV splits: a work-group covers 4 * bpw blocks of one (row, KV head), a
   // run of bpw blocks per wave.  bpw stays 1 until the pass has more blocks
@@ -525,7 +563,6 @@ spr_status forward(spr_model* m, const RowSet& rs, const int32_t* tok_in, int32_
   if (rounds) std::stable_sort(order, order + n, [&](uint8_t i, uint8_t j) { return rs.pos[i] > rs.pos[j]; });
 
   const SplitRoom room = split_room(sc);
-  spr_status st;
   for (int l = 0; l < d.L; ++l) {
     if ((st = qkv_projection<P, KP, false>(m, l, n, sp, room)) != SPR_OK) return st;
     const AttnArgs a = attention_args<P, KP>(m, l, rs, rec, bpw, order, rounds, p.act(1), sc);
@@ -533,17 +570,7 @@ spr_status forward(spr_model* m, const RowSet& rs, const int32_t* tok_in, int32_
     if (st != SPR_OK) return st;
     if ((st = mlp_projections<P, false>(m, l, n, l + 1 < d.L, room)) != SPR_OK) return st;
   }
-  {
-    EpiLogits<P> e{};
-    e.n_rows = n;
-    e.V = d.V;
-    e.dnorm = d.d;
-    e.eps = d.eps;
-    e.logits = logits;
-    e.part = sc.amax;
-    std::memcpy(e.out_row, rs.out_row, sizeof(e.out_row));
-    if ((st = launch_gemm<P>(m, d.nt_lm, p.wlm(), p.act(0), d.kb_d, e, room)) != SPR_OK) return st;
-  }
+  if ((st = lm_head<P>(m, n, rs.out_row, logits, sc)) != SPR_OK) return st;
   {
     ArgmaxArgs a{};
     a.part = sc.amax;
@@ -558,6 +585,60 @@ spr_status forward(spr_model* m, const RowSet& rs, const int32_t* tok_in, int32_
     SPR_LAUNCHED(m, "k_argmax_final");
   }
   return SPR_OK;
+}
+
+// Per-step device scratch of a tree step, in the prefill row table's region.
+struct TreeStepScratch {
+  int32_t *tok, *path, *count;  // each row's input token, the walked nodes, tokens emitted per request
+};
+TreeStepScratch tree_step_scratch(const spr_model* m) {
+  Ptrs p{m->ws, &m->lay};
+  int32_t* base = reinterpret_cast<int32_t*>(p.prow());
+  return TreeStepScratch{base, base + kRows, base + 2 * kRows};
+}
+
+// One forward pass over the nodes of t (input tokens: tok[row] on the device):
+// keys and values go to cache position len + node, rotated by len + depth, and
+// every row's logits to its row of `logits`.
+template <class P, class KP>
+spr_status tree_forward(spr_model* m, const TreeInfo& t, const int32_t* tok, float* logits) {
+  const spr::Dims& d = m->d;
+  Ptrs p{m->ws, &m->lay};
+  const int n = t.rows;
+  const DecodeScratch sc = workspace_scratch(m);
+  const SplitRoom room = split_room(sc);
+  RowSlotPos sp{};
+  int at[kRows] = {}, row[kRows];
+  for (int i = 0; i < t.n; ++i)
+    for (int r = t.row0[i]; r < t.row0[i + 1]; ++r) {
+      sp.slot[r] = t.slot[i];
+      sp.pos[r] = t.len[i] + t.depth[r];
+      at[r] = t.len[i] + r - t.row0[i];
+    }
+  for (int r = 0; r < kRows; ++r) row[r] = r < n ? r : -1;
+  spr_status st = embed_rows<P>(m, n, tok, row, at);
+  if (st != SPR_OK) return st;
+  TreeAttnCall c{};
+  c.st = m->st;
+  c.tree = &t;
+  c.kv = model_view(m);
+  c.H = d.H;
+  c.io = std::is_same_v<P, F32> ? kTreeActF32 : kTreeActBF16;
+  c.q = p.q();
+  c.qs = static_cast<int64_t>(d.H) * d.hd;
+  c.out = p.act(1);
+  c.rec = act_rec(16 * row_tiles(n));
+  c.sc = TreeScratch{sc.part, sc.part_floats, sc.cnt, sc.n_cnt};
+  c.err = m->err_dev;
+  c.n_cu = m->n_cu;
+  for (int l = 0; l < d.L; ++l) {
+    if ((st = qkv_projection<P, KP, false>(m, l, n, sp, room, at)) != SPR_OK) return st;
+    c.layer = l;
+    const hipError_t e = launch_tree_attention(c);
+    if (e != hipSuccess) return hip_fail(m, "k_tree_attn", e);
+    if ((st = mlp_projections<P, false>(m, l, n, l + 1 < d.L, room)) != SPR_OK) return st;
+  }
+  return lm_head<P>(m, n, row, logits, sc);
 }
 
 // Launches one projection of `layer` over n rows (see spr_time_projection).
@@ -758,21 +839,13 @@ spr_status forward_any(spr_model* m, const RowSet& rs, const int32_t* tok_in, in
                                    : forward<BF16, F32>(m, rs, tok_in, tok_out, logits, hist, sc);
 }
 
-// Device check bits (EmbedArgs / ArgmaxArgs `err`), reported by the next call.
-std::string device_check_message(int bits) {
-  std::string s = "a device check failed on an earlier call:";
-  if (bits & kErrTokenRange) s += " a token id outside [0, vocab) was fed (it was read as a clamped id);";
-  if (bits & kErrLogits) s += " a logits row had no finite maximum (its token was set to 0);";
-  return s + " the model's state is unreliable; release it";
-}
-
 spr_status check_model(spr_model* m) {
   if (m == nullptr) return fail(SPR_ERR_INVALID_ARG, "model is null");
   if (m->sticky == SPR_OK && m->err_host != nullptr) {
     const int bits = *reinterpret_cast<volatile int*>(m->err_host);
     if (bits != 0) {
       m->sticky = SPR_ERR_DEVICE_CHECK;
-      m->sticky_msg = device_check_message(bits);
+      m->sticky_msg = spr::device_check_message(bits);
     }
   }
   if (m->sticky != SPR_OK) return fail(m->sticky, m->sticky_msg);
@@ -955,6 +1028,23 @@ struct GpuServe : spr::ServeDevice {
 
 }  // namespace
 
+namespace spr {
+
+spr_status set_error(spr_status s, const std::string& msg) { return fail(s, msg); }
+void clear_error() { g_err.clear(); }
+
+// Device check bits (kErr*), reported by the next call.
+std::string device_check_message(int bits) {
+  std::string s = "a device check failed on an earlier call:";
+  if (bits & kErrTokenRange) s += " a token id outside [0, vocab) was fed (it was read as a clamped id);";
+  if (bits & kErrLogits) s += " a logits row had no finite maximum (its token was set to 0);";
+  if (bits & kErrBlockId) s += " a block id outside the pool was met;";
+  if (bits & kErrPath) s += " a path of tree nodes was malformed;";
+  return s + " the model's state is unreliable; release it";
+}
+
+}  // namespace spr
+
 extern "C" {
 
 size_t spr_workspace_bytes(const spr_config* cfg) {
@@ -1025,6 +1115,7 @@ spr_status spr_init(const spr_config* cfg, uint64_t seed, void* dev_ws, size_t w
                             : d.kv_dtype == SPR_BF16 ? attn_blocks_per_cu<BF16, BF16>(d)
                                                      : attn_blocks_per_cu<BF16, F32>(d);
     if (e == hipSuccess && attn_per_cu >= 1) m->attn_slots = attn_per_cu * ncu;
+    if (e == hipSuccess) m->n_cu = ncu;
   }
   if (e == hipSuccess) e = hipStreamSynchronize(m->st);
   if (e != hipSuccess) {
@@ -1128,6 +1219,77 @@ spr_status spr_decode_step_static_scratch(spr_model* m, int32_t n_active, const 
   SPR_LAUNCHED(m, "k_zero_i32");
   if ((st = forward_any(m, rs, tok, tok, logits, nullptr, sc)) != SPR_OK) return st;
   m->tab.commit_decode(n_active, slots, retired);
+  return SPR_OK;
+}
+
+spr_status spr_model_kv_view(spr_model* m, spr_kv_view* out) {
+  g_err.clear();
+  spr_status st = check_model(m);
+  if (st != SPR_OK) return st;
+  if (out == nullptr) return fail(SPR_ERR_INVALID_ARG, "model_kv_view: out must not be null");
+  *out = model_view(m);
+  return SPR_OK;
+}
+
+spr_status spr_tree_step(spr_model* m, const spr_tree_batch* batch, int32_t* tok, const int32_t* tokens,
+                         const float* draft_probs, const float* temperature, const float* accept, const float* sample,
+                         float* logits, int32_t* emitted, int32_t* count, int32_t* retired) {
+  g_err.clear();
+  spr_status st = check_model(m);
+  if (st != SPR_OK) return st;
+  const spr::Dims& d = m->d;
+  if (tok == nullptr || tokens == nullptr || logits == nullptr || emitted == nullptr || count == nullptr)
+    return fail(SPR_ERR_INVALID_ARG, "tree_step: tok, tokens, logits, emitted and count must not be null");
+  std::string err;
+  TreeInfo t;
+  if ((st = parse_tree(batch, true, d.S, d.mb, "tree_step", &t, &err)) != SPR_OK) return fail(st, err);
+  if ((st = check_temperatures(t.n, temperature, accept, sample, "tree_step", &err)) != SPR_OK) return fail(st, err);
+  if (d.V > tree_max_vocab()) return fail(SPR_ERR_INVALID_ARG, "tree_step: the vocabulary exceeds 1048576");
+  if ((st = m->tab.check_tree(t.n, t.slot, t.len, t.nodes, t.levels, &err)) != SPR_OK) return fail(st, err);
+  const TreeStepScratch ts = tree_step_scratch(m);
+  hipError_t e = launch_tree_tokens(m->st, t, tok, tokens, ts.tok);
+  if (e != hipSuccess) return hip_fail(m, "k_tree_tokens", e);
+  if (d.dtype == SPR_F32) st = tree_forward<F32, F32>(m, t, ts.tok, logits);
+  else if (d.kv_dtype == SPR_BF16) st = tree_forward<BF16, BF16>(m, t, ts.tok, logits);
+  else st = tree_forward<BF16, F32>(m, t, ts.tok, logits);
+  if (st != SPR_OK) return st;
+  Ptrs p{m->ws, &m->lay};
+  TreeVerifyCall v{};
+  v.st = m->st;
+  v.tree = &t;
+  v.V = d.V;
+  v.tokens = tokens;
+  v.logits = logits;
+  v.ls = v.ds = d.V;
+  v.draft = draft_probs;
+  v.temperature = temperature;
+  v.accept = accept;
+  v.sample = sample;
+  v.emitted = emitted;
+  v.path = ts.path;
+  v.count = ts.count;
+  // Verification's sums (24 bytes per row and 4096 tokens) go where the
+  // partials were; where a small model's are too few for a large vocabulary,
+  // the greedy candidates (64 bytes per token) hold them.
+  const bool in_part = tree_verify_bytes(t.rows, d.V) <= m->lay.part_floats * sizeof(float);
+  v.scratch = in_part ? static_cast<void*>(p.part()) : static_cast<void*>(p.amax());
+  v.cnt = p.cnt();
+  v.err = m->err_dev;
+  e = launch_tree_verify(v);
+  if (e != hipSuccess) return hip_fail(m, "k_tree_verify", e);
+  e = launch_tree_keep(m->st, t, model_view(m), ts.path, ts.count, m->err_dev);
+  if (e != hipSuccess) return hip_fail(m, "k_tree_keep", e);
+  e = launch_tree_last(m->st, t, emitted, ts.count, tok);
+  if (e != hipSuccess) return hip_fail(m, "k_tree_last", e);
+  int32_t got[kTreeReqs];
+  SPR_HIP(m, hipMemcpyAsync(got, ts.count, t.n * sizeof(int32_t), hipMemcpyDeviceToHost, m->st));
+  SPR_HIP(m, hipStreamSynchronize(m->st));
+  if ((st = check_model(m)) != SPR_OK) return st;
+  for (int i = 0; i < t.n; ++i) {
+    if (got[i] < 1 || got[i] > t.levels[i]) return fail(SPR_ERR_STATE, "tree_step: internal: token count out of range");
+    count[i] = got[i];
+  }
+  m->tab.commit_tree(t.n, t.slot, count, retired);
   return SPR_OK;
 }
 

@@ -6,20 +6,6 @@
 
 namespace sprk {
 
-// Bits of the device check flag (mapped host memory; the host reports a
-// nonzero flag at the next call).
-constexpr int kErrTokenRange = 1;  // a fed token id outside [0, V)
-constexpr int kErrLogits = 2;      // a logits row with a NaN or no finite maximum
-
-// Sets bit `bit` of the flag.  The flag lives in host memory, so this is a
-// plain load and store (no read-modify-write atomic over the host link); two
-// kernels racing to set different bits may leave only one, and the flag is
-// still nonzero.  Runs only on the error path.
-__device__ __forceinline__ void raise_check(int* err, int bit) {
-  const int v = __hip_atomic_load(err, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-  __hip_atomic_store(err, v | bit, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-}
-
 struct EmbedArgs {
   const void* emb;          // [V][d] row-major
   const int32_t* tok_dev;   // device tokens indexed by slot, or null: use tok[]
@@ -61,13 +47,6 @@ struct ArgmaxArgs {
   int out_row[kRows];       // -1: row emits no token
   int hist_idx[kRows];
 };
-
-__device__ __forceinline__ void better_of(float& v, int& i, float ov, int oi) {
-  if (ov > v || (ov == v && oi < i)) {
-    v = ov;
-    i = oi;
-  }
-}
 
 // A tile whose logits held a NaN reports a NaN candidate value (EpiLogits).
 // A row with such a tile, or with no finite maximum, raises kErrLogits and

@@ -1,0 +1,89 @@
+// Instantiations of the drafted-tree attention kernel and its launch.
+#include <cmath>
+
+#include "tree_attn_kernels.h"
+#include "tree_launch.h"
+
+namespace sprk {
+namespace {
+
+// Work-groups of the kernel that a CU holds at once.
+template <class KP, class IO, int HD, int NT>
+int blocks_per_cu() {
+  static const int n = [] {
+    int o = 0;
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&o, reinterpret_cast<const void*>(&k_tree_attn<KP, IO, HD, NT>),
+                                                     256, 0) != hipSuccess || o < 1)
+      o = 1;
+    return o;
+  }();
+  return n;
+}
+
+template <class KP, class IO, int HD, int NT>
+hipError_t launch(const TreeAttnCall& c) {
+  const TreeInfo& t = *c.tree;
+  TreeAttnArgs a{};
+  const size_t layer = static_cast<size_t>(c.kv.n_blocks) * c.kv.n_kv_heads * 16 * HD * c.layer;
+  a.q = c.q;
+  a.out = c.out;
+  a.qs = c.qs;
+  a.os = c.os;
+  a.kc = static_cast<const typename KP::elem*>(c.kv.k) + layer;
+  a.vc = static_cast<const typename KP::elem*>(c.kv.v) + layer;
+  a.bt = c.kv.block_table;
+  a.part = c.sc.part;
+  a.cnt = c.sc.cnt;
+  a.err = c.err;
+  a.n = t.n;
+  a.H = c.H;
+  a.Hkv = c.kv.n_kv_heads;
+  a.G = a.H / a.Hkv;
+  a.mb = c.kv.max_blocks;
+  a.nb = c.kv.n_blocks;
+  a.qscale = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(HD)));
+  a.rec = c.rec;
+  const size_t floats = std::min(c.sc.part_floats, size_t{1} << 28);
+  a.part_bytes = static_cast<uint32_t>(floats * 4);
+  const TreeSplit sp = tree_split(t, a.G, a.Hkv, HD, NT, KP::per16 == 8 ? 2 : 1,
+                                  blocks_per_cu<KP, IO, HD, NT>() * c.n_cu, floats);
+  a.bpw = sp.bpw;
+  for (int i = 0; i < t.n; ++i) {
+    a.slot[i] = t.slot[i];
+    a.len[i] = t.len[i];
+    a.nodes[i] = static_cast<uint8_t>(t.nodes[i]);
+    a.row0[i] = static_cast<uint8_t>(t.row0[i]);
+    a.ncg[i] = sp.ncg[i];
+    a.cg0[i] = sp.cg0[i];
+    a.item0[i] = sp.item0[i];
+  }
+  a.item0[t.n] = sp.item0[t.n];
+  for (int r = 0; r < t.rows; ++r) a.anc[r] = t.anc[r];
+  k_tree_attn<KP, IO, HD, NT><<<dim3(a.Hkv, sp.item0[t.n]), 256, 0, c.st>>>(a);
+  return hipGetLastError();
+}
+
+template <class KP, class IO>
+hipError_t by_shape(const TreeAttnCall& c) {
+  const int nt = tree_col_tiles(*c.tree, c.H / c.kv.n_kv_heads);
+  if (c.kv.head_dim == 128) {
+    if (nt == 1) return launch<KP, IO, 128, 1>(c);
+    return nt == 2 ? launch<KP, IO, 128, 2>(c) : launch<KP, IO, 128, 4>(c);
+  }
+  if (nt == 1) return launch<KP, IO, 64, 1>(c);
+  return nt == 2 ? launch<KP, IO, 64, 2>(c) : launch<KP, IO, 64, 4>(c);
+}
+
+}  // namespace
+
+hipError_t launch_tree_attention(const TreeAttnCall& c) {
+  const bool bf = c.kv.kv_dtype == SPR_BF16;
+  switch (c.io) {
+    case kTreeF32: return bf ? by_shape<BF16, TreeIoF32>(c) : by_shape<F32, TreeIoF32>(c);
+    case kTreeBF16: return bf ? by_shape<BF16, TreeIoBF16>(c) : by_shape<F32, TreeIoBF16>(c);
+    case kTreeActBF16: return bf ? by_shape<BF16, TreeIoAct<BF16>>(c) : by_shape<F32, TreeIoAct<BF16>>(c);
+    default: return by_shape<F32, TreeIoAct<F32>>(c);
+  }
+}
+
+}  // namespace sprk

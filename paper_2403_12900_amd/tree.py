@@ -1,0 +1,173 @@
+"""Drafted-tree operators on torch tensors: a thin binding of spr_tree_attention, spr_tree_verify and spr_tree_keep.
+
+Argument marshalling only, as in binding.py: shapes, types and devices are checked here (the C ABI sees pointers), all
+other checks are the library's.  PyTorch provides device memory and the stream: each call runs on the device's current
+stream.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Sequence
+
+import numpy as np
+import torch
+
+from .binding import (KV_BLOCK, SPR_BF16, SPR_ERR_INVALID_ARG, SPR_F32, SproutError, SprKvView, SprTreeBatch, _check, _i32,
+                      _ptr, load_library)
+
+_DTYPES = {torch.float32: SPR_F32, torch.bfloat16: SPR_BF16}
+_F32P = ctypes.POINTER(ctypes.c_float)
+
+
+def _refuse(msg: str):
+    raise SproutError(SPR_ERR_INVALID_ARG, msg)
+
+
+class KVView:
+    """A paged KV cache (spr_kv_view): k and v [layers, blocks, KV heads, 16 * head_dim] in the tile order that the header
+    gives, fp32 or bf16, and the int32 block table [slots, blocks per slot], all contiguous on one device."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype not in _DTYPES or v.dtype != k.dtype:
+            _refuse("kv view: k and v must be [layers, blocks, kv_heads, 16 * head_dim] of one type, fp32 or bf16")
+        if k.shape[3] % KV_BLOCK or block_table.dim() != 2 or block_table.dtype != torch.int32:
+            _refuse("kv view: blocks hold 16 positions, and the block table is int32 [slots, blocks per slot]")
+        if not (k.is_contiguous() and v.is_contiguous() and block_table.is_contiguous()):
+            _refuse("kv view: k, v and the block table must be contiguous")
+        if v.device != k.device or block_table.device != k.device:
+            _refuse("kv view: k, v and the block table must be on one device")
+        self.k, self.v, self.block_table, self.device = k, v, block_table, k.device
+        self.head_dim = k.shape[3] // KV_BLOCK
+        self.n_kv_heads = k.shape[2]
+        self._c = SprKvView(k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], k.shape[0], k.shape[1], k.shape[2],
+                            self.head_dim, block_table.data_ptr(), block_table.shape[0], block_table.shape[1])
+        self.ref = ctypes.byref(self._c)
+
+
+class TreeBatch:
+    """The drafted trees of one call (spr_tree_batch): per request its slot, cached positions and number of nodes, and all
+    nodes' parents (-1 for a root), request after request.  slots and lens may be None for verification alone."""
+
+    def __init__(self, slots: Optional[Sequence[int]], lens: Optional[Sequence[int]], n_nodes: Sequence[int],
+                 parents: Sequence[int]):
+        self._a = [None if x is None else _i32(x).reshape(-1) for x in (slots, lens, n_nodes, parents)]
+        n = len(self._a[2])
+        if any(x is not None and len(x) != n for x in self._a[:2]):
+            _refuse("tree batch: slots, lens and n_nodes must be of one length")
+        # A negative count must not make the sum match: every entry is checked by the library, the length here.
+        if len(self._a[3]) != int(np.maximum(self._a[2], 0).sum(dtype=np.int64)):
+            _refuse("tree batch: parents must have sum(n_nodes) entries")
+        self.n, self.rows = n, len(self._a[3])
+        self._c = SprTreeBatch(n, *(None if x is None else _ptr(x) for x in self._a))
+        self.ref = ctypes.byref(self._c)
+
+    def temperatures(self, temperature):
+        """The request temperatures as the C ABI takes them (a list or one number; None: 1)."""
+        if temperature is None:
+            return None
+        t = np.ascontiguousarray(np.broadcast_to(np.asarray(temperature, dtype=np.float32), (self.n,)))
+        p = t.ctypes.data_as(_F32P)
+        p._keep = t
+        return p
+
+
+class TreeOps:
+    """An operator handle on one device (spr_tree_ops_init), in a torch workspace.
+
+    Calls enqueue on the device's current stream; a call on another stream than the handle's last one first waits for
+    that one (not while a graph is captured: the capture's own order holds)."""
+
+    def __init__(self, device: int = 0):
+        self.lib = load_library()
+        self.device = torch.device("cuda", device)
+        self.ws = torch.empty(int(self.lib.spr_tree_ops_workspace_bytes()), dtype=torch.uint8, device=self.device)
+        self.stream = torch.cuda.current_stream(self.device)
+        self.h = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            _check(self.lib.spr_tree_ops_init(self.ws.data_ptr(), self.ws.numel(), self.stream.cuda_stream,
+                                              ctypes.byref(self.h)))
+
+    def _enter(self):
+        s = torch.cuda.current_stream(self.device)
+        if s != self.stream:
+            if not torch.cuda.is_current_stream_capturing():
+                s.wait_stream(self.stream)
+                self.ws.record_stream(s)
+            _check(self.lib.spr_tree_ops_set_stream(self.h, s.cuda_stream))
+            self.stream = s
+
+    def _need(self, what, t, dtype, shape):
+        if t.device != self.device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+            _refuse(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}")
+        return t.data_ptr()
+
+    def attention(self, kv: KVView, layer: int, batch: TreeBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None):
+        """Attention of the trees' nodes (spr_tree_attention): q [rows, heads, head_dim], fp32 or bf16, rows at any stride;
+        returns out like it."""
+        if q.dim() != 3 or q.shape[0] != batch.rows or q.shape[2] != kv.head_dim or q.dtype not in _DTYPES:
+            _refuse("tree attention: q must be [rows, heads, head_dim], fp32 or bf16")
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        elif out.shape != q.shape or out.dtype != q.dtype:
+            _refuse("tree attention: out must be like q")
+        hd = kv.head_dim
+        for t in (q, out):
+            if t.device != self.device or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != hd):
+                _refuse(f"tree attention: q and out must be on {self.device} with contiguous rows")
+        if kv.device != self.device:
+            _refuse(f"tree attention: the cache must be on {self.device}")
+        self._enter()
+        heads = q.shape[1]
+        one = q.shape[0] < 2  # a single row's stride does not matter
+        _check(self.lib.spr_tree_attention(self.h, kv.ref, layer, batch.ref, heads, _DTYPES[q.dtype], q.data_ptr(),
+                                           heads * hd if one else q.stride(0), out.data_ptr(),
+                                           heads * hd if one else out.stride(0)))
+        return out
+
+    def verify(self, batch: TreeBatch, tokens: torch.Tensor, logits: torch.Tensor, accept: Optional[torch.Tensor] = None,
+               sample: Optional[torch.Tensor] = None, draft_probs: Optional[torch.Tensor] = None, temperature=None):
+        """Verification (spr_tree_verify): tokens int32 [rows], logits [rows, vocab] (fp32 or bf16, rows at any stride),
+        accept fp32 [rows] and sample fp32 [n] uniform in [0, 1), draft_probs like logits.  Returns (emitted, path) int32
+        [rows] and count int32 [n]."""
+        if logits.dim() != 2 or logits.shape[0] != batch.rows or logits.dtype not in _DTYPES:
+            _refuse("tree verify: logits must be [rows, vocab], fp32 or bf16")
+        vocab = logits.shape[1]
+        for t in (logits, draft_probs):
+            if t is None:
+                continue
+            if t.device != self.device or t.dtype != logits.dtype or t.shape != logits.shape or (vocab > 1 and t.stride(1) != 1):
+                _refuse(f"tree verify: logits and draft_probs must be alike, on {self.device}, with contiguous rows")
+        p_tokens = self._need("tree verify: tokens", tokens, torch.int32, (batch.rows,))
+        p_accept = None if accept is None else self._need("tree verify: accept", accept, torch.float32, (batch.rows,))
+        p_sample = None if sample is None else self._need("tree verify: sample", sample, torch.float32, (batch.n,))
+        emitted, path = torch.empty((2, batch.rows), dtype=torch.int32, device=self.device).unbind(0)
+        count = torch.empty(batch.n, dtype=torch.int32, device=self.device)
+        self._enter()
+        one = batch.rows < 2
+        _check(self.lib.spr_tree_verify(
+            self.h, batch.ref, vocab, _DTYPES[logits.dtype], p_tokens, logits.data_ptr(),
+            vocab if one else logits.stride(0), None if draft_probs is None else draft_probs.data_ptr(),
+            0 if draft_probs is None else vocab if one else draft_probs.stride(0), batch.temperatures(temperature), p_accept,
+            p_sample, emitted.data_ptr(), path.data_ptr(), count.data_ptr()))
+        return emitted, path, count
+
+    def keep(self, kv: KVView, batch: TreeBatch, path: torch.Tensor, count: torch.Tensor):
+        """Closes the trees in every layer of the cache (spr_tree_keep); path and count as verify returns them."""
+        p_path = self._need("tree keep: path", path, torch.int32, (batch.rows,))
+        p_count = self._need("tree keep: count", count, torch.int32, (batch.n,))
+        if kv.device != self.device:
+            _refuse(f"tree keep: the cache must be on {self.device}")
+        self._enter()
+        _check(self.lib.spr_tree_keep(self.h, kv.ref, batch.ref, p_path, p_count))
+
+    def close(self):
+        if getattr(self, "h", None) is not None and self.h.value:
+            self.lib.spr_tree_ops_release(self.h)
+            self.h = ctypes.c_void_p()
+        self.ws = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
