@@ -7,6 +7,7 @@
 
 #include "host_state.h"
 #include "launch_rule.h"
+#include "tree_rule.h"
 
 namespace {
 thread_local std::string g_err;
@@ -115,6 +116,52 @@ int sprh_slot(void* hp, int slot, int32_t* len, int32_t* produced, int32_t* stop
   *stop = s.stop;
   *state = s.state;
   return 0;
+}
+
+// parse_tree: per row depth, rank, children, ancestor mask; per request levels and most children.
+int sprh_tree_parse(const spr_tree_batch* b, int with_cache, int n_slots, int max_blocks, int32_t* depth, int32_t* rank,
+                    int32_t* kids, uint64_t* anc, int32_t* levels, int32_t* children) {
+  sprk::TreeInfo t;
+  const spr_status st = sprk::parse_tree(b, with_cache != 0, n_slots, max_blocks, "parse", &t, &g_err);
+  if (st != SPR_OK) return st;
+  for (int r = 0; r < t.rows; ++r) {
+    depth[r] = t.depth[r];
+    rank[r] = t.rank[r];
+    kids[r] = t.kids[r];
+    anc[r] = t.anc[r];
+  }
+  for (int i = 0; i < t.n; ++i) {
+    levels[i] = t.levels[i];
+    children[i] = t.children[i];
+  }
+  return SPR_OK;
+}
+
+int sprh_tree_view(const spr_kv_view* v, int layer) { return sprk::check_view(v, layer, "view", &g_err); }
+
+int sprh_tree_temperatures(int n, const float* temperature, const float* accept, const float* sample) {
+  return sprk::check_temperatures(n, temperature, accept, sample, "temperatures", &g_err);
+}
+
+// tree_split of a batch: out = {16-column tiles, bpw, then item0[0 .. n]}.
+int sprh_tree_split(const spr_tree_batch* b, int G, int Hkv, int hd, int step, int slots, size_t floats, int32_t* out) {
+  sprk::TreeInfo t;
+  const spr_status st = sprk::parse_tree(b, true, 64, 1 << 27, "split", &t, &g_err);
+  if (st != SPR_OK) return st;
+  const int nt = sprk::tree_col_tiles(t, G);
+  const sprk::TreeSplit s = sprk::tree_split(t, G, Hkv, hd, nt, step, slots, floats);
+  out[0] = nt;
+  out[1] = s.bpw;
+  for (int i = 0; i <= t.n; ++i) out[2 + i] = s.item0[i];
+  return SPR_OK;
+}
+
+int sprh_tree_step(void* hp, int n, const int32_t* slots, const int32_t* lens, const int32_t* nodes,
+                   const int32_t* levels, const int32_t* count, int32_t* retired) {
+  Host* h = static_cast<Host*>(hp);
+  const spr_status st = h->tab.check_tree(n, slots, lens, nodes, levels, &g_err);
+  if (st == SPR_OK) h->tab.commit_tree(n, slots, count, retired);
+  return st;
 }
 
 void sprh_block_row(void* hp, int slot, int32_t* row) { static_cast<Host*>(hp)->tab.block_row(slot, row); }

@@ -1242,7 +1242,8 @@ spr_status spr_tree_step(spr_model* m, const spr_tree_batch* batch, int32_t* tok
     return fail(SPR_ERR_INVALID_ARG, "tree_step: tok, tokens, logits, emitted and count must not be null");
   std::string err;
   TreeInfo t;
-  if ((st = parse_tree(batch, true, d.S, d.mb, "tree_step", &t, &err)) != SPR_OK) return fail(st, err);
+  // Room is the slot's reserved blocks (check_tree), not the table's width.
+  if ((st = parse_tree(batch, true, d.S, kTreeMaxLen / 16 + 4, "tree_step", &t, &err)) != SPR_OK) return fail(st, err);
   if ((st = check_temperatures(t.n, temperature, accept, sample, "tree_step", &err)) != SPR_OK) return fail(st, err);
   if (d.V > tree_max_vocab()) return fail(SPR_ERR_INVALID_ARG, "tree_step: the vocabulary exceeds 1048576");
   if ((st = m->tab.check_tree(t.n, t.slot, t.len, t.nodes, t.levels, &err)) != SPR_OK) return fail(st, err);
