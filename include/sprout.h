@@ -333,7 +333,7 @@ spr_status spr_serve(spr_model* m, int32_t n, const spr_request* reqs, int32_t m
  * n_slots, max_blocks >= 1; k and v 16-byte aligned.  A block id outside
  * [0, n_blocks) that a call meets in the table is read as block 0 and fails
  * the handle's next call (SPR_ERR_DEVICE_CHECK); spr_tree_keep then moves
- * nothing for that request and layer.
+ * nothing for that request.
  */
 typedef struct {
   void* k; /* device */

@@ -141,11 +141,11 @@ hipError_t launch_tree_verify(const TreeVerifyCall& c) {
     }
     const dim3 grid(a.S, n);
     if (c.bf16) {
-      if (a.k == 0) k_tree_verify<uint16_t, kStats><<<grid, 256, 0, c.st>>>(a);
-      else k_tree_verify<uint16_t, kRest><<<grid, 256, 0, c.st>>>(a);
+      if (a.k == 0) k_tree_verify<uint16_t, kStats><<<grid, kVThreads, 0, c.st>>>(a);
+      else k_tree_verify<uint16_t, kRest><<<grid, kVThreads, 0, c.st>>>(a);
     } else {
-      if (a.k == 0) k_tree_verify<float, kStats><<<grid, 256, 0, c.st>>>(a);
-      else k_tree_verify<float, kRest><<<grid, 256, 0, c.st>>>(a);
+      if (a.k == 0) k_tree_verify<float, kStats><<<grid, kVThreads, 0, c.st>>>(a);
+      else k_tree_verify<float, kRest><<<grid, kVThreads, 0, c.st>>>(a);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -163,7 +163,7 @@ hipError_t launch_tree_keep(hipStream_t st, const TreeInfo& t, const spr_kv_view
   a.path = path;
   a.count = count;
   a.err = err;
-  a.layer_bytes = static_cast<size_t>(kv.n_blocks) * kv.n_kv_heads * 16 * kv.head_dim * (bf ? 2 : 4);
+  a.layer_elems = static_cast<size_t>(kv.n_blocks) * kv.n_kv_heads * 16 * kv.head_dim;
   a.Hkv = kv.n_kv_heads;
   a.hd = kv.head_dim;
   a.mb = kv.max_blocks;
@@ -175,7 +175,12 @@ hipError_t launch_tree_keep(hipStream_t st, const TreeInfo& t, const spr_kv_view
     a.nodes[i] = static_cast<uint8_t>(t.nodes[i]);
   }
   const int columns = a.Hkv * (a.hd + a.hd / (bf ? 8 : 4));
-  const dim3 grid((columns + 255) / 256, kv.n_layers, t.n);
+  // About 4096 work-groups (two rounds of what the chip holds), each through
+  // as many layers as that takes.
+  a.n_layers = kv.n_layers;
+  const int64_t groups = static_cast<int64_t>((columns + 255) / 256) * t.n;
+  a.layers = static_cast<int>(std::min<int64_t>(kv.n_layers, std::max<int64_t>(1, groups * kv.n_layers / 4096)));
+  const dim3 grid((columns + 255) / 256, (kv.n_layers + a.layers - 1) / a.layers, t.n);
   if (bf) k_tree_keep<BF16><<<grid, 256, 0, st>>>(a);
   else k_tree_keep<F32><<<grid, 256, 0, st>>>(a);
   return hipGetLastError();

@@ -7,20 +7,28 @@
 namespace sprk {
 namespace {
 
+// CW columns per work-group: up to 32 on k_tree_attn, 64 and more on
+// k_tree_attn_shared.
+template <class KP, class IO, int HD, int CW>
+constexpr auto kernel() {
+  if constexpr (CW <= 32) return &k_tree_attn<KP, IO, HD, CW / 16>;
+  else return &k_tree_attn_shared<KP, IO, HD, CW / 64>;
+}
+
 // Work-groups of the kernel that a CU holds at once.
-template <class KP, class IO, int HD, int NT>
-int blocks_per_cu() {
+template <class KP, class IO, int HD, int CW>
+int groups_per_cu() {
   static const int n = [] {
     int o = 0;
-    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&o, reinterpret_cast<const void*>(&k_tree_attn<KP, IO, HD, NT>),
-                                                     256, 0) != hipSuccess || o < 1)
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&o, reinterpret_cast<const void*>(kernel<KP, IO, HD, CW>()), 256,
+                                                     0) != hipSuccess || o < 1)
       o = 1;
     return o;
   }();
   return n;
 }
 
-template <class KP, class IO, int HD, int NT>
+template <class KP, class IO, int HD, int CW>
 hipError_t launch(const TreeAttnCall& c) {
   const TreeInfo& t = *c.tree;
   TreeAttnArgs a{};
@@ -45,9 +53,10 @@ hipError_t launch(const TreeAttnCall& c) {
   a.rec = c.rec;
   const size_t floats = std::min(c.sc.part_floats, size_t{1} << 28);
   a.part_bytes = static_cast<uint32_t>(floats * 4);
-  const TreeSplit sp = tree_split(t, a.G, a.Hkv, HD, NT, KP::per16 == 8 ? 2 : 1,
-                                  blocks_per_cu<KP, IO, HD, NT>() * c.n_cu, floats);
-  a.bpw = sp.bpw;
+  constexpr int step = KP::per16 == 8 ? 2 : 1;
+  const int slots = groups_per_cu<KP, IO, HD, CW>() * c.n_cu;
+  const TreeSplit sp = tree_split(t, a.G, a.Hkv, HD, CW, CW <= 32 ? 4 * step : step, slots, floats);
+  a.bps = sp.bps;
   for (int i = 0; i < t.n; ++i) {
     a.slot[i] = t.slot[i];
     a.len[i] = t.len[i];
@@ -59,19 +68,23 @@ hipError_t launch(const TreeAttnCall& c) {
   }
   a.item0[t.n] = sp.item0[t.n];
   for (int r = 0; r < t.rows; ++r) a.anc[r] = t.anc[r];
-  k_tree_attn<KP, IO, HD, NT><<<dim3(a.Hkv, sp.item0[t.n]), 256, 0, c.st>>>(a);
+  kernel<KP, IO, HD, CW>()<<<dim3(a.Hkv, sp.item0[t.n]), 256, 0, c.st>>>(a);
   return hipGetLastError();
+}
+
+template <class KP, class IO, int HD>
+hipError_t by_columns(const TreeAttnCall& c) {
+  switch (tree_cols_per_group(*c.tree, c.H / c.kv.n_kv_heads)) {
+    case 16: return launch<KP, IO, HD, 16>(c);
+    case 32: return launch<KP, IO, HD, 32>(c);
+    case 64: return launch<KP, IO, HD, 64>(c);
+    default: return launch<KP, IO, HD, 128>(c);
+  }
 }
 
 template <class KP, class IO>
 hipError_t by_shape(const TreeAttnCall& c) {
-  const int nt = tree_col_tiles(*c.tree, c.H / c.kv.n_kv_heads);
-  if (c.kv.head_dim == 128) {
-    if (nt == 1) return launch<KP, IO, 128, 1>(c);
-    return nt == 2 ? launch<KP, IO, 128, 2>(c) : launch<KP, IO, 128, 4>(c);
-  }
-  if (nt == 1) return launch<KP, IO, 64, 1>(c);
-  return nt == 2 ? launch<KP, IO, 64, 2>(c) : launch<KP, IO, 64, 4>(c);
+  return c.kv.head_dim == 128 ? by_columns<KP, IO, 128>(c) : by_columns<KP, IO, 64>(c);
 }
 
 }  // namespace

@@ -93,43 +93,44 @@ inline spr_status parse_tree(const spr_tree_batch* b, bool with_cache, int n_slo
   return SPR_OK;
 }
 
-// 16-column tiles a work-group of the attention kernel takes: enough for the
-// widest request where that is one or two, else four (registers hold the
-// accumulators of no more).
-inline int tree_col_tiles(const TreeInfo& t, int G) {
+// Columns that one work-group of the attention kernel takes: 16 or 32 where
+// that holds the widest request (its four waves then share out the blocks),
+// else a multiple of 64 (16, 32 columns per wave).
+inline int tree_cols_per_group(const TreeInfo& t, int G) {
   const int cols = t.max_nodes * G;
-  return cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
+  return cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
 }
 
 // Work items of one attention launch: per request its column groups, each in
-// KV splits of 4 * bpw blocks (a run of bpw blocks per wave).
+// KV splits of bps blocks.
 struct TreeSplit {
-  int bpw = 1;
+  int bps = 1;
   uint8_t ncg[kTreeReqs], cg0[kTreeReqs];
   int item0[kTreeReqs + 1];
 };
 
-// Runs stay as short as one step (`step` blocks) until the launch has more
-// blocks than the resident waves take at once; they grow further while the
-// splits' partials exceed `floats` or a request has more than kTreeSplits.
+// Splits hold `least` blocks (a step of every wave that walks blocks) until
+// the launch has more than its share of resident work-groups (`slots`) takes
+// at once; they grow further while the partials exceed `floats` or a request
+// has more than kTreeSplits.
 constexpr int kTreeSplits = 128;
-inline TreeSplit tree_split(const TreeInfo& t, int G, int Hkv, int hd, int nt, int step, int slots, size_t floats) {
+inline TreeSplit tree_split(const TreeInfo& t, int G, int Hkv, int hd, int cw, int least, int slots, size_t floats) {
   TreeSplit s;
   int64_t blocks = 0;
   int cg = 0;
   for (int i = 0; i < t.n; ++i) {
-    s.ncg[i] = static_cast<uint8_t>((t.nodes[i] * G + 16 * nt - 1) / (16 * nt));
+    s.ncg[i] = static_cast<uint8_t>((t.nodes[i] * G + cw - 1) / cw);
     s.cg0[i] = static_cast<uint8_t>(cg);
     cg += s.ncg[i];
     blocks += static_cast<int64_t>(s.ncg[i]) * ((t.len[i] + t.nodes[i] + 15) / 16);
   }
-  const int64_t per = static_cast<int64_t>(Hkv) * 16 * nt * (hd + 4);
-  int64_t bpw = std::max<int64_t>(1, (blocks * Hkv + 4 * slots - 1) / (4 * slots));
-  for (;; bpw += std::max<int64_t>(step, bpw / 8)) {
-    bpw = (bpw + step - 1) / step * step;
+  const int64_t per = static_cast<int64_t>(Hkv) * cw * (hd + 4);
+  int64_t bps = std::max<int64_t>(1, (blocks * Hkv + slots - 1) / slots);
+  for (;; bps += std::max<int64_t>(least, bps / 8)) {
+    bps = (bps + least - 1) / least * least;
     int64_t items = 0, most = 1;
     for (int i = 0; i < t.n; ++i) {
-      const int64_t ns = ((t.len[i] + t.nodes[i] + 15) / 16 + 4 * bpw - 1) / (4 * bpw);
+      const int64_t ns = ((t.len[i] + t.nodes[i] + 15) / 16 + bps - 1) / bps;
       s.item0[i] = static_cast<int>(items);
       items += ns * s.ncg[i];
       most = std::max(most, ns);
@@ -137,7 +138,7 @@ inline TreeSplit tree_split(const TreeInfo& t, int G, int Hkv, int hd, int nt, i
     s.item0[t.n] = static_cast<int>(items);
     if (most == 1 || (most <= kTreeSplits && items * per <= static_cast<int64_t>(floats))) break;
   }
-  s.bpw = static_cast<int>(bpw);
+  s.bps = static_cast<int>(bps);
   return s;
 }
 

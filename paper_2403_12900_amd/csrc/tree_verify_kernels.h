@@ -30,9 +30,11 @@
 
 namespace sprk {
 
+constexpr int kVThreads = 512;
 constexpr int kVChunk = 4096;
 constexpr int kVMaxChunks = 256;
 constexpr int kVMaxVocab = kVChunk * kVMaxChunks;
+constexpr int kVOwn = kVChunk / kVThreads;  // entries of a chunk per thread
 
 struct TreeVerifyArgs {
   const void* logits;
@@ -57,75 +59,134 @@ struct TreeVerifyArgs {
 };
 static_assert(sizeof(TreeVerifyArgs) <= 2048, "kernel arguments");
 
-// Entries of one vocabulary chunk in registers: entry (j * 256 + thread) * EV
-// + e of the chunk, EV entries per 16 bytes.
+// exp(x) for x <= 0 to 2^-47 of its value: x = n ln 2 + r, |r| <= ln 2 / 2,
+// with ln 2 in two parts, and the Taylor polynomial of degree 11 of e^r (its
+// rest is below r^12 / 12! < 7e-15).  NaN stays NaN; 0 from -745 on.
+__device__ __forceinline__ double exp_neg(double x) {
+  const double n = __builtin_rint(x * 1.4426950408889634);
+  double r = fma(n, -0x1.62e42fefa39efp-1, x);
+  r = fma(n, -0x1.abc9e3b39803fp-56, r);
+  double p = 1.0 / 39916800.0;
+  p = fma(p, r, 1.0 / 3628800.0);
+  p = fma(p, r, 1.0 / 362880.0);
+  p = fma(p, r, 1.0 / 40320.0);
+  p = fma(p, r, 1.0 / 5040.0);
+  p = fma(p, r, 1.0 / 720.0);
+  p = fma(p, r, 1.0 / 120.0);
+  p = fma(p, r, 1.0 / 24.0);
+  p = fma(p, r, 1.0 / 6.0);
+  p = fma(p, r, 0.5);
+  p = fma(p, r, 1.0);
+  p = fma(p, r, 1.0);
+  const double e = __builtin_amdgcn_ldexp(p, static_cast<int>(fmax(n, -1100.0)));
+  return x < -745.0 ? 0.0 : e;
+}
+
+// kVOwn consecutive entries of one vocabulary chunk per thread: entry thread *
+// kVOwn + e, as floats; those past V read as `fill`.
+__device__ __forceinline__ int chunk_index(int chunk) {
+  return chunk * kVChunk + static_cast<int>(threadIdx.x) * kVOwn;
+}
+__device__ __forceinline__ float vocab_value(float x) { return x; }
+__device__ __forceinline__ float vocab_value(uint16_t x) { return bf16_bits_to_f32(x); }
 template <class T>
-struct VChunkRegs {
-  static constexpr int EV = 16 / static_cast<int>(sizeof(T)), NJ = kVChunk / (256 * EV);
-  static __device__ __forceinline__ int index(int chunk, int j, int e) {
-    return chunk * kVChunk + (j * 256 + static_cast<int>(threadIdx.x)) * EV + e;
-  }
-  static __device__ __forceinline__ float value(T x) {
-    if constexpr (sizeof(T) == 4) return x;
-    else return bf16_bits_to_f32(x);
-  }
-  // Entries past V read as `fill`.
-  static __device__ __forceinline__ void load(const T* row, int V, int chunk, int vec, float fill, float (*x)[EV]) {
+__device__ __forceinline__ void load_chunk(const T* row, int V, int chunk, int vec, float fill, float* x) {
+  constexpr int EV = 16 / static_cast<int>(sizeof(T));
+  static_assert(kVOwn % EV == 0, "whole 16-byte loads");
+  const int i0 = chunk_index(chunk);
+  if (vec && i0 + kVOwn <= V) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int i0 = index(chunk, j, 0);
-      if (vec && i0 + EV <= V) {
-        union {
-          uint4 u;
-          T t[EV];
-        } v;
-        v.u = *reinterpret_cast<const uint4*>(row + i0);
+    for (int j = 0; j < kVOwn / EV; ++j) {
+      const uint4 u = *reinterpret_cast<const uint4*>(row + i0 + j * EV);
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int e = 0; e < EV; ++e) x[j][e] = value(v.t[e]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < EV; ++e) x[j][e] = i0 + e < V ? value(row[i0 + e]) : fill;
+      for (int e = 0; e < EV; ++e) {
+        if constexpr (sizeof(T) == 4) x[j * EV + e] = __uint_as_float(w[e]);
+        else x[j * EV + e] = __uint_as_float(e % 2 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
       }
     }
+  } else {
+#pragma unroll
+    for (int e = 0; e < kVOwn; ++e) x[e] = i0 + e < V ? vocab_value(row[i0 + e]) : fill;
   }
-};
+}
 
+constexpr int kVWaves = kVThreads / 64;
 struct TreeVerifySmem {
-  double d[4];
-  float f[4];
-  int i[4];
-  int last, hit, tail;
-  double z[kTreeNodes], m[kTreeNodes], fc[kTreeNodes], fn[kTreeNodes];  // per node: sum, maximum, state past its children
-  double cc[kTreeNodes], cn[kTreeNodes], px[kTreeNodes];                // per node as a child: c_k, N_k, p(token)
-  int best[kTreeNodes], bad[kTreeNodes], tok[kTreeNodes], order[kTreeNodes];
+  double d[kVWaves];
+  float f[kVWaves];
+  int i[kVWaves];
+  int last, hit[kVWaves], tail[kVWaves];
+  double z[kTreeNodes], total[kTreeNodes];      // per node: its row's sum; per array of parts: N_k
+  double px[kTreeNodes];                        // per node as a child: p(its token)
+  float m[kTreeNodes];                          // per node: its row's maximum (NaN: a bad row)
+  int best[kTreeNodes], tok[kTreeNodes], order[kTreeNodes];
+  int8_t parent[kTreeNodes];
   double w[kVMaxChunks];
 };
 
-// Sums and maxima over the work-group, in a fixed order; every thread gets the result.
-__device__ __forceinline__ double wave_sum(double v) {
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+// Wave scans and reductions on DPP moves (row shifts by 1, 2, 4, 8, then the
+// row broadcasts): no trip through LDS.  Lanes that a move has no source for
+// take `old`.
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ int dpp_move(int v, int old) {
+  return __builtin_amdgcn_update_dpp(old, v, kCtrl, kRowMask, 0xF, false);
+}
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ double dpp_add(double v) {
+  const uint64_t u = static_cast<uint64_t>(__double_as_longlong(v));
+  const uint32_t lo = static_cast<uint32_t>(dpp_move<kCtrl, kRowMask>(static_cast<int>(u), 0));
+  const uint32_t hi = static_cast<uint32_t>(dpp_move<kCtrl, kRowMask>(static_cast<int>(u >> 32), 0));
+  return v + __longlong_as_double(static_cast<long long>(static_cast<uint64_t>(hi) << 32 | lo));
+}
+// Inclusive sum over the lanes up to this one.
+__device__ __forceinline__ double wave_scan(double v) {
+  v = dpp_add<0x111, 0xF>(v);
+  v = dpp_add<0x112, 0xF>(v);
+  v = dpp_add<0x114, 0xF>(v);
+  v = dpp_add<0x118, 0xF>(v);
+  v = dpp_add<0x142, 0xA>(v);
+  v = dpp_add<0x143, 0xC>(v);
   return v;
 }
+__device__ __forceinline__ double lane_value(double v, int lane) {
+  const uint64_t u = static_cast<uint64_t>(__double_as_longlong(v));
+  const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(u), lane));
+  const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(u >> 32), lane));
+  return __longlong_as_double(static_cast<long long>(static_cast<uint64_t>(hi) << 32 | lo));
+}
+__device__ __forceinline__ double wave_sum(double v) { return lane_value(wave_scan(v), 63); }
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ float dpp_max(float v) {
+  return fmaxf(v, __int_as_float(dpp_move<kCtrl, kRowMask>(__float_as_int(v), static_cast<int>(0xFF800000u))));
+}
+__device__ __forceinline__ float wave_maximum(float v) {
+  v = dpp_max<0x111, 0xF>(v);
+  v = dpp_max<0x112, 0xF>(v);
+  v = dpp_max<0x114, 0xF>(v);
+  v = dpp_max<0x118, 0xF>(v);
+  v = dpp_max<0x142, 0xA>(v);
+  v = dpp_max<0x143, 0xC>(v);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+// Maximum of the wave and the index that its first lane with it holds.
+__device__ __forceinline__ void wave_best(float& m, int& index) {
+  const float w = wave_maximum(m);
+  const uint64_t who = __ballot(m == w);
+  index = who == 0 ? 0x7fffffff : __builtin_amdgcn_readlane(index, __ffsll(static_cast<unsigned long long>(who)) - 1);
+  m = w;
+}
+
+// Sum over the work-group, in a fixed order; every thread gets it.  sm->d is
+// free (a barrier lies between its last readers and this).
 __device__ __forceinline__ double group_sum(double v, TreeVerifySmem* sm) {
   v = wave_sum(v);
-  __syncthreads();
   if ((threadIdx.x & 63) == 0) sm->d[threadIdx.x >> 6] = v;
   __syncthreads();
-  return ((sm->d[0] + sm->d[1]) + sm->d[2]) + sm->d[3];
-}
-__device__ __forceinline__ float group_max(float v, TreeVerifySmem* sm) {
-  v = wave_max(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sm->f[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return fmaxf(fmaxf(sm->f[0], sm->f[1]), fmaxf(sm->f[2], sm->f[3]));
-}
-__device__ __forceinline__ int group_min(int v, TreeVerifySmem* sm) {
-  for (int o = 32; o >= 1; o >>= 1) v = min(v, __shfl_xor(v, o));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sm->i[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return min(min(sm->i[0], sm->i[1]), min(sm->i[2], sm->i[3]));
+  double s = 0.0;
+#pragma unroll
+  for (int w = 0; w < kVWaves; ++w) s += sm->d[w];
+  return s;
 }
 
 __device__ __forceinline__ void put64(uint64_t* p, uint64_t v) {
@@ -134,33 +195,52 @@ __device__ __forceinline__ void put64(uint64_t* p, uint64_t v) {
 __device__ __forceinline__ uint64_t get64(const uint64_t* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ double get_double(const double* p) {
-  return __longlong_as_double(static_cast<long long>(get64(reinterpret_cast<const uint64_t*>(p))));
-}
+__device__ __forceinline__ double as_double(uint64_t u) { return __longlong_as_double(static_cast<long long>(u)); }
+__device__ __forceinline__ double get_double(const double* p) { return as_double(get64(reinterpret_cast<const uint64_t*>(p))); }
 
 // A draft probability as it counts: entries that are negative or NaN are 0.
 __device__ __forceinline__ double draft_value(float q) { return q > 0.f ? static_cast<double>(q) : 0.0; }
 
-// Maximum and sum of a row from its chunks (all threads of the work-group; S <= 256).
+// Maximum (NaN: a row with a NaN or no finite maximum), its lowest index and
+// sum of a row from its chunks; every wave works them out by itself.  kFresh:
+// the chunks are this launch's.
 struct RowStat {
-  float m;   // NaN: the row holds a NaN or has no finite maximum
+  float m;
   double z;
+  int best;
 };
-__device__ __forceinline__ RowStat row_stat(const TreeVerifyArgs& a, int row, double inv_t, TreeVerifySmem* sm) {
-  float m = -INFINITY;
-  double z = 0.0;
+template <bool kFresh>
+__device__ __forceinline__ RowStat row_stat(const TreeVerifyArgs& a, int row, double inv_t, bool want_z) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t* st = a.stat + static_cast<size_t>(row) * a.S * 2;
+  RowStat r{-INFINITY, 0.0, 0x7fffffff};
   bool bad = false;
-  if (static_cast<int>(threadIdx.x) < a.S) {
-    const uint64_t* st = a.stat + (static_cast<size_t>(row) * a.S + threadIdx.x) * 2;
-    m = __uint_as_float(static_cast<uint32_t>(get64(st)));
-    z = __longlong_as_double(static_cast<long long>(get64(st + 1)));
-    bad = m != m;
+#pragma unroll 1
+  for (int c0 = 0; c0 < a.S; c0 += 64) {
+    const int c = c0 + lane;
+    float m = -INFINITY;
+    double z = 0.0;
+    int best = 0x7fffffff;
+    if (c < a.S) {
+      const uint64_t u = kFresh ? get64(st + 2 * c) : st[2 * c];
+      z = as_double(kFresh ? get64(st + 2 * c + 1) : st[2 * c + 1]);
+      m = __uint_as_float(static_cast<uint32_t>(u));
+      best = static_cast<int>(u >> 32);
+      bad |= m != m;
+    }
+    // The maximum so far, and the sum scaled to it.
+    float wm = m == m ? m : -INFINITY;
+    const float mine = wm;
+    wave_best(wm, best);
+    const float up = fmaxf(r.m, wm);
+    if (wm > r.m) r.best = best;
+    if (want_z && up > -INFINITY) {
+      const double part = wave_sum(mine > -INFINITY ? z * exp_neg((static_cast<double>(mine) - up) * inv_t) : 0.0);
+      r.z = (r.m > -INFINITY ? r.z * exp_neg((static_cast<double>(r.m) - up) * inv_t) : 0.0) + part;
+    }
+    r.m = up;
   }
-  bad = __syncthreads_or(bad);
-  RowStat r;
-  r.m = group_max(bad ? -INFINITY : m, sm);
-  if (bad || !(fabsf(r.m) <= 3.402823466e38f)) r.m = __uint_as_float(0x7FC00000u);
-  r.z = group_sum(m > -INFINITY ? z * exp((static_cast<double>(m) - r.m) * inv_t) : 0.0, sm);
+  if (__ballot(bad) != 0 || !(fabsf(r.m) <= 3.402823466e38f)) r.m = __uint_as_float(0x7FC00000u);
   return r;
 }
 
@@ -171,42 +251,45 @@ __device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVe
 
 // T: storage of logits and draft_probs (float, or uint16_t for bf16).
 template <class T, int kPhase>
-__global__ __launch_bounds__(256) void k_tree_verify(TreeVerifyArgs a) {
-  using Regs = VChunkRegs<T>;
-  constexpr int EV = Regs::EV, NJ = Regs::NJ;
+__global__ __launch_bounds__(kVThreads, 8) void k_tree_verify(TreeVerifyArgs a) {
   __shared__ TreeVerifySmem sm;
   const int chunk = blockIdx.x, row = a.list[blockIdx.y], i = a.req[row];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float temp = a.temp[i];
   const double inv_t = temp > 0.f ? 1.0 / static_cast<double>(temp) : 1.0;
-  float x[NJ][EV];
-  Regs::load(static_cast<const T*>(a.logits) + row * a.ls, a.V, chunk, a.vec_l, -INFINITY, x);
+  float x[kVOwn];
+  load_chunk(static_cast<const T*>(a.logits) + row * a.ls, a.V, chunk, a.vec_l, -INFINITY, x);
   if constexpr (kPhase == kStats) {
+    // Maximum with the lowest index that has it; a NaN anywhere makes it NaN.
     float m = -INFINITY;
     bool nan = false;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-      for (int e = 0; e < EV; ++e) {
-        nan |= x[j][e] != x[j][e];
-        m = fmaxf(m, x[j][e]);
-      }
-    nan = __syncthreads_or(nan);
-    m = group_max(m, &sm);
-    int best = 0x7fffffff;
-#pragma unroll
-    for (int j = NJ - 1; j >= 0; --j)
-#pragma unroll
-      for (int e = EV - 1; e >= 0; --e)
-        if (x[j][e] == m) best = min(best, Regs::index(chunk, j, e));
-    best = group_min(best, &sm);
-    double s = 0.0;
-    if (temp > 0.f && m > -INFINITY && m < INFINITY) {
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-#pragma unroll
-        for (int e = 0; e < EV; ++e) s += exp((static_cast<double>(x[j][e]) - m) * inv_t);
+    for (int e = 0; e < kVOwn; ++e) {
+      nan |= x[e] != x[e];
+      m = fmaxf(m, x[e]);
     }
-    s = group_sum(s, &sm);
+    int best = 0;
+#pragma unroll
+    for (int e = kVOwn - 1; e >= 0; --e) best = x[e] == m ? e : best;
+    best += chunk_index(chunk);
+    wave_best(m, best);
+    if (lane == 0) {
+      sm.f[wave] = m;
+      sm.i[wave] = best;
+    }
+    nan = __syncthreads_or(nan);
+    m = -INFINITY;
+    best = 0x7fffffff;
+#pragma unroll
+    for (int w = 0; w < kVWaves; ++w) better_of(m, best, sm.f[w], sm.i[w]);
+    double s = 0.0;
+    if (temp > 0.f) {
+      if (m > -INFINITY && m < INFINITY && !nan) {
+#pragma unroll
+        for (int e = 0; e < kVOwn; ++e) s += exp_neg((static_cast<double>(x[e]) - m) * inv_t);
+      }
+      s = group_sum(s, &sm);
+    }
     if (threadIdx.x == 0) {
       uint64_t* st = a.stat + (static_cast<size_t>(row) * a.S + chunk) * 2;
       const float mm = nan ? __uint_as_float(0x7FC00000u) : m;
@@ -214,22 +297,20 @@ __global__ __launch_bounds__(256) void k_tree_verify(TreeVerifyArgs a) {
       put64(st + 1, static_cast<uint64_t>(__double_as_longlong(s)));
     }
   } else {
-    float q[NJ][EV];
-    Regs::load(static_cast<const T*>(a.draft) + row * a.ds, a.V, chunk, a.vec_d, 0.f, q);
-    const RowStat st = row_stat(a, row, inv_t, &sm);
+    float q[kVOwn];
+    load_chunk(static_cast<const T*>(a.draft) + row * a.ds, a.V, chunk, a.vec_d, 0.f, q);
+    const RowStat st = row_stat<false>(a, row, inv_t, true);
     // c_k = 1 + N_1 + ... + N_{k-1}: all parts that the earlier passes left.
     const double* rest = a.rest + static_cast<size_t>(a.rest0[row]) * a.S;
     double c = 0.0;
-    for (int t = threadIdx.x; t < (a.k - 1) * a.S; t += 256) c += get_double(rest + t);
-    c = 1.0 + group_sum(c, &sm);
+    for (int t = lane; t < (a.k - 1) * a.S; t += 64) c += rest[t];
+    c = 1.0 + wave_sum(c);
     double s = 0.0;
     if (st.m == st.m) {
       const double inv_z = 1.0 / st.z;
 #pragma unroll
-      for (int j = 0; j < NJ; ++j)
-#pragma unroll
-        for (int e = 0; e < EV; ++e)
-          s += fmax(exp((static_cast<double>(x[j][e]) - st.m) * inv_t) * inv_z - c * draft_value(q[j][e]), 0.0);
+      for (int e = 0; e < kVOwn; ++e)
+        s += fmax(exp_neg((static_cast<double>(x[e]) - st.m) * inv_t) * inv_z - c * draft_value(q[e]), 0.0);
     }
     s = group_sum(s, &sm);
     if (threadIdx.x == 0)
@@ -247,153 +328,94 @@ __global__ __launch_bounds__(256) void k_tree_verify(TreeVerifyArgs a) {
   tree_walk<T>(a, i, &sm);
 }
 
-// Draw from one chunk: the lowest entry whose cumulative weight, from `base`
-// on, exceeds `target`; else its last entry of positive weight.  w: this
-// thread's weights in the chunk's register order.
-template <class T>
-__device__ __forceinline__ int draw_in_chunk(int chunk, const double (*w)[VChunkRegs<T>::EV], double base,
-                                             double target, TreeVerifySmem* sm) {
-  using Regs = VChunkRegs<T>;
-  constexpr int EV = Regs::EV, NJ = Regs::NJ;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (threadIdx.x == 0) {
-    sm->hit = 0x7fffffff;
-    sm->tail = -1;
-  }
-#pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    double own = 0.0;
-#pragma unroll
-    for (int e = 0; e < EV; ++e) own += w[j][e];
-    double scan = own;
-    for (int o = 1; o < 64; o <<= 1) {
-      const double up = __shfl_up(scan, o);
-      if (lane >= o) scan += up;
-    }
-    __syncthreads();
-    if (lane == 63) sm->d[wave] = scan;
-    __syncthreads();
-    double at = base + (scan - own);
-    for (int v = 0; v < wave; ++v) at += sm->d[v];
-#pragma unroll
-    for (int e = 0; e < EV; ++e) {
-      at += w[j][e];
-      if (w[j][e] > 0.0) {
-        if (at > target) atomicMin(&sm->hit, Regs::index(chunk, j, e));
-        atomicMax(&sm->tail, Regs::index(chunk, j, e));
-      }
-    }
-    base += ((sm->d[0] + sm->d[1]) + sm->d[2]) + sm->d[3];
-  }
-  __syncthreads();
-  return sm->hit != 0x7fffffff ? sm->hit : sm->tail;
-}
-
+// One work-group.  The code is written for its size as much as for its work:
+// it runs in one work-group alone, whose instruction fetches nothing hides
+// (unrolled, 32000 entries and one draw took 45 us; this form, see below).
 template <class T>
 __device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVerifySmem* sm) {
-  using Regs = VChunkRegs<T>;
-  constexpr int EV = Regs::EV, NJ = Regs::NJ;
   const int row0 = a.row0[i], nn = a.nodes[i], tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float temp = a.temp[i];
   const bool greedy = !(temp > 0.f), drafted = a.draft != nullptr && !greedy;
   const double inv_t = greedy ? 1.0 : 1.0 / static_cast<double>(temp);
   const T* logits = static_cast<const T*>(a.logits);
   const T* draft = static_cast<const T*>(a.draft);
+  const int base0 = a.rest0[row0];
 
-  // Totals of every node's row, 16 lanes per node.
-  for (int j0 = 0; j0 < nn; j0 += 16) {
-    const int j = j0 + tid / 16, row = row0 + min(j, nn - 1);
-    float m = -INFINITY;
-    int best = 0x7fffffff;
-    bool bad = false;
-    for (int c = tid % 16; c < a.S; c += 16) {
-      const uint64_t u = get64(a.stat + (static_cast<size_t>(row) * a.S + c) * 2);
-      const float mc = __uint_as_float(static_cast<uint32_t>(u));
-      bad |= mc != mc;
-      better_of(m, best, mc, static_cast<int>(u >> 32));
-    }
-    for (int o = 8; o >= 1; o >>= 1) {
-      better_of(m, best, __shfl_xor(m, o), __shfl_xor(best, o));
-      bad |= __shfl_xor(static_cast<int>(bad), o) != 0;
-    }
-    bad |= !(fabsf(m) <= 3.402823466e38f);
-    double z = 0.0;
-    for (int c = tid % 16; c < a.S && !bad; c += 16) {
-      const uint64_t* st = a.stat + (static_cast<size_t>(row) * a.S + c) * 2;
-      const float mc = __uint_as_float(static_cast<uint32_t>(get64(st)));
-      const double zc = __longlong_as_double(static_cast<long long>(get64(st + 1)));
-      if (mc > -INFINITY) z += zc * exp((static_cast<double>(mc) - m) * inv_t);
-    }
-    for (int o = 8; o >= 1; o >>= 1) z += __shfl_xor(z, o);
-    // c_k and N_k at the node, k = 0 .. children, to the child of rank k.
-    double cc = 0.0, cn = 1.0;
-    const int kids = a.kids[row];
-    for (int k = 0;; ++k) {
-      if (tid % 16 == 0 && j < nn) {
-        if (k == kids) {
-          sm->fc[j] = cc;
-          sm->fn[j] = cn;
-        } else {
-          for (int t = j + 1; t < nn; ++t) {
-            if (a.parent[row0 + t] == j && a.rank[row0 + t] == k) {
-              sm->cc[t] = cc;
-              sm->cn[t] = cn;
-            }
-          }
-        }
-      }
-      if (k == kids || !drafted) break;
-      cc += cn;
-      cn = 0.0;
-      const double* rest = a.rest + (static_cast<size_t>(a.rest0[row]) + k) * a.S;
-      for (int c = tid % 16; c < a.S; c += 16) cn += get_double(rest + c);
-      for (int o = 8; o >= 1; o >>= 1) cn += __shfl_xor(cn, o);
-    }
-    if (tid % 16 == 0 && j < nn) {
-      sm->m[j] = m;
-      sm->z[j] = z;
-      sm->best[j] = best;
-      sm->bad[j] = bad;
+  // Lane = node, in every wave: token, uniform, and its entries of the
+  // parent's rows, loaded while the totals below are.
+  const int j = min(lane, nn - 1);
+  const int par = lane < nn ? a.parent[row0 + j] : -1;
+  const bool child = par >= 0;
+  const int t = child ? a.tok[row0 + j] : -1;
+  const bool ranged = child && t >= 0 && t < a.V;
+  float xt = 0.f, qt = 0.f, u = 0.f;
+  if (ranged && !greedy) {
+    u = a.accept[row0 + j];
+    xt = vocab_value(logits[(row0 + par) * a.ls + t]);
+    if (drafted) qt = vocab_value(draft[(row0 + par) * a.ds + t]);
+  }
+  if (wave == 0 && lane < nn) {
+    sm->tok[lane] = t;
+    sm->parent[lane] = static_cast<int8_t>(par);
+    if (child && !ranged) raise_check(a.err, kErrTokenRange);
+  }
+  // Totals: rows by waves, then the arrays of parts (one per child) likewise.
+#pragma unroll 1
+  for (int r = wave; r < nn; r += kVWaves) {
+    const RowStat st = row_stat<true>(a, row0 + r, inv_t, !greedy);
+    if (lane == 0) {
+      sm->m[r] = st.m;
+      sm->z[r] = st.z;
+      sm->best[r] = st.best;
     }
   }
-  if (tid < nn) {
-    const int t = tid > 0 ? a.tok[row0 + tid] : -1;
-    sm->tok[tid] = t;
-    if (tid > 0 && (t < 0 || t >= a.V)) raise_check(a.err, kErrTokenRange);
+  if (drafted) {
+#pragma unroll 1
+    for (int r = wave; r < nn - 1; r += kVWaves) {
+      double s = 0.0;
+      for (int c = lane; c < a.S; c += 64) s += get_double(a.rest + (static_cast<size_t>(base0) + r) * a.S + c);
+      s = wave_sum(s);
+      if (lane == 0) sm->total[r] = s;
+    }
   }
   __syncthreads();
-  const int j = min(lane, nn - 1);  // every wave: lane = node
-  const int par = lane < nn ? a.parent[row0 + j] : -1;
-  const int t = sm->tok[j];
-  const bool child = par >= 0, ranged = child && t >= 0 && t < a.V;
+  const float pm = child ? sm->m[par] : 0.f;
   double px = 0.0;
-  if (!greedy && ranged && !sm->bad[par])
-    px = exp((static_cast<double>(Regs::value(logits[(row0 + par) * a.ls + t])) - sm->m[par]) * inv_t) / sm->z[par];
+  if (ranged && !greedy && pm == pm) px = exp_neg((static_cast<double>(xt) - pm) * inv_t) / sm->z[par];
   if (wave == 0 && lane < nn) sm->px[lane] = px;
   __syncthreads();
-  bool ok = false, again = false;
+  bool ok = false;
   if (ranged && greedy) {
     ok = t == sm->best[par];
-  } else if (ranged) {
-    const double u = a.accept[row0 + j];
-    if (drafted) {
-      const double qx = draft_value(Regs::value(draft[(row0 + par) * a.ds + t]));
-      ok = u * qx * sm->cn[j] < fmax(px - sm->cc[j] * qx, 0.0);
-    } else {
-      // Earlier siblings' tokens are gone, each token once.
-      double left = 1.0;
-      for (int s = 1; s < j; ++s) {
-        if (a.parent[row0 + s] != par) continue;
-        if (sm->tok[s] == t) again = true;
-        bool first = true;
-        for (int r = 1; r < s; ++r) first &= a.parent[row0 + r] != par || sm->tok[r] != sm->tok[s];
-        if (first) left -= sm->px[s];
-      }
-      ok = !again && u * left < px;
+  } else if (ranged && drafted) {
+    // c_k and N_k of its rank at the parent.
+    double c = 0.0, n = 1.0;
+    const int r0 = a.rest0[row0 + par] - base0, rank = a.rank[row0 + j];
+#pragma unroll 1
+    for (int k = 0; k < rank; ++k) {
+      c += n;
+      n = sm->total[r0 + k];
     }
+    const double qx = draft_value(qt);
+    ok = static_cast<double>(u) * qx * n < fmax(px - c * qx, 0.0);
+  } else if (ranged) {
+    // Earlier siblings' tokens are gone, each token once.
+    double left = 1.0;
+    bool again = false;
+#pragma unroll 1
+    for (int s = 1; s < j; ++s) {
+      if (sm->parent[s] != par) continue;
+      bool first = sm->tok[s] != t;
+      again |= !first;
+#pragma unroll 1
+      for (int r = 1; r < s && first; ++r) first = sm->parent[r] != par || sm->tok[r] != sm->tok[s];
+      if (first) left -= sm->px[s];
+    }
+    ok = !again && static_cast<double>(u) * left < px;
   }
   // The path: from the root, the first accepted child each time.
-  const uint64_t oks = __ballot(ok && lane < nn), bads = __ballot(lane < nn && sm->bad[j] != 0);
+  const float mine = sm->m[j];
+  const uint64_t oks = __ballot(ok && lane < nn), bads = __ballot(lane < nn && mine != mine);
   int node = 0, steps = 0;
   bool failed = false;
   for (;;) {
@@ -420,98 +442,147 @@ __device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVe
   int drawn = sm->best[node];
   if (!greedy) {
     const int row = row0 + node, kids = a.kids[row];
-    const float m = static_cast<float>(sm->m[node]);
-    const T* lrow = logits + row * a.ls;
-    // Chunk sums of the weights: of p (times the row's sum), or what the
-    // rejections left of it.
-    const bool rested = drafted && kids > 0 && sm->fn[node] > 0.0;
-    float x[NJ][EV], q[NJ][EV];
-    double w[NJ][EV];
-    const auto weights = [&](int chunk, bool skip) {
-      Regs::load(lrow, a.V, chunk, a.vec_l, -INFINITY, x);
-      if (rested) Regs::load(draft + row * a.ds, a.V, chunk, a.vec_d, 0.f, q);
-      const double inv_z = 1.0 / sm->z[node], c = sm->fc[node];
-      double sum = 0.0;
-#pragma unroll
-      for (int jj = 0; jj < NJ; ++jj)
-#pragma unroll
-        for (int e = 0; e < EV; ++e) {
-          double v = exp((static_cast<double>(x[jj][e]) - m) * inv_t);
-          if (rested) v = fmax(v * inv_z - c * draft_value(q[jj][e]), 0.0);
-          w[jj][e] = v;
-        }
-      if (skip) {  // without the children's tokens
-        for (int s = 1; s < nn; ++s) {
-          if (a.parent[row0 + s] != node) continue;
-          const int gone = sm->tok[s];
-#pragma unroll
-          for (int jj = 0; jj < NJ; ++jj)
-#pragma unroll
-            for (int e = 0; e < EV; ++e)
-              if (Regs::index(chunk, jj, e) == gone) w[jj][e] = 0.0;
-        }
+    const float m = sm->m[node];
+    const double inv_z = 1.0 / sm->z[node];
+    // What the draw takes: p (times its row's sum) without the rejected
+    // tokens, or max(p - c q, 0) after all the children.
+    double c = 0.0, left = 1.0;
+    const int r0 = a.rest0[row] - base0;
+    if (drafted) {
+#pragma unroll 1
+      for (int k = 0; k < kids; ++k) {
+        c += left;
+        left = sm->total[r0 + k];
       }
-#pragma unroll
-      for (int jj = 0; jj < NJ; ++jj)
-#pragma unroll
-        for (int e = 0; e < EV; ++e) sum += w[jj][e];
-      return sum;
-    };
-    const auto chunk_sums = [&](bool use_rest) {
+    }
+    const bool rested = drafted && kids > 0 && left > 0.0;
+    bool skip = !drafted && kids > 0;
+    // Chunk sums of the weights.
+    const auto chunk_sums = [&](bool parts, bool without) {
       __syncthreads();
       if (tid < a.S) {
-        if (use_rest) {
-          sm->w[tid] = get_double(a.rest + (static_cast<size_t>(a.rest0[row]) + kids - 1) * a.S + tid);
+        double w;
+        if (parts) {
+          w = get_double(a.rest + (static_cast<size_t>(base0) + r0 + kids - 1) * a.S + tid);
         } else {
           const uint64_t* st = a.stat + (static_cast<size_t>(row) * a.S + tid) * 2;
           const float mc = __uint_as_float(static_cast<uint32_t>(get64(st)));
-          const double zc = __longlong_as_double(static_cast<long long>(get64(st + 1)));
-          sm->w[tid] = mc > -INFINITY ? zc * exp((static_cast<double>(mc) - m) * inv_t) : 0.0;
+          const double zc = as_double(get64(st + 1));
+          w = mc > -INFINITY ? zc * exp_neg((static_cast<double>(mc) - m) * inv_t) : 0.0;
         }
+        if (without) {
+          // The rejected tokens' weights (each once) leave their chunk's sum.  A
+          // rejection leaves at least 2^-24 of what was there (accept < 1), so
+          // the difference stays far more exact than the draw's 2^-24 steps.
+#pragma unroll 1
+          for (int s = 1; s < nn; ++s) {
+            const int gone = sm->tok[s];
+            if (sm->parent[s] != node || gone < 0 || gone / kVChunk != tid || gone >= a.V) continue;
+            bool first = true;
+#pragma unroll 1
+            for (int r = 1; r < s; ++r) first &= sm->parent[r] != node || sm->tok[r] != gone;
+            if (first) w -= sm->px[s] * sm->z[node];
+          }
+          w = fmax(w, 0.0);
+        }
+        sm->w[tid] = w;
       }
       __syncthreads();
     };
-    bool skip = !drafted && kids > 0;
-    chunk_sums(rested);
-    if (skip) {
-      // Chunks that hold a rejected token are summed again without it.
-      for (int s = 1; s < nn; ++s) {
-        if (a.parent[row0 + s] != node || sm->tok[s] < 0 || sm->tok[s] >= a.V) continue;
-        const int chunk = sm->tok[s] / kVChunk;
-        bool done = false;
-        for (int r = 1; r < s; ++r)
-          done |= a.parent[row0 + r] == node && sm->tok[r] >= 0 && sm->tok[r] < a.V && sm->tok[r] / kVChunk == chunk;
-        if (done) continue;
-        const double sum = group_sum(weights(chunk, true), sm);
-        if (tid == 0) sm->w[chunk] = sum;
+    double all, target, base;
+    int chunk;
+    // The first chunk whose cumulative sum exceeds the target, by every wave.
+    const auto pick = [&]() {
+      double v[4], own = 0.0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int at = 4 * lane + k;
+        v[k] = at < a.S ? sm->w[at] : 0.0;
+        own += v[k];
       }
-      __syncthreads();
-    }
-    double all = 0.0;
-    for (int c = 0; c < a.S; ++c) all += sm->w[c];
+      const double scan = wave_scan(own);
+      all = lane_value(scan, 63);
+      target = static_cast<double>(a.sample[i]) * all;
+      double at = scan - own, start = 0.0;
+      int hit = -1, some = -1;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (v[k] > 0.0) {
+          some = 4 * lane + k;
+          if (hit < 0 && at + v[k] > target) {
+            hit = 4 * lane + k;
+            start = at;
+          }
+        }
+        at += v[k];
+      }
+      const uint64_t hits = __ballot(hit >= 0), somes = __ballot(some >= 0);
+      if (hits != 0) {
+        const int from = __ffsll(static_cast<unsigned long long>(hits)) - 1;
+        chunk = __builtin_amdgcn_readlane(hit, from);
+        base = lane_value(start, from);
+      } else {  // nothing exceeds it: the last entry of positive weight
+        chunk = somes != 0 ? __builtin_amdgcn_readlane(some, 63 - __clzll(static_cast<long long>(somes))) : 0;
+        base = 0.0;
+        target = INFINITY;
+      }
+    };
+    chunk_sums(rested, skip);
+    pick();
     if (skip && !(all > 0.0)) {  // nothing left: draw from p
       skip = false;
-      chunk_sums(false);
-      all = 0.0;
-      for (int c = 0; c < a.S; ++c) all += sm->w[c];
+      chunk_sums(false, false);
+      pick();
     }
-    double target = static_cast<double>(a.sample[i]) * all;
-    double base = 0.0;
-    int chunk = -1, some = 0;
-    for (int c = 0; c < a.S; ++c) {
-      if (sm->w[c] > 0.0) some = c;
-      if (base + sm->w[c] > target) {
-        chunk = c;
-        break;
+    // The chunk's lowest entry whose cumulative weight exceeds the target (else
+    // its last of positive weight), each thread over its kVOwn.
+    float x[kVOwn], q[kVOwn];
+    load_chunk(logits + row * a.ls, a.V, chunk, a.vec_l, -INFINITY, x);
+    if (rested) load_chunk(draft + row * a.ds, a.V, chunk, a.vec_d, 0.f, q);
+    const int i0 = chunk_index(chunk);
+    if (skip) {  // without the children's tokens
+#pragma unroll 1
+      for (int s = 1; s < nn; ++s) {
+        const int gone = sm->parent[s] == node ? sm->tok[s] - i0 : -1;
+#pragma unroll
+        for (int e = 0; e < kVOwn; ++e) x[e] = gone == e ? -INFINITY : x[e];
       }
-      base += sm->w[c];
     }
-    if (chunk < 0) {  // nothing exceeds it: the last entry of positive weight
-      chunk = some;
-      target = INFINITY;
+    double w[kVOwn], own = 0.0;
+#pragma unroll
+    for (int e = 0; e < kVOwn; ++e) {
+      w[e] = exp_neg((static_cast<double>(x[e]) - m) * inv_t);
+      if (rested) w[e] = fmax(w[e] * inv_z - c * draft_value(q[e]), 0.0);
+      own += w[e];
     }
-    weights(chunk, skip);
-    drawn = draw_in_chunk<T>(chunk, w, base, target, sm);
+    const double scan = wave_scan(own);
+    if (lane == 63) sm->d[wave] = scan;
+    __syncthreads();
+    double at = base + (scan - own);
+#pragma unroll
+    for (int v = 0; v < kVWaves - 1; ++v) at += v < wave ? sm->d[v] : 0.0;
+    int hit = 0x7fffffff, tail = -1;
+#pragma unroll
+    for (int e = 0; e < kVOwn; ++e) {
+      at += w[e];
+      if (w[e] > 0.0) {
+        tail = i0 + e;
+        if (at > target) hit = min(hit, tail);
+      }
+    }
+    const uint64_t hits = __ballot(hit != 0x7fffffff), tails = __ballot(tail >= 0);
+    if (lane == 0) {
+      sm->hit[wave] = sm->tail[wave] = -1;
+      if (hits != 0) sm->hit[wave] = __builtin_amdgcn_readlane(hit, __ffsll(static_cast<unsigned long long>(hits)) - 1);
+      if (tails != 0) sm->tail[wave] = __builtin_amdgcn_readlane(tail, 63 - __clzll(static_cast<long long>(tails)));
+    }
+    __syncthreads();
+    int got = -1;
+#pragma unroll
+    for (int v = 0; v < kVWaves; ++v) got = max(got, sm->tail[v]);
+#pragma unroll
+    for (int v = kVWaves - 1; v >= 0; --v) got = sm->hit[v] >= 0 ? sm->hit[v] : got;
+    if (got >= 0) drawn = got;
   }
   // Accepted tokens and the drawn one, then -1.
   if (tid < nn) {

@@ -16,7 +16,6 @@ from .binding import (KV_BLOCK, SPR_BF16, SPR_ERR_INVALID_ARG, SPR_F32, SproutEr
                       _ptr, load_library)
 
 _DTYPES = {torch.float32: SPR_F32, torch.bfloat16: SPR_BF16}
-_F32P = ctypes.POINTER(ctypes.c_float)
 
 
 def _refuse(msg: str):
@@ -36,7 +35,7 @@ class KVView:
             _refuse("kv view: k, v and the block table must be contiguous")
         if v.device != k.device or block_table.device != k.device:
             _refuse("kv view: k, v and the block table must be on one device")
-        self.k, self.v, self.block_table, self.device = k, v, block_table, k.device
+        self.k, self.v, self.block_table, self.index = k, v, block_table, k.get_device()
         self.head_dim = k.shape[3] // KV_BLOCK
         self.n_kv_heads = k.shape[2]
         self._c = SprKvView(k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], k.shape[0], k.shape[1], k.shape[2],
@@ -58,17 +57,19 @@ class TreeBatch:
         if len(self._a[3]) != int(np.maximum(self._a[2], 0).sum(dtype=np.int64)):
             _refuse("tree batch: parents must have sum(n_nodes) entries")
         self.n, self.rows = n, len(self._a[3])
+        self._floats = ctypes.c_float * n
         self._c = SprTreeBatch(n, *(None if x is None else _ptr(x) for x in self._a))
         self.ref = ctypes.byref(self._c)
 
     def temperatures(self, temperature):
-        """The request temperatures as the C ABI takes them (a list or one number; None: 1)."""
+        """The request temperatures as the C ABI takes them (one number, or one per request; None: 1)."""
         if temperature is None:
             return None
-        t = np.ascontiguousarray(np.broadcast_to(np.asarray(temperature, dtype=np.float32), (self.n,)))
-        p = t.ctypes.data_as(_F32P)
-        p._keep = t
-        return p
+        if not hasattr(temperature, "__len__"):
+            temperature = [temperature] * self.n
+        if len(temperature) != self.n:
+            _refuse("tree batch: one temperature per request")
+        return self._floats(*[float(x) for x in temperature])
 
 
 class TreeOps:
@@ -79,83 +80,94 @@ class TreeOps:
 
     def __init__(self, device: int = 0):
         self.lib = load_library()
+        self.index = device
         self.device = torch.device("cuda", device)
         self.ws = torch.empty(int(self.lib.spr_tree_ops_workspace_bytes()), dtype=torch.uint8, device=self.device)
         self.stream = torch.cuda.current_stream(self.device)
+        self.raw_stream = self.stream.cuda_stream
         self.h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
-            _check(self.lib.spr_tree_ops_init(self.ws.data_ptr(), self.ws.numel(), self.stream.cuda_stream,
-                                              ctypes.byref(self.h)))
+            _check(self.lib.spr_tree_ops_init(self.ws.data_ptr(), self.ws.numel(), self.raw_stream, ctypes.byref(self.h)))
 
     def _enter(self):
+        """Moves the handle to the device's current stream."""
+        if torch._C._cuda_getCurrentRawStream(self.index) == self.raw_stream:
+            return
         s = torch.cuda.current_stream(self.device)
-        if s != self.stream:
-            if not torch.cuda.is_current_stream_capturing():
-                s.wait_stream(self.stream)
-                self.ws.record_stream(s)
-            _check(self.lib.spr_tree_ops_set_stream(self.h, s.cuda_stream))
-            self.stream = s
+        if not torch.cuda.is_current_stream_capturing():
+            s.wait_stream(self.stream)
+            self.ws.record_stream(s)
+        _check(self.lib.spr_tree_ops_set_stream(self.h, s.cuda_stream))
+        self.stream, self.raw_stream = s, s.cuda_stream
 
-    def _need(self, what, t, dtype, shape):
-        if t.device != self.device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
-            _refuse(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}")
+    def _vector(self, what, t, dtype, n):
+        """Address of a contiguous vector of n elements on the handle's device."""
+        if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or t.get_device() != self.index or not t.is_contiguous():
+            _refuse(f"{what} must be a contiguous {dtype} tensor of {n} elements on {self.device}")
         return t.data_ptr()
 
     def attention(self, kv: KVView, layer: int, batch: TreeBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None):
         """Attention of the trees' nodes (spr_tree_attention): q [rows, heads, head_dim], fp32 or bf16, rows at any stride;
         returns out like it."""
-        if q.dim() != 3 or q.shape[0] != batch.rows or q.shape[2] != kv.head_dim or q.dtype not in _DTYPES:
+        hd = kv.head_dim
+        if q.dim() != 3 or q.shape[0] != batch.rows or q.shape[2] != hd or q.dtype not in _DTYPES:
             _refuse("tree attention: q must be [rows, heads, head_dim], fp32 or bf16")
+        rows, heads, _ = q.shape
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(rows, heads, hd)
         elif out.shape != q.shape or out.dtype != q.dtype:
             _refuse("tree attention: out must be like q")
-        hd = kv.head_dim
-        for t in (q, out):
-            if t.device != self.device or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != hd):
-                _refuse(f"tree attention: q and out must be on {self.device} with contiguous rows")
-        if kv.device != self.device:
+        qs, os = self._row_stride(q, heads, hd), self._row_stride(out, heads, hd)
+        if kv.index != self.index:
             _refuse(f"tree attention: the cache must be on {self.device}")
         self._enter()
-        heads = q.shape[1]
-        one = q.shape[0] < 2  # a single row's stride does not matter
-        _check(self.lib.spr_tree_attention(self.h, kv.ref, layer, batch.ref, heads, _DTYPES[q.dtype], q.data_ptr(),
-                                           heads * hd if one else q.stride(0), out.data_ptr(),
-                                           heads * hd if one else out.stride(0)))
+        _check(self.lib.spr_tree_attention(self.h, kv.ref, layer, batch.ref, heads, _DTYPES[q.dtype], q.data_ptr(), qs,
+                                           out.data_ptr(), os))
         return out
+
+    def _row_stride(self, t, heads, hd):
+        row, head, one = t.stride()
+        if t.get_device() != self.index or one != 1 or (heads > 1 and head != hd):
+            _refuse(f"tree attention: q and out must be on {self.device} with contiguous rows")
+        return row if t.shape[0] > 1 else heads * hd  # a single row's stride does not matter
 
     def verify(self, batch: TreeBatch, tokens: torch.Tensor, logits: torch.Tensor, accept: Optional[torch.Tensor] = None,
                sample: Optional[torch.Tensor] = None, draft_probs: Optional[torch.Tensor] = None, temperature=None):
         """Verification (spr_tree_verify): tokens int32 [rows], logits [rows, vocab] (fp32 or bf16, rows at any stride),
         accept fp32 [rows] and sample fp32 [n] uniform in [0, 1), draft_probs like logits.  Returns (emitted, path) int32
         [rows] and count int32 [n]."""
-        if logits.dim() != 2 or logits.shape[0] != batch.rows or logits.dtype not in _DTYPES:
+        rows, n = batch.rows, batch.n
+        if logits.dim() != 2 or logits.shape[0] != rows or logits.dtype not in _DTYPES:
             _refuse("tree verify: logits must be [rows, vocab], fp32 or bf16")
         vocab = logits.shape[1]
-        for t in (logits, draft_probs):
-            if t is None:
-                continue
-            if t.device != self.device or t.dtype != logits.dtype or t.shape != logits.shape or (vocab > 1 and t.stride(1) != 1):
-                _refuse(f"tree verify: logits and draft_probs must be alike, on {self.device}, with contiguous rows")
-        p_tokens = self._need("tree verify: tokens", tokens, torch.int32, (batch.rows,))
-        p_accept = None if accept is None else self._need("tree verify: accept", accept, torch.float32, (batch.rows,))
-        p_sample = None if sample is None else self._need("tree verify: sample", sample, torch.float32, (batch.n,))
-        emitted, path = torch.empty((2, batch.rows), dtype=torch.int32, device=self.device).unbind(0)
-        count = torch.empty(batch.n, dtype=torch.int32, device=self.device)
+        ls = self._vocab_stride(logits, rows, vocab)
+        ds, p_draft = 0, None
+        if draft_probs is not None:
+            if draft_probs.shape != logits.shape or draft_probs.dtype != logits.dtype:
+                _refuse("tree verify: draft_probs must be like logits")
+            ds, p_draft = self._vocab_stride(draft_probs, rows, vocab), draft_probs.data_ptr()
+        p_tokens = self._vector("tree verify: tokens", tokens, torch.int32, rows)
+        p_accept = None if accept is None else self._vector("tree verify: accept", accept, torch.float32, rows)
+        p_sample = None if sample is None else self._vector("tree verify: sample", sample, torch.float32, n)
+        temps = batch.temperatures(temperature)
+        emitted, path, count = tokens.new_empty(2 * rows + n).split((rows, rows, n))
         self._enter()
-        one = batch.rows < 2
-        _check(self.lib.spr_tree_verify(
-            self.h, batch.ref, vocab, _DTYPES[logits.dtype], p_tokens, logits.data_ptr(),
-            vocab if one else logits.stride(0), None if draft_probs is None else draft_probs.data_ptr(),
-            0 if draft_probs is None else vocab if one else draft_probs.stride(0), batch.temperatures(temperature), p_accept,
-            p_sample, emitted.data_ptr(), path.data_ptr(), count.data_ptr()))
+        at = emitted.data_ptr()
+        _check(self.lib.spr_tree_verify(self.h, batch.ref, vocab, _DTYPES[logits.dtype], p_tokens, logits.data_ptr(), ls,
+                                        p_draft, ds, temps, p_accept, p_sample, at, at + 4 * rows, at + 8 * rows))
         return emitted, path, count
+
+    def _vocab_stride(self, t, rows, vocab):
+        row, one = t.stride()
+        if t.get_device() != self.index or (vocab > 1 and one != 1):
+            _refuse(f"tree verify: logits and draft_probs must be on {self.device} with contiguous rows")
+        return row if rows > 1 else vocab
 
     def keep(self, kv: KVView, batch: TreeBatch, path: torch.Tensor, count: torch.Tensor):
         """Closes the trees in every layer of the cache (spr_tree_keep); path and count as verify returns them."""
-        p_path = self._need("tree keep: path", path, torch.int32, (batch.rows,))
-        p_count = self._need("tree keep: count", count, torch.int32, (batch.n,))
-        if kv.device != self.device:
+        p_path = self._vector("tree keep: path", path, torch.int32, batch.rows)
+        p_count = self._vector("tree keep: count", count, torch.int32, batch.n)
+        if kv.index != self.index:
             _refuse(f"tree keep: the cache must be on {self.device}")
         self._enter()
         _check(self.lib.spr_tree_keep(self.h, kv.ref, batch.ref, p_path, p_count))

@@ -140,23 +140,23 @@ def test_launch_split_covers_every_block_within_its_room():
         n = int(rng.integers(1, 65))
         nodes = [int(rng.integers(1, max(2, min(65, 128 // n + 1)))) for _ in range(n)]
         lens = [int(2 ** rng.uniform(0, rng.choice([8, 14, 20, 30]))) for _ in range(n)]
-        G, Hkv, hd, step = int(rng.choice([1, 8, 13, 16])), int(rng.choice([1, 8, 40, 512])), int(rng.choice([64, 128])), int(rng.choice([1, 2]))
+        G, Hkv, hd, step = int(rng.choice([1, 8, 13, 16])), int(rng.choice([1, 8, 40, 512])), int(rng.choice([64, 128])), int(rng.choice([1, 2, 4, 8]))
         floats = int(rng.choice([1 << 18, 1 << 23, 1 << 28]))
         out = np.zeros(70, np.int32)
         b = raw_batch(n, range(n), lens, nodes, sum(([-1] + [0] * (k - 1) for k in nodes), []))
         assert L.sprh_tree_split(ctypes.byref(b), G, Hkv, hd, step, int(rng.choice([256, 1024])), floats, p32(out)) == 0
-        nt, bpw = int(out[0]), int(out[1])
-        assert nt in (1, 2, 4) and bpw >= 1 and bpw % step == 0
+        cw, bps = int(out[0]), int(out[1])
+        assert cw in (16, 32, 64, 128) and bps >= 1 and bps % step == 0
         split = False
         for i in range(n):
-            ncg = -(-nodes[i] * G // (16 * nt))
-            ns = -(-(-(-(lens[i] + nodes[i]) // 16)) // (4 * bpw))
+            ncg = -(-nodes[i] * G // cw)
+            ns = -(-(-(-(lens[i] + nodes[i]) // 16)) // bps)
             assert out[2 + i + 1] - out[2 + i] == ncg * ns
             assert ns <= 128
             split |= ns > 1
         assert out[2] == 0 and out[2 + n] <= 65535
         if split:
-            assert int(out[2 + n]) * Hkv * 16 * nt * (hd + 4) <= floats
+            assert int(out[2 + n]) * Hkv * cw * (hd + 4) <= floats
 
 
 def test_tree_step_bookkeeping():
@@ -222,7 +222,7 @@ def test_python_side_refusals():
     b = TreeBatch(None, None, [2, 1], [-1, 0, -1])
     t = b.temperatures(0.5)
     assert [t[0], t[1]] == [0.5, 0.5] and b.temperatures(None) is None
-    with pytest.raises(ValueError):
+    with pytest.raises(SproutError):
         b.temperatures([1.0, 2.0, 3.0])
 
 
