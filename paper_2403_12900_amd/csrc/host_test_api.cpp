@@ -143,16 +143,17 @@ int sprh_tree_temperatures(int n, const float* temperature, const float* accept,
   return sprk::check_temperatures(n, temperature, accept, sample, "temperatures", &g_err);
 }
 
-// tree_split of a batch: out = {columns per work-group, blocks per split, then item0[0 .. n]}.
+// tree_split of a batch: out = {columns per work-group, blocks per split, then item0[0 .. n], then the launch order}.
 int sprh_tree_split(const spr_tree_batch* b, int G, int Hkv, int hd, int step, int slots, size_t floats, int32_t* out) {
   sprk::TreeInfo t;
   const spr_status st = sprk::parse_tree(b, true, 64, 1 << 27, "split", &t, &g_err);
   if (st != SPR_OK) return st;
-  const int cw = sprk::tree_cols_per_group(t, G);
+  const int cw = sprk::tree_cols_per_group(t, G, 256);
   const sprk::TreeSplit s = sprk::tree_split(t, G, Hkv, hd, cw, step, slots, floats);
   out[0] = cw;
   out[1] = s.bps;
   for (int i = 0; i <= t.n; ++i) out[2 + i] = s.item0[i];
+  for (int i = 0; i < t.n; ++i) out[3 + t.n + i] = s.order[i];
   return SPR_OK;
 }
 

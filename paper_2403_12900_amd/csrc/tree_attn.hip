@@ -57,14 +57,15 @@ hipError_t launch(const TreeAttnCall& c) {
   const int slots = groups_per_cu<KP, IO, HD, CW>() * c.n_cu;
   const TreeSplit sp = tree_split(t, a.G, a.Hkv, HD, CW, CW <= 32 ? 4 * step : step, slots, floats);
   a.bps = sp.bps;
-  for (int i = 0; i < t.n; ++i) {
-    a.slot[i] = t.slot[i];
-    a.len[i] = t.len[i];
-    a.nodes[i] = static_cast<uint8_t>(t.nodes[i]);
-    a.row0[i] = static_cast<uint8_t>(t.row0[i]);
-    a.ncg[i] = sp.ncg[i];
-    a.cg0[i] = sp.cg0[i];
-    a.item0[i] = sp.item0[i];
+  for (int r = 0; r < t.n; ++r) {
+    const int i = sp.order[r];
+    a.slot[r] = t.slot[i];
+    a.len[r] = t.len[i];
+    a.nodes[r] = static_cast<uint8_t>(t.nodes[i]);
+    a.row0[r] = static_cast<uint8_t>(t.row0[i]);
+    a.ncg[r] = sp.ncg[r];
+    a.cg0[r] = sp.cg0[r];
+    a.item0[r] = sp.item0[r];
   }
   a.item0[t.n] = sp.item0[t.n];
   for (int r = 0; r < t.rows; ++r) a.anc[r] = t.anc[r];
@@ -72,14 +73,24 @@ hipError_t launch(const TreeAttnCall& c) {
   return hipGetLastError();
 }
 
+// Columns per work-group by what the registers hold beside the accumulators:
+// three-part queries 64, fp32 ones and bf16 ones of 128 dimensions 128, bf16
+// ones of 64 dimensions 256.
 template <class KP, class IO, int HD>
 hipError_t by_columns(const TreeAttnCall& c) {
-  switch (tree_cols_per_group(*c.tree, c.H / c.kv.n_kv_heads)) {
+  constexpr int most = TreeParts<KP, IO>::q == 3 ? 64 : KP::per16 == 4 || HD == 128 ? 128 : 256;
+  switch (tree_cols_per_group(*c.tree, c.H / c.kv.n_kv_heads, most)) {
     case 16: return launch<KP, IO, HD, 16>(c);
     case 32: return launch<KP, IO, HD, 32>(c);
     case 64: return launch<KP, IO, HD, 64>(c);
-    default: return launch<KP, IO, HD, 128>(c);
+    case 128:
+      if constexpr (most >= 128) return launch<KP, IO, HD, 128>(c);
+      break;
+    case 256:
+      if constexpr (most >= 256) return launch<KP, IO, HD, 256>(c);
+      break;
   }
+  return hipErrorInvalidValue;  // not reached: no more than `most`
 }
 
 template <class KP, class IO>

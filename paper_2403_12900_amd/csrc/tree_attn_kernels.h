@@ -36,7 +36,10 @@
 //                       64 NT columns and a wave's work per byte stays high.
 #pragma once
 
+#include <type_traits>
+
 #include "gemm_kernels.h"
+#include "lds_pipe.h"
 #include "tree_rule.h"
 
 namespace sprk {
@@ -63,6 +66,14 @@ struct TreeAttnArgs {
 };
 static_assert(sizeof(TreeAttnArgs) <= 3584, "kernel arguments");
 
+// Two values rounded to bf16 (nearest even), the first in the low half: one
+// conversion instruction.
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{lo, hi}), bf16x2_t));
+}
+
 // Formats of q and out.  load: per16 values of a row as floats (kRaw: as the
 // 16-byte bf16 fragment piece itself).
 struct TreeIoF32 {
@@ -76,10 +87,8 @@ struct TreeIoBF16 {
   using elem = uint16_t;
   static constexpr bool kRaw = true;
   static __device__ __forceinline__ void store4(const TreeAttnArgs& a, int row, int n0, f32x4_t v) {
-    uint2 o;
-    o.x = f32_to_bf16_bits(v[0]) | static_cast<uint32_t>(f32_to_bf16_bits(v[1])) << 16;
-    o.y = f32_to_bf16_bits(v[2]) | static_cast<uint32_t>(f32_to_bf16_bits(v[3])) << 16;
-    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + row * a.os + n0) = o;
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + row * a.os + n0) =
+        make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
   }
 };
 // Inside a model pass: fp32 queries, and the output as the next projection's
@@ -102,54 +111,42 @@ __device__ __forceinline__ uint4 next_part(float* v) {
     if constexpr (KP::per16 == 4) {
       w[j] = __float_as_uint(v[j]);
     } else {
-      const uint32_t lo = f32_to_bf16_bits(v[2 * j]), hi = f32_to_bf16_bits(v[2 * j + 1]);
-      w[j] = lo | hi << 16;
-      v[2 * j] -= bf16_bits_to_f32(lo);
-      v[2 * j + 1] -= bf16_bits_to_f32(hi);
+      w[j] = bf16_pair(v[2 * j], v[2 * j + 1]);
+      v[2 * j] -= __uint_as_float(w[j] << 16);
+      v[2 * j + 1] -= __uint_as_float(w[j] & 0xFFFF0000u);
     }
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Zeroes the infinite and NaN values of a 16-byte piece; returns whether it
-// had one.
+// A V word without its infinite and NaN values; odd is raised where it had one.
 template <class KP>
-__device__ __forceinline__ bool clean_piece(uint4& u) {
-  bool odd = false;
-  const auto clean = [&](uint32_t x) {
-    if constexpr (KP::per16 == 4) {
-      const bool o = (x & 0x7F800000u) == 0x7F800000u;
-      odd |= o;
-      return o ? 0u : x;
-    } else {
-      const bool lo = (x & 0x7F80u) == 0x7F80u, hi = (x & 0x7F800000u) == 0x7F800000u;
-      odd |= lo || hi;
-      return x & ((lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u));
-    }
-  };
-  u.x = clean(u.x);
-  u.y = clean(u.y);
-  u.z = clean(u.z);
-  u.w = clean(u.w);
-  return odd;
+__device__ __forceinline__ uint32_t clean_word(uint32_t x, uint32_t& odd) {
+  if constexpr (KP::per16 == 4) {
+    const bool o = (x & 0x7F800000u) == 0x7F800000u;
+    odd |= o ? 1u : 0u;
+    return o ? 0u : x;
+  } else {
+    const uint32_t keep = ((x & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((x & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+    odd |= ~keep;
+    return x & keep;
+  }
+}
+template <class KP>
+__device__ __forceinline__ u32x4_t clean_piece(u32x4_t u, uint32_t& odd) {
+  return u32x4_t{clean_word<KP>(u.x, odd), clean_word<KP>(u.y, odd), clean_word<KP>(u.z, odd), clean_word<KP>(u.w, odd)};
 }
 
-// Zeroes the positions of a 16-byte V piece (4 g .. 4 g + 3 of its block) whose
-// bit of keep is clear.
+// A 16-byte V piece (positions 4 g .. 4 g + 3 of its block) without the
+// positions whose bit of keep is clear.
 template <class KP>
-__device__ __forceinline__ void keep_piece(uint4& u, uint32_t keep) {
+__device__ __forceinline__ u32x4_t keep_piece(u32x4_t u, uint32_t keep) {
   if constexpr (KP::per16 == 4) {
-    u.x = keep & 1 ? u.x : 0u;
-    u.y = keep & 2 ? u.y : 0u;
-    u.z = keep & 4 ? u.z : 0u;
-    u.w = keep & 8 ? u.w : 0u;
+    return u32x4_t{keep & 1 ? u.x : 0u, keep & 2 ? u.y : 0u, keep & 4 ? u.z : 0u, keep & 8 ? u.w : 0u};
   } else {
     const uint32_t m01 = (keep & 1 ? 0xFFFFu : 0u) | (keep & 2 ? 0xFFFF0000u : 0u);
     const uint32_t m23 = (keep & 4 ? 0xFFFFu : 0u) | (keep & 8 ? 0xFFFF0000u : 0u);
-    u.x &= m01;
-    u.y &= m23;
-    u.z &= m01;
-    u.w &= m23;
+    return u32x4_t{u.x & m01, u.y & m23, u.z & m01, u.w & m23};
   }
 }
 
@@ -170,25 +167,24 @@ __device__ __forceinline__ uint32_t seen_bits(int pos, int len, uint64_t anc) {
 
 // Infinite and NaN values were zeroed in the products (0 times one must not
 // reach the columns that do not see it): adds p times each of them to the
-// columns that do.  One step's blocks tile[] of one KV head, p and sees as the
+// columns that do.  One step's blocks (tile0, tile1) of one KV head, p and sees as the
 // step's scores are held; values are read again, element by element.
 template <class KP, int HD, int BP>
 __device__ __forceinline__ void add_odd_values(f32x4_t* O, const float (*p)[4], const uint32_t* sees, const void* vc,
-                                               const size_t* tile, const uint32_t* live, int lane) {
+                                               size_t tile0, size_t tile1, const uint32_t* live, int lane) {
   const int h = lane & 15, g = lane >> 4;
 #pragma unroll 1
   for (int t = 0; t < 16 * BP; ++t) {
     const int b = t >> 4, gt = t >> 2 & 3, r = t & 3;
     float pt = 0.f;
     uint32_t st = 0, lt = 0;
-    size_t at = tile[0];
+    const size_t at = b == 0 ? tile0 : tile1;
 #pragma unroll
     for (int k = 0; k < BP; ++k)
       if (k == b) {
         pt = r == 0 ? p[k][0] : r == 1 ? p[k][1] : r == 2 ? p[k][2] : p[k][3];
         st = sees[k];
         lt = live[k];
-        at = tile[k];
       }
     pt = __shfl(pt, h + 16 * gt);
     st = __shfl(static_cast<int>(st), h + 16 * gt) >> r & 1;
@@ -212,35 +208,41 @@ struct TreeStep;
 template <int HD>
 struct TreeStep<BF16, HD> {
   static constexpr int kBlocks = 2, NF = HD / 32, NV = HD / 32;
-  uint4 k[2][NF], v[2][NV];
+  u32x4_t k0[NF], k1[NF], v0[NV], v1[NV];
 
-  __device__ __forceinline__ void load(const void* kc, const void* vc, const size_t* tile, int lane) {
+  static __device__ __forceinline__ const u32x4_t* tile_at(const void* pool, size_t tile, int lane) {
+    return reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(pool) + tile * 16 * HD) + lane;
+  }
+  __device__ __forceinline__ void load_k(const void* kc, size_t t0, size_t t1, int lane) {
+    const u32x4_t *p0 = tile_at(kc, t0, lane), *p1 = tile_at(kc, t1, lane);
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const uint4* kt = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(kc) + tile[b] * 16 * HD) + lane;
-      const uint4* vt = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(vc) + tile[b] * 16 * HD) + lane;
+    for (int f = 0; f < NF; ++f) k0[f] = __builtin_nontemporal_load(p0 + f * 64);
 #pragma unroll
-      for (int f = 0; f < NF; ++f) k[b][f] = kt[f * 64];
+    for (int f = 0; f < NF; ++f) k1[f] = __builtin_nontemporal_load(p1 + f * 64);
+  }
+  __device__ __forceinline__ void load_v(const void* vc, size_t t0, size_t t1, int lane) {
+    const u32x4_t *p0 = tile_at(vc, t0, lane), *p1 = tile_at(vc, t1, lane);
 #pragma unroll
-      for (int f = 0; f < NV; ++f) v[b][f] = vt[f * 64];
-    }
+    for (int f = 0; f < NV; ++f) v0[f] = __builtin_nontemporal_load(p0 + f * 64);
+#pragma unroll
+    for (int f = 0; f < NV; ++f) v1[f] = __builtin_nontemporal_load(p1 + f * 64);
+  }
+  // S[b] += K block b . x for K-block c.
+  __device__ __forceinline__ void qk(f32x4_t* S, int c, const uint4& x) const {
+    S[0] = BF16::mma(S[0], __builtin_bit_cast(uint4, k0[c]), x);
+    S[1] = BF16::mma(S[1], __builtin_bit_cast(uint4, k1[c]), x);
   }
   // Zeroes the values of this lane's positions 4 g + i of block b whose bit i
-  // of keep[b] is clear.
-  __device__ __forceinline__ void keep_v(const uint32_t* keep) {
+  // of keep[b] is clear, and infinite and NaN ones; returns whether this lane
+  // had one of the latter.
+  __device__ __forceinline__ bool mask_v(const uint32_t* keep) {
+    uint32_t odd = 0;
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int f = 0; f < NV; ++f) keep_piece<BF16>(v[b][f], keep[b]);
-  }
-  // Zeroes infinite and NaN values; returns whether this lane had one.
-  __device__ __forceinline__ bool clean_v() {
-    bool odd = false;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int f = 0; f < NV; ++f) odd |= clean_piece<BF16>(v[b][f]);
-    return odd;
+    for (int f = 0; f < NV; ++f) {
+      v0[f] = clean_piece<BF16>(keep_piece<BF16>(v0[f], keep[0]), odd);
+      v1[f] = clean_piece<BF16>(keep_piece<BF16>(v1[f], keep[1]), odd);
+    }
+    return odd != 0;
   }
   template <int PP>
   __device__ __forceinline__ void pv(f32x4_t* O, const float (*p)[4]) const {
@@ -254,8 +256,8 @@ struct TreeStep<BF16, HD> {
     }
 #pragma unroll
     for (int f = 0; f < NV; ++f) {
-      const uint4 a0 = make_uint4(v[0][f].x, v[0][f].y, v[1][f].x, v[1][f].y);
-      const uint4 a1 = make_uint4(v[0][f].z, v[0][f].w, v[1][f].z, v[1][f].w);
+      const uint4 a0 = make_uint4(v0[f].x, v0[f].y, v1[f].x, v1[f].y);
+      const uint4 a1 = make_uint4(v0[f].z, v0[f].w, v1[f].z, v1[f].w);
 #pragma unroll
       for (int q = 0; q < PP; ++q) {
         O[2 * f] = BF16::mma(O[2 * f], a0, b[q]);
@@ -268,34 +270,38 @@ struct TreeStep<BF16, HD> {
 template <int HD>
 struct TreeStep<F32, HD> {
   static constexpr int kBlocks = 1, NF = HD / 16, NV = HD / 16;
-  uint4 k[1][NF], v[1][NV];
+  u32x4_t k[NF], v[NV];
 
-  __device__ __forceinline__ void load(const void* kc, const void* vc, const size_t* tile, int lane) {
-    const uint4* kt = reinterpret_cast<const uint4*>(static_cast<const float*>(kc) + tile[0] * 16 * HD) + lane;
-    const uint4* vt = reinterpret_cast<const uint4*>(static_cast<const float*>(vc) + tile[0] * 16 * HD) + lane;
-#pragma unroll
-    for (int f = 0; f < NF; ++f) k[0][f] = kt[f * 64];
-#pragma unroll
-    for (int f = 0; f < NV; ++f) v[0][f] = vt[f * 64];
+  static __device__ __forceinline__ const u32x4_t* tile_at(const void* pool, size_t tile, int lane) {
+    return reinterpret_cast<const u32x4_t*>(static_cast<const float*>(pool) + tile * 16 * HD) + lane;
   }
-  __device__ __forceinline__ void keep_v(const uint32_t* keep) {
+  __device__ __forceinline__ void load_k(const void* kc, size_t t0, size_t, int lane) {
+    const u32x4_t* p0 = tile_at(kc, t0, lane);
 #pragma unroll
-    for (int f = 0; f < NV; ++f) keep_piece<F32>(v[0][f], keep[0]);
+    for (int f = 0; f < NF; ++f) k[f] = __builtin_nontemporal_load(p0 + f * 64);
   }
-  __device__ __forceinline__ bool clean_v() {
-    bool odd = false;
+  __device__ __forceinline__ void load_v(const void* vc, size_t t0, size_t, int lane) {
+    const u32x4_t* p0 = tile_at(vc, t0, lane);
 #pragma unroll
-    for (int f = 0; f < NV; ++f) odd |= clean_piece<F32>(v[0][f]);
-    return odd;
+    for (int f = 0; f < NV; ++f) v[f] = __builtin_nontemporal_load(p0 + f * 64);
+  }
+  __device__ __forceinline__ void qk(f32x4_t* S, int c, const uint4& x) const {
+    S[0] = F32::mma(S[0], __builtin_bit_cast(uint4, k[c]), x);
+  }
+  __device__ __forceinline__ bool mask_v(const uint32_t* keep) {
+    uint32_t odd = 0;
+#pragma unroll
+    for (int f = 0; f < NV; ++f) v[f] = clean_piece<F32>(keep_piece<F32>(v[f], keep[0]), odd);
+    return odd != 0;
   }
   template <int PP>
   __device__ __forceinline__ void pv(f32x4_t* O, const float (*p)[4]) const {
 #pragma unroll
     for (int f = 0; f < NV; ++f) {
-      O[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[0][f].x), p[0][0], O[f], 0, 0, 0);
-      O[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[0][f].y), p[0][1], O[f], 0, 0, 0);
-      O[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[0][f].z), p[0][2], O[f], 0, 0, 0);
-      O[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[0][f].w), p[0][3], O[f], 0, 0, 0);
+      O[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[f].x), p[0][0], O[f], 0, 0, 0);
+      O[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[f].y), p[0][1], O[f], 0, 0, 0);
+      O[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[f].z), p[0][2], O[f], 0, 0, 0);
+      O[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[f].w), p[0][3], O[f], 0, 0, 0);
     }
   }
 };
@@ -313,6 +319,7 @@ struct TreeSmem {
   union {
     uint4 q[NT][NF][TreeParts<KP, IO>::q][64];
     f32x4_t so[4][HD / 16][64];
+    float weights[kTreeSplits * 16 * NT];
   };
   float2 sml[4][NT][16];
   int last;
@@ -362,15 +369,28 @@ __device__ __forceinline__ void load_query(const TreeAttnArgs& a, const TreeColu
   }
 }
 
-// Online softmax of one column tile's scores of one step: raises the running
-// maximum where needed, turns S into probabilities and adds them to l.
+// Online softmax of one column tile's scores of one step: turns S into
+// probabilities, adds them to l, and raises the running maximum first where a
+// score exceeds it by more than kRaise.  (The test runs on the exponents, which
+// are needed anyway.)
 template <int BP, int NE>
 __device__ __forceinline__ void softmax_step(const f32x4_t* S, float qscale, float& m, float& l, f32x4_t* O, float (*p)[4]) {
-  float mx = fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3]));
+  const auto highest = [](const float (*x)[4]) {
+    float v = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3]));
 #pragma unroll
-  for (int b = 1; b < BP; ++b) mx = fmaxf(mx, fmaxf(fmaxf(S[b][0], S[b][1]), fmaxf(S[b][2], S[b][3])));
-  mx *= qscale;
-  if (__ballot(mx > m + kRaise) != 0) {
+    for (int b = 1; b < BP; ++b) v = fmaxf(fmaxf(v, fmaxf(x[b][0], x[b][1])), fmaxf(x[b][2], x[b][3]));
+    return v;
+  };
+#pragma unroll
+  for (int b = 0; b < BP; ++b)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[b][r] = fmaf(S[b][r], qscale, -m);
+  if (__ballot(highest(p) > kRaise) != 0) {
+#pragma unroll
+    for (int b = 0; b < BP; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p[b][r] = S[b][r] * qscale;
+    float mx = highest(p);
     mx = fmaxf(mx, __shfl_xor(mx, 16));
     mx = fmaxf(mx, __shfl_xor(mx, 32));
     const float up = fmaxf(m, mx);
@@ -379,11 +399,15 @@ __device__ __forceinline__ void softmax_step(const f32x4_t* S, float qscale, flo
     m = up;
 #pragma unroll
     for (int e = 0; e < NE; ++e) O[e] *= alpha;
+#pragma unroll
+    for (int b = 0; b < BP; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p[b][r] = fmaf(S[b][r], qscale, -m);
   }
 #pragma unroll
   for (int b = 0; b < BP; ++b) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) p[b][r] = __builtin_amdgcn_exp2f(fmaf(S[b][r], qscale, -m));
+    for (int r = 0; r < 4; ++r) p[b][r] = __builtin_amdgcn_exp2f(p[b][r]);
     l += (p[b][0] + p[b][1]) + (p[b][2] + p[b][3]);
   }
 }
@@ -429,10 +453,11 @@ __device__ __forceinline__ int block_id(const TreeAttnArgs& a, const int32_t* bt
 
 // Counts a split in and, in the one that arrives last, merges all partials of
 // its column group (CW columns): no work-group waits on another.  The
-// caller's partials are stored (agent-coherent).
+// caller's partials are stored (agent-coherent).  weights: LDS for kTreeSplits
+// * CW floats that no wave reads or writes any more.
 template <class IO, int HD, int CW>
 __device__ __forceinline__ void merge_splits(const TreeAttnArgs& a, const TreeItem& t, int kvh, const CoherentBuffer& pb,
-                                             int* last) {
+                                             int* last, float* weights) {
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's partial stores are complete
   __syncthreads();
   int32_t* cnt = a.cnt + (a.cg0[t.rank] + t.cg) * a.Hkv + kvh;
@@ -443,44 +468,69 @@ __device__ __forceinline__ void merge_splits(const TreeAttnArgs& a, const TreeIt
   if (threadIdx.x == 0) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   const uint32_t base = (static_cast<uint32_t>(a.item0[t.rank] + t.cg) * a.Hkv + kvh) * CW * (HD + 4) * 4;
   const uint32_t stride = static_cast<uint32_t>(t.ncg) * a.Hkv * CW * (HD + 4) * 4;
-  constexpr int kChunk = 8;  // partials read per round
   const int c0 = CW * t.cg, mine = min(t.cols - c0, CW);
-  for (int idx = threadIdx.x; idx < mine * (HD / 4); idx += 256) {
-    const int c = idx / (HD / 4), d0 = idx % (HD / 4) * 4;
-    const uint32_t at = base + c * (HD + 4) * 4;
+  // Weight of each (split, column), exp2(m - M) / L, in LDS: lanes of one
+  // column side by side, kLanes each.
+  constexpr int kLanes = 256 / CW >= 4 ? 256 / CW : 4;
+  for (int c = threadIdx.x / kLanes; c < CW; c += 256 / kLanes) {
+    const uint32_t at = base + min(c, mine - 1) * (HD + 4) * 4;
     float M = kTreeFloor, L = 0.f;
-    f32x4_t R = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int t0 = 0; t0 < t.nsplit; t0 += kChunk) {
-      f32x4_t ml[kChunk], o[kChunk];
+    for (int s = threadIdx.x % kLanes; s < t.nsplit; s += kLanes) {
+      const f32x4_t ml = pb.load4(at + s * stride);
+      const float up = fmaxf(M, ml[0]);
+      L = L * __builtin_amdgcn_exp2f(M - up) + ml[1] * __builtin_amdgcn_exp2f(ml[0] - up);
+      M = up;
+      weights[s * CW + c] = ml[0];
+    }
 #pragma unroll
-      for (int k = 0; k < kChunk; ++k) {
-        const uint32_t b = at + min(t0 + k, t.nsplit - 1) * stride;
-        ml[k] = pb.load4(b);
-        o[k] = pb.load4(b + 16 + d0 * 4);
-      }
-      float up = M;
-#pragma unroll
-      for (int k = 0; k < kChunk; ++k) up = t0 + k < t.nsplit ? fmaxf(up, ml[k][0]) : up;
-      const float sc = __builtin_amdgcn_exp2f(M - up);
-      L *= sc;
-      R *= sc;
-#pragma unroll
-      for (int k = 0; k < kChunk; ++k) {
-        if (t0 + k < t.nsplit) {
-          const float wt = __builtin_amdgcn_exp2f(ml[k][0] - up);
-          L += wt * ml[k][1];
-          R += wt * o[k];
-        }
-      }
+    for (int o = kLanes / 2; o >= 1; o >>= 1) {
+      const float m2 = __shfl_xor(M, o), l2 = __shfl_xor(L, o), up = fmaxf(M, m2);
+      L = L * __builtin_amdgcn_exp2f(M - up) + l2 * __builtin_amdgcn_exp2f(m2 - up);
       M = up;
     }
-    const TreeColumn col = tree_column(a, t.row0, kvh, c0 + c);
-    IO::store4(a, col.row, col.hq * HD + d0, R * (1.f / L));
+    const float inv = 1.f / L;
+    for (int s = threadIdx.x % kLanes; s < t.nsplit; s += kLanes)
+      weights[s * CW + c] = __builtin_amdgcn_exp2f(weights[s * CW + c] - M) * inv;
+  }
+  __syncthreads();
+  // Outputs, 16 bytes each: kItems per thread and kSplits partials of each in flight.
+  constexpr int kItems = CW * HD / 4 / 256 >= 4 ? 4 : CW * HD / 4 / 256, kChunk = 4;
+  for (int x0 = threadIdx.x; x0 < mine * (HD / 4); x0 += 256 * kItems) {
+    f32x4_t R[kItems];
+    uint32_t at[kItems];
+    int c[kItems];
+#pragma unroll
+    for (int n = 0; n < kItems; ++n) {
+      const int idx = min(x0 + 256 * n, mine * (HD / 4) - 1);
+      c[n] = idx / (HD / 4);
+      at[n] = base + (c[n] * (HD + 4) + 4 + idx % (HD / 4) * 4) * 4;
+      R[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int s0 = 0; s0 < t.nsplit; s0 += kChunk) {
+      f32x4_t o[kItems][kChunk];
+#pragma unroll
+      for (int k = 0; k < kChunk; ++k)
+#pragma unroll
+        for (int n = 0; n < kItems; ++n) o[n][k] = pb.load4(at[n] + min(s0 + k, t.nsplit - 1) * stride);
+#pragma unroll
+      for (int k = 0; k < kChunk; ++k)
+        if (s0 + k < t.nsplit) {
+#pragma unroll
+          for (int n = 0; n < kItems; ++n) R[n] += weights[(s0 + k) * CW + c[n]] * o[n][k];
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < kItems; ++n) {
+      const int idx = x0 + 256 * n;
+      if (idx >= mine * (HD / 4)) break;
+      const TreeColumn col = tree_column(a, t.row0, kvh, c0 + c[n]);
+      IO::store4(a, col.row, col.hq * HD + idx % (HD / 4) * 4, R[n]);
+    }
   }
 }
 
 template <class KP, class IO, int HD, int NT>
-__global__ __launch_bounds__(256) void k_tree_attn(TreeAttnArgs a) {
+__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_tree_attn(TreeAttnArgs a) {
   using Step = TreeStep<KP, HD>;
   using Parts = TreeParts<KP, IO>;
   constexpr int BP = Step::kBlocks, NF = Step::NF, NE = HD / 16, EPW = NE / 4, CW = 16 * NT;
@@ -521,52 +571,69 @@ __global__ __launch_bounds__(256) void k_tree_attn(TreeAttnArgs a) {
     for (int e = 0; e < NE; ++e) O[jt][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
+  // The step's K registers take the next step's keys as soon as its scores are
+  // there, the V registers the next values after its products: a wave always
+  // has loads in flight, in the registers of one step.
+  Step B;
+  size_t t0 = 0, t1 = 0;  // tiles of the blocks that are being loaded
+  const auto block_tile = [&](int i) {
+    return static_cast<size_t>(__builtin_amdgcn_readlane(ids, (i - lo) & 63)) * a.Hkv + kvh;
+  };
+  const auto next_tiles = [&](int i) {
+    if (((i - lo) & 63) == 0 && i != lo) ids = block_id(a, t.btrow, i + lane, hi);
+    t0 = block_tile(i);
+    if constexpr (BP == 2) t1 = block_tile(i + 1 < hi ? i + 1 : i);  // a missing second block re-reads the first, masked
+  };
+  if (lo < hi) {
+    next_tiles(lo);
+    B.load_k(a.kc, t0, t1, lane);
+    B.load_v(a.vc, t0, t1, lane);
+  }
   for (int i = lo; i < hi; i += BP) {
-    const int k = i - lo;
-    if ((k & 63) == 0 && k != 0) ids = block_id(a, t.btrow, i + lane, hi);
-    Step B;
-    size_t tile[BP];
-#pragma unroll
-    for (int b = 0; b < BP; ++b)  // a missing second block re-reads the first, masked
-      tile[b] = static_cast<size_t>(__builtin_amdgcn_readlane(ids, (i + b < hi ? k + b : k) & 63)) * a.Hkv + kvh;
-    B.load(a.kc, a.vc, tile, lane);
-    // A step that reaches past the cached positions or the run is masked.
-    const bool tail = 16 * (i + BP) > t.len || i + BP > hi;
-    uint32_t live[BP];  // bits: this lane's positions of the block that hold a cached position or a node
-    bool odd = false;
-    if (tail) {
-#pragma unroll
-      for (int b = 0; b < BP; ++b) live[b] = i + b < hi ? live_bits(16 * (i + b) + 4 * g, t.total) : 0u;
-      B.keep_v(live);
-      odd = __ballot(B.clean_v()) != 0;
-    }
+    const bool more = i + BP < hi;
+    f32x4_t S[NT][BP];
 #pragma unroll
     for (int jt = 0; jt < NT; ++jt) {
-      f32x4_t S[BP];
 #pragma unroll
-      for (int b = 0; b < BP; ++b) S[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int b = 0; b < BP; ++b) S[jt][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < NF; ++c)
 #pragma unroll
         for (int q = 0; q < Parts::q; ++q) {
-          const uint4 x = sm.q[jt][c][q][lane];
-#pragma unroll
-          for (int b = 0; b < BP; ++b) S[b] = KP::mma(S[b], B.k[b][c], x);
+          B.qk(S[jt], c, sm.q[jt][c][q][lane]);
         }
-      uint32_t sees[BP];
-      if (tail) {
+    }
+    const size_t now0 = t0, now1 = t1;
+    if (more) {
+      next_tiles(i + BP);
+      B.load_k(a.kc, t0, t1, lane);
+    }
+    // A step that reaches past the cached positions or the run is masked.
+    const bool tail = 16 * (i + BP) > t.len || i + BP > hi;
+    uint32_t live[BP], sees[NT][BP];  // bits of this lane's positions: cached or a node; seen by the column
+    bool odd = false;
+    if (tail) {
 #pragma unroll
-        for (int b = 0; b < BP; ++b) {
-          sees[b] = live[b] & seen_bits(16 * (i + b) + 4 * g, t.len, anc[jt]);
+      for (int b = 0; b < BP; ++b) {
+        const int pos = 16 * (i + b) + 4 * g;
+        live[b] = i + b < hi ? live_bits(pos, t.total) : 0u;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) S[b][r] = sees[b] >> r & 1 ? S[b][r] : -INFINITY;
+        for (int jt = 0; jt < NT; ++jt) {
+          sees[jt][b] = live[b] & seen_bits(pos, t.len, anc[jt]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) S[jt][b][r] = sees[jt][b] >> r & 1 ? S[jt][b][r] : -INFINITY;
         }
       }
-      float p[BP][4];
-      softmax_step<BP, NE>(S, a.qscale, m[jt], l[jt], O[jt], p);
-      B.template pv<Parts::p>(O[jt], p);
-      if (odd) add_odd_values<KP, HD, BP>(O[jt], p, sees, a.vc, tile, live, lane);
+      odd = __ballot(B.mask_v(live)) != 0;
     }
+#pragma unroll
+    for (int jt = 0; jt < NT; ++jt) {
+      float p[BP][4];
+      softmax_step<BP, NE>(S[jt], a.qscale, m[jt], l[jt], O[jt], p);
+      B.template pv<Parts::p>(O[jt], p);
+      if (odd) add_odd_values<KP, HD, BP>(O[jt], p, sees[jt], a.vc, now0, now1, live, lane);
+    }
+    if (more) B.load_v(a.vc, t0, t1, lane);
   }
 
   // Merge of the four waves, column tile by column tile; wave w combines and
@@ -618,31 +685,37 @@ __global__ __launch_bounds__(256) void k_tree_attn(TreeAttnArgs a) {
       }
     }
   }
-  if (t.nsplit > 1) merge_splits<IO, HD, CW>(a, t, kvh, pb, &sm.last);
+  if (t.nsplit > 1) merge_splits<IO, HD, CW>(a, t, kvh, pb, &sm.last, sm.weights);
 }
 
 // ---------------------------------------------------------------------------
 
-// K and V blocks of one step in LDS, [K block 0][K block 1]..[V block 0].., each
-// in its tile's order, two steps deep.
+// One step's blocks in LDS, two steps deep: the K tiles in their own order
+// (fragment by fragment), then the V operands.  For bf16 an operand's lane
+// holds its 8 bytes of block 0 and of block 1 side by side, as the 16x16x32
+// product takes them.
 template <class KP, int HD>
 struct TreeStage {
   static constexpr int BP = KP::per16 == 8 ? 2 : 1;
   static constexpr int kTile = 16 * HD * static_cast<int>(sizeof(typename KP::elem)) / 16;  // 16-byte pieces of a tile
   static constexpr int kPieces = 2 * BP * kTile;                                             // of a step
   static constexpr int kPer = kPieces / 256;                                                 // per thread
+  static_assert(kPer >= 2 && (kTile % 256 == 0 || kTile == 128), "pieces of a wave lie in one tile");
 };
 
 // Work-group: a request's column group of 64 NT columns (16 NT per wave) over
-// the blocks of one split.  The blocks of step s + 1 are on their way into
-// registers while step s is computed from LDS, and go to the other LDS buffer
-// after it: one barrier per step.
+// the blocks of one split.  While a step is computed from LDS, the next one's
+// blocks lie in registers or arrive there, and the one's after it are asked
+// for; after the step the next one goes to the other LDS buffer: one barrier
+// per step.  Steps that reach past the cached positions or the split (the last
+// few) run masked, the others without a test.
 template <class KP, class IO, int HD, int NT>
-__global__ __launch_bounds__(256) void k_tree_attn_shared(TreeAttnArgs a) {
+__global__ __launch_bounds__(256, (NT == 1 && TreeParts<KP, IO>::q == 1 ? 3 : 2)) void k_tree_attn_shared(TreeAttnArgs a) {
   using Stage = TreeStage<KP, HD>;
   using Parts = TreeParts<KP, IO>;
-  constexpr int BP = Stage::BP, NF = HD / KP::kblk, NV = Stage::kTile / 64, NE = HD / 16, CW = 64 * NT;
-  __shared__ uint4 buf[2][Stage::kPieces];
+  constexpr int BP = Stage::BP, NF = HD / KP::kblk, NE = HD / 16, CW = 64 * NT;
+  // Two steps, or the weights of the merge.
+  __shared__ uint4 lds[2 * Stage::kPieces >= kTreeSplits * CW / 4 ? 2 * Stage::kPieces : kTreeSplits * CW / 4];
   __shared__ int odd_s[2], last;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -671,131 +744,172 @@ __global__ __launch_bounds__(256) void k_tree_attn_shared(TreeAttnArgs a) {
     for (int e = 0; e < NE; ++e) O[jt][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  int ids = 0;
-  uint4 next[Stage::kPer];
-  // Pieces of the step from block i on: this thread's 16 bytes of each 4 KiB.
-  const auto fetch = [&](int i) {
+  // Piece r of this thread: piece r * 256 + tid of the step, in tile r * 256 /
+  // kTile (of 128 pieces: plus the wave's half); K tiles first.
+  const int half = Stage::kTile == 128 ? wave >> 1 : 0;
+  const int in_tile = tid % Stage::kTile;
+  constexpr int kRounds = Stage::kTile >= 256 ? Stage::kTile / 256 : 1;  // rounds of 256 pieces per tile
+  const auto round_tile = [&](int r) { return Stage::kTile == 128 ? 2 * r + half : r / kRounds; };
+  const auto round_piece = [&](int r) { return in_tile + (r % kRounds) * 256; };
+
+  // Byte offsets of the next 64 blocks' tiles of this KV head, one per lane.
+  uint64_t off = 0;
+  u32x4_t next[2][Stage::kPer];  // of even and odd steps
+  const auto fetch = [&](int i, auto parity) {
     const int k = i - t.first;
-    if ((k & 63) == 0) ids = block_id(a, t.btrow, i + lane, end);
+    if ((k & 63) == 0)
+      off = (static_cast<uint64_t>(block_id(a, t.btrow, i + lane, end)) * a.Hkv + kvh) * (Stage::kTile * 16);
+    uint64_t at[BP];
+#pragma unroll
+    for (int b = 0; b < BP; ++b) {
+      const int from = (i + b < end ? k + b : k) & 63;  // a missing second block re-reads the first, masked
+      at[b] = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(off), from)) |
+              static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(off >> 32), from))) << 32;
+    }
 #pragma unroll
     for (int r = 0; r < Stage::kPer; ++r) {
-      const int piece = r * 256 + tid;
-      // The tile is the same for all lanes of a wave.
-      const int which = __builtin_amdgcn_readfirstlane(piece / Stage::kTile), b = which % BP;
-      const size_t tile = static_cast<size_t>(__builtin_amdgcn_readlane(ids, (i + b < end ? k + b : k) & 63)) * a.Hkv + kvh;
-      const char* base = static_cast<const char*>(which < BP ? a.kc : a.vc) + tile * Stage::kTile * 16;
-      next[r] = reinterpret_cast<const uint4*>(base)[piece % Stage::kTile];
+      const int which = round_tile(r);
+      const char* pool = static_cast<const char*>(r * 256 / Stage::kTile < BP ? a.kc : a.vc);
+      const char* base = pool + (BP == 2 && which % 2 == 1 ? at[BP - 1] : at[0]);
+      next[decltype(parity)::value][r] = reinterpret_cast<const u32x4_t*>(base)[round_piece(r)];
     }
   };
-  // Into LDS; V pieces of a masked step without stale positions and without
-  // infinite or NaN values.
-  const auto put = [&](int i, int to) {
-    bool odd = false;
-    const bool tail = 16 * (i + BP) > t.len || i + BP > end;
+  // Into LDS.  tail: V pieces without stale positions and without infinite or
+  // NaN values.
+  const auto put = [&](int i, auto parity, auto tail) {
+    constexpr int to = decltype(parity)::value;
+    uint32_t odd = 0;
 #pragma unroll
     for (int r = 0; r < Stage::kPer; ++r) {
-      const int piece = r * 256 + tid;
-      const int which = __builtin_amdgcn_readfirstlane(piece / Stage::kTile), b = which % BP;
-      if (tail && which >= BP) {
-        // Piece n of a V tile: positions 4 g .. 4 g + 3 with g = n / 16 % 4.
-        const int gp = piece % Stage::kTile / 16 % 4;
-        keep_piece<KP>(next[r], i + b < end ? live_bits(16 * (i + b) + 4 * gp, t.total) : 0u);
-        odd |= clean_piece<KP>(next[r]);
+      const int which = round_tile(r), n = round_piece(r);
+      u32x4_t x = next[to][r];
+      if (r * 256 / Stage::kTile < BP) {
+        lds[to * Stage::kPieces + which * Stage::kTile + n] = __builtin_bit_cast(uint4, x);
+        continue;
       }
-      buf[to][piece] = next[r];
+      const int b = which - BP;
+      if constexpr (decltype(tail)::value) {
+        // Piece n of a V tile: positions 4 g .. 4 g + 3 with g = n / 16 % 4.
+        const uint32_t live = i + b < end ? live_bits(16 * (i + b) + 4 * (n / 16 % 4), t.total) : 0u;
+        x = clean_piece<KP>(keep_piece<KP>(x, live), odd);
+      }
+      uint4* v = lds + to * Stage::kPieces + BP * Stage::kTile;
+      if constexpr (BP == 1) {
+        v[n] = __builtin_bit_cast(uint4, x);
+      } else {
+        // Load n / 64 holds operands 2 (n / 64) and 2 (n / 64) + 1.
+        uint2* op = reinterpret_cast<uint2*>(v + (n / 64) * 128 + n % 64) + b;
+        op[0] = make_uint2(x.x, x.y);
+        op[128] = make_uint2(x.z, x.w);
+      }
     }
-    if (tail && __ballot(odd) != 0 && lane == 0) odd_s[to] = 1;
+    if constexpr (decltype(tail)::value)
+      if (__ballot(odd != 0) != 0 && lane == 0) odd_s[to] = 1;
+  };
+  const auto is_tail = [&](int i) { return 16 * (i + BP) > t.len || i + BP > end; };
+  const auto compute = [&](int i, auto parity, auto tail) {
+    constexpr int at = decltype(parity)::value;
+    const uint4* kb = lds + at * Stage::kPieces + lane;
+    const uint4* vb = kb + BP * Stage::kTile;
+    f32x4_t S[NT][BP];
+#pragma unroll
+    for (int jt = 0; jt < NT; ++jt)
+#pragma unroll
+      for (int b = 0; b < BP; ++b) S[jt][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < NF; ++c)
+#pragma unroll
+      for (int b = 0; b < BP; ++b) {
+        const uint4 x = kb[b * Stage::kTile + c * 64];
+#pragma unroll
+        for (int q = 0; q < Parts::q; ++q)
+#pragma unroll
+          for (int jt = 0; jt < NT; ++jt) S[jt][b] = KP::mma(S[jt][b], x, Q[jt][c][q]);
+      }
+    uint32_t live[BP], sees[NT][BP];
+    if constexpr (decltype(tail)::value) {
+#pragma unroll
+      for (int b = 0; b < BP; ++b) {
+        const int pos = 16 * (i + b) + 4 * g;
+        live[b] = i + b < end ? live_bits(pos, t.total) : 0u;
+#pragma unroll
+        for (int jt = 0; jt < NT; ++jt) {
+          sees[jt][b] = live[b] & seen_bits(pos, t.len, anc[jt]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) S[jt][b][r] = sees[jt][b] >> r & 1 ? S[jt][b][r] : -INFINITY;
+        }
+      }
+    }
+    float p[NT][BP][4];
+#pragma unroll
+    for (int jt = 0; jt < NT; ++jt) softmax_step<BP, NE>(S[jt], a.qscale, m[jt], l[jt], O[jt], p[jt]);
+    if constexpr (BP == 2) {
+      uint4 pp[NT][Parts::p];
+#pragma unroll
+      for (int jt = 0; jt < NT; ++jt) {
+        float v[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] = p[jt][r / 4][r % 4];
+#pragma unroll
+        for (int q = 0; q < Parts::p; ++q) pp[jt][q] = next_part<BF16>(v);
+      }
+#pragma unroll
+      for (int e = 0; e < NE; ++e) {
+        const uint4 x = vb[e * 64];
+#pragma unroll
+        for (int q = 0; q < Parts::p; ++q)
+#pragma unroll
+          for (int jt = 0; jt < NT; ++jt) O[jt][e] = BF16::mma(O[jt][e], x, pp[jt][q]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < NE; ++e) {
+        const uint4 x = vb[e * 64];
+#pragma unroll
+        for (int jt = 0; jt < NT; ++jt) {
+          const float* pj = p[jt][0];
+          O[jt][e] = F32::mma(O[jt][e], x, make_uint4(__float_as_uint(pj[0]), __float_as_uint(pj[1]),
+                                                       __float_as_uint(pj[2]), __float_as_uint(pj[3])));
+        }
+      }
+    }
+    if constexpr (decltype(tail)::value) {
+      if (odd_s[at]) {
+        const size_t tile0 = static_cast<size_t>(block_id(a, t.btrow, i, end)) * a.Hkv + kvh;
+        const size_t tile1 = static_cast<size_t>(block_id(a, t.btrow, min(i + 1, end - 1), end)) * a.Hkv + kvh;
+#pragma unroll
+        for (int jt = 0; jt < NT; ++jt)
+          add_odd_values<KP, HD, BP>(O[jt], p[jt], sees[jt], a.vc, tile0, tile1, live, lane);
+      }
+    }
+  };
+  constexpr std::false_type kPlain{};
+  constexpr std::true_type kTail{};
+
+  constexpr std::integral_constant<int, 0> kEven{};
+  constexpr std::integral_constant<int, 1> kOdd{};
+  // One step: ask for the one after the next, compute, put the next.
+  const auto step = [&](int i, auto parity, auto other, auto tail) {
+    __syncthreads();  // this step is in its buffer; the other buffer has been read
+    if (i + 2 * BP < end) fetch(i + 2 * BP, parity);
+    if (busy) compute(i, parity, tail);
+    if (i + BP < end) put(i + BP, other, tail);
   };
 
   if (tid < 2) odd_s[tid] = 0;
   __syncthreads();
-  fetch(t.first);
-  put(t.first, 0);
-  for (int i = t.first; i < end; i += BP) {
-    const int at = (i - t.first) / BP & 1;
-    __syncthreads();  // step i is in buf[at]; the other buffer has been read
-    if (i + BP < end) fetch(i + BP);
-    if (busy) {
-      const bool tail = 16 * (i + BP) > t.len || i + BP > end;
-      const uint4* kb = buf[at] + lane;
-      const uint4* vb = buf[at] + BP * Stage::kTile + lane;
-      f32x4_t S[NT][BP];
-#pragma unroll
-      for (int jt = 0; jt < NT; ++jt)
-#pragma unroll
-        for (int b = 0; b < BP; ++b) S[jt][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int c = 0; c < NF; ++c)
-#pragma unroll
-        for (int b = 0; b < BP; ++b) {
-          const uint4 x = kb[b * Stage::kTile + c * 64];
-#pragma unroll
-          for (int jt = 0; jt < NT; ++jt)
-#pragma unroll
-            for (int q = 0; q < Parts::q; ++q) S[jt][b] = KP::mma(S[jt][b], x, Q[jt][c][q]);
-        }
-      uint32_t live[BP], sees[NT][BP];
-      if (tail) {
-#pragma unroll
-        for (int b = 0; b < BP; ++b) {
-          const int pos = 16 * (i + b) + 4 * g;
-          live[b] = i + b < end ? live_bits(pos, t.total) : 0u;
-#pragma unroll
-          for (int jt = 0; jt < NT; ++jt) {
-            sees[jt][b] = live[b] & seen_bits(pos, t.len, anc[jt]);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[jt][b][r] = sees[jt][b] >> r & 1 ? S[jt][b][r] : -INFINITY;
-          }
-        }
-      }
-      float p[NT][BP][4];
-#pragma unroll
-      for (int jt = 0; jt < NT; ++jt) softmax_step<BP, NE>(S[jt], a.qscale, m[jt], l[jt], O[jt], p[jt]);
-      if constexpr (KP::per16 == 8) {
-        uint4 pp[NT][Parts::p];
-#pragma unroll
-        for (int jt = 0; jt < NT; ++jt) {
-          float v[8];
-#pragma unroll
-          for (int r = 0; r < 8; ++r) v[r] = p[jt][r / 4][r % 4];
-#pragma unroll
-          for (int q = 0; q < Parts::p; ++q) pp[jt][q] = next_part<BF16>(v);
-        }
-#pragma unroll
-        for (int c = 0; c < NV; ++c) {
-          const uint4 v0 = vb[c * 64], v1 = vb[Stage::kTile + c * 64];
-          const uint4 a0 = make_uint4(v0.x, v0.y, v1.x, v1.y), a1 = make_uint4(v0.z, v0.w, v1.z, v1.w);
-#pragma unroll
-          for (int jt = 0; jt < NT; ++jt)
-#pragma unroll
-            for (int q = 0; q < Parts::p; ++q) {
-              O[jt][2 * c] = BF16::mma(O[jt][2 * c], a0, pp[jt][q]);
-              O[jt][2 * c + 1] = BF16::mma(O[jt][2 * c + 1], a1, pp[jt][q]);
-            }
-        }
-      } else {
-#pragma unroll
-        for (int c = 0; c < NV; ++c) {
-          const uint4 x = vb[c * 64];
-#pragma unroll
-          for (int jt = 0; jt < NT; ++jt) {
-            const float* pj = p[jt][0];
-            O[jt][c] = F32::mma(O[jt][c], x, make_uint4(__float_as_uint(pj[0]), __float_as_uint(pj[1]),
-                                                         __float_as_uint(pj[2]), __float_as_uint(pj[3])));
-          }
-        }
-      }
-      if (tail && odd_s[at]) {
-        size_t tile[BP];
-#pragma unroll
-        for (int b = 0; b < BP; ++b)
-          tile[b] = static_cast<size_t>(block_id(a, t.btrow, min(i + b, end - 1), end)) * a.Hkv + kvh;
-#pragma unroll
-        for (int jt = 0; jt < NT; ++jt)
-          add_odd_values<KP, HD, BP>(O[jt], p[jt], sees[jt], a.vc, tile, live, lane);
-      }
-    }
-    if (i + BP < end) put(i + BP, at ^ 1);
+  int i = t.first;
+  fetch(i, kEven);
+  if (i + BP < end) fetch(i + BP, kOdd);
+  if (is_tail(i)) put(i, kEven, kTail);
+  else put(i, kEven, kPlain);
+  for (; i + 2 * BP < end && !is_tail(i + 2 * BP); i += 2 * BP) {  // two steps and the one after them are whole
+    step(i, kEven, kOdd, kPlain);
+    step(i + BP, kOdd, kEven, kPlain);
+  }
+  for (; i < end; i += 2 * BP) {
+    step(i, kEven, kOdd, kTail);
+    if (i + BP < end) step(i + BP, kOdd, kEven, kTail);
   }
 
   const CoherentBuffer pb(a.part, a.part_bytes);
@@ -819,7 +933,7 @@ __global__ __launch_bounds__(256) void k_tree_attn_shared(TreeAttnArgs a) {
       if (t.nsplit > 1 && g == 0) pb.store4(item + c * (HD + 4) * 4, f32x4_t{m[jt], L, 0.f, 0.f});
     }
   }
-  if (t.nsplit > 1) merge_splits<IO, HD, CW>(a, t, kvh, pb, &last);
+  if (t.nsplit > 1) merge_splits<IO, HD, CW>(a, t, kvh, pb, &last, reinterpret_cast<float*>(lds));
 }
 
 }  // namespace sprk

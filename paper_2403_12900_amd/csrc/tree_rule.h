@@ -95,17 +95,22 @@ inline spr_status parse_tree(const spr_tree_batch* b, bool with_cache, int n_slo
 
 // Columns that one work-group of the attention kernel takes: 16 or 32 where
 // that holds the widest request (its four waves then share out the blocks),
-// else a multiple of 64 (16, 32 columns per wave).
-inline int tree_cols_per_group(const TreeInfo& t, int G) {
+// else 64, 128 or 256 (16, 32, 64 columns per wave), as far as `most`.
+inline int tree_cols_per_group(const TreeInfo& t, int G, int most) {
   const int cols = t.max_nodes * G;
-  return cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
+  int cw = 16;
+  while (cw < cols && cw < most) cw *= 2;
+  return cw;
 }
 
 // Work items of one attention launch: per request its column groups, each in
 // KV splits of bps blocks.
 struct TreeSplit {
   int bps = 1;
-  uint8_t ncg[kTreeReqs], cg0[kTreeReqs];
+  // In launch order, the requests with the longest splits first, so that the
+  // last work-groups to start are short ones: the request, its column groups,
+  // the first of them and its first work item.
+  uint8_t order[kTreeReqs], ncg[kTreeReqs], cg0[kTreeReqs];
   int item0[kTreeReqs + 1];
 };
 
@@ -113,26 +118,45 @@ struct TreeSplit {
 // the launch has more than its share of resident work-groups (`slots`) takes
 // at once; they grow further while the partials exceed `floats` or a request
 // has more than kTreeSplits.
-constexpr int kTreeSplits = 128;
+constexpr int kTreeSplits = 32;
 inline TreeSplit tree_split(const TreeInfo& t, int G, int Hkv, int hd, int cw, int least, int slots, size_t floats) {
   TreeSplit s;
+  const auto blocks_of = [&](int i) { return (t.len[i] + t.nodes[i] + 15) / 16; };
+  for (int i = 0; i < t.n; ++i) s.order[i] = static_cast<uint8_t>(i);
+  std::stable_sort(s.order, s.order + t.n, [&](int i, int j) { return blocks_of(i) > blocks_of(j); });
   int64_t blocks = 0;
   int cg = 0;
-  for (int i = 0; i < t.n; ++i) {
-    s.ncg[i] = static_cast<uint8_t>((t.nodes[i] * G + cw - 1) / cw);
-    s.cg0[i] = static_cast<uint8_t>(cg);
-    cg += s.ncg[i];
-    blocks += static_cast<int64_t>(s.ncg[i]) * ((t.len[i] + t.nodes[i] + 15) / 16);
+  for (int r = 0; r < t.n; ++r) {
+    const int i = s.order[r];
+    s.ncg[r] = static_cast<uint8_t>((t.nodes[i] * G + cw - 1) / cw);
+    s.cg0[r] = static_cast<uint8_t>(cg);
+    cg += s.ncg[r];
+    blocks += static_cast<int64_t>(s.ncg[r]) * blocks_of(i);
   }
   const int64_t per = static_cast<int64_t>(Hkv) * cw * (hd + 4);
   int64_t bps = std::max<int64_t>(1, (blocks * Hkv + slots - 1) / slots);
+  // Rounding every request up to whole splits can leave more work-groups than
+  // stay resident; splits up to twice as long that fit them into one round are
+  // taken, but not longer ones.
+  const auto groups = [&](int64_t w) {
+    int64_t n = 0;
+    for (int r = 0; r < t.n; ++r) n += (blocks_of(s.order[r]) + w - 1) / w * s.ncg[r];
+    return n * Hkv;
+  };
+  for (int k = 0; k <= 8; ++k) {
+    const int64_t whole = (bps + bps * k / 8 + least - 1) / least * least;
+    if (groups(whole) <= slots) {
+      bps = whole;
+      break;
+    }
+  }
   for (;; bps += std::max<int64_t>(least, bps / 8)) {
     bps = (bps + least - 1) / least * least;
     int64_t items = 0, most = 1;
-    for (int i = 0; i < t.n; ++i) {
-      const int64_t ns = ((t.len[i] + t.nodes[i] + 15) / 16 + bps - 1) / bps;
-      s.item0[i] = static_cast<int>(items);
-      items += ns * s.ncg[i];
+    for (int r = 0; r < t.n; ++r) {
+      const int64_t ns = (blocks_of(s.order[r]) + bps - 1) / bps;
+      s.item0[r] = static_cast<int>(items);
+      items += ns * s.ncg[r];
       most = std::max(most, ns);
     }
     s.item0[t.n] = static_cast<int>(items);

@@ -142,17 +142,21 @@ def test_launch_split_covers_every_block_within_its_room():
         lens = [int(2 ** rng.uniform(0, rng.choice([8, 14, 20, 30]))) for _ in range(n)]
         G, Hkv, hd, step = int(rng.choice([1, 8, 13, 16])), int(rng.choice([1, 8, 40, 512])), int(rng.choice([64, 128])), int(rng.choice([1, 2, 4, 8]))
         floats = int(rng.choice([1 << 18, 1 << 23, 1 << 28]))
-        out = np.zeros(70, np.int32)
+        out = np.zeros(140, np.int32)
         b = raw_batch(n, range(n), lens, nodes, sum(([-1] + [0] * (k - 1) for k in nodes), []))
         assert L.sprh_tree_split(ctypes.byref(b), G, Hkv, hd, step, int(rng.choice([256, 1024])), floats, p32(out)) == 0
         cw, bps = int(out[0]), int(out[1])
-        assert cw in (16, 32, 64, 128) and bps >= 1 and bps % step == 0
+        assert cw in (16, 32, 64, 128, 256) and bps >= 1 and bps % step == 0
         split = False
-        for i in range(n):
+        order = out[3 + n:3 + 2 * n].tolist()
+        assert sorted(order) == list(range(n))
+        size = [-(-(lens[i] + nodes[i]) // 16) for i in order]
+        assert size == sorted(size, reverse=True)
+        for r, i in enumerate(order):
             ncg = -(-nodes[i] * G // cw)
             ns = -(-(-(-(lens[i] + nodes[i]) // 16)) // bps)
-            assert out[2 + i + 1] - out[2 + i] == ncg * ns
-            assert ns <= 128
+            assert out[2 + r + 1] - out[2 + r] == ncg * ns
+            assert ns <= 32
             split |= ns > 1
         assert out[2] == 0 and out[2 + n] <= 65535
         if split:
