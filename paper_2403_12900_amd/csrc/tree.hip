@@ -129,16 +129,14 @@ hipError_t launch_tree_verify(const TreeVerifyCall& c) {
     }
   }
   for (a.k = 0; a.k <= last; ++a.k) {
-    int n = 0;
-    for (int i = 0; i < t.n; ++i) {
-      int rows = 0;
+    int n = 0, rows[kTreeReqs] = {};
+    for (int i = 0; i < t.n; ++i)
       for (int r = t.row0[i]; r < t.row0[i + 1]; ++r) {
         if (a.k > 0 && (passes[i] == 0 || t.kids[r] < a.k)) continue;
         a.list[n++] = static_cast<uint8_t>(r);
-        ++rows;
+        ++rows[i];
       }
-      a.expect[i] = static_cast<uint16_t>(passes[i] == a.k ? rows * a.S : 0);
-    }
+    for (int i = 0; i < t.n; ++i) a.expect[i] = static_cast<uint16_t>(passes[i] == a.k ? rows[i] * a.S : 0);
     const dim3 grid(a.S, n);
     if (c.bf16) {
       if (a.k == 0) k_tree_verify<uint16_t, kStats><<<grid, kVThreads, 0, c.st>>>(a);

@@ -209,25 +209,30 @@ struct RowStat {
   double z;
   int best;
 };
+struct ChunkStat {
+  uint64_t top, z;  // (maximum, its index); sum
+};
 template <bool kFresh>
-__device__ __forceinline__ RowStat row_stat(const TreeVerifyArgs& a, int row, double inv_t, bool want_z) {
+__device__ __forceinline__ ChunkStat load_stat(const TreeVerifyArgs& a, int row, int c) {
+  ChunkStat s{0xFF800000u, 0};  // no entries: maximum -inf
+  if (c < a.S) {
+    const uint64_t* st = a.stat + (static_cast<size_t>(row) * a.S + c) * 2;
+    s.top = kFresh ? get64(st) : st[0];
+    s.z = kFresh ? get64(st + 1) : st[1];
+  }
+  return s;
+}
+// s: this lane's chunk of the first 64, loaded before.
+template <bool kFresh>
+__device__ __forceinline__ RowStat row_stat(const TreeVerifyArgs& a, int row, ChunkStat s, double inv_t, bool want_z) {
   const int lane = threadIdx.x & 63;
-  const uint64_t* st = a.stat + static_cast<size_t>(row) * a.S * 2;
   RowStat r{-INFINITY, 0.0, 0x7fffffff};
   bool bad = false;
 #pragma unroll 1
-  for (int c0 = 0; c0 < a.S; c0 += 64) {
-    const int c = c0 + lane;
-    float m = -INFINITY;
-    double z = 0.0;
-    int best = 0x7fffffff;
-    if (c < a.S) {
-      const uint64_t u = kFresh ? get64(st + 2 * c) : st[2 * c];
-      z = as_double(kFresh ? get64(st + 2 * c + 1) : st[2 * c + 1]);
-      m = __uint_as_float(static_cast<uint32_t>(u));
-      best = static_cast<int>(u >> 32);
-      bad |= m != m;
-    }
+  for (int c0 = 0;;) {
+    const float m = __uint_as_float(static_cast<uint32_t>(s.top));
+    int best = static_cast<int>(s.top >> 32);
+    bad |= m != m;
     // The maximum so far, and the sum scaled to it.
     float wm = m == m ? m : -INFINITY;
     const float mine = wm;
@@ -235,10 +240,13 @@ __device__ __forceinline__ RowStat row_stat(const TreeVerifyArgs& a, int row, do
     const float up = fmaxf(r.m, wm);
     if (wm > r.m) r.best = best;
     if (want_z && up > -INFINITY) {
-      const double part = wave_sum(mine > -INFINITY ? z * exp_neg((static_cast<double>(mine) - up) * inv_t) : 0.0);
+      const double part = wave_sum(mine > -INFINITY ? as_double(s.z) * exp_neg((static_cast<double>(mine) - up) * inv_t) : 0.0);
       r.z = (r.m > -INFINITY ? r.z * exp_neg((static_cast<double>(r.m) - up) * inv_t) : 0.0) + part;
     }
     r.m = up;
+    c0 += 64;
+    if (c0 >= a.S) break;
+    s = load_stat<kFresh>(a, row, c0 + lane);
   }
   if (__ballot(bad) != 0 || !(fabsf(r.m) <= 3.402823466e38f)) r.m = __uint_as_float(0x7FC00000u);
   return r;
@@ -246,12 +254,12 @@ __device__ __forceinline__ RowStat row_stat(const TreeVerifyArgs& a, int row, do
 
 enum { kStats = 0, kRest = 1 };
 
-template <class T>
+template <class T, int kAhead>
 __device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVerifySmem* sm);
 
 // T: storage of logits and draft_probs (float, or uint16_t for bf16).
 template <class T, int kPhase>
-__global__ __launch_bounds__(kVThreads, 8) void k_tree_verify(TreeVerifyArgs a) {
+__global__ __launch_bounds__(kVThreads, (kPhase == kStats ? 8 : 4)) void k_tree_verify(TreeVerifyArgs a) {
   __shared__ TreeVerifySmem sm;
   const int chunk = blockIdx.x, row = a.list[blockIdx.y], i = a.req[row];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -291,19 +299,20 @@ __global__ __launch_bounds__(kVThreads, 8) void k_tree_verify(TreeVerifyArgs a) 
       s = group_sum(s, &sm);
     }
     if (threadIdx.x == 0) {
-      uint64_t* st = a.stat + (static_cast<size_t>(row) * a.S + chunk) * 2;
+      uint64_t* to = a.stat + (static_cast<size_t>(row) * a.S + chunk) * 2;
       const float mm = nan ? __uint_as_float(0x7FC00000u) : m;
-      put64(st, __float_as_uint(mm) | static_cast<uint64_t>(static_cast<uint32_t>(best)) << 32);
-      put64(st + 1, static_cast<uint64_t>(__double_as_longlong(s)));
+      put64(to, __float_as_uint(mm) | static_cast<uint64_t>(static_cast<uint32_t>(best)) << 32);
+      put64(to + 1, static_cast<uint64_t>(__double_as_longlong(s)));
     }
   } else {
     float q[kVOwn];
     load_chunk(static_cast<const T*>(a.draft) + row * a.ds, a.V, chunk, a.vec_d, 0.f, q);
-    const RowStat st = row_stat<false>(a, row, inv_t, true);
+    const ChunkStat first = load_stat<false>(a, row, lane);
     // c_k = 1 + N_1 + ... + N_{k-1}: all parts that the earlier passes left.
     const double* rest = a.rest + static_cast<size_t>(a.rest0[row]) * a.S;
     double c = 0.0;
     for (int t = lane; t < (a.k - 1) * a.S; t += 64) c += rest[t];
+    const RowStat st = row_stat<false>(a, row, first, inv_t, true);
     c = 1.0 + wave_sum(c);
     double s = 0.0;
     if (st.m == st.m) {
@@ -325,13 +334,13 @@ __global__ __launch_bounds__(kVThreads, 8) void k_tree_verify(TreeVerifyArgs a) 
   __syncthreads();
   if (!sm.last) return;
   if (threadIdx.x == 0) __hip_atomic_store(a.cnt + i, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  tree_walk<T>(a, i, &sm);
+  tree_walk<T, kPhase == kStats ? 1 : 4>(a, i, &sm);
 }
 
 // One work-group.  The code is written for its size as much as for its work:
 // it runs in one work-group alone, whose instruction fetches nothing hides
 // (unrolled, 32000 entries and one draw took 45 us; this form, see below).
-template <class T>
+template <class T, int kAhead>
 __device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVerifySmem* sm) {
   const int row0 = a.row0[i], nn = a.nodes[i], tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float temp = a.temp[i];
@@ -359,23 +368,41 @@ __device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVe
     sm->parent[lane] = static_cast<int8_t>(par);
     if (child && !ranged) raise_check(a.err, kErrTokenRange);
   }
-  // Totals: rows by waves, then the arrays of parts (one per child) likewise.
+  // Totals: rows by waves, then the arrays of parts (one per child) likewise,
+  // kAhead of them asked for at once (four cost the statistics kernel the
+  // registers that let four of its work-groups share a CU).
 #pragma unroll 1
-  for (int r = wave; r < nn; r += kVWaves) {
-    const RowStat st = row_stat<true>(a, row0 + r, inv_t, !greedy);
-    if (lane == 0) {
-      sm->m[r] = st.m;
-      sm->z[r] = st.z;
-      sm->best[r] = st.best;
+  for (int r0 = wave; r0 < nn; r0 += kAhead * kVWaves) {
+    ChunkStat s[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) s[k] = load_stat<true>(a, row0 + min(r0 + k * kVWaves, nn - 1), lane);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int r = r0 + k * kVWaves;
+      if (r >= nn) break;
+      const RowStat st = row_stat<true>(a, row0 + r, s[k], inv_t, !greedy);
+      if (lane == 0) {
+        sm->m[r] = st.m;
+        sm->z[r] = st.z;
+        sm->best[r] = st.best;
+      }
     }
   }
   if (drafted) {
 #pragma unroll 1
-    for (int r = wave; r < nn - 1; r += kVWaves) {
-      double s = 0.0;
-      for (int c = lane; c < a.S; c += 64) s += get_double(a.rest + (static_cast<size_t>(base0) + r) * a.S + c);
-      s = wave_sum(s);
-      if (lane == 0) sm->total[r] = s;
+    for (int r0 = wave; r0 < nn - 1; r0 += kAhead * kVWaves) {
+      double s[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const double* parts = a.rest + (static_cast<size_t>(base0) + min(r0 + k * kVWaves, nn - 2)) * a.S;
+        s[k] = lane < a.S ? get_double(parts + lane) : 0.0;
+        for (int c = lane + 64; c < a.S; c += 64) s[k] += get_double(parts + c);
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const double sum = wave_sum(s[k]);
+        if (lane == 0 && r0 + k * kVWaves < nn - 1) sm->total[r0 + k * kVWaves] = sum;
+      }
     }
   }
   __syncthreads();
