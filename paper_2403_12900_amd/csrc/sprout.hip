@@ -1274,7 +1274,6 @@ spr_status spr_tree_step(spr_model* m, const spr_tree_batch* batch, int32_t* tok
   // the greedy candidates (64 bytes per token) hold them.
   const bool in_part = tree_verify_bytes(t.rows, d.V) <= m->lay.part_floats * sizeof(float);
   v.scratch = in_part ? static_cast<void*>(p.part()) : static_cast<void*>(p.amax());
-  v.cnt = p.cnt();
   v.err = m->err_dev;
   e = launch_tree_verify(v);
   if (e != hipSuccess) return hip_fail(m, "k_tree_verify", e);

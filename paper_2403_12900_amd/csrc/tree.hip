@@ -11,10 +11,10 @@
 
 using namespace sprk;
 
-// Operator workspace: attention partials (or verification's sums), counters.
+// Operator workspace: attention partials (or verification's sums), and
+// attention's counters: one per column group and KV head.
 constexpr size_t kTreePartBytes = size_t{32} << 20;
 constexpr int kTreeCounters = kTreeRows * 512;
-static_assert(kTreeCounters >= kTreeReqs, "verification's counters");
 
 struct spr_tree_ops {
   char* ws = nullptr;
@@ -104,7 +104,6 @@ hipError_t launch_tree_verify(const TreeVerifyCall& c) {
   a.n = t.n;
   a.stat = static_cast<uint64_t*>(c.scratch);
   a.rest = reinterpret_cast<double*>(a.stat + static_cast<size_t>(t.rows) * a.S * 2);
-  a.cnt = c.cnt;
   const int size = c.bf16 ? 2 : 4;
   const auto aligned = [&](const void* p, int64_t stride) {
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride * size % 16 == 0;
@@ -112,13 +111,13 @@ hipError_t launch_tree_verify(const TreeVerifyCall& c) {
   a.vec_l = aligned(c.logits, c.ls);
   a.vec_d = c.draft != nullptr && aligned(c.draft, c.ds);
   int arrays = 0, last = 0;
-  int passes[kTreeReqs];  // of the request: its nodes' most children, where they are tested against q
+  bool drafted[kTreeReqs];  // children are tested against q
   for (int i = 0; i < t.n; ++i) {
     a.temp[i] = c.temperature != nullptr ? c.temperature[i] : 1.f;
     a.row0[i] = static_cast<uint8_t>(t.row0[i]);
     a.nodes[i] = static_cast<uint8_t>(t.nodes[i]);
-    passes[i] = c.draft != nullptr && a.temp[i] > 0.f ? t.children[i] : 0;
-    last = std::max(last, passes[i]);
+    drafted[i] = c.draft != nullptr && a.temp[i] > 0.f;
+    if (drafted[i]) last = std::max(last, t.children[i]);
     for (int r = t.row0[i]; r < t.row0[i + 1]; ++r) {
       a.req[r] = static_cast<uint8_t>(i);
       a.kids[r] = t.kids[r];
@@ -128,27 +127,23 @@ hipError_t launch_tree_verify(const TreeVerifyCall& c) {
       arrays += t.kids[r];
     }
   }
-  for (a.k = 0; a.k <= last; ++a.k) {
-    int n = 0, rows[kTreeReqs] = {};
+  hipError_t e;
+  const dim3 grid(a.S, t.rows);
+  if (c.bf16) k_tree_stats<uint16_t><<<grid, kSumThreads, 0, c.st>>>(a);
+  else k_tree_stats<float><<<grid, kSumThreads, 0, c.st>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  for (a.k = 1; a.k <= last; ++a.k) {
+    int n = 0;
     for (int i = 0; i < t.n; ++i)
-      for (int r = t.row0[i]; r < t.row0[i + 1]; ++r) {
-        if (a.k > 0 && (passes[i] == 0 || t.kids[r] < a.k)) continue;
-        a.list[n++] = static_cast<uint8_t>(r);
-        ++rows[i];
-      }
-    for (int i = 0; i < t.n; ++i) a.expect[i] = static_cast<uint16_t>(passes[i] == a.k ? rows[i] * a.S : 0);
-    const dim3 grid(a.S, n);
-    if (c.bf16) {
-      if (a.k == 0) k_tree_verify<uint16_t, kStats><<<grid, kVThreads, 0, c.st>>>(a);
-      else k_tree_verify<uint16_t, kRest><<<grid, kVThreads, 0, c.st>>>(a);
-    } else {
-      if (a.k == 0) k_tree_verify<float, kStats><<<grid, kVThreads, 0, c.st>>>(a);
-      else k_tree_verify<float, kRest><<<grid, kVThreads, 0, c.st>>>(a);
-    }
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+      for (int r = t.row0[i]; r < t.row0[i + 1]; ++r)
+        if (drafted[i] && t.kids[r] >= a.k) a.list[n++] = static_cast<uint8_t>(r);
+    if (c.bf16) k_tree_rest<uint16_t><<<dim3(a.S, n), kSumThreads, 0, c.st>>>(a);
+    else k_tree_rest<float><<<dim3(a.S, n), kSumThreads, 0, c.st>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  return hipSuccess;
+  if (c.bf16) k_tree_walk<uint16_t><<<t.n, kDrawThreads, 0, c.st>>>(a);
+  else k_tree_walk<float><<<t.n, kDrawThreads, 0, c.st>>>(a);
+  return hipGetLastError();
 }
 
 hipError_t launch_tree_keep(hipStream_t st, const TreeInfo& t, const spr_kv_view& kv, const int32_t* path,
@@ -372,7 +367,6 @@ spr_status spr_tree_verify(spr_tree_ops* o, const spr_tree_batch* batch, int32_t
     c.path = path;
     c.count = count;
     c.scratch = o->ws;
-    c.cnt = reinterpret_cast<int32_t*>(o->ws + kTreePartBytes);
     c.err = o->err_dev;
     const hipError_t e = launch_tree_verify(c);
     return e == hipSuccess ? SPR_OK : hip_failed(o, "tree_verify", e);

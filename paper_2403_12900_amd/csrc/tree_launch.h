@@ -50,7 +50,6 @@ struct TreeVerifyCall {
   const float *accept, *sample;
   int32_t *emitted, *path, *count;
   void* scratch;             // tree_verify_bytes, 8-byte aligned
-  int32_t* cnt;              // at least kTreeReqs counters, zero between launches
   int* err;
 };
 size_t tree_verify_bytes(int rows, int V);

@@ -16,25 +16,31 @@
 //
 // Each vocabulary row is cut into chunks of kVChunk entries, one work-group
 // each, so that few rows still fill the chip:
-//   k_tree_verify<.., kStats>  per (row, chunk): maximum, its lowest index, sum of exp
-//   k_tree_verify<.., kRest>   per (row with >= k children, chunk): its part of N_k
-//                              (one launch per k; none without draft_probs)
-// The work-group that finishes a request's last chunk walks its tree: every
-// child's test at once (it depends on its parent's row alone), then the path
-// by bit masks, then the draw: the chunk sums locate the chunk, which alone is
-// read again.  No work-group waits on another, and all sums run in a fixed
-// order.
+//   k_tree_stats  per (row, chunk): maximum, its lowest index, sum of exp
+//   k_tree_rest   per (row with >= k children, chunk): its part of N_k (one
+//                 launch per k; none without draft_probs)
+//   k_tree_walk   per request: every child's test at once (it depends on its
+//                 parent's row alone), then the path by bit masks, then the
+//                 draw: the chunk sums locate the chunk, which alone is read
+//                 again.
+// No work-group waits on another, nothing is counted, and all sums run in a
+// fixed order.  (The walk as the end of the last sums' launch, in the work-group
+// that finishes a request's last chunk, cost what the launch saves -- 13.5 us at
+// 5 rows of 32000 -- and held greedy requests' walks between two launches.)
 #pragma once
 
 #include "tree_attn_kernels.h"
 
 namespace sprk {
 
-constexpr int kVThreads = 512;
 constexpr int kVChunk = 4096;
 constexpr int kVMaxChunks = 256;
 constexpr int kVMaxVocab = kVChunk * kVMaxChunks;
-constexpr int kVOwn = kVChunk / kVThreads;  // entries of a chunk per thread
+// Entries of a chunk per thread: 16 where the sums are taken (256 threads: 4000
+// work-groups of twice the waves took 26 us, as long as it takes to start
+// them), 8 in the walk's draw, which one work-group makes alone.
+constexpr int kSumOwn = 16, kDrawOwn = 8;
+constexpr int kSumThreads = kVChunk / kSumOwn, kDrawThreads = kVChunk / kDrawOwn;
 
 struct TreeVerifyArgs {
   const void* logits;
@@ -47,11 +53,9 @@ struct TreeVerifyArgs {
   int* err;
   uint64_t* stat;          // [rows][S][2]: (maximum, its index), sum of exp((x - maximum) / T)
   double* rest;            // [rest0[row] + k - 1][S]: parts of N_k
-  int32_t* cnt;            // [n] finished work-groups; zero between launches
-  int V, S, n, k;          // k: the pass (0: statistics)
+  int V, S, n, k;          // k: the pass of k_tree_rest
   int vec_l, vec_d;        // rows of logits / draft_probs are 16-byte aligned
   float temp[kTreeReqs];
-  uint16_t expect[kTreeReqs];  // work-groups of the request in this launch, if it ends with it (0: it does not)
   uint8_t row0[kTreeReqs], nodes[kTreeReqs];
   uint8_t list[kTreeRows];     // rows of this launch
   uint8_t req[kTreeRows], kids[kTreeRows], rank[kTreeRows], rest0[kTreeRows];
@@ -59,11 +63,15 @@ struct TreeVerifyArgs {
 };
 static_assert(sizeof(TreeVerifyArgs) <= 2048, "kernel arguments");
 
-// exp(x) for x <= 0 to 2^-47 of its value: x = n ln 2 + r, |r| <= ln 2 / 2,
-// with ln 2 in two parts, and the Taylor polynomial of degree 11 of e^r (its
-// rest is below r^12 / 12! < 7e-15).  NaN stays NaN; 0 from -745 on.
+// exp(x) for x <= 0 to 2^-47 of its value, 0 below -708 (where the result
+// would leave the normal range): x = n ln 2 + r, |r| <= ln 2 / 2, with ln 2 in
+// two parts, and the Taylor polynomial of degree 11 of e^r (its rest is below
+// r^12 / 12! < 7e-15).  Adding 1.5 * 2^52 leaves n, rounded, in the low bits
+// of the sum, from where it goes into the exponent: no conversions, which run
+// at a quarter of the rate of the products.
 __device__ __forceinline__ double exp_neg(double x) {
-  const double n = __builtin_rint(x * 1.4426950408889634);
+  constexpr double kShift = 6755399441055744.0;
+  const double t = fma(x, 1.4426950408889634, kShift), n = t - kShift;
   double r = fma(n, -0x1.62e42fefa39efp-1, x);
   r = fma(n, -0x1.abc9e3b39803fp-56, r);
   double p = 1.0 / 39916800.0;
@@ -78,25 +86,28 @@ __device__ __forceinline__ double exp_neg(double x) {
   p = fma(p, r, 0.5);
   p = fma(p, r, 1.0);
   p = fma(p, r, 1.0);
-  const double e = __builtin_amdgcn_ldexp(p, static_cast<int>(fmax(n, -1100.0)));
-  return x < -745.0 ? 0.0 : e;
+  const uint64_t bits = static_cast<uint64_t>(__double_as_longlong(p));
+  const uint32_t hi = static_cast<uint32_t>(bits >> 32) + (static_cast<uint32_t>(__double_as_longlong(t)) << 20);
+  const double e = __longlong_as_double(static_cast<long long>(static_cast<uint64_t>(hi) << 32 | static_cast<uint32_t>(bits)));
+  return x < -708.0 ? 0.0 : e;
 }
 
-// kVOwn consecutive entries of one vocabulary chunk per thread: entry thread *
-// kVOwn + e, as floats; those past V read as `fill`.
+// OWN consecutive entries of one vocabulary chunk per thread: entry thread *
+// OWN + e, as floats; those past V read as `fill`.
+template <int OWN>
 __device__ __forceinline__ int chunk_index(int chunk) {
-  return chunk * kVChunk + static_cast<int>(threadIdx.x) * kVOwn;
+  return chunk * kVChunk + static_cast<int>(threadIdx.x) * OWN;
 }
 __device__ __forceinline__ float vocab_value(float x) { return x; }
 __device__ __forceinline__ float vocab_value(uint16_t x) { return bf16_bits_to_f32(x); }
-template <class T>
+template <int OWN, class T>
 __device__ __forceinline__ void load_chunk(const T* row, int V, int chunk, int vec, float fill, float* x) {
   constexpr int EV = 16 / static_cast<int>(sizeof(T));
-  static_assert(kVOwn % EV == 0, "whole 16-byte loads");
-  const int i0 = chunk_index(chunk);
-  if (vec && i0 + kVOwn <= V) {
+  static_assert(OWN % EV == 0, "whole 16-byte loads");
+  const int i0 = chunk_index<OWN>(chunk);
+  if (vec && i0 + OWN <= V) {
 #pragma unroll
-    for (int j = 0; j < kVOwn / EV; ++j) {
+    for (int j = 0; j < OWN / EV; ++j) {
       const uint4 u = *reinterpret_cast<const uint4*>(row + i0 + j * EV);
       const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -107,16 +118,14 @@ __device__ __forceinline__ void load_chunk(const T* row, int V, int chunk, int v
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < kVOwn; ++e) x[e] = i0 + e < V ? vocab_value(row[i0 + e]) : fill;
+    for (int e = 0; e < OWN; ++e) x[e] = i0 + e < V ? vocab_value(row[i0 + e]) : fill;
   }
 }
 
-constexpr int kVWaves = kVThreads / 64;
-struct TreeVerifySmem {
-  double d[kVWaves];
-  float f[kVWaves];
-  int i[kVWaves];
-  int last, hit[kVWaves], tail[kVWaves];
+constexpr int kSumWaves = kSumThreads / 64, kDrawWaves = kDrawThreads / 64;
+struct TreeWalkSmem {
+  double d[kDrawWaves];
+  int hit[kDrawWaves], tail[kDrawWaves];
   double z[kTreeNodes], total[kTreeNodes];      // per node: its row's sum; per array of parts: N_k
   double px[kTreeNodes];                        // per node as a child: p(its token)
   float m[kTreeNodes];                          // per node: its row's maximum (NaN: a bad row)
@@ -177,33 +186,24 @@ __device__ __forceinline__ void wave_best(float& m, int& index) {
   m = w;
 }
 
-// Sum over the work-group, in a fixed order; every thread gets it.  sm->d is
-// free (a barrier lies between its last readers and this).
-__device__ __forceinline__ double group_sum(double v, TreeVerifySmem* sm) {
+// Sum over the work-group, in a fixed order; every thread gets it.
+__device__ __forceinline__ double group_sum(double v, double* part) {
   v = wave_sum(v);
-  if ((threadIdx.x & 63) == 0) sm->d[threadIdx.x >> 6] = v;
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
   __syncthreads();
   double s = 0.0;
 #pragma unroll
-  for (int w = 0; w < kVWaves; ++w) s += sm->d[w];
+  for (int w = 0; w < kSumWaves; ++w) s += part[w];
   return s;
 }
 
-__device__ __forceinline__ void put64(uint64_t* p, uint64_t v) {
-  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ uint64_t get64(const uint64_t* p) {
-  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
 __device__ __forceinline__ double as_double(uint64_t u) { return __longlong_as_double(static_cast<long long>(u)); }
-__device__ __forceinline__ double get_double(const double* p) { return as_double(get64(reinterpret_cast<const uint64_t*>(p))); }
 
 // A draft probability as it counts: entries that are negative or NaN are 0.
 __device__ __forceinline__ double draft_value(float q) { return q > 0.f ? static_cast<double>(q) : 0.0; }
 
 // Maximum (NaN: a row with a NaN or no finite maximum), its lowest index and
-// sum of a row from its chunks; every wave works them out by itself.  kFresh:
-// the chunks are this launch's.
+// sum of a row from its chunks; every wave works them out by itself.
 struct RowStat {
   float m;
   double z;
@@ -212,18 +212,16 @@ struct RowStat {
 struct ChunkStat {
   uint64_t top, z;  // (maximum, its index); sum
 };
-template <bool kFresh>
 __device__ __forceinline__ ChunkStat load_stat(const TreeVerifyArgs& a, int row, int c) {
   ChunkStat s{0xFF800000u, 0};  // no entries: maximum -inf
   if (c < a.S) {
     const uint64_t* st = a.stat + (static_cast<size_t>(row) * a.S + c) * 2;
-    s.top = kFresh ? get64(st) : st[0];
-    s.z = kFresh ? get64(st + 1) : st[1];
+    s.top = st[0];
+    s.z = st[1];
   }
   return s;
 }
 // s: this lane's chunk of the first 64, loaded before.
-template <bool kFresh>
 __device__ __forceinline__ RowStat row_stat(const TreeVerifyArgs& a, int row, ChunkStat s, double inv_t, bool want_z) {
   const int lane = threadIdx.x & 63;
   RowStat r{-INFINITY, 0.0, 0x7fffffff};
@@ -246,102 +244,98 @@ __device__ __forceinline__ RowStat row_stat(const TreeVerifyArgs& a, int row, Ch
     r.m = up;
     c0 += 64;
     if (c0 >= a.S) break;
-    s = load_stat<kFresh>(a, row, c0 + lane);
+    s = load_stat(a, row, c0 + lane);
   }
   if (__ballot(bad) != 0 || !(fabsf(r.m) <= 3.402823466e38f)) r.m = __uint_as_float(0x7FC00000u);
   return r;
 }
 
-enum { kStats = 0, kRest = 1 };
-
-template <class T, int kAhead>
-__device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVerifySmem* sm);
-
-// T: storage of logits and draft_probs (float, or uint16_t for bf16).
-template <class T, int kPhase>
-__global__ __launch_bounds__(kVThreads, (kPhase == kStats ? 8 : 4)) void k_tree_verify(TreeVerifyArgs a) {
-  __shared__ TreeVerifySmem sm;
-  const int chunk = blockIdx.x, row = a.list[blockIdx.y], i = a.req[row];
+// T: storage of logits and draft_probs (float, or uint16_t for bf16).  Grid
+// (chunks, rows); 8 waves per SIMD, which the fp64 exponentials need to overlap.
+template <class T>
+__global__ __launch_bounds__(kSumThreads, 8) void k_tree_stats(TreeVerifyArgs a) {
+  __shared__ double part[kSumWaves];
+  __shared__ float top_s[kSumWaves];
+  __shared__ int best_s[kSumWaves];
+  const int chunk = blockIdx.x, row = blockIdx.y;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const float temp = a.temp[i];
-  const double inv_t = temp > 0.f ? 1.0 / static_cast<double>(temp) : 1.0;
-  float x[kVOwn];
-  load_chunk(static_cast<const T*>(a.logits) + row * a.ls, a.V, chunk, a.vec_l, -INFINITY, x);
-  if constexpr (kPhase == kStats) {
-    // Maximum with the lowest index that has it; a NaN anywhere makes it NaN.
-    float m = -INFINITY;
-    bool nan = false;
+  const float temp = a.temp[a.req[row]];
+  float x[kSumOwn];
+  load_chunk<kSumOwn>(static_cast<const T*>(a.logits) + row * a.ls, a.V, chunk, a.vec_l, -INFINITY, x);
+  // Maximum with the lowest index that has it; a NaN anywhere makes it NaN.
+  float m = -INFINITY;
+  bool nan = false;
 #pragma unroll
-    for (int e = 0; e < kVOwn; ++e) {
-      nan |= x[e] != x[e];
-      m = fmaxf(m, x[e]);
-    }
-    int best = 0;
-#pragma unroll
-    for (int e = kVOwn - 1; e >= 0; --e) best = x[e] == m ? e : best;
-    best += chunk_index(chunk);
-    wave_best(m, best);
-    if (lane == 0) {
-      sm.f[wave] = m;
-      sm.i[wave] = best;
-    }
-    nan = __syncthreads_or(nan);
-    m = -INFINITY;
-    best = 0x7fffffff;
-#pragma unroll
-    for (int w = 0; w < kVWaves; ++w) better_of(m, best, sm.f[w], sm.i[w]);
-    double s = 0.0;
-    if (temp > 0.f) {
-      if (m > -INFINITY && m < INFINITY && !nan) {
-#pragma unroll
-        for (int e = 0; e < kVOwn; ++e) s += exp_neg((static_cast<double>(x[e]) - m) * inv_t);
-      }
-      s = group_sum(s, &sm);
-    }
-    if (threadIdx.x == 0) {
-      uint64_t* to = a.stat + (static_cast<size_t>(row) * a.S + chunk) * 2;
-      const float mm = nan ? __uint_as_float(0x7FC00000u) : m;
-      put64(to, __float_as_uint(mm) | static_cast<uint64_t>(static_cast<uint32_t>(best)) << 32);
-      put64(to + 1, static_cast<uint64_t>(__double_as_longlong(s)));
-    }
-  } else {
-    float q[kVOwn];
-    load_chunk(static_cast<const T*>(a.draft) + row * a.ds, a.V, chunk, a.vec_d, 0.f, q);
-    const ChunkStat first = load_stat<false>(a, row, lane);
-    // c_k = 1 + N_1 + ... + N_{k-1}: all parts that the earlier passes left.
-    const double* rest = a.rest + static_cast<size_t>(a.rest0[row]) * a.S;
-    double c = 0.0;
-    for (int t = lane; t < (a.k - 1) * a.S; t += 64) c += rest[t];
-    const RowStat st = row_stat<false>(a, row, first, inv_t, true);
-    c = 1.0 + wave_sum(c);
-    double s = 0.0;
-    if (st.m == st.m) {
-      const double inv_z = 1.0 / st.z;
-#pragma unroll
-      for (int e = 0; e < kVOwn; ++e)
-        s += fmax(exp_neg((static_cast<double>(x[e]) - st.m) * inv_t) * inv_z - c * draft_value(q[e]), 0.0);
-    }
-    s = group_sum(s, &sm);
-    if (threadIdx.x == 0)
-      put64(reinterpret_cast<uint64_t*>(a.rest + (static_cast<size_t>(a.rest0[row]) + a.k - 1) * a.S + chunk),
-            static_cast<uint64_t>(__double_as_longlong(s)));
+  for (int e = 0; e < kSumOwn; ++e) {
+    nan |= x[e] != x[e];
+    m = fmaxf(m, x[e]);
   }
-  if (a.expect[i] == 0) return;
-  // The work-group that completes the request walks its tree.
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this work-group's sums are stored
-  if (threadIdx.x == 0)
-    sm.last = __hip_atomic_fetch_add(a.cnt + i, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.expect[i] - 1;
-  __syncthreads();
-  if (!sm.last) return;
-  if (threadIdx.x == 0) __hip_atomic_store(a.cnt + i, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  tree_walk<T, kPhase == kStats ? 1 : 4>(a, i, &sm);
+  int best = 0;
+#pragma unroll
+  for (int e = kSumOwn - 1; e >= 0; --e) best = x[e] == m ? e : best;
+  best += chunk_index<kSumOwn>(chunk);
+  wave_best(m, best);
+  if (lane == 0) {
+    top_s[wave] = m;
+    best_s[wave] = best;
+  }
+  nan = __syncthreads_or(nan);
+  m = -INFINITY;
+  best = 0x7fffffff;
+#pragma unroll
+  for (int w = 0; w < kSumWaves; ++w) better_of(m, best, top_s[w], best_s[w]);
+  double s = 0.0;
+  if (temp > 0.f) {
+    const double inv_t = 1.0 / static_cast<double>(temp);
+    if (m > -INFINITY && m < INFINITY && !nan) {
+#pragma unroll
+      for (int e = 0; e < kSumOwn; ++e) s += exp_neg((static_cast<double>(x[e]) - m) * inv_t);
+    }
+    s = group_sum(s, part);
+  }
+  if (threadIdx.x == 0) {
+    uint64_t* to = a.stat + (static_cast<size_t>(row) * a.S + chunk) * 2;
+    const float mm = nan ? __uint_as_float(0x7FC00000u) : m;
+    to[0] = __float_as_uint(mm) | static_cast<uint64_t>(static_cast<uint32_t>(best)) << 32;
+    to[1] = static_cast<uint64_t>(__double_as_longlong(s));
+  }
 }
 
-// One work-group.  The code is written for its size as much as for its work:
-// it runs in one work-group alone, whose instruction fetches nothing hides
-// (unrolled, 32000 entries and one draw took 45 us; this form, see below).
-template <class T, int kAhead>
-__device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVerifySmem* sm) {
+// Grid (chunks, rows of a.list).
+template <class T>
+__global__ __launch_bounds__(kSumThreads) void k_tree_rest(TreeVerifyArgs a) {
+  __shared__ double part[kSumWaves];
+  const int chunk = blockIdx.x, row = a.list[blockIdx.y], lane = threadIdx.x & 63;
+  const double inv_t = 1.0 / static_cast<double>(a.temp[a.req[row]]);
+  float x[kSumOwn], q[kSumOwn];
+  load_chunk<kSumOwn>(static_cast<const T*>(a.logits) + row * a.ls, a.V, chunk, a.vec_l, -INFINITY, x);
+  load_chunk<kSumOwn>(static_cast<const T*>(a.draft) + row * a.ds, a.V, chunk, a.vec_d, 0.f, q);
+  const ChunkStat first = load_stat(a, row, lane);
+  // c_k = 1 + N_1 + ... + N_{k-1}: all parts that the earlier passes left.
+  double* rest = a.rest + static_cast<size_t>(a.rest0[row]) * a.S;
+  double c = 0.0;
+  for (int t = lane; t < (a.k - 1) * a.S; t += 64) c += rest[t];
+  const RowStat st = row_stat(a, row, first, inv_t, true);
+  c = 1.0 + wave_sum(c);
+  double s = 0.0;
+  if (st.m == st.m) {
+    const double inv_z = 1.0 / st.z;
+#pragma unroll
+    for (int e = 0; e < kSumOwn; ++e)
+      s += fmax(exp_neg((static_cast<double>(x[e]) - st.m) * inv_t) * inv_z - c * draft_value(q[e]), 0.0);
+  }
+  s = group_sum(s, part);
+  if (threadIdx.x == 0) rest[static_cast<size_t>(a.k - 1) * a.S + chunk] = s;
+}
+
+// Grid (requests).  The code is written for its size as much as for its work:
+// it runs in a few work-groups, whose instruction fetches nothing hides
+// (unrolled over 16 entries per thread, one draw from 32000 took 45 us).
+template <class T>
+__global__ __launch_bounds__(kDrawThreads) void k_tree_walk(TreeVerifyArgs a) {
+  __shared__ TreeWalkSmem shared;
+  TreeWalkSmem* const sm = &shared;
+  const int i = blockIdx.x;
   const int row0 = a.row0[i], nn = a.nodes[i], tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float temp = a.temp[i];
   const bool greedy = !(temp > 0.f), drafted = a.draft != nullptr && !greedy;
@@ -369,18 +363,18 @@ __device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVe
     if (child && !ranged) raise_check(a.err, kErrTokenRange);
   }
   // Totals: rows by waves, then the arrays of parts (one per child) likewise,
-  // kAhead of them asked for at once (four cost the statistics kernel the
-  // registers that let four of its work-groups share a CU).
+  // kAhead of them asked for at once.
+  constexpr int kAhead = 4;
 #pragma unroll 1
-  for (int r0 = wave; r0 < nn; r0 += kAhead * kVWaves) {
+  for (int r0 = wave; r0 < nn; r0 += kAhead * kDrawWaves) {
     ChunkStat s[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) s[k] = load_stat<true>(a, row0 + min(r0 + k * kVWaves, nn - 1), lane);
+    for (int k = 0; k < kAhead; ++k) s[k] = load_stat(a, row0 + min(r0 + k * kDrawWaves, nn - 1), lane);
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const int r = r0 + k * kVWaves;
+      const int r = r0 + k * kDrawWaves;
       if (r >= nn) break;
-      const RowStat st = row_stat<true>(a, row0 + r, s[k], inv_t, !greedy);
+      const RowStat st = row_stat(a, row0 + r, s[k], inv_t, !greedy);
       if (lane == 0) {
         sm->m[r] = st.m;
         sm->z[r] = st.z;
@@ -390,18 +384,18 @@ __device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVe
   }
   if (drafted) {
 #pragma unroll 1
-    for (int r0 = wave; r0 < nn - 1; r0 += kAhead * kVWaves) {
+    for (int r0 = wave; r0 < nn - 1; r0 += kAhead * kDrawWaves) {
       double s[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        const double* parts = a.rest + (static_cast<size_t>(base0) + min(r0 + k * kVWaves, nn - 2)) * a.S;
-        s[k] = lane < a.S ? get_double(parts + lane) : 0.0;
-        for (int c = lane + 64; c < a.S; c += 64) s[k] += get_double(parts + c);
+        const double* parts = a.rest + (static_cast<size_t>(base0) + min(r0 + k * kDrawWaves, nn - 2)) * a.S;
+        s[k] = lane < a.S ? parts[lane] : 0.0;
+        for (int c = lane + 64; c < a.S; c += 64) s[k] += parts[c];
       }
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         const double sum = wave_sum(s[k]);
-        if (lane == 0 && r0 + k * kVWaves < nn - 1) sm->total[r0 + k * kVWaves] = sum;
+        if (lane == 0 && r0 + k * kDrawWaves < nn - 1) sm->total[r0 + k * kDrawWaves] = sum;
       }
     }
   }
@@ -490,12 +484,11 @@ __device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVe
       if (tid < a.S) {
         double w;
         if (parts) {
-          w = get_double(a.rest + (static_cast<size_t>(base0) + r0 + kids - 1) * a.S + tid);
+          w = a.rest[(static_cast<size_t>(base0) + r0 + kids - 1) * a.S + tid];
         } else {
-          const uint64_t* st = a.stat + (static_cast<size_t>(row) * a.S + tid) * 2;
-          const float mc = __uint_as_float(static_cast<uint32_t>(get64(st)));
-          const double zc = as_double(get64(st + 1));
-          w = mc > -INFINITY ? zc * exp_neg((static_cast<double>(mc) - m) * inv_t) : 0.0;
+          const ChunkStat s = load_stat(a, row, tid);
+          const float mc = __uint_as_float(static_cast<uint32_t>(s.top));
+          w = mc > -INFINITY ? as_double(s.z) * exp_neg((static_cast<double>(mc) - m) * inv_t) : 0.0;
         }
         if (without) {
           // The rejected tokens' weights (each once) leave their chunk's sum.  A
@@ -562,22 +555,22 @@ __device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVe
       pick();
     }
     // The chunk's lowest entry whose cumulative weight exceeds the target (else
-    // its last of positive weight), each thread over its kVOwn.
-    float x[kVOwn], q[kVOwn];
-    load_chunk(logits + row * a.ls, a.V, chunk, a.vec_l, -INFINITY, x);
-    if (rested) load_chunk(draft + row * a.ds, a.V, chunk, a.vec_d, 0.f, q);
-    const int i0 = chunk_index(chunk);
+    // its last of positive weight), each thread over its kDrawOwn.
+    float x[kDrawOwn], q[kDrawOwn];
+    load_chunk<kDrawOwn>(logits + row * a.ls, a.V, chunk, a.vec_l, -INFINITY, x);
+    if (rested) load_chunk<kDrawOwn>(draft + row * a.ds, a.V, chunk, a.vec_d, 0.f, q);
+    const int i0 = chunk_index<kDrawOwn>(chunk);
     if (skip) {  // without the children's tokens
 #pragma unroll 1
       for (int s = 1; s < nn; ++s) {
         const int gone = sm->parent[s] == node ? sm->tok[s] - i0 : -1;
 #pragma unroll
-        for (int e = 0; e < kVOwn; ++e) x[e] = gone == e ? -INFINITY : x[e];
+        for (int e = 0; e < kDrawOwn; ++e) x[e] = gone == e ? -INFINITY : x[e];
       }
     }
-    double w[kVOwn], own = 0.0;
+    double w[kDrawOwn], own = 0.0;
 #pragma unroll
-    for (int e = 0; e < kVOwn; ++e) {
+    for (int e = 0; e < kDrawOwn; ++e) {
       w[e] = exp_neg((static_cast<double>(x[e]) - m) * inv_t);
       if (rested) w[e] = fmax(w[e] * inv_z - c * draft_value(q[e]), 0.0);
       own += w[e];
@@ -587,10 +580,10 @@ __device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVe
     __syncthreads();
     double at = base + (scan - own);
 #pragma unroll
-    for (int v = 0; v < kVWaves - 1; ++v) at += v < wave ? sm->d[v] : 0.0;
+    for (int v = 0; v < kDrawWaves - 1; ++v) at += v < wave ? sm->d[v] : 0.0;
     int hit = 0x7fffffff, tail = -1;
 #pragma unroll
-    for (int e = 0; e < kVOwn; ++e) {
+    for (int e = 0; e < kDrawOwn; ++e) {
       at += w[e];
       if (w[e] > 0.0) {
         tail = i0 + e;
@@ -606,9 +599,9 @@ __device__ __forceinline__ void tree_walk(const TreeVerifyArgs& a, int i, TreeVe
     __syncthreads();
     int got = -1;
 #pragma unroll
-    for (int v = 0; v < kVWaves; ++v) got = max(got, sm->tail[v]);
+    for (int v = 0; v < kDrawWaves; ++v) got = max(got, sm->tail[v]);
 #pragma unroll
-    for (int v = kVWaves - 1; v >= 0; --v) got = sm->hit[v] >= 0 ? sm->hit[v] : got;
+    for (int v = kDrawWaves - 1; v >= 0; --v) got = sm->hit[v] >= 0 ? sm->hit[v] : got;
     if (got >= 0) drawn = got;
   }
   // Accepted tokens and the drawn one, then -1.

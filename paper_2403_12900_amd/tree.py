@@ -69,7 +69,7 @@ class TreeBatch:
             temperature = [temperature] * self.n
         if len(temperature) != self.n:
             _refuse("tree batch: one temperature per request")
-        return self._floats(*[float(x) for x in temperature])
+        return self._floats(*temperature)
 
 
 class TreeOps:
