@@ -375,7 +375,8 @@ size_t spr_tree_ops_workspace_bytes(void);
  * only and may be captured into a graph; a captured call keeps the host
  * arguments it was given.  Calls of one handle share its workspace: run its
  * graphs and its eager calls one after the other, and give concurrent streams
- * a handle each.  Calls may come while another device is current.
+ * a handle each.  Calls may come while another device is current.  Release a
+ * handle when its work, and its graphs' last replay, have completed.
  */
 spr_status spr_tree_ops_init(void* dev_ws, size_t ws_bytes, void* hip_stream, spr_tree_ops** out);
 
@@ -396,7 +397,8 @@ spr_status spr_tree_ops_release(spr_tree_ops* ops);
  * (head h reads KV head h / (n_heads / n_kv_heads)).  The nodes' keys and
  * values are in the cache already.  One-node trees are ordinary decode
  * attention.  What lies in the cache behind a request's nodes, or at nodes
- * that a row does not see, does not reach its output, whatever it holds.
+ * that a row does not see, does not reach its output, whatever it holds; an
+ * infinite or NaN key or value that it sees makes its output infinite or NaN.
  *   n_heads    a multiple of n_kv_heads, n_heads / n_kv_heads <= 16
  *   io_dtype   of q and out; scores, sums and products are held in fp32
  *   q          device [rows] x [n_heads * head_dim], row r at q + r * q_stride

@@ -12,8 +12,8 @@ from typing import Optional, Sequence
 import numpy as np
 import torch
 
-from .binding import (KV_BLOCK, SPR_BF16, SPR_ERR_INVALID_ARG, SPR_F32, SproutError, SprKvView, SprTreeBatch, _check, _i32,
-                      _ptr, load_library)
+from .binding import (KV_BLOCK, SPR_BF16, SPR_ERR_INVALID_ARG, SPR_F32, SproutError, SprKvView, SprTreeBatch, _check, _ptr,
+                      load_library)
 
 _DTYPES = {torch.float32: SPR_F32, torch.bfloat16: SPR_BF16}
 
@@ -49,7 +49,8 @@ class TreeBatch:
 
     def __init__(self, slots: Optional[Sequence[int]], lens: Optional[Sequence[int]], n_nodes: Sequence[int],
                  parents: Sequence[int]):
-        self._a = [None if x is None else _i32(x).reshape(-1) for x in (slots, lens, n_nodes, parents)]
+        # Copies: what the library reads later stays as it was checked here.
+        self._a = [None if x is None else np.array(x, dtype=np.int32).reshape(-1) for x in (slots, lens, n_nodes, parents)]
         n = len(self._a[2])
         if any(x is not None and len(x) != n for x in self._a[:2]):
             _refuse("tree batch: slots, lens and n_nodes must be of one length")

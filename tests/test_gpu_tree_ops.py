@@ -94,6 +94,17 @@ def test_attention_lengths_and_splits(ops, kv, lens, nodes):
 
 
 @pytest.mark.parametrize("kv", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("io", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H,Hkv,hd,nodes", [(16, 2, 128, 64), (16, 2, 64, 64), (32, 2, 128, 5), (4, 4, 128, 33), (8, 8, 64, 20)])
+def test_attention_of_wide_trees_over_long_contexts(ops, H, Hkv, hd, nodes, kv, io):
+    """Several column groups and KV splits at once, whole steps of either parity, beside a short request."""
+    rng = np.random.default_rng(hd + nodes)
+    for lens in ([1700, 5], [1683, 40]):
+        trees = [ref.random_tree(rng, nodes, "random"), ref.random_tree(rng, 3, "chain")]
+        check_attention(ops, rng, H, Hkv, hd, kv, io, lens, trees, tag="wide")
+
+
+@pytest.mark.parametrize("kv", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("hd", [64, 128])
 def test_attention_ignores_what_a_row_does_not_see(ops, kv, hd):
     """NaN and infinities in other branches' keys and values reach only the rows that see them."""
@@ -114,6 +125,26 @@ def test_attention_ignores_what_a_row_does_not_see(ops, kv, hd):
             d = np.abs(out[blind] - want[blind]).max()
             assert d <= tol, (where, bad, length, d, tol)
             assert not np.isfinite(out[[2, 4, 5]]).all(), (where, bad, length)
+
+
+def test_wide_trees_ignore_what_a_row_does_not_see(ops):
+    """The same for column groups that share their blocks: many heads per KV head, poison in one branch."""
+    rng = np.random.default_rng(18)
+    par = [-1, 0, 0, 1, 2, 4, 3, 0]
+    for kv in (torch.float32, torch.bfloat16):
+        for hd in (64, 128):
+            for length in (0, 30, 200):
+                cache = ref.Cache(rng, 1, 1, hd, [length + 8], kv, fill=float("inf"))
+                p = length + 2
+                cache.v[0, cache.table[0, p // 16], :, p % 16, ::3] = float("nan")
+                cache.k[0, cache.table[0, p // 16], :, p % 16] = float("inf")
+                q = torch.from_numpy(rng.standard_normal((8, 16, hd), dtype=np.float32))
+                out = ops.attention(cache.device(), 0, batch_of([0], [length], [par]), q.cuda()).double().cpu().numpy()
+                want = ref.attention(cache, 0, [0], [length], [par], q)
+                blind = [0, 1, 3, 6, 7]
+                assert np.isfinite(want[blind]).all()
+                assert np.abs(out[blind] - want[blind]).max() <= attention_tolerance(cache, q, length + 8, torch.float32), (kv, hd, length)
+                assert not np.isfinite(out[[2, 4, 5]]).all()
 
 
 def test_attention_of_strided_rows_leaves_the_rest(ops):
@@ -440,6 +471,69 @@ def test_another_stream(ops):
     again = ops.attention(view, 0, b, qd)
     torch.cuda.synchronize()
     assert torch.equal(got, want) and torch.equal(again, want)
+
+
+def test_captured_without_a_call_before():
+    """A handle's first call of a kernel may be the captured one."""
+    rng = np.random.default_rng(43)
+    o = fresh_ops()
+    cache = ref.Cache(rng, 1, 1, 128, [90], torch.bfloat16)
+    view, b = cache.device(), batch_of([0], [80], [[-1, 0, 0, 1, 1]])
+    q = torch.from_numpy(rng.standard_normal((5, 5, 128), dtype=np.float32)).to(torch.bfloat16).cuda()
+    logits = torch.randn(5, 77, device="cuda").to(torch.bfloat16)
+    tokens = torch.zeros(5, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = o.attention(view, 0, b, q)
+        e, p, c = o.verify(b, tokens, logits, temperature=0.0)
+        o.keep(view, b, p, c)
+    k0 = view.k.clone()
+    for _ in range(3):
+        view.k.copy_(k0)
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        want = ref.attention(cache, 0, [0], [80], [[-1, 0, 0, 1, 1]], q.cpu())
+        assert np.abs(out.double().cpu().numpy() - want).max() <= attention_tolerance(cache, q.cpu(), 90, torch.bfloat16)
+        same([x.cpu().numpy() for x in (e, p, c)], ref.verify([[-1, 0, 0, 1, 1]], np.zeros(5, np.int32), logits.double().cpu().numpy(),
+                                                              None, None, None, [0]))
+    o.close()
+
+
+def test_refusals_leave_the_handle_usable(ops):
+    from paper_2403_12900_amd.binding import SPR_ERR_INVALID_ARG, SproutError
+    rng = np.random.default_rng(44)
+    cache = ref.Cache(rng, 2, 2, 64, [40, 40], torch.bfloat16)
+    view, b = cache.device(), batch_of([0, 1], [20, 30], [[-1, 0, 0], [-1]])
+    q = torch.randn(4, 4, 64, device="cuda")
+    f = torch.rand(4, device="cuda")
+    tok = torch.zeros(4, dtype=torch.int32, device="cuda")
+    z = torch.randn(4, 50, device="cuda")
+    n2 = torch.zeros(2, dtype=torch.int32, device="cuda")
+    calls = [lambda: ops.attention(view, 2, b, q), lambda: ops.attention(view, -1, b, q),
+             lambda: ops.attention(view, 0, batch_of([0, 2], [20, 30], [[-1, 0, 0], [-1]]), q),
+             lambda: ops.attention(view, 0, batch_of([0, 1], [20, 48], [[-1, 0, 0], [-1]]), q),
+             lambda: ops.attention(view, 0, b, q[:3]), lambda: ops.attention(view, 0, b, q.half()), lambda: ops.attention(view, 0, b, q.cpu()),
+             lambda: ops.attention(view, 0, b, torch.randn(4, 3, 64, device="cuda")),
+             lambda: ops.attention(view, 0, b, torch.randn(4, 34, 64, device="cuda")),
+             lambda: ops.attention(view, 0, b, torch.randn(4, 4, 128, device="cuda")[..., ::2]),
+             lambda: ops.attention(view, 0, b, torch.randn(4, 4, 65, device="cuda")[..., 1:]),
+             lambda: ops.attention(view, 0, b, q, out=q[:, :2]),
+             lambda: ops.verify(b, tok[:3], z, f, f[:2]), lambda: ops.verify(b, tok.long(), z, f, f[:2]),
+             lambda: ops.verify(b, tok, z, None, None), lambda: ops.verify(b, tok, z, f, None), lambda: ops.verify(b, tok, z, f, f),
+             lambda: ops.verify(b, tok, z.half(), f, f[:2]), lambda: ops.verify(b, tok, z.t().contiguous().t(), f, f[:2]),
+             lambda: ops.verify(b, tok, z, f, f[:2], draft_probs=z[:, :40]), lambda: ops.verify(b, tok, z, f, f[:2], draft_probs=z.bfloat16()),
+             lambda: ops.verify(b, tok, z, f, f[:2], temperature=-1.0), lambda: ops.verify(b, tok, z, f, f[:2], temperature=[1.0]),
+             lambda: ops.verify(b, tok, z[:, :0], f, f[:2]),
+             lambda: ops.keep(view, b, tok[:3], n2), lambda: ops.keep(view, b, tok, n2.long()), lambda: ops.keep(view, b, tok.cpu(), n2)]
+    for k, call in enumerate(calls):
+        with pytest.raises(SproutError) as e:
+            call()
+        assert e.value.status == SPR_ERR_INVALID_ARG, k
+    ops.attention(view, 1, b, q)
+    ops.verify(b, tok, z, temperature=0.0)
+    torch.cuda.synchronize()
 
 
 def test_captured_and_replayed():

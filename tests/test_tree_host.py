@@ -224,6 +224,10 @@ def test_python_side_refusals():
         with pytest.raises(SproutError):
             TreeBatch(*bad)
     b = TreeBatch(None, None, [2, 1], [-1, 0, -1])
+    parents = np.array([-1, 0, -1], dtype=np.int32)
+    b2 = TreeBatch(None, None, [2, 1], parents)
+    parents[:] = 99  # the batch keeps what it was given
+    assert [b2._c.parents[i] for i in range(3)] == [-1, 0, -1]
     t = b.temperatures(0.5)
     assert [t[0], t[1]] == [0.5, 0.5] and b.temperatures(None) is None
     with pytest.raises(SproutError):
