@@ -397,8 +397,8 @@ spr_status spr_tree_ops_release(spr_tree_ops* ops);
  * (head h reads KV head h / (n_heads / n_kv_heads)).  The nodes' keys and
  * values are in the cache already.  One-node trees are ordinary decode
  * attention.  What lies in the cache behind a request's nodes, or at nodes
- * that a row does not see, does not reach its output, whatever it holds; an
- * infinite or NaN key or value that it sees makes its output infinite or NaN.
+ * that a row does not see, does not reach its output, whatever it holds (a row
+ * that sees an infinite key may get NaN where the formula gives it no weight).
  *   n_heads    a multiple of n_kv_heads, n_heads / n_kv_heads <= 16
  *   io_dtype   of q and out; scores, sums and products are held in fp32
  *   q          device [rows] x [n_heads * head_dim], row r at q + r * q_stride
@@ -454,7 +454,8 @@ spr_status spr_tree_verify(spr_tree_ops* ops, const spr_tree_batch* batch, int32
  * Positions from lens[i] + count[i] on are left as they were or hold what
  * rejected nodes left there.  Per request, nodes 0 <= path[0] < path[1] < ...
  * < n_nodes[i] and count[i] <= n_nodes[i]; one that breaks this is left as it
- * is and fails the handle's next call.  count[i] < 1 moves nothing.
+ * is and fails the handle's next call.  count[i] < 1 moves nothing.  The blocks
+ * that hold a request's nodes are its alone (cached ones may be shared).
  *   path    device int32 [rows], count device int32 [n]: as spr_tree_verify
  *           writes them
  */

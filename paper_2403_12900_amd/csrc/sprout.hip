@@ -839,13 +839,23 @@ spr_status forward_any(spr_model* m, const RowSet& rs, const int32_t* tok_in, in
                                    : forward<BF16, F32>(m, rs, tok_in, tok_out, logits, hist, sc);
 }
 
+// Device check bits (kErr*), reported by the next call.
+std::string device_check_message(int bits) {
+  std::string s = "a device check failed on an earlier call:";
+  if (bits & kErrTokenRange) s += " a token id outside [0, vocab) was fed (it was read as a clamped id);";
+  if (bits & kErrLogits) s += " a logits row had no finite maximum (its token was set to 0);";
+  if (bits & kErrBlockId) s += " a block id outside the pool was met;";
+  if (bits & kErrPath) s += " a path of tree nodes was malformed;";
+  return s + " the model's state is unreliable; release it";
+}
+
 spr_status check_model(spr_model* m) {
   if (m == nullptr) return fail(SPR_ERR_INVALID_ARG, "model is null");
   if (m->sticky == SPR_OK && m->err_host != nullptr) {
     const int bits = *reinterpret_cast<volatile int*>(m->err_host);
     if (bits != 0) {
       m->sticky = SPR_ERR_DEVICE_CHECK;
-      m->sticky_msg = spr::device_check_message(bits);
+      m->sticky_msg = device_check_message(bits);
     }
   }
   if (m->sticky != SPR_OK) return fail(m->sticky, m->sticky_msg);
@@ -1032,16 +1042,6 @@ namespace spr {
 
 spr_status set_error(spr_status s, const std::string& msg) { return fail(s, msg); }
 void clear_error() { g_err.clear(); }
-
-// Device check bits (kErr*), reported by the next call.
-std::string device_check_message(int bits) {
-  std::string s = "a device check failed on an earlier call:";
-  if (bits & kErrTokenRange) s += " a token id outside [0, vocab) was fed (it was read as a clamped id);";
-  if (bits & kErrLogits) s += " a logits row had no finite maximum (its token was set to 0);";
-  if (bits & kErrBlockId) s += " a block id outside the pool was met;";
-  if (bits & kErrPath) s += " a path of tree nodes was malformed;";
-  return s + " the model's state is unreliable; release it";
-}
 
 }  // namespace spr
 

@@ -214,7 +214,12 @@ spr_status check_ops(spr_tree_ops* o) {
     const int bits = *reinterpret_cast<volatile int*>(o->err_host);
     if (bits != 0) {
       o->sticky = SPR_ERR_DEVICE_CHECK;
-      o->sticky_msg = spr::device_check_message(bits);
+      o->sticky_msg = "a device check failed on an earlier call:";
+      if (bits & kErrTokenRange) o->sticky_msg += " a drafted token outside [0, vocab);";
+      if (bits & kErrLogits) o->sticky_msg += " a logits row with a NaN or no finite maximum;";
+      if (bits & kErrBlockId) o->sticky_msg += " a block id outside the pool;";
+      if (bits & kErrPath) o->sticky_msg += " a malformed path of tree nodes;";
+      o->sticky_msg += " release the handle";
     }
   }
   return o->sticky == SPR_OK ? SPR_OK : set_error(o->sticky, o->sticky_msg);

@@ -32,6 +32,7 @@ template <class KP, class IO, int HD, int CW>
 hipError_t launch(const TreeAttnCall& c) {
   const TreeInfo& t = *c.tree;
   TreeAttnArgs a{};
+  if (static_cast<int64_t>(t.rows) * c.kv.n_kv_heads > c.sc.n_cnt) return hipErrorInvalidValue;  // a column group has a row at least
   const size_t layer = static_cast<size_t>(c.kv.n_blocks) * c.kv.n_kv_heads * 16 * HD * c.layer;
   a.q = c.q;
   a.out = c.out;

@@ -325,7 +325,10 @@ struct TreeSmem {
   int last;
 };
 
-constexpr float kTreeFloor = -1e38f;  // running maximum before the first score
+// Running maximum before the first score: below every finite one (a score times
+// log2(e) / 8 stays above -6.2e37), and finite, so that a masked score less it is
+// -infinity and not NaN.
+constexpr float kTreeFloor = -1e38f;
 constexpr float kRaise = 8.f;
 
 // Column c of a request (c < its nodes * G): token row and query head.

@@ -73,6 +73,4 @@ namespace spr {
 // The calling thread's last error message (spr_last_error).
 spr_status set_error(spr_status s, const std::string& msg);
 void clear_error();
-// Text of a device check flag.
-std::string device_check_message(int bits);
 }  // namespace spr

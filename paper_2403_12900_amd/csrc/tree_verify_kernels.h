@@ -476,7 +476,7 @@ __global__ __launch_bounds__(kDrawThreads) void k_tree_walk(TreeVerifyArgs a) {
         left = sm->total[r0 + k];
       }
     }
-    const bool rested = drafted && kids > 0 && left > 0.0;
+    bool rested = drafted && kids > 0 && left > 0.0;
     bool skip = !drafted && kids > 0;
     // Chunk sums of the weights.
     const auto chunk_sums = [&](bool parts, bool without) {
@@ -549,60 +549,72 @@ __global__ __launch_bounds__(kDrawThreads) void k_tree_walk(TreeVerifyArgs a) {
     };
     chunk_sums(rested, skip);
     pick();
-    if (skip && !(all > 0.0)) {  // nothing left: draw from p
-      skip = false;
-      chunk_sums(false, false);
+    // A chunk whose sum is above 0 by rounding alone (its weights were all
+    // rejected) has no entry to draw: its sum is cleared, and the draw made again.
+#pragma unroll 1
+    for (;;) {
+      if ((skip || rested) && !(all > 0.0)) {  // nothing left: draw from p
+        skip = rested = false;
+        chunk_sums(false, false);
+        pick();
+      }
+      // The chunk's lowest entry whose cumulative weight exceeds the target (else
+      // its last of positive weight), each thread over its kDrawOwn.
+      float x[kDrawOwn], q[kDrawOwn];
+      load_chunk<kDrawOwn>(logits + row * a.ls, a.V, chunk, a.vec_l, -INFINITY, x);
+      if (rested) load_chunk<kDrawOwn>(draft + row * a.ds, a.V, chunk, a.vec_d, 0.f, q);
+      const int i0 = chunk_index<kDrawOwn>(chunk);
+      if (skip) {  // without the children's tokens
+#pragma unroll 1
+        for (int s = 1; s < nn; ++s) {
+          const int gone = sm->parent[s] == node ? sm->tok[s] - i0 : -1;
+#pragma unroll
+          for (int e = 0; e < kDrawOwn; ++e) x[e] = gone == e ? -INFINITY : x[e];
+        }
+      }
+      double w[kDrawOwn], own = 0.0;
+#pragma unroll
+      for (int e = 0; e < kDrawOwn; ++e) {
+        w[e] = exp_neg((static_cast<double>(x[e]) - m) * inv_t);
+        if (rested) w[e] = fmax(w[e] * inv_z - c * draft_value(q[e]), 0.0);
+        own += w[e];
+      }
+      const double scan = wave_scan(own);
+      if (lane == 63) sm->d[wave] = scan;
+      __syncthreads();
+      double at = base + (scan - own);
+#pragma unroll
+      for (int v = 0; v < kDrawWaves - 1; ++v) at += v < wave ? sm->d[v] : 0.0;
+      int hit = 0x7fffffff, tail = -1;
+#pragma unroll
+      for (int e = 0; e < kDrawOwn; ++e) {
+        at += w[e];
+        if (w[e] > 0.0) {
+          tail = i0 + e;
+          if (at > target) hit = min(hit, tail);
+        }
+      }
+      const uint64_t hits = __ballot(hit != 0x7fffffff), tails = __ballot(tail >= 0);
+      if (lane == 0) {
+        sm->hit[wave] = sm->tail[wave] = -1;
+        if (hits != 0) sm->hit[wave] = __builtin_amdgcn_readlane(hit, __ffsll(static_cast<unsigned long long>(hits)) - 1);
+        if (tails != 0) sm->tail[wave] = __builtin_amdgcn_readlane(tail, 63 - __clzll(static_cast<long long>(tails)));
+      }
+      __syncthreads();
+      int got = -1;
+#pragma unroll
+      for (int v = 0; v < kDrawWaves; ++v) got = max(got, sm->tail[v]);
+#pragma unroll
+      for (int v = kDrawWaves - 1; v >= 0; --v) got = sm->hit[v] >= 0 ? sm->hit[v] : got;
+      if (got >= 0) {
+        drawn = got;
+        break;
+      }
+      if (!(all > 0.0)) break;
+      if (tid == 0) sm->w[chunk] = 0.0;
+      __syncthreads();
       pick();
     }
-    // The chunk's lowest entry whose cumulative weight exceeds the target (else
-    // its last of positive weight), each thread over its kDrawOwn.
-    float x[kDrawOwn], q[kDrawOwn];
-    load_chunk<kDrawOwn>(logits + row * a.ls, a.V, chunk, a.vec_l, -INFINITY, x);
-    if (rested) load_chunk<kDrawOwn>(draft + row * a.ds, a.V, chunk, a.vec_d, 0.f, q);
-    const int i0 = chunk_index<kDrawOwn>(chunk);
-    if (skip) {  // without the children's tokens
-#pragma unroll 1
-      for (int s = 1; s < nn; ++s) {
-        const int gone = sm->parent[s] == node ? sm->tok[s] - i0 : -1;
-#pragma unroll
-        for (int e = 0; e < kDrawOwn; ++e) x[e] = gone == e ? -INFINITY : x[e];
-      }
-    }
-    double w[kDrawOwn], own = 0.0;
-#pragma unroll
-    for (int e = 0; e < kDrawOwn; ++e) {
-      w[e] = exp_neg((static_cast<double>(x[e]) - m) * inv_t);
-      if (rested) w[e] = fmax(w[e] * inv_z - c * draft_value(q[e]), 0.0);
-      own += w[e];
-    }
-    const double scan = wave_scan(own);
-    if (lane == 63) sm->d[wave] = scan;
-    __syncthreads();
-    double at = base + (scan - own);
-#pragma unroll
-    for (int v = 0; v < kDrawWaves - 1; ++v) at += v < wave ? sm->d[v] : 0.0;
-    int hit = 0x7fffffff, tail = -1;
-#pragma unroll
-    for (int e = 0; e < kDrawOwn; ++e) {
-      at += w[e];
-      if (w[e] > 0.0) {
-        tail = i0 + e;
-        if (at > target) hit = min(hit, tail);
-      }
-    }
-    const uint64_t hits = __ballot(hit != 0x7fffffff), tails = __ballot(tail >= 0);
-    if (lane == 0) {
-      sm->hit[wave] = sm->tail[wave] = -1;
-      if (hits != 0) sm->hit[wave] = __builtin_amdgcn_readlane(hit, __ffsll(static_cast<unsigned long long>(hits)) - 1);
-      if (tails != 0) sm->tail[wave] = __builtin_amdgcn_readlane(tail, 63 - __clzll(static_cast<long long>(tails)));
-    }
-    __syncthreads();
-    int got = -1;
-#pragma unroll
-    for (int v = 0; v < kDrawWaves; ++v) got = max(got, sm->tail[v]);
-#pragma unroll
-    for (int v = kDrawWaves - 1; v >= 0; --v) got = sm->hit[v] >= 0 ? sm->hit[v] : got;
-    if (got >= 0) drawn = got;
   }
   // Accepted tokens and the drawn one, then -1.
   if (tid < nn) {

@@ -77,7 +77,8 @@ class TreeOps:
     """An operator handle on one device (spr_tree_ops_init), in a torch workspace.
 
     Calls enqueue on the device's current stream; a call on another stream than the handle's last one first waits for
-    that one (not while a graph is captured: the capture's own order holds)."""
+    that one (not while a graph is captured: the capture's own order holds).  The handle outlives the graphs that hold
+    its calls."""
 
     def __init__(self, device: int = 0):
         self.lib = load_library()
@@ -95,9 +96,10 @@ class TreeOps:
         if torch._C._cuda_getCurrentRawStream(self.index) == self.raw_stream:
             return
         s = torch.cuda.current_stream(self.device)
-        if not torch.cuda.is_current_stream_capturing():
-            s.wait_stream(self.stream)
-            self.ws.record_stream(s)
+        with torch.cuda.device(self.device):
+            if not torch.cuda.is_current_stream_capturing():
+                s.wait_stream(self.stream)
+                self.ws.record_stream(s)
         _check(self.lib.spr_tree_ops_set_stream(self.h, s.cuda_stream))
         self.stream, self.raw_stream = s, s.cuda_stream
 

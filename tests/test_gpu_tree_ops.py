@@ -286,6 +286,34 @@ def test_verify_ties_and_repeated_tokens(ops):
     assert got[0][5] == 4500 and got[2][1] == 1
 
 
+def test_verify_never_draws_a_rejected_token(ops):
+    """Whole chunks of the vocabulary whose weight the rejected tokens took, where rounding (49 * (1 / 49) < 1) leaves a
+    trace of it, at both ends of the draw."""
+    V = 12000
+    for others in (48, 97, 102):
+        for home in (10, 5000, 11999):
+            z = torch.full((3, V), -float("inf"))
+            z[:, home] = 0.0
+            at = [t for t in range(1000, 1000 + 50 * others, 50) if t // 4096 != home // 4096][:others]
+            at += [t for t in range(9000, 11900) if t // 4096 != home // 4096][:others - len(at)]
+            at += list(range(2000, 4000))[:others - len(at)]
+            z[:, at] = 0.0
+            tokens = torch.tensor([0, home, home], dtype=torch.int32)
+            ua = torch.tensor([0.0, 0.99, 0.99])
+            for us in (0.0, 0.5, 1 - 2.0**-24):
+                # Equal weights: the k-th entry's cumulative weight is (k + 1) / others up to rounding, so a target that
+                # is exactly k / others may fall to entry k - 1 as well.
+                x = us * others
+                right = [sorted(at)[k] for k in {int(np.floor(x)), int(np.ceil(x)) - 1} if k >= 0]
+                # a child that is the chunk's only weight, once and twice; and the same as a draft that puts all on it
+                e, p, c = run_verify(ops, [[-1, 0, 0]], tokens, z, ua, torch.tensor([us]))
+                assert c[0] == 1 and e[0] in right, (others, home, us)
+                q = torch.zeros(3, V)
+                q[:, home] = 1.0
+                e, p, c = run_verify(ops, [[-1, 0, 0]], tokens, z, ua, torch.tensor([us]), q)
+                assert c[0] == 1 and e[0] in right, (others, home, us)
+
+
 def test_verify_strides_and_alignment(ops):
     rng = np.random.default_rng(21)
     trees = [ref.random_tree(rng, 7, "levels"), ref.random_tree(rng, 4, "chain")]
@@ -398,6 +426,24 @@ def test_keep_moves_paths(ops, kv, Hkv, hd, layers):
         assert torch.equal(view.v.cpu(), ref.to_tiles(cache.v, True)), trial
 
 
+def test_keep_with_a_bad_block_id_moves_nothing():
+    rng = np.random.default_rng(32)
+    for pos, bad in ((40, -1), (16, 99)):  # a source's block, a target's
+        o = fresh_ops()
+        cache = ref.Cache(rng, 2, 2, 64, [46, 30], torch.float32)
+        view = cache.device()
+        view.block_table[0, pos // 16] = bad
+        b = batch_of([0, 1], [28, 9], [[-1] + [0] * 15, [-1, 0, 0]])
+        p = torch.tensor([0, 13] + [-1] * 14 + [0, 2, -1], dtype=torch.int32).cuda()
+        o.keep(view, b, p, torch.tensor([2, 2], dtype=torch.int32).cuda())
+        torch.cuda.synchronize()
+        ref.keep(cache, [1], [9], [[-1, 0, 0]], [0, 2], [2])  # the other request's
+        assert torch.equal(view.k.cpu(), ref.to_tiles(cache.k, False)) and torch.equal(view.v.cpu(), ref.to_tiles(cache.v, True))
+        with pytest.raises(Exception, match="block id"):
+            o.keep(view, b, p, torch.tensor([2, 2], dtype=torch.int32).cuda())
+        o.close()
+
+
 def test_keep_refuses_malformed_paths():
     rng = np.random.default_rng(31)
     for path, count in (([0, 3, 2, -1], 3), ([0, 0, 1, -1], 3), ([0, 1, 4, -1], 3), ([0, 1, 2, 3], 5), ([0, -1, 2, 3], 3),
@@ -471,6 +517,33 @@ def test_another_stream(ops):
     again = ops.attention(view, 0, b, qd)
     torch.cuda.synchronize()
     assert torch.equal(got, want) and torch.equal(again, want)
+
+
+def test_two_handles_on_two_streams():
+    """Concurrent calls of a handle each; split rows, so that shared counters or partials would show."""
+    rng = np.random.default_rng(45)
+    handles, jobs = [fresh_ops(), fresh_ops()], []
+    for o in handles:
+        cache = ref.Cache(rng, 1, 2, 128, [5000, 900], torch.bfloat16)
+        b = batch_of([0, 1], [4990, 880], [ref.random_tree(rng, 9, "levels"), ref.random_tree(rng, 12, "random")])
+        q = torch.from_numpy(rng.standard_normal((21, 8, 128), dtype=np.float32)).cuda()
+        z = torch.randn(21, 20000, device="cuda")
+        tok = torch.randint(0, 20000, (21,), dtype=torch.int32, device="cuda")
+        view, f = cache.device(), torch.rand(21, device="cuda")
+        want = (o.attention(view, 0, b, q), *o.verify(b, tok, z, f, f[:2]))
+        jobs.append((o, view, b, q, z, tok, f, want))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for _ in range(20):
+        for s, (o, view, b, q, z, tok, f, _) in zip(streams, jobs):
+            with torch.cuda.stream(s):
+                got.append((o.attention(view, 0, b, q), *o.verify(b, tok, z, f, f[:2])))
+    torch.cuda.synchronize()
+    for k, outs in enumerate(got):
+        assert all(torch.equal(x, y) for x, y in zip(outs, jobs[k % 2][-1])), k
+    for o in handles:
+        o.close()
 
 
 def test_captured_without_a_call_before():
