@@ -443,15 +443,17 @@ __device__ __forceinline__ TreeItem tree_item(const TreeAttnArgs& a, int f) {
   return t;
 }
 
-// Block id of block i (< end) of the table row; one outside the pool is
-// reported and reads block 0.
-__device__ __forceinline__ int block_id(const TreeAttnArgs& a, const int32_t* btrow, int i, int end) {
-  int id = i < end ? btrow[i] : 0;
+// A block id from the table; one outside the pool is reported and reads block 0.
+__device__ __forceinline__ int in_pool(const TreeAttnArgs& a, int id) {
   if (static_cast<unsigned>(id) >= static_cast<unsigned>(a.nb)) {
     raise_check(a.err, kErrBlockId);
     id = 0;
   }
   return id;
+}
+// Id of block i (< end) of the table row.
+__device__ __forceinline__ int block_id(const TreeAttnArgs& a, const int32_t* btrow, int i, int end) {
+  return in_pool(a, i < end ? btrow[i] : 0);
 }
 
 // Counts a split in and, in the one that arrives last, merges all partials of
@@ -755,20 +757,22 @@ __global__ __launch_bounds__(256, (NT == 1 && TreeParts<KP, IO>::q == 1 ? 3 : 2)
   const auto round_tile = [&](int r) { return Stage::kTile == 128 ? 2 * r + half : r / kRounds; };
   const auto round_piece = [&](int r) { return in_tile + (r % kRounds) * 256; };
 
-  // Byte offsets of the next 64 blocks' tiles of this KV head, one per lane.
-  uint64_t off = 0;
+  // Block ids are asked for one step before the blocks they name; past the
+  // split's end they are its last one's, so that every fetch reads the cache (a
+  // missing second block re-reads the first, masked).
+  int ids[BP];
+  const auto ask = [&](int i) {
+#pragma unroll
+    for (int b = 0; b < BP; ++b) ids[b] = t.btrow[min(i + b, end - 1)];
+  };
   u32x4_t next[2][Stage::kPer];  // of even and odd steps
-  const auto fetch = [&](int i, auto parity) {
-    const int k = i - t.first;
-    if ((k & 63) == 0)
-      off = (static_cast<uint64_t>(block_id(a, t.btrow, i + lane, end)) * a.Hkv + kvh) * (Stage::kTile * 16);
+  // The blocks whose ids were asked for, then the ids of the step at `then`.
+  const auto fetch = [&](int then, auto parity) {
     uint64_t at[BP];
 #pragma unroll
-    for (int b = 0; b < BP; ++b) {
-      const int from = (i + b < end ? k + b : k) & 63;  // a missing second block re-reads the first, masked
-      at[b] = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(off), from)) |
-              static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(off >> 32), from))) << 32;
-    }
+    for (int b = 0; b < BP; ++b)
+      at[b] = (static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(in_pool(a, ids[b]))) * a.Hkv + kvh) * (Stage::kTile * 16);
+    ask(then);
 #pragma unroll
     for (int r = 0; r < Stage::kPer; ++r) {
       const int which = round_tile(r);
@@ -891,22 +895,26 @@ __global__ __launch_bounds__(256, (NT == 1 && TreeParts<KP, IO>::q == 1 ? 3 : 2)
 
   constexpr std::integral_constant<int, 0> kEven{};
   constexpr std::integral_constant<int, 1> kOdd{};
-  // One step: ask for the one after the next, compute, put the next.
+  // One step: fetch the one after the next, compute, put the next.  Whole steps
+  // do so without a condition: behind a fetch that may not have been made the
+  // put would wait for all loads, the newest included.
   const auto step = [&](int i, auto parity, auto other, auto tail) {
+    constexpr bool whole = !decltype(tail)::value;
     __syncthreads();  // this step is in its buffer; the other buffer has been read
-    if (i + 2 * BP < end) fetch(i + 2 * BP, parity);
+    if (whole || i + 2 * BP < end) fetch(i + 3 * BP, parity);
     if (busy) compute(i, parity, tail);
-    if (i + BP < end) put(i + BP, other, tail);
+    if (whole || i + BP < end) put(i + BP, other, tail);
   };
 
   if (tid < 2) odd_s[tid] = 0;
   __syncthreads();
   int i = t.first;
-  fetch(i, kEven);
-  if (i + BP < end) fetch(i + BP, kOdd);
+  ask(i);
+  fetch(i + BP, kEven);
+  fetch(i + 2 * BP, kOdd);
   if (is_tail(i)) put(i, kEven, kTail);
   else put(i, kEven, kPlain);
-  for (; i + 2 * BP < end && !is_tail(i + 2 * BP); i += 2 * BP) {  // two steps and the one after them are whole
+  for (; i + 3 * BP < end && !is_tail(i + 2 * BP); i += 2 * BP) {  // two steps and the one after them are whole
     step(i, kEven, kOdd, kPlain);
     step(i + BP, kOdd, kEven, kPlain);
   }
