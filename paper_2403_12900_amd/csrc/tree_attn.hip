@@ -15,6 +15,12 @@ constexpr auto kernel() {
   else return &k_tree_attn_shared<KP, IO, HD, CW / 64>;
 }
 
+// Floats of partial outputs that the last split's work-group merges by itself:
+// more cost more there than a second launch does (192 columns times splits of
+// 128 dimensions: 12.5 us against 13.0 with the launch, 1 request of 352: 14.2
+// against 13.3, of 1024: 20.2 against 16.3).
+constexpr int kMergeInside = 192 * 128;
+
 // Work-groups of the kernel that a CU holds at once.
 template <class KP, class IO, int HD, int CW>
 int groups_per_cu() {
@@ -70,8 +76,20 @@ hipError_t launch(const TreeAttnCall& c) {
   }
   a.item0[t.n] = sp.item0[t.n];
   for (int r = 0; r < t.rows; ++r) a.anc[r] = t.anc[r];
+  // Where the last work-group of a column group would have much to read, the
+  // merge is a launch of its own over all outputs; else it stays in the kernel.
+  const int groups = sp.cg0[t.n - 1] + sp.ncg[t.n - 1];
+  int most = 0;  // columns times splits of one merge
+  for (int r = 0; r < t.n; ++r)
+    most = std::max(most, std::min(CW, t.nodes[sp.order[r]] * a.G) * ((sp.item0[r + 1] - sp.item0[r]) / sp.ncg[r]));
+  a.apart = sp.item0[t.n] > groups && (CW > 32 || most * HD > kMergeInside);
   kernel<KP, IO, HD, CW>()<<<dim3(a.Hkv, sp.item0[t.n]), 256, 0, c.st>>>(a);
-  return hipGetLastError();
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && a.apart) {
+    k_tree_merge<IO, HD, CW><<<dim3(a.Hkv, groups, CW / kMergeColumns), 256, 0, c.st>>>(a);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 // Columns per work-group by what the registers hold beside the accumulators:

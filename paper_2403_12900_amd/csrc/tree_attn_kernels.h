@@ -28,12 +28,29 @@
 // the rescaling of O.
 //
 // Two kernels.  Both cut a request's blocks into KV splits, one work-group
-// each, merged by the split that arrives last:
+// each, and write a partial result where a request has several:
 //   k_tree_attn         up to 32 columns: the four waves of a work-group take
 //                       runs of blocks, K and V go straight into registers.
+//                       Bound by the cache's bytes: 32 requests of 32 heads,
+//                       4 nodes, about 470 positions (bf16 cache of 253 MB):
+//                       45 us, 5.6 TB/s.  One request of 600 positions and 9
+//                       nodes: 9.6 us, nearly all of it latency (arguments,
+//                       block ids, blocks, merge, one after the other).
 //   k_tree_attn_shared  more: the four waves take 16 NT columns each and share
 //                       every block through LDS, so the cache is read once per
-//                       64 NT columns and a wave's work per byte stays high.
+//                       64 NT columns and a wave's work per byte stays high
+//                       (64 columns on the other kernel's plan: 110 us where
+//                       this took 78 at first; 512 columns: 504 and 227).
+//                       Bound by the matrix
+//                       unit in fp32 (64 columns, 16 x 5632 positions: 230 us,
+//                       103 of 157 TFLOP/s), by products, exponentials and LDS
+//                       reads in turn in bf16 (512 columns, 2 x 24000 positions:
+//                       147 us, 690 TFLOP/s), and at short contexts by its ends:
+//                       about 8 us until the first step runs, 6 us from the
+//                       last to the outputs.
+// The partials are merged by the split that arrives last where that is little,
+// else by k_tree_merge.  (With 64 columns and more in that one work-group: 512
+// columns over 2 x 6000 positions 65 us, with k_tree_merge 51.)
 #pragma once
 
 #include <type_traits>
@@ -55,6 +72,7 @@ struct TreeAttnArgs {
   int32_t* cnt;        // [column group][Hkv] arrived splits; zero between launches
   int* err;
   int n, H, Hkv, G, mb, nb, bps;  // bps: blocks per split
+  int apart;           // splits are merged by k_tree_merge
   uint32_t part_bytes;
   float qscale;        // log2(e) / sqrt(hd)
   ActRec rec;          // layout of out, where it is an activation record
@@ -74,8 +92,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{lo, hi}), bf16x2_t));
 }
 
-// Formats of q and out.  load: per16 values of a row as floats (kRaw: as the
-// 16-byte bf16 fragment piece itself).
+// Formats of q and out (kRaw: bf16, which a bf16 cache's operand takes as it is).
 struct TreeIoF32 {
   using elem = float;
   static constexpr bool kRaw = false;
@@ -340,35 +357,39 @@ __device__ __forceinline__ TreeColumn tree_column(const TreeAttnArgs& a, int row
   return TreeColumn{row0 + node, kvh * a.G + c - node * a.G};
 }
 
-// This lane's piece (K-block c, group g) of one column's query, in fp32, or
-// (kRaw with a bf16 cache) as the fragment piece itself.
+// This lane's piece (K-block c, group g) of one column's query: as it is stored,
+// and in the operand's parts.
+struct QueryPiece {
+  uint4 x, y;
+};
 template <class KP, class IO, int HD>
-__device__ __forceinline__ void load_query(const TreeAttnArgs& a, const TreeColumn& col, int c, int g, uint4* out) {
+__device__ __forceinline__ QueryPiece load_query(const TreeAttnArgs& a, const TreeColumn& col, int c, int g) {
   const typename IO::elem* src =
       static_cast<const typename IO::elem*>(a.q) + col.row * a.qs + col.hq * HD + c * KP::kblk + g * KP::per16;
-  constexpr int QP = TreeParts<KP, IO>::q;
-  if constexpr (IO::kRaw && KP::per16 == 8) {
-    out[0] = *reinterpret_cast<const uint4*>(src);
+  QueryPiece p{};
+  if constexpr (IO::kRaw && KP::per16 == 4) {
+    const uint2 u = *reinterpret_cast<const uint2*>(src);
+    p.x.x = u.x;
+    p.x.y = u.y;
   } else {
-    float v[KP::per16];
-    if constexpr (IO::kRaw) {
-      const uint2 u = *reinterpret_cast<const uint2*>(src);
-      v[0] = __uint_as_float(u.x << 16);
-      v[1] = __uint_as_float(u.x & 0xFFFF0000u);
-      v[2] = __uint_as_float(u.y << 16);
-      v[3] = __uint_as_float(u.y & 0xFFFF0000u);
-    } else {
+    p.x = *reinterpret_cast<const uint4*>(src);
+    if constexpr (!IO::kRaw && KP::per16 == 8) p.y = *reinterpret_cast<const uint4*>(src + 4);
+  }
+  return p;
+}
+template <class KP, class IO>
+__device__ __forceinline__ void query_parts(const QueryPiece& p, uint4* out) {
+  if constexpr (IO::kRaw == (KP::per16 == 8)) {  // stored as the operand takes it
+    out[0] = p.x;
+  } else if constexpr (IO::kRaw) {
+    out[0] = make_uint4(p.x.x << 16, p.x.x & 0xFFFF0000u, p.x.y << 16, p.x.y & 0xFFFF0000u);
+  } else {
+    const uint32_t w[8] = {p.x.x, p.x.y, p.x.z, p.x.w, p.y.x, p.y.y, p.y.z, p.y.w};
+    float v[8];
 #pragma unroll
-      for (int j = 0; j < KP::per16; j += 4) {
-        const float4 x = *reinterpret_cast<const float4*>(src + j);
-        v[j] = x.x;
-        v[j + 1] = x.y;
-        v[j + 2] = x.z;
-        v[j + 3] = x.w;
-      }
-    }
+    for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
 #pragma unroll
-    for (int q = 0; q < QP; ++q) out[q] = next_part<KP>(v);
+    for (int q = 0; q < TreeParts<KP, IO>::q; ++q) out[q] = next_part<KP>(v);
   }
 }
 
@@ -417,7 +438,7 @@ __device__ __forceinline__ void softmax_step(const f32x4_t* S, float qscale, flo
 
 // What a work item is: its request, blocks and columns.
 struct TreeItem {
-  int rank, cg, nsplit, ncg;
+  int cg, cg0, nsplit, ncg, item0;
   int len, total, nblk, row0, cols;
   int first, count;          // blocks of the split
   const int32_t* btrow;
@@ -425,21 +446,28 @@ struct TreeItem {
 __device__ __forceinline__ TreeItem tree_item(const TreeAttnArgs& a, int f) {
   const int lane = threadIdx.x & 63;
   TreeItem t;
+  // Lane = request, all of it at once: one trip to memory.
+  const int r = min(lane, a.n - 1);
+  const int item0 = a.item0[r], item1 = a.item0[r + 1], slot = a.slot[r], len = a.len[r];
+  const int nodes = a.nodes[r], ncg = a.ncg[r], row0 = a.row0[r], cg0 = a.cg0[r];
   // Request: the number of requests whose items all precede f.
-  t.rank = __builtin_amdgcn_readfirstlane(
-      __popcll(__ballot(lane < a.n - 1 && a.item0[min(lane + 1, kTreeReqs)] <= f)));
-  t.ncg = a.ncg[t.rank];
-  const int w = f - a.item0[t.rank], s = w / t.ncg;
+  const int rank = __popcll(__ballot(lane < a.n && item1 <= f));
+  const auto mine = [&](int v) { return __builtin_amdgcn_readlane(v, rank); };
+  t.ncg = mine(ncg);
+  t.cg0 = mine(cg0);
+  t.item0 = mine(item0);
+  const int w = f - t.item0, s = w / t.ncg;
   t.cg = w - s * t.ncg;  // column groups of one split run side by side and share its blocks
-  t.nsplit = (a.item0[t.rank + 1] - a.item0[t.rank]) / t.ncg;
-  t.len = a.len[t.rank];
-  t.total = t.len + a.nodes[t.rank];
+  t.nsplit = (mine(item1) - t.item0) / t.ncg;
+  t.len = mine(len);
+  const int n = mine(nodes);
+  t.total = t.len + n;
   t.nblk = (t.total + 15) >> 4;
-  t.row0 = a.row0[t.rank];
-  t.cols = a.nodes[t.rank] * a.G;
+  t.row0 = mine(row0);
+  t.cols = n * a.G;
   t.first = a.bps * s;
   t.count = min(t.nblk - t.first, a.bps);
-  t.btrow = a.bt + static_cast<size_t>(a.slot[t.rank]) * a.mb;
+  t.btrow = a.bt + static_cast<size_t>(mine(slot)) * a.mb;
   return t;
 }
 
@@ -465,13 +493,13 @@ __device__ __forceinline__ void merge_splits(const TreeAttnArgs& a, const TreeIt
                                              int* last, float* weights) {
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's partial stores are complete
   __syncthreads();
-  int32_t* cnt = a.cnt + (a.cg0[t.rank] + t.cg) * a.Hkv + kvh;
+  int32_t* cnt = a.cnt + (t.cg0 + t.cg) * a.Hkv + kvh;
   if (threadIdx.x == 0)
     *last = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == t.nsplit - 1;
   __syncthreads();
   if (!*last) return;
   if (threadIdx.x == 0) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  const uint32_t base = (static_cast<uint32_t>(a.item0[t.rank] + t.cg) * a.Hkv + kvh) * CW * (HD + 4) * 4;
+  const uint32_t base = (static_cast<uint32_t>(t.item0 + t.cg) * a.Hkv + kvh) * CW * (HD + 4) * 4;
   const uint32_t stride = static_cast<uint32_t>(t.ncg) * a.Hkv * CW * (HD + 4) * 4;
   const int c0 = CW * t.cg, mine = min(t.cols - c0, CW);
   // Weight of each (split, column), exp2(m - M) / L, in LDS: lanes of one
@@ -557,7 +585,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_tree_attn(TreeAttnArgs
     const int k = wave + 4 * n, jt = k / NF, c = k % NF;
     if (k >= NT * NF) break;
     uint4 x[Parts::q];
-    load_query<KP, IO, HD>(a, tree_column(a, t.row0, kvh, min(16 * jt + h, t.cols - 1)), c, g, x);
+    query_parts<KP, IO>(load_query<KP, IO, HD>(a, tree_column(a, t.row0, kvh, min(16 * jt + h, t.cols - 1)), c, g), x);
 #pragma unroll
     for (int q = 0; q < Parts::q; ++q) sm.q[jt][c][q][lane] = x[q];
   }
@@ -690,7 +718,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_tree_attn(TreeAttnArgs
       }
     }
   }
-  if (t.nsplit > 1) merge_splits<IO, HD, CW>(a, t, kvh, pb, &sm.last, sm.weights);
+  if (t.nsplit > 1 && !a.apart) merge_splits<IO, HD, CW>(a, t, kvh, pb, &sm.last, sm.weights);
 }
 
 // ---------------------------------------------------------------------------
@@ -719,9 +747,8 @@ __global__ __launch_bounds__(256, (NT == 1 && TreeParts<KP, IO>::q == 1 ? 3 : 2)
   using Stage = TreeStage<KP, HD>;
   using Parts = TreeParts<KP, IO>;
   constexpr int BP = Stage::BP, NF = HD / KP::kblk, NE = HD / 16, CW = 64 * NT;
-  // Two steps, or the weights of the merge.
-  __shared__ uint4 lds[2 * Stage::kPieces >= kTreeSplits * CW / 4 ? 2 * Stage::kPieces : kTreeSplits * CW / 4];
-  __shared__ int odd_s[2], last;
+  __shared__ uint4 lds[2 * Stage::kPieces];  // two steps
+  __shared__ int odd_s[2];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane & 15, g = lane >> 4;
@@ -730,6 +757,16 @@ __global__ __launch_bounds__(256, (NT == 1 && TreeParts<KP, IO>::q == 1 ? 3 : 2)
   const int end = t.first + t.count, c0 = CW * t.cg + 16 * NT * wave;
   const bool busy = c0 < t.cols;  // this wave has columns
 
+  // Block ids are asked for one step before the blocks they name; past the
+  // split's end they are its last one's, so that every fetch reads the cache (a
+  // missing second block re-reads the first, masked).
+  int ids[BP];
+  const auto ask = [&](int i) {
+#pragma unroll
+    for (int b = 0; b < BP; ++b) ids[b] = t.btrow[min(i + b, end - 1)];
+  };
+  ask(t.first);
+
   uint4 Q[NT][NF][Parts::q];
   uint64_t anc[NT];
 #pragma unroll
@@ -737,7 +774,7 @@ __global__ __launch_bounds__(256, (NT == 1 && TreeParts<KP, IO>::q == 1 ? 3 : 2)
     const TreeColumn col = tree_column(a, t.row0, kvh, min(c0 + 16 * jt + h, t.cols - 1));
     anc[jt] = a.anc[col.row];
 #pragma unroll
-    for (int c = 0; c < NF; ++c) load_query<KP, IO, HD>(a, col, c, g, Q[jt][c]);
+    for (int c = 0; c < NF; ++c) query_parts<KP, IO>(load_query<KP, IO, HD>(a, col, c, g), Q[jt][c]);
   }
   f32x4_t O[NT][NE];
   float m[NT], l[NT];
@@ -757,14 +794,6 @@ __global__ __launch_bounds__(256, (NT == 1 && TreeParts<KP, IO>::q == 1 ? 3 : 2)
   const auto round_tile = [&](int r) { return Stage::kTile == 128 ? 2 * r + half : r / kRounds; };
   const auto round_piece = [&](int r) { return in_tile + (r % kRounds) * 256; };
 
-  // Block ids are asked for one step before the blocks they name; past the
-  // split's end they are its last one's, so that every fetch reads the cache (a
-  // missing second block re-reads the first, masked).
-  int ids[BP];
-  const auto ask = [&](int i) {
-#pragma unroll
-    for (int b = 0; b < BP; ++b) ids[b] = t.btrow[min(i + b, end - 1)];
-  };
   u32x4_t next[2][Stage::kPer];  // of even and odd steps
   // The blocks whose ids were asked for, then the ids of the step at `then`.
   const auto fetch = [&](int then, auto parity) {
@@ -909,7 +938,6 @@ __global__ __launch_bounds__(256, (NT == 1 && TreeParts<KP, IO>::q == 1 ? 3 : 2)
   if (tid < 2) odd_s[tid] = 0;
   __syncthreads();
   int i = t.first;
-  ask(i);
   fetch(i + BP, kEven);
   fetch(i + 2 * BP, kOdd);
   if (is_tail(i)) put(i, kEven, kTail);
@@ -944,7 +972,90 @@ __global__ __launch_bounds__(256, (NT == 1 && TreeParts<KP, IO>::q == 1 ? 3 : 2)
       if (t.nsplit > 1 && g == 0) pb.store4(item + c * (HD + 4) * 4, f32x4_t{m[jt], L, 0.f, 0.f});
     }
   }
-  if (t.nsplit > 1) merge_splits<IO, HD, CW>(a, t, kvh, pb, &last, reinterpret_cast<float*>(lds));
+}
+
+// ---------------------------------------------------------------------------
+
+// Merge of the splits in a launch of its own, whose work-groups share out all
+// outputs: 16 columns of one (column group of CW, KV head) each, a thread kMine
+// pieces of 16 bytes with the first kChunk splits' loads in flight while it
+// finds the weights.  The partials (25 to 32 MB at 256 to 768 work-groups of 64
+// to 128 columns) take 4 to 6 us.
+constexpr int kMergeColumns = 16;
+template <class IO, int HD, int CW>
+__global__ __launch_bounds__(256) void k_tree_merge(TreeAttnArgs a) {
+  constexpr int kPer = HD / 4, kMine = kMergeColumns * kPer / 256, kChunk = 8;
+  __shared__ float weights[kTreeSplits * kMergeColumns];
+  const int kvh = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  // Request: the last one whose first column group is not behind this one.
+  const int rank = __builtin_amdgcn_readfirstlane(
+      __popcll(__ballot(lane < a.n && a.cg0[min(lane, a.n - 1)] <= static_cast<int>(blockIdx.y))) - 1);
+  const int ncg = a.ncg[rank], cg = blockIdx.y - a.cg0[rank], cols = a.nodes[rank] * a.G;
+  const int nsplit = (a.item0[rank + 1] - a.item0[rank]) / ncg;
+  const int c0 = blockIdx.z * kMergeColumns;  // within the group
+  if (nsplit == 1 || CW * cg + c0 >= cols) return;
+  const int mine = min(cols - CW * cg - c0, kMergeColumns);
+  constexpr size_t kColumn = HD + 4;
+  const float* part = a.part + ((static_cast<size_t>(a.item0[rank] + cg) * a.Hkv + kvh) * CW + c0) * kColumn;
+  const size_t stride = static_cast<size_t>(ncg) * a.Hkv * CW * kColumn;
+  // A lane per (column, split): maximum and sum; sixteen lanes share a column.
+  const float* ml = part + min(tid / 16, mine - 1) * kColumn;
+  float sm[2], sl[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int s = tid % 16 + 16 * k;
+    const float2 x = *reinterpret_cast<const float2*>(ml + min(s, nsplit - 1) * stride);
+    sm[k] = s < nsplit ? x.x : kTreeFloor;
+    sl[k] = s < nsplit ? x.y : 0.f;
+  }
+  const float* at[kMine];
+  f32x4_t R[kMine], o[kMine][kChunk];
+#pragma unroll
+  for (int n = 0; n < kMine; ++n) {
+    const int idx = tid + 256 * n;
+    at[n] = part + min(idx / kPer, mine - 1) * kColumn + 4 + idx % kPer * 4;
+    R[n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const auto load = [&](int s0) {
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k)
+#pragma unroll
+      for (int n = 0; n < kMine; ++n) o[n][k] = *reinterpret_cast<const f32x4_t*>(at[n] + min(s0 + k, nsplit - 1) * stride);
+  };
+  load(0);
+  float M = fmaxf(sm[0], sm[1]);
+#pragma unroll
+  for (int x = 8; x >= 1; x >>= 1) M = fmaxf(M, __shfl_xor(M, x));
+  float w[2], L = 0.f;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    w[k] = __builtin_amdgcn_exp2f(sm[k] - M);
+    L += sl[k] * w[k];
+  }
+#pragma unroll
+  for (int x = 8; x >= 1; x >>= 1) L += __shfl_xor(L, x);
+  const float inv = 1.f / L;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) weights[(tid % 16 + 16 * k) * kMergeColumns + tid / 16] = w[k] * inv;
+  __syncthreads();
+  for (int s0 = 0;;) {
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k)
+      if (s0 + k < nsplit) {
+#pragma unroll
+        for (int n = 0; n < kMine; ++n) R[n] += weights[(s0 + k) * kMergeColumns + (tid + 256 * n) / kPer] * o[n][k];
+      }
+    s0 += kChunk;
+    if (s0 >= nsplit) break;
+    load(s0);
+  }
+#pragma unroll
+  for (int n = 0; n < kMine; ++n) {
+    const int idx = tid + 256 * n, c = idx / kPer;
+    if (c >= mine) break;
+    const TreeColumn col = tree_column(a, a.row0[rank], kvh, CW * cg + c0 + c);
+    IO::store4(a, col.row, col.hq * HD + idx % kPer * 4, R[n]);
+  }
 }
 
 }  // namespace sprk
