@@ -148,7 +148,7 @@ int sprh_tree_split(const spr_tree_batch* b, int G, int Hkv, int hd, int step, i
   sprk::TreeInfo t;
   const spr_status st = sprk::parse_tree(b, true, 64, 1 << 27, "split", &t, &g_err);
   if (st != SPR_OK) return st;
-  const int cw = sprk::tree_cols_per_group(t, G, 256);
+  const int cw = sprk::tree_cols_per_group(t, G, 128);
   const sprk::TreeSplit s = sprk::tree_split(t, G, Hkv, hd, cw, step, slots, floats);
   out[0] = cw;
   out[1] = s.bps;

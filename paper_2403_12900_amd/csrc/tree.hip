@@ -168,12 +168,7 @@ hipError_t launch_tree_keep(hipStream_t st, const TreeInfo& t, const spr_kv_view
     a.nodes[i] = static_cast<uint8_t>(t.nodes[i]);
   }
   const int columns = a.Hkv * (a.hd + a.hd / (bf ? 8 : 4));
-  // About 4096 work-groups (two rounds of what the chip holds), each through
-  // as many layers as that takes.
-  a.n_layers = kv.n_layers;
-  const int64_t groups = static_cast<int64_t>((columns + 255) / 256) * t.n;
-  a.layers = static_cast<int>(std::min<int64_t>(kv.n_layers, std::max<int64_t>(1, groups * kv.n_layers / 4096)));
-  const dim3 grid((columns + 255) / 256, (kv.n_layers + a.layers - 1) / a.layers, t.n);
+  const dim3 grid((columns + 255) / 256, kv.n_layers, t.n);
   if (bf) k_tree_keep<BF16><<<grid, 256, 0, st>>>(a);
   else k_tree_keep<F32><<<grid, 256, 0, st>>>(a);
   return hipGetLastError();

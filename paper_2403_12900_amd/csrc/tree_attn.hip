@@ -92,21 +92,19 @@ hipError_t launch(const TreeAttnCall& c) {
   return e;
 }
 
-// Columns per work-group by what the registers hold beside the accumulators:
-// three-part queries 64, fp32 ones and bf16 ones of 128 dimensions 128, bf16
-// ones of 64 dimensions 256.
+// Columns per work-group: two-byte operands 128 (8 x 128 columns of 128
+// dimensions, 6000 positions: 59 us, of 64 columns 63; at 700 positions 23 and
+// 22), the others 64 (fp32, the same columns: 246 us against 259 with 128, at 700
+// positions 46 against 49; three-part queries leave no registers for more).
 template <class KP, class IO, int HD>
 hipError_t by_columns(const TreeAttnCall& c) {
-  constexpr int most = TreeParts<KP, IO>::q == 3 ? 64 : KP::per16 == 4 || HD == 128 ? 128 : 256;
+  constexpr int most = KP::per16 == 8 && TreeParts<KP, IO>::q == 1 ? 128 : 64;
   switch (tree_cols_per_group(*c.tree, c.H / c.kv.n_kv_heads, most)) {
     case 16: return launch<KP, IO, HD, 16>(c);
     case 32: return launch<KP, IO, HD, 32>(c);
     case 64: return launch<KP, IO, HD, 64>(c);
     case 128:
-      if constexpr (most >= 128) return launch<KP, IO, HD, 128>(c);
-      break;
-    case 256:
-      if constexpr (most >= 256) return launch<KP, IO, HD, 256>(c);
+      if constexpr (most == 128) return launch<KP, IO, HD, 128>(c);
       break;
   }
   return hipErrorInvalidValue;  // not reached: no more than `most`

@@ -95,7 +95,7 @@ inline spr_status parse_tree(const spr_tree_batch* b, bool with_cache, int n_slo
 
 // Columns that one work-group of the attention kernel takes: 16 or 32 where
 // that holds the widest request (its four waves then share out the blocks),
-// else 64, 128 or 256 (16, 32, 64 columns per wave), as far as `most`.
+// else 64 or 128 (16 or 32 columns per wave), as far as `most`.
 inline int tree_cols_per_group(const TreeInfo& t, int G, int most) {
   const int cols = t.max_nodes * G;
   int cw = 16;
@@ -137,7 +137,8 @@ inline TreeSplit tree_split(const TreeInfo& t, int G, int Hkv, int hd, int cw, i
   int64_t bps = std::max<int64_t>(1, (blocks * Hkv + slots - 1) / slots);
   // Rounding every request up to whole splits can leave more work-groups than
   // stay resident; splits up to twice as long that fit them into one round are
-  // taken, but not longer ones.
+  // taken, but not longer ones (16 requests of 64 columns, 100 to 1500
+  // positions: 56 us, without this 62).
   const auto groups = [&](int64_t w) {
     int64_t n = 0;
     for (int r = 0; r < t.n; ++r) n += (blocks_of(s.order[r]) + w - 1) / w * s.ncg[r];

@@ -24,7 +24,12 @@
 //                 draw: the chunk sums locate the chunk, which alone is read
 //                 again.
 // No work-group waits on another, nothing is counted, and all sums run in a
-// fixed order.  (The walk as the end of the last sums' launch, in the work-group
+// fixed order.  Bound by latency while the rows are few -- 5 rows of 32000: 13
+// us, sums 4.4 and walk 8.8 (8 of its loads and barriers follow one another) --
+// and by fp64 arithmetic where they are many: 128 rows of 131072 with draft
+// probabilities, up to 4 children a node, 64 us: sums 23 (16.4 M exponentials of
+// 20 fp64 operations; the 33 MB alone would take 6), four N_k passes of 9, walk
+// 11.5.  16 x 8 nodes of 32000: 28 us.  (The walk as the end of the last sums' launch, in the work-group
 // that finishes a request's last chunk, cost what the launch saves -- 13.5 us at
 // 5 rows of 32000 -- and held greedy requests' walks between two launches.)
 #pragma once
