@@ -25,7 +25,8 @@
 // The running maximum of a column is raised only when a step exceeds it by
 // kRaise (in log2 units): until then probabilities of at most 2^kRaise stay
 // exact enough in fp32, and steps need neither the exchange between lanes nor
-// the rescaling of O.
+// the rescaling of O (512 columns over 2 x 24000 positions: 156 us, raised at
+// every larger score 174).
 //
 // Two kernels.  Both cut a request's blocks into KV splits, one work-group
 // each, and write a partial result where a request has several:
@@ -46,8 +47,8 @@
 //                       103 of 157 TFLOP/s), by products, exponentials and LDS
 //                       reads in turn in bf16 (512 columns, 2 x 24000 positions:
 //                       147 us, 690 TFLOP/s), and at short contexts by its ends:
-//                       about 8 us until the first step runs, 6 us from the
-//                       last to the outputs.
+//                       several trips to memory until the first step runs, 8 to
+//                       9 us of merge at its end.
 // The partials are merged by the split that arrives last where that is little,
 // else by k_tree_merge.  (With 64 columns and more in that one work-group: 512
 // columns over 2 x 6000 positions 65 us, with k_tree_merge 51.)
@@ -979,8 +980,8 @@ __global__ __launch_bounds__(256, (NT == 1 && TreeParts<KP, IO>::q == 1 ? 3 : 2)
 // Merge of the splits in a launch of its own, whose work-groups share out all
 // outputs: 16 columns of one (column group of CW, KV head) each, a thread kMine
 // pieces of 16 bytes with the first kChunk splits' loads in flight while it
-// finds the weights.  The partials (25 to 32 MB at 256 to 768 work-groups of 64
-// to 128 columns) take 4 to 6 us.
+// finds the weights.  22 to 32 MB of partials (480 to 744 work-groups of 64 or
+// 128 columns): 8 to 9 us, half of it the launch and two trips to memory.
 constexpr int kMergeColumns = 16;
 template <class IO, int HD, int CW>
 __global__ __launch_bounds__(256) void k_tree_merge(TreeAttnArgs a) {

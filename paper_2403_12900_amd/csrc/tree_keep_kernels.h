@@ -14,7 +14,7 @@
 // for 20 MB of moved bytes (the counters show twice as much written and more
 // read); 8 heads in fp32, 80 layers, 16 requests: 18 us.  The number of
 // work-groups does not matter from 1000 to 6400 of them (several layers each or
-// one), nor does the order of loads.  One request, 32 layers: 4.2 us.
+// one).  One request, 32 layers: 4.2 us.
 #pragma once
 
 #include "tree_attn_kernels.h"

@@ -105,6 +105,22 @@ def test_attention_of_wide_trees_over_long_contexts(ops, H, Hkv, hd, nodes, kv, 
 
 
 @pytest.mark.parametrize("kv", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("io", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H,Hkv,hd,nodes,L", [(8, 1, 128, 4, 700), (8, 1, 128, 4, 3000), (8, 1, 64, 4, 6000), (3, 3, 64, 16, 4100),
+                                              (4, 2, 128, 3, 7001)])
+def test_attention_merged_in_the_kernel_and_apart(ops, H, Hkv, hd, nodes, L, kv, io):
+    """Few columns and many splits, beside a request of one split and an almost empty one; twice, bit for bit."""
+    rng = np.random.default_rng(L)
+    trees = [ref.random_tree(rng, nodes, "random"), [-1], ref.random_tree(rng, 2, "chain")]
+    check_attention(ops, rng, H, Hkv, hd, kv, io, [L, 9, 0], trees, tag="merge")
+    cache = ref.Cache(rng, 1, Hkv, hd, [L + nodes], kv)
+    view, b = cache.device(), batch_of([0], [L], trees[:1])
+    q = torch.from_numpy(rng.standard_normal((nodes, H, hd), dtype=np.float32)).to(io).cuda()
+    first = ops.attention(view, 0, b, q)
+    assert all(torch.equal(ops.attention(view, 0, b, q), first) for _ in range(3))
+
+
+@pytest.mark.parametrize("kv", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("hd", [64, 128])
 def test_attention_ignores_what_a_row_does_not_see(ops, kv, hd):
     """NaN and infinities in other branches' keys and values reach only the rows that see them."""
