@@ -21,7 +21,7 @@ constexpr auto kernel() {
 // against 13.3, of 1024: 20.2 against 16.3).
 constexpr int kMergeInside = 192 * 128;
 
-// Work-groups of the kernel that a CU holds at once.
+// Work-groups of the kernel that a CU holds, or is to hold, at once.
 template <class KP, class IO, int HD, int CW>
 int groups_per_cu() {
   static const int n = [] {
@@ -29,7 +29,7 @@ int groups_per_cu() {
     if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&o, reinterpret_cast<const void*>(kernel<KP, IO, HD, CW>()), 256,
                                                      0) != hipSuccess || o < 1)
       o = 1;
-    return o;
+    return CW > 32 ? std::min(o, kSharedPerCu<KP>) : o;
   }();
   return n;
 }

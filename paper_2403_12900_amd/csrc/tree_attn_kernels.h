@@ -743,8 +743,14 @@ struct TreeStage {
 // for; after the step the next one goes to the other LDS buffer: one barrier
 // per step.  Steps that reach past the cached positions or the split (the last
 // few) run masked, the others without a test.
+//
+// Work-groups of a CU: three with fp32 operands (16 x 5632 positions, 64 columns:
+// 225 us, with two 253), two with bf16 ones (that: 81 us, with three 86; 16 x 704
+// positions 20 and 25).
+template <class KP>
+constexpr int kSharedPerCu = KP::per16 == 4 ? 3 : 2;
 template <class KP, class IO, int HD, int NT>
-__global__ __launch_bounds__(256, (NT == 1 && TreeParts<KP, IO>::q == 1 ? 3 : 2)) void k_tree_attn_shared(TreeAttnArgs a) {
+__global__ __launch_bounds__(256, kSharedPerCu<KP>) void k_tree_attn_shared(TreeAttnArgs a) {
   using Stage = TreeStage<KP, HD>;
   using Parts = TreeParts<KP, IO>;
   constexpr int BP = Stage::BP, NF = HD / KP::kblk, NE = HD / 16, CW = 64 * NT;
