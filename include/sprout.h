@@ -398,9 +398,11 @@ spr_status spr_tree_ops_release(spr_tree_ops* ops);
  * values are in the cache already.  One-node trees are ordinary decode
  * attention.  What lies in the cache behind a request's nodes, or at nodes
  * that a row does not see, does not reach its output, whatever it holds (a row
- * that sees an infinite key may get NaN where the formula gives it no weight).
+ * that sees an infinite key or value may get NaN where the formula gives it no
+ * weight or an infinity: operands enter the products in parts).
  *   n_heads    a multiple of n_kv_heads, n_heads / n_kv_heads <= 16
- *   io_dtype   of q and out; scores, sums and products are held in fp32
+ *   io_dtype   of q and out; scores, sums and products are held in fp32, the
+ *              probabilities of bf16 outputs over a bf16 cache to 2^-16
  *   q          device [rows] x [n_heads * head_dim], row r at q + r * q_stride
  *              elements; out likewise.  16-byte aligned, strides a multiple of
  *              16 bytes and >= n_heads * head_dim.  out must not overlap q.

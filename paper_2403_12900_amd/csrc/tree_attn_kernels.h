@@ -19,8 +19,9 @@
 // fp32 queries meet a bf16 cache in three bf16 parts (all 24 bits), and the
 // probabilities enter their product in three parts too, so that an fp32
 // output is an fp32 result (two parts of the probabilities alone put 1e-6 of
-// error on it); a bf16 output takes bf16 probabilities (their rounding, 2^-8
-// relative and independent per position, is at most that of the output).
+// error on it).  A bf16 output takes them in two parts: 2^-16 of a probability
+// is left out, so its error is the output's one rounding (2 x 24000 positions:
+// 0.00166 of the outputs' norm; with one part 0.0023).
 //
 // The running maximum of a column is raised only when a step exceeds it by
 // kRaise (in log2 units): until then probabilities of at most 2^kRaise stay
@@ -328,7 +329,7 @@ struct TreeStep<F32, HD> {
 template <class KP, class IO>
 struct TreeParts {
   static constexpr int q = KP::per16 == 4 || IO::kRaw ? 1 : 3;
-  static constexpr int p = KP::per16 == 4 || IO::kRaw ? 1 : 3;
+  static constexpr int p = KP::per16 == 4 ? 1 : IO::kRaw ? 2 : 3;
 };
 
 template <class KP, class IO, int HD, int NT>
