@@ -102,6 +102,7 @@ hipError_t launch_tree_verify(const TreeVerifyCall& c) {
   a.V = c.V;
   a.S = (c.V + kVChunk - 1) / kVChunk;
   a.n = t.n;
+  a.rows = t.rows;
   a.stat = static_cast<uint64_t*>(c.scratch);
   a.rest = reinterpret_cast<double*>(a.stat + static_cast<size_t>(t.rows) * a.S * 2);
   const int size = c.bf16 ? 2 : 4;
@@ -123,6 +124,7 @@ hipError_t launch_tree_verify(const TreeVerifyCall& c) {
       a.kids[r] = t.kids[r];
       a.rank[r] = t.rank[r];
       a.parent[r] = t.parent[r];
+      a.parent_row[r] = static_cast<uint8_t>(t.parent[r] < 0 ? kTreeRows : t.row0[i] + t.parent[r]);
       a.rest0[r] = static_cast<uint8_t>(arrays);
       arrays += t.kids[r];
     }

@@ -9,14 +9,18 @@
 //   N_k = sum_v max(p(v) - c_k q(v), 0),
 // (the nested maxima collapse: q >= 0), so every N_k is one pass over p and q
 // and no distribution is ever written.  A point mass at the child instead
-// removes its token: r_k is p without the rejected tokens, N_k = 1 - their sum.
+// removes its token: r_k is p without the rejected tokens, N_k the sum of the
+// others.  It is added up (the sum without any child's token, then those of the
+// children yet to be tried) and never a difference: k rejections may leave
+// 2^-24k, which 1 less their sum does not hold from the second one on.
 //
 // A chosen token is a whole number that an error in a sum can flip, so
 // exponentials, sums and cumulative sums are fp64.
 //
 // Each vocabulary row is cut into chunks of kVChunk entries, one work-group
 // each, so that few rows still fill the chip:
-//   k_tree_stats  per (row, chunk): maximum, its lowest index, sum of exp
+//   k_tree_stats  per (row, chunk): maximum, its lowest index, sum of exp, and
+//                 without draft_probs the sum without the children's tokens
 //   k_tree_rest   per (row with >= k children, chunk): its part of N_k (one
 //                 launch per k; none without draft_probs)
 //   k_tree_walk   per request: every child's test at once (it depends on its
@@ -24,14 +28,15 @@
 //                 draw: the chunk sums locate the chunk, which alone is read
 //                 again.
 // No work-group waits on another, nothing is counted, and all sums run in a
-// fixed order.  Bound by latency while the rows are few -- 5 rows of 32000: 13
-// us, sums 4.4 and walk 8.8 (8 of its loads and barriers follow one another) --
-// and by fp64 arithmetic where they are many: 128 rows of 131072 with draft
-// probabilities, up to 4 children a node, 64 us: sums 23 (16.4 M exponentials of
-// 20 fp64 operations; the 33 MB alone would take 6), four N_k passes of 9, walk
-// 11.5.  16 x 8 nodes of 32000: 28 us.  (The walk as the end of the last sums' launch, in the work-group
-// that finishes a request's last chunk, cost what the launch saves -- 13.5 us at
-// 5 rows of 32000 -- and held greedy requests' walks between two launches.)
+// fixed order.  Bound by latency while the rows are few -- 5 rows of 32000: 14.5
+// us, sums 5.5 (4.4 without the children's own) and walk 9.2 (8 of its loads and
+// barriers follow one another) -- and by fp64 arithmetic where they are many: 128
+// rows of 131072 with draft probabilities, up to 4 children a node, 65 us: sums
+// 23 (16.4 M exponentials of 20 fp64 operations; the 33 MB alone would take 6),
+// four N_k passes of 9, walk 11.5.  16 x 8 nodes of 32000: 28 us.  (The walk as
+// the end of the last sums' launch, in the work-group that finishes a request's
+// last chunk, cost what the launch saves and held greedy requests' walks between
+// two launches.)
 #pragma once
 
 #include "tree_attn_kernels.h"
@@ -57,13 +62,15 @@ struct TreeVerifyArgs {
   int32_t *emitted, *path, *count;
   int* err;
   uint64_t* stat;          // [rows][S][2]: (maximum, its index), sum of exp((x - maximum) / T)
-  double* rest;            // [rest0[row] + k - 1][S]: parts of N_k
-  int V, S, n, k;          // k: the pass of k_tree_rest
+  double* rest;            // with draft: [rest0[row] + k - 1][S], parts of N_k; without:
+                           // [row][S], the chunk's sum without the children's tokens
+  int V, S, n, k, rows;    // k: the pass of k_tree_rest
   int vec_l, vec_d;        // rows of logits / draft_probs are 16-byte aligned
   float temp[kTreeReqs];
   uint8_t row0[kTreeReqs], nodes[kTreeReqs];
   uint8_t list[kTreeRows];     // rows of this launch
   uint8_t req[kTreeRows], kids[kTreeRows], rank[kTreeRows], rest0[kTreeRows];
+  uint8_t parent_row[kTreeRows];  // kTreeRows for a root
   int8_t parent[kTreeRows];
 };
 static_assert(sizeof(TreeVerifyArgs) <= 2048, "kernel arguments");
@@ -131,7 +138,9 @@ constexpr int kSumWaves = kSumThreads / 64, kDrawWaves = kDrawThreads / 64;
 struct TreeWalkSmem {
   double d[kDrawWaves];
   int hit[kDrawWaves], tail[kDrawWaves];
-  double z[kTreeNodes], total[kTreeNodes];      // per node: its row's sum; per array of parts: N_k
+  // Per node: its row's sum; with draft per array of parts: N_k, without per
+  // node: its row's sum without the children's tokens.
+  double z[kTreeNodes], total[kTreeNodes];
   double px[kTreeNodes];                        // per node as a child: p(its token)
   float m[kTreeNodes];                          // per node: its row's maximum (NaN: a bad row)
   int best[kTreeNodes], tok[kTreeNodes], order[kTreeNodes];
@@ -211,25 +220,30 @@ __device__ __forceinline__ double draft_value(float q) { return q > 0.f ? static
 // sum of a row from its chunks; every wave works them out by itself.
 struct RowStat {
   float m;
-  double z;
+  double z, rest;
   int best;
 };
 struct ChunkStat {
   uint64_t top, z;  // (maximum, its index); sum
+  double rest;      // sum without the children's tokens
 };
-__device__ __forceinline__ ChunkStat load_stat(const TreeVerifyArgs& a, int row, int c) {
-  ChunkStat s{0xFF800000u, 0};  // no entries: maximum -inf
+template <bool kRest>
+__device__ __forceinline__ ChunkStat load_stat(const TreeVerifyArgs& a, int row, int c, bool with_rest = kRest) {
+  ChunkStat s{0xFF800000u, 0, 0.0};  // no entries: maximum -inf
   if (c < a.S) {
-    const uint64_t* st = a.stat + (static_cast<size_t>(row) * a.S + c) * 2;
-    s.top = st[0];
-    s.z = st[1];
+    const size_t at = static_cast<size_t>(row) * a.S + c;
+    s.top = a.stat[at * 2];
+    s.z = a.stat[at * 2 + 1];
+    if (kRest && with_rest) s.rest = a.rest[at];
   }
   return s;
 }
 // s: this lane's chunk of the first 64, loaded before.
-__device__ __forceinline__ RowStat row_stat(const TreeVerifyArgs& a, int row, ChunkStat s, double inv_t, bool want_z) {
+template <bool kRest>
+__device__ __forceinline__ RowStat row_stat(const TreeVerifyArgs& a, int row, ChunkStat s, double inv_t, bool want_z,
+                                            bool with_rest = kRest) {
   const int lane = threadIdx.x & 63;
-  RowStat r{-INFINITY, 0.0, 0x7fffffff};
+  RowStat r{-INFINITY, 0.0, 0.0, 0x7fffffff};
   bool bad = false;
 #pragma unroll 1
   for (int c0 = 0;;) {
@@ -243,13 +257,15 @@ __device__ __forceinline__ RowStat row_stat(const TreeVerifyArgs& a, int row, Ch
     const float up = fmaxf(r.m, wm);
     if (wm > r.m) r.best = best;
     if (want_z && up > -INFINITY) {
-      const double part = wave_sum(mine > -INFINITY ? as_double(s.z) * exp_neg((static_cast<double>(mine) - up) * inv_t) : 0.0);
-      r.z = (r.m > -INFINITY ? r.z * exp_neg((static_cast<double>(r.m) - up) * inv_t) : 0.0) + part;
+      const double scale = mine > -INFINITY ? exp_neg((static_cast<double>(mine) - up) * inv_t) : 0.0;
+      const double before = r.m > -INFINITY ? exp_neg((static_cast<double>(r.m) - up) * inv_t) : 0.0;
+      r.z = r.z * before + wave_sum(as_double(s.z) * scale);
+      if (kRest && with_rest) r.rest = r.rest * before + wave_sum(s.rest * scale);
     }
     r.m = up;
     c0 += 64;
     if (c0 >= a.S) break;
-    s = load_stat(a, row, c0 + lane);
+    s = load_stat<kRest>(a, row, c0 + lane, with_rest);
   }
   if (__ballot(bad) != 0 || !(fabsf(r.m) <= 3.402823466e38f)) r.m = __uint_as_float(0x7FC00000u);
   return r;
@@ -259,7 +275,7 @@ __device__ __forceinline__ RowStat row_stat(const TreeVerifyArgs& a, int row, Ch
 // (chunks, rows); 8 waves per SIMD, which the fp64 exponentials need to overlap.
 template <class T>
 __global__ __launch_bounds__(kSumThreads, 8) void k_tree_stats(TreeVerifyArgs a) {
-  __shared__ double part[kSumWaves];
+  __shared__ double part[kSumWaves], part2[kSumWaves];
   __shared__ float top_s[kSumWaves];
   __shared__ int best_s[kSumWaves];
   const int chunk = blockIdx.x, row = blockIdx.y;
@@ -267,6 +283,17 @@ __global__ __launch_bounds__(kSumThreads, 8) void k_tree_stats(TreeVerifyArgs a)
   const float temp = a.temp[a.req[row]];
   float x[kSumOwn];
   load_chunk<kSumOwn>(static_cast<const T*>(a.logits) + row * a.ls, a.V, chunk, a.vec_l, -INFINITY, x);
+  // Without draft_probs: the call's tokens, two per lane, and whether their
+  // parent is this row (all asked for at once, with the logits).
+  int tok[2] = {-1, -1};
+  bool child[2] = {false, false};
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    if (a.draft == nullptr && 64 * h < a.rows) {
+      const int r = min(64 * h + lane, a.rows - 1);
+      tok[h] = a.tok[r];
+      child[h] = 64 * h + lane < a.rows && a.parent_row[r] == row;
+    }
   // Maximum with the lowest index that has it; a NaN anywhere makes it NaN.
   float m = -INFINITY;
   bool nan = false;
@@ -284,25 +311,48 @@ __global__ __launch_bounds__(kSumThreads, 8) void k_tree_stats(TreeVerifyArgs a)
     top_s[wave] = m;
     best_s[wave] = best;
   }
+  uint64_t children[2];  // with a token in this chunk
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    children[h] = __ballot(child[h] && tok[h] >= chunk * kVChunk && tok[h] < min(a.V, (chunk + 1) * kVChunk));
   nan = __syncthreads_or(nan);
   m = -INFINITY;
   best = 0x7fffffff;
 #pragma unroll
   for (int w = 0; w < kSumWaves; ++w) better_of(m, best, top_s[w], best_s[w]);
-  double s = 0.0;
+  double s = 0.0, rest = 0.0;
   if (temp > 0.f) {
     const double inv_t = 1.0 / static_cast<double>(temp);
+    double taken = 0.0;
     if (m > -INFINITY && m < INFINITY && !nan) {
+      // The children's entries leave the others' sum, each once, and have one of their own.
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll 1
+        for (uint64_t left = children[h]; left != 0; left &= left - 1) {
+          const int at = __builtin_amdgcn_readlane(tok[h], __ffsll(static_cast<unsigned long long>(left)) - 1) -
+                         chunk_index<kSumOwn>(chunk);
+          float v = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < kSumOwn; ++e) {
+            v = at == e ? x[e] : v;
+            x[e] = at == e ? -INFINITY : x[e];
+          }
+          if (__ballot(v > -INFINITY) != 0) taken += exp_neg((static_cast<double>(v) - m) * inv_t);
+        }
+      }
 #pragma unroll
       for (int e = 0; e < kSumOwn; ++e) s += exp_neg((static_cast<double>(x[e]) - m) * inv_t);
     }
-    s = group_sum(s, part);
+    rest = s = group_sum(s, part);
+    if ((children[0] | children[1]) != 0) s += group_sum(taken, part2);
   }
   if (threadIdx.x == 0) {
-    uint64_t* to = a.stat + (static_cast<size_t>(row) * a.S + chunk) * 2;
+    const size_t at = static_cast<size_t>(row) * a.S + chunk;
     const float mm = nan ? __uint_as_float(0x7FC00000u) : m;
-    to[0] = __float_as_uint(mm) | static_cast<uint64_t>(static_cast<uint32_t>(best)) << 32;
-    to[1] = static_cast<uint64_t>(__double_as_longlong(s));
+    a.stat[at * 2] = __float_as_uint(mm) | static_cast<uint64_t>(static_cast<uint32_t>(best)) << 32;
+    a.stat[at * 2 + 1] = static_cast<uint64_t>(__double_as_longlong(s));
+    if (a.draft == nullptr) a.rest[at] = rest;
   }
 }
 
@@ -315,12 +365,12 @@ __global__ __launch_bounds__(kSumThreads) void k_tree_rest(TreeVerifyArgs a) {
   float x[kSumOwn], q[kSumOwn];
   load_chunk<kSumOwn>(static_cast<const T*>(a.logits) + row * a.ls, a.V, chunk, a.vec_l, -INFINITY, x);
   load_chunk<kSumOwn>(static_cast<const T*>(a.draft) + row * a.ds, a.V, chunk, a.vec_d, 0.f, q);
-  const ChunkStat first = load_stat(a, row, lane);
+  const ChunkStat first = load_stat<false>(a, row, lane);
   // c_k = 1 + N_1 + ... + N_{k-1}: all parts that the earlier passes left.
   double* rest = a.rest + static_cast<size_t>(a.rest0[row]) * a.S;
   double c = 0.0;
   for (int t = lane; t < (a.k - 1) * a.S; t += 64) c += rest[t];
-  const RowStat st = row_stat(a, row, first, inv_t, true);
+  const RowStat st = row_stat<false>(a, row, first, inv_t, true);
   c = 1.0 + wave_sum(c);
   double s = 0.0;
   if (st.m == st.m) {
@@ -343,7 +393,7 @@ __global__ __launch_bounds__(kDrawThreads) void k_tree_walk(TreeVerifyArgs a) {
   const int i = blockIdx.x;
   const int row0 = a.row0[i], nn = a.nodes[i], tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float temp = a.temp[i];
-  const bool greedy = !(temp > 0.f), drafted = a.draft != nullptr && !greedy;
+  const bool greedy = !(temp > 0.f), drafted = a.draft != nullptr && !greedy, pointed = !greedy && !drafted;
   const double inv_t = greedy ? 1.0 : 1.0 / static_cast<double>(temp);
   const T* logits = static_cast<const T*>(a.logits);
   const T* draft = static_cast<const T*>(a.draft);
@@ -374,15 +424,19 @@ __global__ __launch_bounds__(kDrawThreads) void k_tree_walk(TreeVerifyArgs a) {
   for (int r0 = wave; r0 < nn; r0 += kAhead * kDrawWaves) {
     ChunkStat s[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) s[k] = load_stat(a, row0 + min(r0 + k * kDrawWaves, nn - 1), lane);
+    for (int k = 0; k < kAhead; ++k) {
+      const int r = row0 + min(r0 + k * kDrawWaves, nn - 1);
+      s[k] = load_stat<true>(a, r, lane, pointed && a.kids[r] > 0);
+    }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int r = r0 + k * kDrawWaves;
       if (r >= nn) break;
-      const RowStat st = row_stat(a, row0 + r, s[k], inv_t, !greedy);
+      const RowStat st = row_stat<true>(a, row0 + r, s[k], inv_t, !greedy, pointed && a.kids[row0 + r] > 0);
       if (lane == 0) {
         sm->m[r] = st.m;
         sm->z[r] = st.z;
+        if (pointed) sm->total[r] = st.rest;
         sm->best[r] = st.best;
       }
     }
@@ -424,20 +478,21 @@ __global__ __launch_bounds__(kDrawThreads) void k_tree_walk(TreeVerifyArgs a) {
     }
     const double qx = draft_value(qt);
     ok = static_cast<double>(u) * qx * n < fmax(px - c * qx, 0.0);
-  } else if (ranged) {
-    // Earlier siblings' tokens are gone, each token once.
-    double left = 1.0;
+  } else if (pointed) {
+    // What the earlier siblings left: the tokens of none of the children, then
+    // those of this child and the later ones, each once (at the first child
+    // that has it).
     bool again = false;
 #pragma unroll 1
-    for (int s = 1; s < j; ++s) {
-      if (sm->parent[s] != par) continue;
-      bool first = sm->tok[s] != t;
-      again |= !first;
+    for (int s = 1; s < nn - 1; ++s) again |= s < j && sm->parent[s] == par && sm->tok[s] == t;
+    const uint64_t firsts = __ballot(ranged && !again);
+    double left = 1.0;
+    if (ranged && a.rank[row0 + j] > 0) {
+      left = sm->total[par] / sm->z[par];
 #pragma unroll 1
-      for (int r = 1; r < s && first; ++r) first = sm->parent[r] != par || sm->tok[r] != sm->tok[s];
-      if (first) left -= sm->px[s];
+      for (int s = j; s < nn; ++s) left += sm->parent[s] == par && (firsts >> s & 1) ? sm->px[s] : 0.0;
     }
-    ok = !again && static_cast<double>(u) * left < px;
+    ok = ranged && !again && static_cast<double>(u) * left < px;
   }
   // The path: from the root, the first accepted child each time.
   const float mine = sm->m[j];
@@ -482,7 +537,7 @@ __global__ __launch_bounds__(kDrawThreads) void k_tree_walk(TreeVerifyArgs a) {
       }
     }
     bool rested = drafted && kids > 0 && left > 0.0;
-    bool skip = !drafted && kids > 0;
+    bool skip = pointed && kids > 0;
     // Chunk sums of the weights.
     const auto chunk_sums = [&](bool parts, bool without) {
       __syncthreads();
@@ -491,24 +546,9 @@ __global__ __launch_bounds__(kDrawThreads) void k_tree_walk(TreeVerifyArgs a) {
         if (parts) {
           w = a.rest[(static_cast<size_t>(base0) + r0 + kids - 1) * a.S + tid];
         } else {
-          const ChunkStat s = load_stat(a, row, tid);
+          const ChunkStat s = load_stat<true>(a, row, tid, without);
           const float mc = __uint_as_float(static_cast<uint32_t>(s.top));
-          w = mc > -INFINITY ? as_double(s.z) * exp_neg((static_cast<double>(mc) - m) * inv_t) : 0.0;
-        }
-        if (without) {
-          // The rejected tokens' weights (each once) leave their chunk's sum.  A
-          // rejection leaves at least 2^-24 of what was there (accept < 1), so
-          // the difference stays far more exact than the draw's 2^-24 steps.
-#pragma unroll 1
-          for (int s = 1; s < nn; ++s) {
-            const int gone = sm->tok[s];
-            if (sm->parent[s] != node || gone < 0 || gone / kVChunk != tid || gone >= a.V) continue;
-            bool first = true;
-#pragma unroll 1
-            for (int r = 1; r < s; ++r) first &= sm->parent[r] != node || sm->tok[r] != gone;
-            if (first) w -= sm->px[s] * sm->z[node];
-          }
-          w = fmax(w, 0.0);
+          w = mc > -INFINITY ? (without ? s.rest : as_double(s.z)) * exp_neg((static_cast<double>(mc) - m) * inv_t) : 0.0;
         }
         sm->w[tid] = w;
       }
@@ -554,8 +594,9 @@ __global__ __launch_bounds__(kDrawThreads) void k_tree_walk(TreeVerifyArgs a) {
     };
     chunk_sums(rested, skip);
     pick();
-    // A chunk whose sum is above 0 by rounding alone (its weights were all
-    // rejected) has no entry to draw: its sum is cleared, and the draw made again.
+    // A chunk whose sum is above 0 by rounding alone (c q took all of its weights,
+    // or they are below what exp_neg holds) has no entry to draw: its sum is
+    // cleared, and the draw made again.
 #pragma unroll 1
     for (;;) {
       if ((skip || rested) && !(all > 0.0)) {  // nothing left: draw from p
