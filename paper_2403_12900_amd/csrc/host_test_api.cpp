@@ -7,6 +7,7 @@
 
 #include "host_state.h"
 #include "launch_rule.h"
+#include "tree_exp.h"
 #include "tree_rule.h"
 
 namespace {
@@ -155,6 +156,10 @@ int sprh_tree_split(const spr_tree_batch* b, int G, int Hkv, int hd, int step, i
   for (int i = 0; i <= t.n; ++i) out[2 + i] = s.item0[i];
   for (int i = 0; i < t.n; ++i) out[3 + t.n + i] = s.order[i];
   return SPR_OK;
+}
+
+void sprh_exp_neg(const double* x, double* y, int n) {
+  for (int i = 0; i < n; ++i) y[i] = sprk::exp_neg(x[i]);
 }
 
 int sprh_tree_step(void* hp, int n, const int32_t* slots, const int32_t* lens, const int32_t* nodes,

@@ -40,6 +40,7 @@
 #pragma once
 
 #include "tree_attn_kernels.h"
+#include "tree_exp.h"
 
 namespace sprk {
 
@@ -74,35 +75,6 @@ struct TreeVerifyArgs {
   int8_t parent[kTreeRows];
 };
 static_assert(sizeof(TreeVerifyArgs) <= 2048, "kernel arguments");
-
-// exp(x) for x <= 0 to 2^-47 of its value, 0 below -708 (where the result
-// would leave the normal range): x = n ln 2 + r, |r| <= ln 2 / 2, with ln 2 in
-// two parts, and the Taylor polynomial of degree 11 of e^r (its rest is below
-// r^12 / 12! < 7e-15).  Adding 1.5 * 2^52 leaves n, rounded, in the low bits
-// of the sum, from where it goes into the exponent: no conversions, which run
-// at a quarter of the rate of the products.
-__device__ __forceinline__ double exp_neg(double x) {
-  constexpr double kShift = 6755399441055744.0;
-  const double t = fma(x, 1.4426950408889634, kShift), n = t - kShift;
-  double r = fma(n, -0x1.62e42fefa39efp-1, x);
-  r = fma(n, -0x1.abc9e3b39803fp-56, r);
-  double p = 1.0 / 39916800.0;
-  p = fma(p, r, 1.0 / 3628800.0);
-  p = fma(p, r, 1.0 / 362880.0);
-  p = fma(p, r, 1.0 / 40320.0);
-  p = fma(p, r, 1.0 / 5040.0);
-  p = fma(p, r, 1.0 / 720.0);
-  p = fma(p, r, 1.0 / 120.0);
-  p = fma(p, r, 1.0 / 24.0);
-  p = fma(p, r, 1.0 / 6.0);
-  p = fma(p, r, 0.5);
-  p = fma(p, r, 1.0);
-  p = fma(p, r, 1.0);
-  const uint64_t bits = static_cast<uint64_t>(__double_as_longlong(p));
-  const uint32_t hi = static_cast<uint32_t>(bits >> 32) + (static_cast<uint32_t>(__double_as_longlong(t)) << 20);
-  const double e = __longlong_as_double(static_cast<long long>(static_cast<uint64_t>(hi) << 32 | static_cast<uint32_t>(bits)));
-  return x < -708.0 ? 0.0 : e;
-}
 
 // OWN consecutive entries of one vocabulary chunk per thread: entry thread *
 // OWN + e, as floats; those past V read as `fill`.
