@@ -7,6 +7,7 @@ stream.
 from __future__ import annotations
 
 import ctypes
+from array import array
 from typing import Optional, Sequence
 
 import numpy as np
@@ -20,6 +21,26 @@ _DTYPES = {torch.float32: SPR_F32, torch.bfloat16: SPR_BF16}
 
 def _refuse(msg: str):
     raise SproutError(SPR_ERR_INVALID_ARG, msg)
+
+
+def _int32(x, name):
+    """x as a vector of int32 of its own, each entry with its value."""
+    try:
+        if isinstance(x, (list, tuple)) and len(x):
+            return np.frombuffer(array("i", x), dtype=np.int32)  # whole numbers of any type; OverflowError past 32 bits
+    except OverflowError:
+        _refuse(f"tree batch: {name} must be whole numbers of 32 bits")
+    except TypeError:
+        pass  # floats, for one
+    try:
+        a = np.array(x.tolist() if isinstance(x, torch.Tensor) else x).reshape(-1)
+        if a.size == 0 or a.dtype.kind in "biu" or a.dtype.kind == "f" and (np.abs(a) < 2 ** 31).all():
+            b = a.astype(np.int32)
+            if (a == b).all():
+                return b
+    except (TypeError, ValueError, OverflowError):
+        pass
+    _refuse(f"tree batch: {name} must be whole numbers of 32 bits")
 
 
 class KVView:
@@ -50,7 +71,8 @@ class TreeBatch:
     def __init__(self, slots: Optional[Sequence[int]], lens: Optional[Sequence[int]], n_nodes: Sequence[int],
                  parents: Sequence[int]):
         # Copies: what the library reads later stays as it was checked here.
-        self._a = [None if x is None else np.array(x, dtype=np.int32).reshape(-1) for x in (slots, lens, n_nodes, parents)]
+        self._a = [None if x is None else _int32(x, name) for x, name in
+                   ((slots, "slots"), (lens, "lens"), (n_nodes, "n_nodes"), (parents, "parents"))]
         n = len(self._a[2])
         if any(x is not None and len(x) != n for x in self._a[:2]):
             _refuse("tree batch: slots, lens and n_nodes must be of one length")
