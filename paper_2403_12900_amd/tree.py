@@ -133,11 +133,13 @@ class TreeOps:
 
     def attention(self, kv: KVView, layer: int, batch: TreeBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None):
         """Attention of the trees' nodes (spr_tree_attention): q [rows, heads, head_dim], fp32 or bf16, rows at any stride;
-        returns out like it."""
+        returns out like it.  Inference only: inputs that want gradients are refused."""
         hd = kv.head_dim
         if q.dim() != 3 or q.shape[0] != batch.rows or q.shape[2] != hd or q.dtype not in _DTYPES:
             _refuse("tree attention: q must be [rows, heads, head_dim], fp32 or bf16")
         rows, heads, _ = q.shape
+        if (q.requires_grad or kv.k.requires_grad or kv.v.requires_grad) and torch.is_grad_enabled():
+            _refuse("tree attention: it has no gradient; detach its inputs, or call it under torch.no_grad()")
         if out is None:
             out = q.new_empty(rows, heads, hd)
         elif out.shape != q.shape or out.dtype != q.dtype:
