@@ -158,6 +158,10 @@ int sprh_tree_split(const spr_tree_batch* b, int G, int Hkv, int hd, int step, i
   return SPR_OK;
 }
 
+int sprh_rows_overlap(uint64_t a, int64_t a_stride, uint64_t b, int64_t b_stride, int64_t width, int rows) {
+  return sprk::rows_overlap(a, a_stride, b, b_stride, width, rows);
+}
+
 void sprh_exp_neg(const double* x, double* y, int n) {
   for (int i = 0; i < n; ++i) y[i] = sprk::exp_neg(x[i]);
 }

@@ -305,6 +305,9 @@ spr_status spr_tree_attention(spr_tree_ops* o, const spr_kv_view* kv, int32_t la
     if (q_stride < width || out_stride < width || q_stride > most || out_stride > most || q_stride * size % 16 != 0 ||
         out_stride * size % 16 != 0)
       return bad_arg("tree_attention: row strides must be >= n_heads * head_dim and a multiple of 16 bytes");
+    if (rows_overlap(reinterpret_cast<uintptr_t>(q), q_stride * size, reinterpret_cast<uintptr_t>(out), out_stride * size,
+                     width * size, t.rows))
+      return bad_arg("tree_attention: out must not overlap q");
     DeviceGuard dev(o->dev);
     if (dev.e != hipSuccess) return hip_failed(o, "tree_attention", dev.e);
     TreeAttnCall c{};

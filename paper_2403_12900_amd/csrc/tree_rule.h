@@ -187,6 +187,20 @@ inline spr_status check_view(const spr_kv_view* v, int layer, const char* what, 
   return SPR_OK;
 }
 
+// Whether two sets of `rows` rows of `width` bytes share a byte; rows of a set
+// do not overlap each other (stride >= width > 0).
+inline bool rows_overlap(uint64_t a, int64_t a_stride, uint64_t b, int64_t b_stride, int64_t width, int rows) {
+  const int64_t off = static_cast<int64_t>(b - a);  // of b's first row
+  for (int r = 0; r < rows; ++r) {
+    // Row k of b starts at off + k b_stride; the last that starts before a's row r ends.
+    const int64_t end = r * a_stride + width - 1 - off;
+    if (end < 0) continue;
+    const int64_t k = std::min<int64_t>(end / b_stride, rows - 1);
+    if (off + k * b_stride + width > r * a_stride) return true;
+  }
+  return false;
+}
+
 // Temperatures (host, or null: 1) are finite and >= 0; random numbers may be
 // missing only where every request is greedy.
 inline spr_status check_temperatures(int n, const float* temperature, const float* accept, const float* sample,

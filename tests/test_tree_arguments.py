@@ -69,3 +69,49 @@ def test_attention_refuses_tensors_that_want_gradients():
             call()
     o.attention(KVView(k, v, table), 0, b, grad(q).detach())
     assert o.lib.calls == 2 + len(calls)
+
+
+def test_rows_that_overlap():
+    """The rule that attention's q and out go by, against the sets of bytes themselves."""
+    import ctypes
+    from .test_abi_host import HOST_LIB
+    L = ctypes.CDLL(HOST_LIB)
+    L.sprh_rows_overlap.argtypes = [ctypes.c_uint64, ctypes.c_int64] * 2 + [ctypes.c_int64, ctypes.c_int]
+    rng = np.random.default_rng(6)
+    seen = [0, 0]
+    for _ in range(4000):
+        rows, width = int(rng.integers(1, 9)), int(rng.integers(1, 20))
+        a, b = (int(x) for x in 1000 + rng.integers(0, 300, 2))
+        sa, sb = (width + int(rng.choice([0, 1, width, 3 * width, 40])) for _ in range(2))
+        if rng.random() < 0.5:
+            sb = sa  # columns of one tensor
+        cells = lambda at, s: {at + r * s + k for r in range(rows) for k in range(width)}  # noqa: E731
+        want = bool(cells(a, sa) & cells(b, sb))
+        assert bool(L.sprh_rows_overlap(a, sa, b, sb, width, rows)) == want, (a, sa, b, sb, width, rows)
+        seen[want] += 1
+    assert min(seen) > 500
+    top = 1 << 40
+    assert L.sprh_rows_overlap(1 << 47, 4 * top, (1 << 47) + 127 * 4 * top + 8, 4 * top, 16, 128)
+    assert not L.sprh_rows_overlap(1 << 47, 4 * top, (1 << 47) + 127 * 4 * top + 16, 4 * top, 16, 128)
+
+
+@pytest.mark.gpu
+def test_attention_refuses_an_output_over_its_queries():
+    from paper_2403_12900_amd.tree import KVView, TreeOps
+    o = TreeOps()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.randn(1, 6, 2, 1024, device="cuda", generator=g) for _ in range(2))
+    view = KVView(k, v, torch.arange(6, dtype=torch.int32, device="cuda").view(1, 6))
+    b = TreeBatch([0], [80], [5], [-1, 0, 0, 1, 1])
+    packed = torch.randn(7, 12, 64, device="cuda", generator=g)
+    want = o.attention(view, 0, b, packed[:5, :4].contiguous())
+    for q, out in ((packed[:5, :4], packed[:5, :4]), (packed[:5, :4], packed[:5, 3:7]), (packed[:5, :4], packed[1:6, 2:6]),
+                   (packed[2:7, 4:8], packed[:5, 5:9])):
+        before = packed.clone()
+        with pytest.raises(SproutError, match="overlap") as e:
+            o.attention(view, 0, b, q, out=out)
+        assert e.value.status == binding.SPR_ERR_INVALID_ARG and torch.equal(packed, before)
+    # Side by side in one tensor they do not.
+    got = o.attention(view, 0, b, packed[:5, :4], out=packed[:5, 4:8])
+    assert torch.equal(got, want) and torch.equal(packed[:5, 4:8], want)
+    o.close()
