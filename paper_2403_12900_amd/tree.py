@@ -98,32 +98,39 @@ class TreeBatch:
 class TreeOps:
     """An operator handle on one device (spr_tree_ops_init), in a torch workspace.
 
-    Calls enqueue on the device's current stream; a call on another stream than the handle's last one first waits for
-    that one (not while a graph is captured: the capture's own order holds).  The handle outlives the graphs that hold
-    its calls."""
+    Calls enqueue on the device's current stream; a call on another stream than the last one's first waits for that one.
+    Calls that a graph captures wait for nothing and are waited for by nothing (the capture's own order holds, and the
+    caller orders replays): eager calls before and after a capture wait for each other.  The handle outlives the graphs
+    that hold its calls."""
 
     def __init__(self, device: int = 0):
         self.lib = load_library()
         self.index = device
         self.device = torch.device("cuda", device)
         self.ws = torch.empty(int(self.lib.spr_tree_ops_workspace_bytes()), dtype=torch.uint8, device=self.device)
+        # The last eager call's stream; the handle's own (a captured call's, too), and whether they are one.
         self.stream = torch.cuda.current_stream(self.device)
-        self.raw_stream = self.stream.cuda_stream
+        self.raw_stream, self.eager = self.stream.cuda_stream, True
         self.h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             _check(self.lib.spr_tree_ops_init(self.ws.data_ptr(), self.ws.numel(), self.raw_stream, ctypes.byref(self.h)))
 
     def _enter(self):
         """Moves the handle to the device's current stream."""
-        if torch._C._cuda_getCurrentRawStream(self.index) == self.raw_stream:
+        raw = torch._C._cuda_getCurrentRawStream(self.index)
+        if raw == self.raw_stream and self.eager:
             return
         s = torch.cuda.current_stream(self.device)
         with torch.cuda.device(self.device):
-            if not torch.cuda.is_current_stream_capturing():
-                s.wait_stream(self.stream)
-                self.ws.record_stream(s)
-        _check(self.lib.spr_tree_ops_set_stream(self.h, s.cuda_stream))
-        self.stream, self.raw_stream = s, s.cuda_stream
+            self.eager = not torch.cuda.is_current_stream_capturing()
+            if self.eager:
+                if raw != self.stream.cuda_stream:
+                    s.wait_stream(self.stream)
+                    self.ws.record_stream(s)
+                self.stream = s
+        if raw != self.raw_stream:
+            _check(self.lib.spr_tree_ops_set_stream(self.h, raw))
+            self.raw_stream = raw
 
     def _vector(self, what, t, dtype, n):
         """Address of a contiguous vector of n elements on the handle's device."""
