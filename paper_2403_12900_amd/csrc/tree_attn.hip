@@ -93,9 +93,10 @@ hipError_t launch(const TreeAttnCall& c) {
 }
 
 // Columns per work-group: two-byte operands 128 (8 x 128 columns of 128
-// dimensions, 6000 positions: 59 us, of 64 columns 63; at 700 positions 23 and
-// 22), the others 64 (fp32, the same columns: 246 us against 259 with 128, at 700
-// positions 46 against 49; three-part queries leave no registers for more).
+// dimensions, 6000 positions: 66 us, of 64 columns 70; 2 x 512 columns, 24000
+// positions: 180 and 197; but at 700 positions 24 and 21), the others 64 (fp32,
+// 8 x 128 columns, 6000 positions: 222 us against 366 with 128, at 700 positions
+// 41 against 67; three-part queries leave no registers for more).
 template <class KP, class IO, int HD>
 hipError_t by_columns(const TreeAttnCall& c) {
   constexpr int most = KP::per16 == 8 && TreeParts<KP, IO>::q == 1 ? 128 : 64;

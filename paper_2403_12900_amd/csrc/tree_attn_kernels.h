@@ -26,8 +26,8 @@
 // The running maximum of a column is raised only when a step exceeds it by
 // kRaise (in log2 units): until then probabilities of at most 2^kRaise stay
 // exact enough in fp32, and steps need neither the exchange between lanes nor
-// the rescaling of O (512 columns over 2 x 24000 positions: 156 us, raised at
-// every larger score 174).
+// the rescaling of O (512 columns over 2 x 24000 positions: 180 us, raised at
+// every larger score 196).
 //
 // Two kernels.  Both cut a request's blocks into KV splits, one work-group
 // each, and write a partial result where a request has several:
@@ -44,15 +44,18 @@
 //                       (64 columns on the other kernel's plan: 110 us where
 //                       this took 78 at first; 512 columns: 504 and 227).
 //                       Bound by the matrix
-//                       unit in fp32 (64 columns, 16 x 5632 positions: 230 us,
-//                       103 of 157 TFLOP/s), by products, exponentials and LDS
+//                       unit in fp32 (64 columns, 16 x 5632 positions: 236 us,
+//                       100 of 154 TFLOP/s), by products, exponentials and LDS
 //                       reads in turn in bf16 (512 columns, 2 x 24000 positions:
-//                       147 us, 690 TFLOP/s), and at short contexts by its ends:
+//                       175 us, 575 TFLOP/s of the formula's products, half as
+//                       many again for the probabilities' second part; with one
+//                       part 147 us), and at short contexts by its ends:
 //                       several trips to memory until the first step runs, 8 to
 //                       9 us of merge at its end.
 // The partials are merged by the split that arrives last where that is little,
-// else by k_tree_merge.  (With 64 columns and more in that one work-group: 512
-// columns over 2 x 6000 positions 65 us, with k_tree_merge 51.)
+// else by k_tree_merge.  (With 64 columns and more in that one work-group, and
+// one-part probabilities: 512 columns over 2 x 6000 positions 65 us, with
+// k_tree_merge 51; with two parts now 57.)
 #pragma once
 
 #include <type_traits>
@@ -746,8 +749,9 @@ struct TreeStage {
 // few) run masked, the others without a test.
 //
 // Work-groups of a CU: three with fp32 operands (16 x 5632 positions, 64 columns:
-// 225 us, with two 253), two with bf16 ones (that: 81 us, with three 86; 16 x 704
-// positions 20 and 25).
+// 236 us, with two 241; 128 columns, 8 x 6000: 222 and 230; but 16 x 704: 46 and
+// 44), two with bf16 ones (16 x 5632: 85 us, with three 89; 16 x 704: 21.6 and
+// 26; with 128 columns three leave too few registers, 8 x 6000: 66 and 137).
 template <class KP>
 constexpr int kSharedPerCu = KP::per16 == 4 ? 3 : 2;
 template <class KP, class IO, int HD, int NT>

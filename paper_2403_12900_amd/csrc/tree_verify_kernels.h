@@ -30,11 +30,14 @@
 // No work-group waits on another, nothing is counted, and all sums run in a
 // fixed order.  Bound by latency while the rows are few -- 5 rows of 32000: 14.5
 // us, sums 5.5 (4.4 without the children's own) and walk 9.2 (8 of its loads and
-// barriers follow one another) -- and by fp64 arithmetic where they are many: 128
-// rows of 131072 with draft probabilities, up to 4 children a node, 65 us: sums
-// 23 (16.4 M exponentials of 20 fp64 operations; the 33 MB alone would take 6),
-// four N_k passes of 9, walk 11.5.  16 x 8 nodes of 32000: 28 us.  (The walk as
-// the end of the last sums' launch, in the work-group that finishes a request's
+// barriers follow one another) -- and by vector instructions where they are many:
+// 128 rows of 131072 with draft probabilities, up to 4 children a node, 65 us: sums
+// 23 (16.4 M entries of 42 instructions, 21 of them the exponential's fp64
+// operations, the rest maximum, index, NaN test and conversion; the 33 MB alone
+// would take 5), four N_k passes of 9, walk 12.  16 x 8 nodes of 32000: 28 us.  A
+// node of many children costs a pass for each: 63 below the root, 64 rows of
+// 32000, 335 us (of 131072: 414); without draft probabilities 45 (52).  (The walk
+// as the end of the last sums' launch, in the work-group that finishes a request's
 // last chunk, cost what the launch saves and held greedy requests' walks between
 // two launches.)
 #pragma once
