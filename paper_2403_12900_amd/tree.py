@@ -34,6 +34,8 @@ def _int32(x, name):
         pass  # floats, for one
     try:
         a = np.array(x.tolist() if isinstance(x, torch.Tensor) else x).reshape(-1)
+        if a.dtype.kind == "O":
+            return np.frombuffer(array("i", a.tolist()), dtype=np.int32)
         if a.size == 0 or a.dtype.kind in "biu" or a.dtype.kind == "f" and (np.abs(a) < 2 ** 31).all():
             b = a.astype(np.int32)
             if (a == b).all():

@@ -21,7 +21,8 @@ def test_numbers_that_are_no_int32_are_refused(which, bad):
 
 
 @pytest.mark.parametrize("kind", [list, tuple, lambda x: np.array(x, dtype=np.int64), lambda x: np.array(x, dtype=np.uint8), lambda x: np.array(x, dtype=np.float64),
-                                  lambda x: torch.tensor(x), lambda x: [np.int64(v) for v in x]])
+                                  lambda x: torch.tensor(x), lambda x: np.array(x, dtype=object), lambda x: [[v] for v in x],
+                                  lambda x: [torch.tensor(v) for v in x], lambda x: [float(v) for v in x], lambda x: [np.int64(v) for v in x]])
 def test_whole_numbers_of_any_type_are_taken(kind):
     b = TreeBatch(kind([3, 1]), kind([70, 200]), kind([2, 1]), np.array([-1, 0, -1], dtype=np.int64))
     assert [b._c.slots[i] for i in (0, 1)] == [3, 1] and [b._c.lens[i] for i in (0, 1)] == [70, 200]
