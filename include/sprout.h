@@ -500,6 +500,194 @@ spr_status spr_tree_step(spr_model* m, const spr_tree_batch* batch, int32_t* tok
                          const float* draft_probs, const float* temperature, const float* accept, const float* sample,
                          float* logits, int32_t* emitted, int32_t* count, int32_t* retired);
 
+/* ---------------------------------------------------------------------------
+ * A paged KV cache held in 4 bits (Section II-A's cached keys and values at a
+ * quarter of bf16's bytes), and what a serving loop does with it: rotary
+ * positions, appending a step's keys and values, reading them back, attention
+ * over the cache, and the sharing and moving of its blocks.
+ *
+ * Stored values: 32 consecutive dimensions of one position and head share a
+ * scale 2^s, s in -120..125, and each is a 4-bit code (sign, two exponent bits,
+ * one mantissa bit) for +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} times that scale.  s is
+ * the smallest with max|x| <= 7 * 2^s (so that no element is off by more than
+ * half a step; from 7 * 2^125 on elements are cut to 6 * 2^125); an element is rounded to
+ * the nearest value, of two as near the one whose code is even.  A group that
+ * holds an infinity or a NaN is stored as NaN, all 32 of it.
+ *
+ * The operators run on caller-owned tensors through an operator handle of
+ * their own, under the conventions of spr_tree_ops_init.
+ * ------------------------------------------------------------------------ */
+
+#define SPR_MAX_CACHE_REQUESTS 128  /* requests (or forks) of one call */
+#define SPR_MAX_CACHE_ROWS 1048576  /* token rows of one call */
+
+/*
+ * Block b of layer l holds 16 positions of every KV head: n_kv_heads tiles of
+ * 17 * head_dim bytes from byte ((l * n_blocks + b) * n_kv_heads) * 17 *
+ * head_dim of data.  With P = head_dim / 32, position t < 16 and dimension d
+ * of a tile:
+ *   key codes    byte (d / 32 * 16 + t) * 16 + d % 32 / 2, low nibble for even d
+ *   value codes  byte 8 * head_dim + ((t / 4 * 16 + d % 16) * P + d / 32) * 4 + t % 4,
+ *                low nibble for d % 32 < 16
+ *   key scales   byte 16 * head_dim + d / 32 * 16 + t: s + 127, or 255 for NaN
+ *   value scales byte 16.5 * head_dim + (t / 4 * P + d / 32) * 4 + t % 4, likewise
+ * (keys as the matrix unit's operand of K q^T, values of V^T p).  Constraints
+ * and block ids outside the pool: as for spr_kv_view; data is 16-byte aligned.
+ * Positions that a call attends to or reads hold what spr_cache_append wrote
+ * (other scale bytes are not told apart from 2^(byte - 127)).
+ */
+typedef struct {
+  void* data; /* device */
+  int32_t n_layers, n_blocks, n_kv_heads, head_dim;
+  const int32_t* block_table; /* device [n_slots][max_blocks] */
+  int32_t n_slots, max_blocks;
+} spr_kv4_view;
+
+/*
+ * The requests of one call (host memory, read during the call): request i's
+ * rows are positions lens[i] .. lens[i] + rows[i] - 1 of its slot, and the
+ * token rows of a call's tensors are those of all requests, one after the other.
+ *   n      1..SPR_MAX_CACHE_REQUESTS
+ *   slots  [n]: distinct rows of the block table
+ *   lens   [n]: positions before the rows, 0..2^30
+ *   rows   [n]: >= 1 each, at most SPR_MAX_CACHE_ROWS in all
+ * lens[i] + rows[i] must not exceed max_blocks * 16.
+ */
+typedef struct {
+  int32_t n;
+  const int32_t *slots, *lens, *rows;
+} spr_cache_batch;
+
+/*
+ * Rotary positions: pair k of a head's first dims dimensions is turned by
+ * position * 2 pi * turns[k] and scaled by amplitude; the dimensions behind
+ * them stay as they are.  Filled in by spr_rotary_init.
+ */
+typedef struct {
+  int32_t dims;  /* even, 2..128 */
+  int32_t pairs; /* pair k is dimensions 0: (k, k + dims / 2), 1: (2k, 2k + 1) */
+  double amplitude;
+  double turns[64];
+} spr_rotary;
+
+/*
+ * Frequencies w_k = base^(-2k / dims).  For contexts longer than the
+ * `original` positions a model was made for (factor > 1), a frequency that
+ * turns t = original * w / (2 pi) times over those is taken as
+ *   w (keep + (1 - keep) / factor),  keep = clamp((t - low) / (high - low), 0, 1):
+ * quick ones as they are, slow ones divided by the factor.  factor 1 does not
+ * read original, low and high.  Host only, enqueues nothing.
+ *   base > 0; factor >= 1; original > 0; high > low; amplitude finite
+ */
+spr_status spr_rotary_init(int32_t dims, int32_t pairs, double base, double factor, double original, double low,
+                           double high, double amplitude, spr_rotary* out);
+
+typedef struct spr_cache_ops spr_cache_ops; /* opaque, library-owned host state */
+
+/*
+ * Workspace, creation, stream and release of a handle: as for spr_tree_ops.
+ * Its device checks: a block id out of range, a fork's fresh block that another
+ * of its forks copies from.
+ */
+size_t spr_cache_ops_workspace_bytes(void);
+spr_status spr_cache_ops_init(void* dev_ws, size_t ws_bytes, void* hip_stream, spr_cache_ops** out);
+spr_status spr_cache_ops_set_stream(spr_cache_ops* ops, void* hip_stream);
+spr_status spr_cache_ops_release(spr_cache_ops* ops);
+
+/*
+ * Rotary positions of queries (or of anything in heads): row r and head h of
+ * out are x's turned at positions[r], each element rounded once (angles,
+ * sines and products are held in 64 bits).
+ *   rows       1..SPR_MAX_CACHE_ROWS; n_heads 1..8192; head_dim 64 or 128, >= rotary->dims
+ *   rotary     host, read during the call
+ *   dtype      of x and out
+ *   positions  device int32 [rows], of any sign
+ *   x, out     device [rows] x [n_heads * head_dim], row r at r * stride
+ *              elements; 16-byte aligned, strides a multiple of 16 bytes and >=
+ *              n_heads * head_dim.  out may be x itself, else they must not overlap
+ */
+spr_status spr_cache_rotary(spr_cache_ops* ops, const spr_rotary* rotary, int32_t rows, int32_t n_heads, int32_t head_dim,
+                            int32_t dtype, const int32_t* positions, const void* x, int64_t x_stride, void* out,
+                            int64_t out_stride);
+
+/*
+ * Writes the keys and values of the batch's rows to layer `layer` of the
+ * cache, keys turned at their cache positions first (rotary NULL: as they
+ * are).  Nothing but the rows' own positions is written; a row whose block id
+ * lies outside the pool is not.  The blocks that rows go to are their
+ * request's alone (earlier ones may be shared).
+ *   dtype  of k and v: device [rows] x [n_kv_heads * head_dim], strides in elements,
+ *          aligned as in spr_cache_rotary
+ */
+spr_status spr_cache_append(spr_cache_ops* ops, const spr_kv4_view* kv, int32_t layer, const spr_cache_batch* batch,
+                            const spr_rotary* rotary, int32_t dtype, const void* k, int64_t k_stride, const void* v,
+                            int64_t v_stride);
+
+/*
+ * The other way: the values that the cache holds at the batch's rows, into k
+ * and v (exact in either dtype).  k and v must not overlap.
+ */
+spr_status spr_cache_read(spr_cache_ops* ops, const spr_kv4_view* kv, int32_t layer, const spr_cache_batch* batch,
+                          int32_t dtype, void* k, int64_t k_stride, void* v, int64_t v_stride);
+
+/*
+ * Attention of the batch's rows over layer `layer`: row j of request i and
+ * head h attend to positions 0 .. lens[i] + j, the row's own the last of them
+ * (its keys and values are in the cache already),
+ *   out[r][h] = softmax(q[r][h] . K^T / sqrt(head_dim)) V
+ * (head h reads KV head h / (n_heads / n_kv_heads)).  One row a request is a
+ * decode step, more a prompt's chunk or drafted tokens in a line.  What lies
+ * in the cache behind a row's last position does not reach its output,
+ * whatever it holds.
+ *   n_heads  a multiple of n_kv_heads, n_heads / n_kv_heads <= 16
+ *   dtype    of q and out; scores, sums and products are held in fp32, the
+ *            probabilities of bf16 outputs to 2^-12
+ *   q, out   device [rows] x [n_heads * head_dim], aligned as in
+ *            spr_cache_rotary.  out must not overlap q.
+ */
+spr_status spr_cache_attention(spr_cache_ops* ops, const spr_kv4_view* kv, int32_t layer, const spr_cache_batch* batch,
+                               int32_t n_heads, int32_t dtype, const void* q, int64_t q_stride, void* out,
+                               int64_t out_stride);
+
+/*
+ * The blocks of any paged cache as bytes: block b of layer l is block_bytes
+ * bytes from byte (l * n_blocks + b) * block_bytes of k, and of v where that
+ * is not NULL (a 4-bit cache has one pool: data as k).  block_bytes is a
+ * multiple of 16, the pools are 16-byte aligned.  Views of a model's own cache
+ * are not for spr_cache_fork and spr_cache_move: its slots own its blocks.
+ */
+typedef struct {
+  void* k; /* device */
+  void* v; /* device or NULL */
+  int64_t block_bytes;
+  int32_t n_layers, n_blocks;
+  int32_t* block_table; /* device [n_slots][max_blocks] */
+  int32_t n_slots, max_blocks;
+} spr_pages;
+
+/*
+ * Forks requests: slot target[i] continues the first lens[i] positions of slot
+ * source[i].  Its table row gets the source's full blocks (lens[i] / 16 of
+ * them, shared from now on) and, where positions are left, block fresh[i] with
+ * a copy of the source's next block in every layer; entries behind stay.
+ *   n       1..SPR_MAX_CACHE_REQUESTS
+ *   source, target  host [n]: slots; targets distinct, and none of them a source
+ *   lens    host [n]: 0 .. max_blocks * 16
+ *   fresh   host [n]: distinct free blocks (not read where lens[i] % 16 == 0)
+ * A source entry outside the pool, or one that is a fresh block of the call,
+ * is not copied and fails the handle's next call.
+ */
+spr_status spr_cache_fork(spr_cache_ops* ops, const spr_pages* pages, int32_t n, const int32_t* source,
+                          const int32_t* target, const int32_t* lens, const int32_t* fresh);
+
+/*
+ * Moves block src[i] to dst[i] in every layer, and every table entry that is
+ * src[i] to dst[i] (compaction, say).  What src[i] holds stays there.
+ *   n         1..n_blocks
+ *   src, dst  host [n]: blocks of the pool, distinct, and no dst is a src
+ */
+spr_status spr_cache_move(spr_cache_ops* ops, const spr_pages* pages, int32_t n, const int32_t* src, const int32_t* dst);
+
 /* Releases the host state.  The workspace is the caller's to free afterwards. */
 spr_status spr_release(spr_model* m);
 

@@ -64,6 +64,27 @@ class SprKvView(ctypes.Structure):
                 ("max_blocks", ctypes.c_int32)]
 
 
+class SprKv4View(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n_layers", ctypes.c_int32), ("n_blocks", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("block_table", ctypes.c_void_p),
+                ("n_slots", ctypes.c_int32), ("max_blocks", ctypes.c_int32)]
+
+
+class SprCacheBatch(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("slots", _I32P), ("lens", _I32P), ("rows", _I32P)]
+
+
+class SprRotary(ctypes.Structure):
+    _fields_ = [("dims", ctypes.c_int32), ("pairs", ctypes.c_int32), ("amplitude", ctypes.c_double),
+                ("turns", ctypes.c_double * 64)]
+
+
+class SprPages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("block_bytes", ctypes.c_int64),
+                ("n_layers", ctypes.c_int32), ("n_blocks", ctypes.c_int32), ("block_table", ctypes.c_void_p),
+                ("n_slots", ctypes.c_int32), ("max_blocks", ctypes.c_int32)]
+
+
 class SprTreeBatch(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int32), ("slots", _I32P), ("lens", _I32P), ("n_nodes", _I32P), ("parents", _I32P)]
 
@@ -124,6 +145,22 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                        ("spr_tree_keep", [vp, view, batch, vp, vp]),
                        ("spr_model_kv_view", [vp, view]),
                        ("spr_tree_step", [vp, batch, vp, vp, vp, f32p, vp, vp, vp, vp, _I32P, _I32P])):
+        getattr(L, name).restype = ctypes.c_int
+        getattr(L, name).argtypes = args
+    kv4, rows, rotary, pages = (ctypes.POINTER(t) for t in (SprKv4View, SprCacheBatch, SprRotary, SprPages))
+    f64 = ctypes.c_double
+    L.spr_cache_ops_workspace_bytes.restype = ctypes.c_size_t
+    L.spr_cache_ops_workspace_bytes.argtypes = []
+    for name, args in (("spr_rotary_init", [i32, i32, f64, f64, f64, f64, f64, f64, rotary]),
+                       ("spr_cache_ops_init", [vp, ctypes.c_size_t, vp, ctypes.POINTER(vp)]),
+                       ("spr_cache_ops_set_stream", [vp, vp]),
+                       ("spr_cache_ops_release", [vp]),
+                       ("spr_cache_rotary", [vp, rotary, i32, i32, i32, i32, vp, vp, i64, vp, i64]),
+                       ("spr_cache_append", [vp, kv4, i32, rows, rotary, i32, vp, i64, vp, i64]),
+                       ("spr_cache_read", [vp, kv4, i32, rows, i32, vp, i64, vp, i64]),
+                       ("spr_cache_attention", [vp, kv4, i32, rows, i32, i32, vp, i64, vp, i64]),
+                       ("spr_cache_fork", [vp, pages, i32, _I32P, _I32P, _I32P, _I32P]),
+                       ("spr_cache_move", [vp, pages, i32, _I32P, _I32P])):
         getattr(L, name).restype = ctypes.c_int
         getattr(L, name).argtypes = args
     L.spr_release.restype = ctypes.c_int

@@ -34,7 +34,8 @@ def _run(cmd, verbose):
 
 # Translation units of libsprout.so, the slowest to compile first; compiled in parallel.
 SOURCES = ["panel_qkv.hip", "panel_qkv_rows.hip", "panel_mlp.hip", "sprout.hip", "panel_resid.hip", "tile_qkv.hip",
-           "tile_resid.hip", "tile_mlp.hip", "tree_attn.hip", "tree.hip", "host_state.cpp"]
+           "tile_resid.hip", "tile_mlp.hip", "tree_attn.hip", "cache_attn.hip", "tree.hip",
+           "cache.hip", "host_state.cpp"]
 
 
 def build(verbose: bool = True) -> None:

@@ -1,0 +1,182 @@
+"""The 4-bit KV cache's operators on torch tensors: a thin binding of spr_cache_rotary, spr_cache_append, spr_cache_read,
+spr_cache_attention, spr_cache_fork and spr_cache_move.
+
+Argument marshalling only, as in tree.py: shapes, types and devices are checked here, all other checks are the library's.
+Inference only: inputs that want gradients are refused.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Sequence, Union
+
+import numpy as np
+import torch
+
+from .binding import SprCacheBatch, SprKv4View, SprPages, SprRotary, _check, _ptr, load_library
+from .tree import _DTYPES, KVView, OpHandle, _int32, _refuse
+
+
+class KV4View:
+    """A paged KV cache in 4 bits (spr_kv4_view): data [layers, blocks, KV heads, 17 * head_dim] bytes in the tile order that
+    the header gives, and the int32 block table [slots, blocks per slot], contiguous on one device.  A fresh cache may hold
+    anything: no operator reads positions that were not appended."""
+
+    def __init__(self, data: torch.Tensor, block_table: torch.Tensor):
+        if data.dim() != 4 or data.dtype != torch.uint8 or data.shape[3] % 17:
+            _refuse("kv4 view: data must be uint8 [layers, blocks, kv_heads, 17 * head_dim]")
+        if block_table.dim() != 2 or block_table.dtype != torch.int32:
+            _refuse("kv4 view: the block table must be int32 [slots, blocks per slot]")
+        if not (data.is_contiguous() and block_table.is_contiguous()):
+            _refuse("kv4 view: data and the block table must be contiguous")
+        if block_table.device != data.device:
+            _refuse("kv4 view: data and the block table must be on one device")
+        self.data, self.block_table, self.index = data, block_table, data.get_device()
+        self.head_dim = data.shape[3] // 17
+        self.n_kv_heads = data.shape[2]
+        self._c = SprKv4View(data.data_ptr(), data.shape[0], data.shape[1], data.shape[2], self.head_dim,
+                             block_table.data_ptr(), block_table.shape[0], block_table.shape[1])
+        self.ref = ctypes.byref(self._c)
+
+    @staticmethod
+    def empty(layers: int, blocks: int, n_kv_heads: int, head_dim: int, slots: int, blocks_per_slot: int, device=0) -> "KV4View":
+        """A cache of its own, with a table of zeros."""
+        return KV4View(torch.empty(layers, blocks, n_kv_heads, 17 * head_dim, dtype=torch.uint8, device=device),
+                       torch.zeros(slots, blocks_per_slot, dtype=torch.int32, device=device))
+
+
+class CacheBatch:
+    """The requests of one call (spr_cache_batch): per request its slot, the positions before its rows, and its rows."""
+
+    def __init__(self, slots: Sequence[int], lens: Sequence[int], rows: Sequence[int]):
+        # Copies: what the library reads later stays as it was checked here.
+        self._a = [_int32(x, name, "cache batch") for x, name in ((slots, "slots"), (lens, "lens"), (rows, "rows"))]
+        n = len(self._a[0])
+        if any(len(x) != n for x in self._a):
+            _refuse("cache batch: slots, lens and rows must be of one length")
+        self.n, self.rows = n, int(np.maximum(self._a[2], 0).sum(dtype=np.int64))
+        self._c = SprCacheBatch(n, *(_ptr(x) for x in self._a))
+        self.ref = ctypes.byref(self._c)
+
+
+class Rotary:
+    """Rotary positions (spr_rotary_init): the first dims dimensions of a head, in pairs (d, d + dims / 2) (layout "half") or
+    (2d, 2d + 1) ("pairs"), turned at base^(-2k / dims); factor > 1 lowers the frequencies that turn seldom over the
+    original length, and amplitude scales what is turned."""
+
+    def __init__(self, dims: int, layout: str = "half", base: float = 10000.0, factor: float = 1.0, original: float = 0.0,
+                 low: float = 1.0, high: float = 32.0, amplitude: float = 1.0):
+        if layout not in ("half", "pairs"):
+            _refuse('rotary: layout must be "half" or "pairs"')
+        self._c = SprRotary()
+        self.ref = ctypes.byref(self._c)
+        _check(load_library().spr_rotary_init(dims, layout == "pairs", base, factor, original, low, high, amplitude, self.ref))
+        self.dims, self.layout = dims, layout
+
+
+class CacheOps(OpHandle):
+    """The 4-bit cache's operators of one device (spr_cache_ops_init)."""
+
+    _prefix = "spr_cache_ops"
+
+    def rotary(self, rotary: Rotary, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None):
+        """Rotary positions (spr_cache_rotary): x [rows, heads, head_dim], fp32 or bf16, rows at any stride, positions int32
+        [rows]; returns out like it (which may be x itself)."""
+        if x.dim() != 3 or x.dtype not in _DTYPES:
+            _refuse("cache rotary: x must be [rows, heads, head_dim], fp32 or bf16")
+        self._no_grad("cache rotary", x)
+        rows, heads, hd = x.shape
+        p_positions = self._vector("cache rotary: positions", positions, torch.int32, rows)
+        out = self._out("cache rotary", x, out)
+        xs, os = self._row_stride("cache rotary", x, heads, hd), self._row_stride("cache rotary", out, heads, hd)
+        self._enter()
+        _check(self.lib.spr_cache_rotary(self.h, rotary.ref, rows, heads, hd, _DTYPES[x.dtype], p_positions, x.data_ptr(), xs,
+                                         out.data_ptr(), os))
+        return out
+
+    def append(self, kv: KV4View, layer: int, batch: CacheBatch, k: torch.Tensor, v: torch.Tensor, rotary: Optional[Rotary] = None):
+        """Writes the rows' keys and values (spr_cache_append): k and v [rows, KV heads, head_dim], fp32 or bf16, rows at any
+        stride; keys are turned at their cache positions first where rotary is given."""
+        shape = (batch.rows, kv.n_kv_heads, kv.head_dim)
+        if k.shape != shape or v.shape != shape or k.dtype not in _DTYPES or v.dtype != k.dtype:
+            _refuse("cache append: k and v must be [rows, kv_heads, head_dim] of one type, fp32 or bf16")
+        self._no_grad("cache append", k, v)
+        ks, vs = (self._row_stride("cache append", t, *shape[1:]) for t in (k, v))
+        self._same_device("cache append", kv)
+        self._enter()
+        _check(self.lib.spr_cache_append(self.h, kv.ref, layer, batch.ref, None if rotary is None else rotary.ref,
+                                         _DTYPES[k.dtype], k.data_ptr(), ks, v.data_ptr(), vs))
+
+    def read(self, kv: KV4View, layer: int, batch: CacheBatch, dtype: torch.dtype = torch.float32):
+        """The values that the cache holds at the rows (spr_cache_read): k and v [rows, KV heads, head_dim]."""
+        if dtype not in _DTYPES:
+            _refuse("cache read: dtype must be fp32 or bf16")
+        self._same_device("cache read", kv)
+        width = kv.n_kv_heads * kv.head_dim
+        k, v = (torch.empty(batch.rows, kv.n_kv_heads, kv.head_dim, dtype=dtype, device=kv.data.device) for _ in range(2))
+        self._enter()
+        _check(self.lib.spr_cache_read(self.h, kv.ref, layer, batch.ref, _DTYPES[dtype], k.data_ptr(), width, v.data_ptr(), width))
+        return k, v
+
+    def attention(self, kv: KV4View, layer: int, batch: CacheBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None):
+        """Attention of the rows over the cache (spr_cache_attention): q [rows, heads, head_dim], fp32 or bf16, rows at any
+        stride; returns out like it."""
+        if q.dim() != 3 or q.shape[0] != batch.rows or q.shape[2] != kv.head_dim or q.dtype not in _DTYPES:
+            _refuse("cache attention: q must be [rows, heads, head_dim], fp32 or bf16")
+        self._no_grad("cache attention", q)
+        _, heads, hd = q.shape
+        out = self._out("cache attention", q, out)
+        qs, os = self._row_stride("cache attention", q, heads, hd), self._row_stride("cache attention", out, heads, hd)
+        self._same_device("cache attention", kv)
+        self._enter()
+        _check(self.lib.spr_cache_attention(self.h, kv.ref, layer, batch.ref, heads, _DTYPES[q.dtype], q.data_ptr(), qs,
+                                            out.data_ptr(), os))
+        return out
+
+    def fork(self, kv: Union[KV4View, KVView], source: Sequence[int], target: Sequence[int], lens: Sequence[int],
+             fresh: Sequence[int]):
+        """Forks requests (spr_cache_fork): slot target[i] continues the first lens[i] positions of slot source[i], whose full
+        blocks it shares; fresh[i] takes a copy of the last, partly filled one.  Any paged cache."""
+        a = [_int32(x, name, "cache fork") for x, name in
+             ((source, "source"), (target, "target"), (lens, "lens"), (fresh, "fresh"))]
+        if any(len(x) != len(a[0]) for x in a):
+            _refuse("cache fork: source, target, lens and fresh must be of one length")
+        pages = self._pages("cache fork", kv)
+        self._enter()
+        _check(self.lib.spr_cache_fork(self.h, pages, len(a[0]), *(_ptr(x) for x in a)))
+
+    def move(self, kv: Union[KV4View, KVView], src: Sequence[int], dst: Sequence[int]):
+        """Moves blocks src[i] to dst[i] in every layer, and the table's entries with them (spr_cache_move).  Any paged cache."""
+        a = [_int32(src, "src", "cache move"), _int32(dst, "dst", "cache move")]
+        if len(a[0]) != len(a[1]):
+            _refuse("cache move: src and dst must be of one length")
+        pages = self._pages("cache move", kv)
+        self._enter()
+        _check(self.lib.spr_cache_move(self.h, pages, len(a[0]), *(_ptr(x) for x in a)))
+
+    def _pages(self, what, kv):
+        self._same_device(what, kv)
+        k, v = (kv.data, None) if isinstance(kv, KV4View) else (kv.k, kv.v)
+        layers, blocks, heads, tile = k.shape
+        return ctypes.byref(SprPages(k.data_ptr(), None if v is None else v.data_ptr(), heads * tile * k.element_size(), layers,
+                                     blocks, kv.block_table.data_ptr(), *kv.block_table.shape))
+
+    def _same_device(self, what, kv):
+        if kv.index != self.index:
+            _refuse(f"{what}: the cache must be on {self.device}")
+
+    def _no_grad(self, what, *tensors):
+        if torch.is_grad_enabled() and any(t.requires_grad for t in tensors):
+            _refuse(f"{what}: it has no gradient; detach its inputs, or call it under torch.no_grad()")
+
+    def _out(self, what, x, out):
+        if out is None:
+            return x.new_empty(x.shape)
+        if out.shape != x.shape or out.dtype != x.dtype:
+            _refuse(f"{what}: out must be like its input")
+        return out
+
+    def _row_stride(self, what, t, heads, hd):
+        row, head, one = t.stride()
+        if t.get_device() != self.index or one != 1 or (heads > 1 and head != hd):
+            _refuse(f"{what}: its tensors must be on {self.device} with contiguous rows")
+        return row if t.shape[0] > 1 else heads * hd  # a single row's stride does not matter

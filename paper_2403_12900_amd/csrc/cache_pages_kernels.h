@@ -1,0 +1,137 @@
+// Forking and moving the blocks of a paged cache: copies of whole blocks in
+// every layer, and the block table's entries.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "cache_rule.h"
+#include "device_common.h"
+
+namespace sprk {
+
+typedef unsigned int page_piece_t __attribute__((ext_vector_type(4)));
+
+// How a block's bytes are shared out: chunks of `chunk` 16-byte pieces, for
+// every layer of every pool.
+struct PageCopy {
+  char* pool[2];
+  int pools, layers, chunks, chunk, pieces;  // pieces of a block
+  int64_t block_bytes, layer_bytes;
+};
+
+constexpr int kPageDeep = 4;  // pieces of a thread in flight
+
+// Work item w of a block: its chunk in some layer of some pool.
+struct PageItem {
+  char* base;  // of block 0 of the layer
+  int first, end;
+};
+__device__ __forceinline__ PageItem page_item(const PageCopy& c, int w) {
+  const int chunk = w % c.chunks, l = w / c.chunks;
+  PageItem it;
+  it.base = (l < c.layers ? c.pool[0] : c.pool[1]) + (l < c.layers ? l : l - c.layers) * c.layer_bytes;
+  it.first = chunk * c.chunk;
+  it.end = min(it.first + c.chunk, c.pieces);
+  return it;
+}
+
+struct ForkArgs {
+  PageCopy c;
+  int32_t* bt;
+  int* err;
+  int mb, nb, n, groups;
+  int source[kCacheReqs], target[kCacheReqs], len[kCacheReqs], fresh[kCacheReqs];
+  int first[kCacheReqs + 1];
+};
+static_assert(sizeof(ForkArgs) <= 3584, "kernel arguments");
+
+// Work-groups: n for the table rows, then the chunks of each group of forks
+// that copy one block: it is read once and written to all of their blocks.
+__global__ __launch_bounds__(256) void k_cache_fork(ForkArgs a) {
+  const int tid = threadIdx.x;
+  if (static_cast<int>(blockIdx.x) < a.n) {
+    const int i = blockIdx.x, full = a.len[i] / 16;
+    const int32_t* from = a.bt + static_cast<size_t>(a.source[i]) * a.mb;
+    int32_t* to = a.bt + static_cast<size_t>(a.target[i]) * a.mb;
+    for (int e = tid; e < full; e += 256) to[e] = from[e];
+    if (tid == 0 && a.fresh[i] >= 0) to[full] = a.fresh[i];
+    return;
+  }
+  const int items = a.c.pools * a.c.layers * a.c.chunks;
+  const int w = blockIdx.x - a.n, group = w / items;
+  const int f0 = a.first[group], f1 = a.first[group + 1];
+  const int id = a.bt[static_cast<size_t>(a.source[f0]) * a.mb + a.len[f0] / 16];
+  bool fresh = false;
+  for (int i = tid; i < a.first[a.groups]; i += 256) fresh |= a.fresh[i] == id;
+  const bool lost = static_cast<unsigned>(id) >= static_cast<unsigned>(a.nb);
+  if (__syncthreads_or(fresh) || lost) {
+    if (tid == 0) raise_check(a.err, lost ? kErrBlockId : kErrFresh);
+    return;
+  }
+  const PageItem it = page_item(a.c, w - group * items);
+  const page_piece_t* src = reinterpret_cast<const page_piece_t*>(it.base + id * a.c.block_bytes);
+  for (int x = it.first + tid; x < it.end; x += 256 * kPageDeep) {
+    page_piece_t v[kPageDeep];
+#pragma unroll
+    for (int k = 0; k < kPageDeep; ++k) v[k] = src[min(x + 256 * k, it.end - 1)];
+    for (int f = f0; f < f1; ++f) {
+      page_piece_t* dst = reinterpret_cast<page_piece_t*>(it.base + a.fresh[f] * a.c.block_bytes);
+#pragma unroll
+      for (int k = 0; k < kPageDeep; ++k)
+        if (x + 256 * k < it.end) dst[x + 256 * k] = v[k];
+    }
+  }
+}
+
+constexpr int kMoves = 384;  // of one launch
+struct MoveArgs {
+  PageCopy c;
+  int32_t* bt;
+  int n, table_groups;
+  int64_t entries;
+  int src[kMoves], dst[kMoves];  // src ascending
+};
+static_assert(sizeof(MoveArgs) <= 3584, "kernel arguments");
+
+constexpr int kTableEntries = 1024;  // of one work-group
+
+// Work-groups: table_groups for the table's entries (each looked up among the
+// moved blocks), then the chunks of each moved block.
+__global__ __launch_bounds__(256) void k_cache_move(MoveArgs a) {
+  const int tid = threadIdx.x;
+  if (static_cast<int>(blockIdx.x) < a.table_groups) {
+    __shared__ int src[kMoves], dst[kMoves];
+    for (int i = tid; i < a.n; i += 256) {
+      src[i] = a.src[i];
+      dst[i] = a.dst[i];
+    }
+    __syncthreads();
+    const int64_t e1 = min(static_cast<int64_t>(blockIdx.x + 1) * kTableEntries, a.entries);
+    for (int64_t e = static_cast<int64_t>(blockIdx.x) * kTableEntries + tid; e < e1; e += 256) {
+      const int id = a.bt[e];
+      int lo = 0, hi = a.n;  // the first src >= id lies in [lo, hi]
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (src[mid] < id) lo = mid + 1;
+        else hi = mid;
+      }
+      if (lo < a.n && src[lo] == id) a.bt[e] = dst[lo];
+    }
+    return;
+  }
+  const int items = a.c.pools * a.c.layers * a.c.chunks;
+  const int w = blockIdx.x - a.table_groups, m = w / items;
+  const PageItem it = page_item(a.c, w - m * items);
+  const page_piece_t* src = reinterpret_cast<const page_piece_t*>(it.base + a.src[m] * a.c.block_bytes);
+  page_piece_t* dst = reinterpret_cast<page_piece_t*>(it.base + a.dst[m] * a.c.block_bytes);
+  for (int x = it.first + tid; x < it.end; x += 256 * kPageDeep) {
+    page_piece_t v[kPageDeep];
+#pragma unroll
+    for (int k = 0; k < kPageDeep; ++k) v[k] = src[min(x + 256 * k, it.end - 1)];
+#pragma unroll
+    for (int k = 0; k < kPageDeep; ++k)
+      if (x + 256 * k < it.end) dst[x + 256 * k] = v[k];
+  }
+}
+
+}  // namespace sprk

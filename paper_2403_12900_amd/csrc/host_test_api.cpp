@@ -5,6 +5,7 @@
 #include <string>
 #include <vector>
 
+#include "cache_rule.h"
 #include "host_state.h"
 #include "launch_rule.h"
 #include "tree_exp.h"
@@ -160,6 +161,66 @@ int sprh_tree_split(const spr_tree_batch* b, int G, int Hkv, int hd, int step, i
 
 int sprh_rows_overlap(uint64_t a, int64_t a_stride, uint64_t b, int64_t b_stride, int64_t width, int rows) {
   return sprk::rows_overlap(a, a_stride, b, b_stride, width, rows);
+}
+
+int sprh_cache_parse(const spr_cache_batch* b, int n_slots, int max_blocks, int32_t* row0) {
+  sprk::CacheInfo t;
+  const spr_status st = sprk::parse_cache(b, n_slots, max_blocks, "batch", &t, &g_err);
+  if (st == SPR_OK)
+    for (int i = 0; i <= t.n; ++i) row0[i] = t.row0[i];
+  return st;
+}
+
+int sprh_kv4_view(const spr_kv4_view* v, int layer) { return sprk::check_kv4_view(v, layer, "view", &g_err); }
+
+// out = {columns per group, blocks per split, groups, any split}, then item0[0..n], order[n], ncg[n] and cg0[n].
+int sprh_cache_split(const spr_cache_batch* b, int G, int Hkv, int hd, int most, int least, int slots, size_t floats,
+                     int counters, int32_t* out) {
+  sprk::CacheInfo t;
+  const spr_status st = sprk::parse_cache(b, 1 << 20, 1 << 27, "split", &t, &g_err);
+  if (st != SPR_OK) return st;
+  const int cw = sprk::cache_cols_per_group(t, G, most);
+  const sprk::CacheSplit s = sprk::cache_split(t, G, Hkv, hd, cw, least, slots, floats, counters);
+  int32_t* o = out;
+  for (int v : {cw, s.bps, s.groups, static_cast<int>(s.split)}) *o++ = v;
+  for (int i = 0; i <= t.n; ++i) *o++ = s.item0[i];
+  for (int i = 0; i < t.n; ++i) *o++ = s.order[i];
+  for (int i = 0; i < t.n; ++i) *o++ = s.ncg[i];
+  for (int i = 0; i < t.n; ++i) *o++ = s.cg0[i];
+  return SPR_OK;
+}
+
+int sprh_rotary(int dims, int pairs, double base, double factor, double original, double low, double high,
+                double amplitude, spr_rotary* out, int head_dim) {
+  const spr_status st = sprk::make_rotary(dims, pairs, base, factor, original, low, high, amplitude, out, &g_err);
+  return st != SPR_OK ? st : sprk::check_rotary(out, head_dim, "rotary", &g_err);
+}
+int sprh_rotary_check(const spr_rotary* r, int head_dim) { return sprk::check_rotary(r, head_dim, "rotary", &g_err); }
+
+// out = {groups}, then source[n], target[n], len[n], fresh[n] in order and first[0..groups].
+int sprh_fork(const spr_pages* p, int n, const int32_t* source, const int32_t* target, const int32_t* lens,
+              const int32_t* fresh, int32_t* out) {
+  sprk::ForkPlan f;
+  spr_status st = sprk::check_pages(p, "cache_fork", &g_err);
+  if (st == SPR_OK) st = sprk::plan_fork(p, n, source, target, lens, fresh, &f, &g_err);
+  if (st != SPR_OK) return st;
+  *out++ = f.groups;
+  for (const int* a : {f.source, f.target, f.len, f.fresh})
+    for (int i = 0; i < n; ++i) *out++ = a[i];
+  for (int i = 0; i <= f.groups; ++i) *out++ = f.first[i];
+  return SPR_OK;
+}
+
+int sprh_move(const spr_pages* p, int n, const int32_t* src, const int32_t* dst, int32_t* out) {
+  std::vector<std::pair<int32_t, int32_t>> m;
+  spr_status st = sprk::check_pages(p, "cache_move", &g_err);
+  if (st == SPR_OK) st = sprk::plan_move(p, n, src, dst, &m, &g_err);
+  if (st != SPR_OK) return st;
+  for (int i = 0; i < n; ++i) {
+    out[i] = m[i].first;
+    out[n + i] = m[i].second;
+  }
+  return SPR_OK;
 }
 
 void sprh_exp_neg(const double* x, double* y, int n) {

@@ -1,33 +1,18 @@
 // C ABI of the drafted-tree operators: the operator handle, argument checks
 // and the launches of verification and compaction (attention: tree_attn.hip).
 #include <cmath>
-#include <exception>
-#include <new>
 #include <string>
 
+#include "op_handle.h"
 #include "tree_keep_kernels.h"
 #include "tree_launch.h"
 #include "tree_verify_kernels.h"
 
 using namespace sprk;
 
-// Operator workspace: attention partials (or verification's sums), and
-// attention's counters: one per column group and KV head.
-constexpr size_t kTreePartBytes = size_t{32} << 20;
-constexpr int kTreeCounters = kTreeRows * 512;
+static_assert(kOpCounters >= kTreeRows * 512, "one per column group and KV head");
 
-struct spr_tree_ops {
-  char* ws = nullptr;
-  hipStream_t st = nullptr;
-  int dev = 0, n_cu = 1;
-  spr_status sticky = SPR_OK;
-  std::string sticky_msg;
-  int* err_host = nullptr;  // device check flag in mapped pinned host memory
-  int* err_dev = nullptr;
-  ~spr_tree_ops() {
-    if (err_host != nullptr) (void)hipHostFree(err_host);
-  }
-};
+struct spr_tree_ops : OpHandle {};
 
 namespace sprk {
 namespace {
@@ -178,98 +163,14 @@ hipError_t launch_tree_keep(hipStream_t st, const TreeInfo& t, const spr_kv_view
 
 }  // namespace sprk
 
-namespace {
-
 using spr::set_error;
-
-// Makes the handle's device current for the call.
-struct DeviceGuard {
-  int before = -1;
-  hipError_t e;
-  explicit DeviceGuard(int dev) {
-    e = hipGetDevice(&before);
-    if (e == hipSuccess && before != dev) e = hipSetDevice(dev);
-    else before = -1;
-  }
-  ~DeviceGuard() {
-    if (before >= 0) (void)hipSetDevice(before);
-  }
-};
-
-spr_status hip_failed(spr_tree_ops* o, const char* what, hipError_t e) {
-  const std::string msg = std::string(what) + ": " + hipGetErrorString(e);
-  if (o != nullptr) {
-    o->sticky = SPR_ERR_HIP;
-    o->sticky_msg = "an earlier HIP error left the handle unusable; release it (" + msg + ")";
-  }
-  return set_error(SPR_ERR_HIP, msg);
-}
-
-spr_status check_ops(spr_tree_ops* o) {
-  if (o == nullptr) return set_error(SPR_ERR_INVALID_ARG, "operator handle is null");
-  if (o->sticky == SPR_OK) {
-    const int bits = *reinterpret_cast<volatile int*>(o->err_host);
-    if (bits != 0) {
-      o->sticky = SPR_ERR_DEVICE_CHECK;
-      o->sticky_msg = "a device check failed on an earlier call:";
-      if (bits & kErrTokenRange) o->sticky_msg += " a drafted token outside [0, vocab);";
-      if (bits & kErrLogits) o->sticky_msg += " a logits row with a NaN or no finite maximum;";
-      if (bits & kErrBlockId) o->sticky_msg += " a block id outside the pool;";
-      if (bits & kErrPath) o->sticky_msg += " a malformed path of tree nodes;";
-      o->sticky_msg += " release the handle";
-    }
-  }
-  return o->sticky == SPR_OK ? SPR_OK : set_error(o->sticky, o->sticky_msg);
-}
-
-// No exception crosses the ABI (a failed host allocation is the only source).
-template <class F>
-spr_status guarded(F f) {
-  try {
-    spr::clear_error();
-    return f();
-  } catch (const std::exception&) {
-    return SPR_ERR_HIP;
-  }
-}
-
-spr_status bad_arg(const char* msg) { return set_error(SPR_ERR_INVALID_ARG, msg); }
-
-}  // namespace
 
 extern "C" {
 
-size_t spr_tree_ops_workspace_bytes(void) { return kTreePartBytes + kTreeCounters * sizeof(int32_t); }
+size_t spr_tree_ops_workspace_bytes(void) { return kOpWorkspaceBytes; }
 
 spr_status spr_tree_ops_init(void* dev_ws, size_t ws_bytes, void* hip_stream, spr_tree_ops** out) {
-  return guarded([&]() -> spr_status {
-    if (out == nullptr) return bad_arg("tree_ops_init: out must not be null");
-    *out = nullptr;
-    if (dev_ws == nullptr || (reinterpret_cast<uintptr_t>(dev_ws) & 255) != 0)
-      return set_error(SPR_ERR_WORKSPACE, "tree_ops_init: workspace must be a non-null, 256-byte aligned device pointer");
-    if (ws_bytes < spr_tree_ops_workspace_bytes())
-      return set_error(SPR_ERR_WORKSPACE, "tree_ops_init: workspace has " + std::to_string(ws_bytes) + " bytes, " +
-                                              std::to_string(spr_tree_ops_workspace_bytes()) + " needed");
-    spr_tree_ops* o = new (std::nothrow) spr_tree_ops();
-    if (o == nullptr) return SPR_ERR_HIP;
-    o->ws = static_cast<char*>(dev_ws);
-    o->st = static_cast<hipStream_t>(hip_stream);
-    hipError_t e = hipGetDevice(&o->dev);
-    if (e == hipSuccess) e = hipDeviceGetAttribute(&o->n_cu, hipDeviceAttributeMultiprocessorCount, o->dev);
-    if (e == hipSuccess) e = hipHostMalloc(reinterpret_cast<void**>(&o->err_host), sizeof(int), hipHostMallocMapped);
-    if (e == hipSuccess) {
-      *o->err_host = 0;
-      e = hipHostGetDevicePointer(reinterpret_cast<void**>(&o->err_dev), o->err_host, 0);
-    }
-    if (e == hipSuccess) e = hipMemsetAsync(o->ws + kTreePartBytes, 0, kTreeCounters * sizeof(int32_t), o->st);
-    if (e == hipSuccess) e = hipStreamSynchronize(o->st);
-    if (e != hipSuccess) {
-      delete o;
-      return hip_failed(nullptr, "tree_ops_init", e);
-    }
-    *out = o;
-    return SPR_OK;
-  });
+  return init_handle("tree_ops_init", dev_ws, ws_bytes, hip_stream, out);
 }
 
 spr_status spr_tree_ops_set_stream(spr_tree_ops* o, void* hip_stream) {
@@ -288,7 +189,7 @@ spr_status spr_tree_attention(spr_tree_ops* o, const spr_kv_view* kv, int32_t la
                               int32_t n_heads, int32_t io_dtype, const void* q, int64_t q_stride, void* out,
                               int64_t out_stride) {
   return guarded([&]() -> spr_status {
-    spr_status s = check_ops(o);
+    spr_status s = check_handle(o);
     if (s != SPR_OK) return s;
     std::string err;
     if ((s = check_view(kv, layer, "tree_attention", &err)) != SPR_OK) return set_error(s, err);
@@ -321,8 +222,7 @@ spr_status spr_tree_attention(spr_tree_ops* o, const spr_kv_view* kv, int32_t la
     c.qs = q_stride;
     c.out = out;
     c.os = out_stride;
-    c.sc = TreeScratch{reinterpret_cast<float*>(o->ws), kTreePartBytes / sizeof(float),
-                       reinterpret_cast<int32_t*>(o->ws + kTreePartBytes), kTreeCounters};
+    c.sc = TreeScratch{o->part(), kOpPartBytes / sizeof(float), o->counters(), kOpCounters};
     c.err = o->err_dev;
     c.n_cu = o->n_cu;
     const hipError_t e = launch_tree_attention(c);
@@ -335,7 +235,7 @@ spr_status spr_tree_verify(spr_tree_ops* o, const spr_tree_batch* batch, int32_t
                            int64_t draft_stride, const float* temperature, const float* accept, const float* sample,
                            int32_t* emitted, int32_t* path, int32_t* count) {
   return guarded([&]() -> spr_status {
-    spr_status s = check_ops(o);
+    spr_status s = check_handle(o);
     if (s != SPR_OK) return s;
     std::string err;
     TreeInfo t;
@@ -381,7 +281,7 @@ spr_status spr_tree_verify(spr_tree_ops* o, const spr_tree_batch* batch, int32_t
 spr_status spr_tree_keep(spr_tree_ops* o, const spr_kv_view* kv, const spr_tree_batch* batch, const int32_t* path,
                          const int32_t* count) {
   return guarded([&]() -> spr_status {
-    spr_status s = check_ops(o);
+    spr_status s = check_handle(o);
     if (s != SPR_OK) return s;
     std::string err;
     if ((s = check_view(kv, 0, "tree_keep", &err)) != SPR_OK) return set_error(s, err);

@@ -101,14 +101,16 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 struct TreeIoF32 {
   using elem = float;
   static constexpr bool kRaw = false;
-  static __device__ __forceinline__ void store4(const TreeAttnArgs& a, int row, int n0, f32x4_t v) {
+  template <class Args>
+  static __device__ __forceinline__ void store4(const Args& a, int row, int n0, f32x4_t v) {
     *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + row * a.os + n0) = v;
   }
 };
 struct TreeIoBF16 {
   using elem = uint16_t;
   static constexpr bool kRaw = true;
-  static __device__ __forceinline__ void store4(const TreeAttnArgs& a, int row, int n0, f32x4_t v) {
+  template <class Args>
+  static __device__ __forceinline__ void store4(const Args& a, int row, int n0, f32x4_t v) {
     *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + row * a.os + n0) =
         make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
   }
@@ -119,7 +121,8 @@ template <class AP>
 struct TreeIoAct {
   using elem = float;
   static constexpr bool kRaw = false;
-  static __device__ __forceinline__ void store4(const TreeAttnArgs& a, int row, int n0, f32x4_t v) {
+  template <class Args>
+  static __device__ __forceinline__ void store4(const Args& a, int row, int n0, f32x4_t v) {
     store_act4<AP>(static_cast<typename AP::elem*>(a.out), a.rec, row, n0, v[0], v[1], v[2], v[3]);
   }
 };
@@ -357,7 +360,8 @@ constexpr float kRaise = 8.f;
 struct TreeColumn {
   int row, hq;
 };
-__device__ __forceinline__ TreeColumn tree_column(const TreeAttnArgs& a, int row0, int kvh, int c) {
+template <class Args>
+__device__ __forceinline__ TreeColumn tree_column(const Args& a, int row0, int kvh, int c) {
   const int node = c / a.G;
   return TreeColumn{row0 + node, kvh * a.G + c - node * a.G};
 }
@@ -402,7 +406,9 @@ __device__ __forceinline__ void query_parts(const QueryPiece& p, uint4* out) {
 // probabilities, adds them to l, and raises the running maximum first where a
 // score exceeds it by more than kRaise.  (The test runs on the exponents, which
 // are needed anyway.)
-template <int BP, int NE>
+// kLift: the maximum is held so much lower, and the largest exponents lie so
+// much higher (a fp16 probability then has its 11 bits further down).
+template <int BP, int NE, int kLift = 0>
 __device__ __forceinline__ void softmax_step(const f32x4_t* S, float qscale, float& m, float& l, f32x4_t* O, float (*p)[4]) {
   const auto highest = [](const float (*x)[4]) {
     float v = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3]));
@@ -414,7 +420,7 @@ __device__ __forceinline__ void softmax_step(const f32x4_t* S, float qscale, flo
   for (int b = 0; b < BP; ++b)
 #pragma unroll
     for (int r = 0; r < 4; ++r) p[b][r] = fmaf(S[b][r], qscale, -m);
-  if (__ballot(highest(p) > kRaise) != 0) {
+  if (__ballot(highest(p) > kRaise + kLift) != 0) {
 #pragma unroll
     for (int b = 0; b < BP; ++b)
 #pragma unroll
@@ -422,7 +428,7 @@ __device__ __forceinline__ void softmax_step(const f32x4_t* S, float qscale, flo
     float mx = highest(p);
     mx = fmaxf(mx, __shfl_xor(mx, 16));
     mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float up = fmaxf(m, mx);
+    const float up = fmaxf(m, mx - kLift);
     const float alpha = __builtin_amdgcn_exp2f(m - up);
     l *= alpha;
     m = up;
@@ -491,11 +497,11 @@ __device__ __forceinline__ int block_id(const TreeAttnArgs& a, const int32_t* bt
 
 // Counts a split in and, in the one that arrives last, merges all partials of
 // its column group (CW columns): no work-group waits on another.  The
-// caller's partials are stored (agent-coherent).  weights: LDS for kTreeSplits
-// * CW floats that no wave reads or writes any more.
-template <class IO, int HD, int CW>
-__device__ __forceinline__ void merge_splits(const TreeAttnArgs& a, const TreeItem& t, int kvh, const CoherentBuffer& pb,
-                                             int* last, float* weights) {
+// caller's partials are stored (agent-coherent).  weights: LDS for CW floats of
+// every split, which no wave reads or writes any more.
+template <class IO, int HD, int CW, class Args, class Item>
+__device__ __forceinline__ void merge_splits(const Args& a, const Item& t, int kvh, const CoherentBuffer& pb, int* last,
+                                             float* weights) {
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's partial stores are complete
   __syncthreads();
   int32_t* cnt = a.cnt + (t.cg0 + t.cg) * a.Hkv + kvh;

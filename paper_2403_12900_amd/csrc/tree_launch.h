@@ -68,9 +68,3 @@ hipError_t launch_tree_keep(hipStream_t st, const TreeInfo& t, const spr_kv_view
                             const int32_t* count, int* err);
 
 }  // namespace sprk
-
-namespace spr {
-// The calling thread's last error message (spr_last_error).
-spr_status set_error(spr_status s, const std::string& msg);
-void clear_error();
-}  // namespace spr

@@ -23,13 +23,13 @@ def _refuse(msg: str):
     raise SproutError(SPR_ERR_INVALID_ARG, msg)
 
 
-def _int32(x, name):
+def _int32(x, name, what="tree batch"):
     """x as a vector of int32 of its own, each entry with its value."""
     try:
         if isinstance(x, (list, tuple)) and len(x):
             return np.frombuffer(array("i", x), dtype=np.int32)  # whole numbers of any type; OverflowError past 32 bits
     except OverflowError:
-        _refuse(f"tree batch: {name} must be whole numbers of 32 bits")
+        _refuse(f"{what}: {name} must be whole numbers of 32 bits")
     except TypeError:
         pass  # floats, for one
     try:
@@ -42,7 +42,7 @@ def _int32(x, name):
                 return b
     except (TypeError, ValueError, OverflowError):
         pass
-    _refuse(f"tree batch: {name} must be whole numbers of 32 bits")
+    _refuse(f"{what}: {name} must be whole numbers of 32 bits")
 
 
 class KVView:
@@ -97,25 +97,30 @@ class TreeBatch:
         return self._floats(*temperature)
 
 
-class TreeOps:
-    """An operator handle on one device (spr_tree_ops_init), in a torch workspace.
+class OpHandle:
+    """An operator handle of the library on one device, in a torch workspace.
 
     Calls enqueue on the device's current stream; a call on another stream than the last one's first waits for that one.
     Calls that a graph captures wait for nothing and are waited for by nothing (the capture's own order holds, and the
     caller orders replays): eager calls before and after a capture wait for each other.  The handle outlives the graphs
     that hold its calls."""
 
+    _prefix: str  # of the handle's entry points
+
     def __init__(self, device: int = 0):
         self.lib = load_library()
         self.index = device
         self.device = torch.device("cuda", device)
-        self.ws = torch.empty(int(self.lib.spr_tree_ops_workspace_bytes()), dtype=torch.uint8, device=self.device)
+        self.ws = torch.empty(int(self._entry("workspace_bytes")()), dtype=torch.uint8, device=self.device)
         # The last eager call's stream; the handle's own (a captured call's, too), and whether they are one.
         self.stream = torch.cuda.current_stream(self.device)
         self.raw_stream, self.eager = self.stream.cuda_stream, True
         self.h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
-            _check(self.lib.spr_tree_ops_init(self.ws.data_ptr(), self.ws.numel(), self.raw_stream, ctypes.byref(self.h)))
+            _check(self._entry("init")(self.ws.data_ptr(), self.ws.numel(), self.raw_stream, ctypes.byref(self.h)))
+
+    def _entry(self, name):
+        return getattr(self.lib, f"{self._prefix}_{name}")
 
     def _enter(self):
         """Moves the handle to the device's current stream."""
@@ -131,7 +136,7 @@ class TreeOps:
                     self.ws.record_stream(s)
                 self.stream = s
         if raw != self.raw_stream:
-            _check(self.lib.spr_tree_ops_set_stream(self.h, raw))
+            _check(self._entry("set_stream")(self.h, raw))
             self.raw_stream = raw
 
     def _vector(self, what, t, dtype, n):
@@ -139,6 +144,24 @@ class TreeOps:
         if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or t.get_device() != self.index or not t.is_contiguous():
             _refuse(f"{what} must be a contiguous {dtype} tensor of {n} elements on {self.device}")
         return t.data_ptr()
+
+    def close(self):
+        if getattr(self, "h", None) is not None and self.h.value:
+            self._entry("release")(self.h)
+            self.h = ctypes.c_void_p()
+        self.ws = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class TreeOps(OpHandle):
+    """The drafted-tree operators of one device (spr_tree_ops_init)."""
+
+    _prefix = "spr_tree_ops"
 
     def attention(self, kv: KVView, layer: int, batch: TreeBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None):
         """Attention of the trees' nodes (spr_tree_attention): q [rows, heads, head_dim], fp32 or bf16, rows at any stride;
@@ -207,15 +230,3 @@ class TreeOps:
             _refuse(f"tree keep: the cache must be on {self.device}")
         self._enter()
         _check(self.lib.spr_tree_keep(self.h, kv.ref, batch.ref, p_path, p_count))
-
-    def close(self):
-        if getattr(self, "h", None) is not None and self.h.value:
-            self.lib.spr_tree_ops_release(self.h)
-            self.h = ctypes.c_void_p()
-        self.ws = None
-
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass

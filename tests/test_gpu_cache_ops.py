@@ -1,0 +1,742 @@
+"""The 4-bit cache's operators against plain 64-bit implementations (needs an MI355X).
+
+What is stored is exact: codes and scales are compared byte by byte with the oracle's.  A turned key is first computed in 64
+bits on either side; the sides differ by a few 2^-53 of it, and no input here lies so near a border of two codes.
+
+Tolerances of the rest, derived (eps = 2^-24, half a step of fp32; half a step of bf16 is 2^-8):
+  * rotary: angles, sines and products are held in 64 bits (the angle's product rounds at 2^-53 of it, 2^-32 of a radian at
+    2^21 radians), so that an output is off by its one rounding, half a step of the output, and by 2^-30 of the pair's length;
+  * attention, for inputs of unit variance:
+    - stored values and their products with queries are exact in the kernel's parts; a score is a sum whose roundings
+      of random sign add up to less than 4 sqrt(hd) eps |q| |k|, which the scale 1 / sqrt(hd) takes to ds = 4 eps |q| |k|;
+      a change of at most ds in every score changes the weighted mean of v by at most 2 ds max|v|;
+    - exp2 (1 ulp, and its argument's rounding: |s log2 e| <= 2^5 here, 2^5 eps ln 2 < 24 eps), the sums over T positions
+      (4 sqrt(T) eps, on numerator and denominator) and the merges add (26 + 8 sqrt(T)) eps max|v|;
+    - fp32 outputs: probabilities enter their product to 2^-22 of themselves, which moves the mean by at most 2^-22 max|v|;
+    - bf16 outputs: probabilities enter it to 2^-12 of themselves, and the output's own rounding is 2^-8 of it.
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2403_12900_amd import binding
+from paper_2403_12900_amd.binding import SproutError
+from paper_2403_12900_amd.cache import CacheBatch, CacheOps, KV4View, Rotary
+from paper_2403_12900_amd.tree import KVView
+
+from . import cache_ref as ref
+from ._harness import say
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def ops():
+    o = CacheOps()
+    yield o
+    o.close()
+
+
+def rounded(x, dtype):
+    """x as the device gets it, and its value in 64 bits."""
+    t = torch.from_numpy(np.ascontiguousarray(x)).to(dtype)
+    return t.cuda(), t.double().numpy()
+
+
+def columns(t, before=1, behind=2):
+    """The same values as columns of a wider tensor, other values around them."""
+    wide = torch.full((t.shape[0], t.shape[1] + before + behind, t.shape[2]), 7.0, dtype=t.dtype, device=t.device)
+    wide[:, before:before + t.shape[1]] = t
+    return wide[:, before:before + t.shape[1]]
+
+
+# ------------------------------------------------------------------------------------------------ rotary
+
+
+def check_rotary(ops, rng, H, hd, dims, layout, io, positions, scaling=None, strided=False, in_place=False):
+    scaling = scaling or {}
+    say(f"rotary: H {H} hd {hd} dims {dims} {layout} {io} rows {len(positions)} {scaling} strided {strided} in place {in_place}")
+    x, want = rounded(rng.standard_normal((len(positions), H, hd)), io)
+    exact = ref.turn(want, positions, dims, layout, **scaling)
+    if strided:
+        x = columns(x)
+    pos = torch.from_numpy(np.asarray(positions, dtype=np.int32)).cuda()
+    before = x.clone()
+    out = ops.rotary(Rotary(dims, layout=layout, **scaling), x, pos, out=x if in_place else None)
+    torch.cuda.synchronize()
+    assert (out.data_ptr() == x.data_ptr()) == in_place and (in_place or torch.equal(x, before))
+    got = out.double().cpu().numpy()
+    half = EPS if io == F32 else 2.0 ** -8
+    pair = np.abs(want).max() * 1.5 * abs(scaling.get("amplitude", 1.0))
+    assert (np.abs(got - exact) <= half * np.abs(exact) + 2.0 ** -30 * pair).all(), np.abs(got - exact).max()
+    assert np.array_equal(got[..., dims:], want[..., dims:])
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("hd,dims", [(64, 64), (128, 128), (64, 2), (128, 2), (64, 46), (128, 126), (128, 32), (64, 24), (128, 90)])
+def test_rotary_layouts_and_parts(ops, hd, dims, layout, io):
+    rng = np.random.default_rng(hd + dims)
+    for H, positions in ((1, [0]), (3, [0, 1, 17, 4095]), (33, rng.integers(0, 10000, 5))):
+        check_rotary(ops, rng, H, hd, dims, layout, io, positions)
+
+
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+def test_rotary_far_positions_and_long_contexts(ops, layout):
+    rng = np.random.default_rng(9)
+    positions = np.concatenate([rng.integers(0, 2 ** 21, 40), [2 ** 21, 0, 1], -rng.integers(1, 5000, 5)])
+    for scaling in (None, dict(base=500000.0, factor=8.0, original=8192, low=1.0, high=4.0, amplitude=1.2),
+                    dict(base=10000.0, factor=32.0, original=64, low=1.0, high=32.0, amplitude=-0.5)):
+        for hd, dims in ((128, 128), (64, 40)):
+            check_rotary(ops, rng, 5, hd, dims, layout, F32, positions, scaling)
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("hd,dims", [(64, 64), (128, 90), (128, 128), (64, 6)])
+def test_rotary_strides_and_in_place(ops, hd, dims, io):
+    rng = np.random.default_rng(3)
+    for layout in ("half", "pairs"):
+        for strided, in_place in ((True, False), (False, True), (True, True)):
+            check_rotary(ops, rng, 21, hd, dims, layout, io, rng.integers(0, 5000, 37), strided=strided, in_place=in_place)
+
+
+def test_rotary_of_many_rows_and_heads(ops):
+    rng = np.random.default_rng(4)
+    check_rotary(ops, rng, 64, 64, 64, "half", BF16, np.arange(700) + 5)
+    check_rotary(ops, rng, 300, 128, 128, "pairs", F32, [3, 70000])
+
+
+def test_rotary_refusals(ops):
+    x, pos, r = torch.zeros(4, 2, 64, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda"), Rotary(64)
+    wide = torch.zeros(5, 8, 64, device="cuda")
+    for call, what in ((lambda: ops.rotary(Rotary(128), x, pos), "dims"),
+                       (lambda: ops.rotary(r, torch.zeros(4, 2, 96, device="cuda"), pos), "head_dim"),
+                       (lambda: ops.rotary(r, torch.zeros(0, 2, 64, device="cuda"), pos[:0]), "rows"),
+                       (lambda: ops.rotary(r, wide[:4, :2], pos, out=wide[:4, 1:3]), "overlap"),
+                       (lambda: ops.rotary(r, wide[:4, :2], pos, out=wide[1:, :2]), "overlap"),
+                       (lambda: ops.rotary(r, torch.zeros(4 * 131, device="cuda")[:524].view(4, 131)[:, 1:129].view(4, 2, 64), pos), "aligned")):
+        with pytest.raises(SproutError, match=what) as e:
+            call()
+        assert e.value.status == binding.SPR_ERR_INVALID_ARG
+    ops.rotary(r, wide[:4, :2], pos, out=wide[:4, 2:4])
+
+
+# ------------------------------------------------------------------------------------------------ append and read
+
+
+def check_append(ops, rng, Hkv, hd, io, lens, rows, rotary=None, strided=False, k=None, v=None, layers=2, layer=1):
+    """The whole cache, byte by byte, after an append; then what is read back."""
+    n, R = len(lens), sum(rows)
+    slots = [int(s) for s in rng.permutation(n)]
+    positions = [0] * n
+    for i, s in enumerate(slots):
+        positions[s] = lens[i] + rows[i]
+    cache = ref.Cache(rng, layers, Hkv, hd, positions, spare=1)
+    say(f"append: Hkv {Hkv} hd {hd} {io} lens {lens} rows {rows} rotary {rotary} strided {strided}")
+    gain = np.exp(0.7 * rng.standard_normal((Hkv, hd)))
+    k, kx = rounded(gain * rng.standard_normal((R, Hkv, hd)) if k is None else k, io)
+    v, vx = rounded(rng.standard_normal((R, Hkv, hd)) if v is None else v, io)
+    if strided:
+        k, v = columns(k), columns(v, 3, 1)
+    view, batch = cache.device(), CacheBatch(slots, lens, rows)
+    ops.append(view, layer, batch, k, v, rotary=Rotary(**rotary) if rotary else None)
+    gk, gv = ops.read(view, layer, batch, dtype=io)
+    fk, fv = ops.read(view, layer, batch)
+    torch.cuda.synchronize()
+    pos = np.concatenate([length + np.arange(m) for length, m in zip(lens, rows)])
+    if rotary:
+        kx = ref.turn(kx, pos, **rotary)
+    r0 = 0
+    for s, length, m in zip(slots, lens, rows):
+        cache.append(layer, s, length, kx[r0:r0 + m], vx[r0:r0 + m])
+        r0 += m
+    got = view.data.cpu().numpy()
+    assert np.array_equal(got, cache.data), f"{(got != cache.data).sum()} bytes differ"
+    for got, want in ((gk, kx), (gv, vx), (fk, kx), (fv, vx)):
+        np.testing.assert_array_equal(got.double().cpu().numpy(), ref.values(*ref.quantise(want)))
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("Hkv,hd", [(1, 64), (1, 128), (4, 64), (5, 64), (8, 128), (3, 128), (11, 64)])
+def test_append_and_read(ops, Hkv, hd, io):
+    rng = np.random.default_rng(Hkv * 1000 + hd)
+    check_append(ops, rng, Hkv, hd, io, [0, 3, 15, 16, 31, 5, 0], [1, 1, 1, 1, 2, 11, 16])
+    check_append(ops, rng, Hkv, hd, io, [7, 0], [50, 33], strided=True)
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("hd,dims", [(64, 64), (128, 128), (64, 2), (128, 126), (128, 32), (64, 46)])
+def test_append_turns_keys(ops, hd, dims, layout, io):
+    rng = np.random.default_rng(hd * 7 + dims)
+    check_append(ops, rng, 4, hd, io, [0, 30, 4000, 9], [1, 5, 20, 40], rotary=dict(dims=dims, layout=layout))
+    check_append(ops, rng, 2, hd, io, [100], [3], strided=True,
+                 rotary=dict(dims=dims, layout=layout, base=5e5, factor=8.0, original=512, low=1.0, high=32.0, amplitude=1.1))
+
+
+def test_append_many_requests_and_long_prompts(ops):
+    rng = np.random.default_rng(8)
+    check_append(ops, rng, 2, 64, BF16, [int(x) for x in rng.integers(0, 60, 128)], [1] * 128, rotary=dict(dims=64), layers=1, layer=0)
+    check_append(ops, rng, 40, 64, F32, [5], [300], layers=1, layer=0)
+    check_append(ops, rng, 8, 128, BF16, [0, 17, 300], [200, 1, 90], rotary=dict(dims=128, layout="pairs"), layers=1, layer=0)
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+def test_append_ties_extremes_and_odd_values(ops, io):
+    """Ties at every scale, borders of scales, zeros of both signs, the largest and smallest numbers, infinities and NaN."""
+    rng = np.random.default_rng(2)
+    x = np.zeros((40, 2, 64))
+    ties = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.5])
+    for r in range(24):  # the 7 pins the scale; the border itself, and just above it
+        x[r] = rng.choice(ties, (2, 64)) * rng.choice([-1, 1], (2, 64)) * 2.0 ** (5 * r - 60)
+        x[r, :, ::32] = 7 * 2.0 ** (5 * r - 60) * (1 + (2.0 ** -7 if r % 2 else 0))
+    x[24], x[25], x[26] = -0.0, 0.0, 1e-44
+    x[27], x[28], x[29] = 3.3e38, 2.0 ** -122, 2.0 ** -121 * rng.choice(ties, (2, 64))
+    x[30, 0, 5], x[31, 1, 40], x[32, 0, 63] = np.inf, -np.inf, np.nan
+    x[33] = np.nan
+    x[34:] = rng.standard_normal((6, 2, 64)) * np.exp(rng.normal(0, 30, (6, 2, 64)))
+    check_append(ops, rng, 2, 64, io, [3], [40], k=x, v=x[::-1])
+
+
+def test_append_of_odd_values_that_are_turned(ops):
+    """An infinity or NaN spoils its pair and so both their groups; huge ones stay finite."""
+    rng = np.random.default_rng(6)
+    x = rng.standard_normal((6, 1, 64))
+    x[1, 0, 3], x[2, 0, 40] = np.inf, np.nan
+    x[3] *= 2.9e38 / np.abs(x[3]).max()
+    with np.errstate(invalid="ignore"):
+        check_append(ops, rng, 1, 64, F32, [77], [6], k=x, rotary=dict(dims=64))
+
+
+def test_append_and_read_refusals(ops):
+    rng = np.random.default_rng(1)
+    view = ref.Cache(rng, 1, 2, 64, [40]).device()
+    b = CacheBatch([0], [5], [3])
+    k = torch.zeros(3, 2, 64, device="cuda")
+    odd = torch.zeros(3 * 131, device="cuda").view(3, 131)[:, 1:129].view(3, 2, 64)
+    before = view.data.clone()
+    for call, what in ((lambda: ops.append(view, 1, b, k, k), "layer"), (lambda: ops.append(view, 0, b, k, odd), "aligned"),
+                       (lambda: ops.append(view, 0, CacheBatch([0], [46], [3]), k, k), "block-table row"),
+                       (lambda: ops.append(view, 0, CacheBatch([1], [5], [3]), k, k), "slot"),
+                       (lambda: ops.append(view, 0, b, k, k, rotary=Rotary(128)), "dims"),
+                       (lambda: ops.read(view, -1, b), "layer"), (lambda: ops.read(view, 0, CacheBatch([0], [0], [49])), "block-table row"),
+                       (lambda: ops.attention(view, 0, b, torch.zeros(3, 3, 64, device="cuda")), "n_heads"),
+                       (lambda: ops.attention(view, 0, b, torch.zeros(3, 34, 64, device="cuda")), "n_heads"),
+                       (lambda: ops.attention(view, 0, b, k, out=k), "overlap"), (lambda: ops.attention(view, 2, b, k), "layer"),
+                       (lambda: ops.attention(view, 0, b, odd), "aligned")):
+        with pytest.raises(SproutError, match=what) as e:
+            call()
+        assert e.value.status == binding.SPR_ERR_INVALID_ARG
+    with pytest.raises(SproutError, match="overlap"):
+        binding._check(ops.lib.spr_cache_read(ops.h, view.ref, 0, b.ref, 0, k.data_ptr(), 128, k.data_ptr() + 256, 128))
+    assert torch.equal(view.data, before)
+
+
+def test_a_block_outside_the_pool_is_not_written():
+    rng = np.random.default_rng(12)
+    for bad in (-1, 4, 2 ** 31 - 1):
+        for call in ("append", "read", "attention"):
+            o = CacheOps()
+            cache = ref.Cache(rng, 1, 2, 64, [20, 20], extra_blocks=0)
+            cache.table[0, 1] = bad
+            view, b = cache.device(), CacheBatch([0, 1], [14, 14], [4, 4])
+            k, kx = rounded(rng.standard_normal((8, 2, 64)), F32)
+            if call == "append":
+                o.append(view, 0, b, k, k)
+            elif call == "read":
+                o.read(view, 0, b)
+            else:
+                o.attention(view, 0, b, k)
+            torch.cuda.synchronize()
+            if call == "append":  # all other rows are
+                cache.table[0, 1] = cache.table[0, 0]
+                want = cache.data.copy()
+                cache.append(0, 0, 14, kx[:2], kx[:2])
+                cache.append(0, 1, 14, kx[4:], kx[4:])
+                assert np.array_equal(view.data.cpu().numpy(), cache.data) and not np.array_equal(want, cache.data)
+            with pytest.raises(SproutError, match="block id") as e:
+                o.read(view, 0, CacheBatch([1], [0], [1]))
+            assert e.value.status == binding.SPR_ERR_DEVICE_CHECK
+            o.close()
+
+
+# ------------------------------------------------------------------------------------------------ attention
+
+
+def tolerance(cache, layer, slots, lens, rows, q, io, want):
+    kn = vm = 0.0
+    for s, length, n in zip(slots, lens, rows):
+        k, v = cache.rows(layer, s, length + n)
+        kn = max(kn, np.sqrt((np.nan_to_num(k) ** 2).sum(-1)).max())
+        vm = max(vm, np.abs(np.nan_to_num(v)).max())
+    qn, T = np.sqrt((np.nan_to_num(q) ** 2).sum(-1)).max(), max(a + b for a, b in zip(lens, rows))
+    tol = (2 * 4 * EPS * qn * kn + (26 + 8 * np.sqrt(T)) * EPS) * vm
+    if io == F32:
+        return tol + 2.0 ** -22 * vm
+    return tol + 2 * 2.0 ** -12 * vm + 2.0 ** -8 * np.abs(want)
+
+
+def filled(rng, layers, layer, Hkv, hd, slots, lens, rows, spare=1, extra_blocks=2):
+    """A cache of random bytes (scale bytes of all kinds among them) that holds the requests' positions in one layer."""
+    positions = [0] * len(slots)
+    for i, s in enumerate(slots):
+        positions[s] = lens[i] + rows[i]
+    cache = ref.Cache(rng, layers, Hkv, hd, positions, spare=spare, extra_blocks=extra_blocks)
+    for s, p in enumerate(positions):
+        blocks = cache.table[s, :(p + 15) // 16]
+        x = rng.standard_normal((2, len(blocks), Hkv, 16, hd))
+        (kc, ks), (vc, vs) = ref.quantise(x[0]), ref.quantise(x[1])
+        ko, vo, kso, vso, khi, vhi = ref.offsets(hd)
+        for j, b in enumerate(blocks):
+            n = min(16, p - 16 * j)
+            for h in range(Hkv):
+                tile = cache.data[layer, b, h]
+                for at, high, c in ((ko, khi, kc), (vo, vhi, vc)):
+                    byte = np.zeros(17 * hd, np.int64)
+                    np.add.at(byte, at[:n], c[j, h, :n].astype(np.int64) << np.where(high[:n], 4, 0))
+                    tile[np.unique(at[:n])] = byte[np.unique(at[:n])]
+                tile[kso[:n]] = np.repeat(ks[j, h, :n], 32, -1)
+                tile[vso[:n]] = np.repeat(vs[j, h, :n], 32, -1)
+    return cache
+
+
+def check_attention(ops, rng, H, Hkv, hd, io, lens, rows, layers=1, layer=0, strided=False, tag="", slots=None):
+    slots = [int(s) for s in rng.permutation(len(lens))] if slots is None else slots
+    cache = filled(rng, layers, layer, Hkv, hd, slots, lens, rows)
+    q, qx = rounded(rng.standard_normal((sum(rows), H, hd)), io)
+    say(f"attention {tag}: H {H}/{Hkv} hd {hd} {io} lens {lens[:9]} rows {rows[:9]} strided {strided}")
+    if strided:
+        q = columns(q)
+    out = ops.attention(cache.device(), layer, CacheBatch(slots, lens, rows), q)
+    torch.cuda.synchronize()
+    want = ref.attention(cache, layer, slots, lens, rows, qx)
+    got = out.double().cpu().numpy()
+    tol = tolerance(cache, layer, slots, lens, rows, qx, io, want)
+    assert np.isfinite(got).all()
+    worst = (np.abs(got - want) / tol).max()
+    assert worst <= 1, f"{worst} of the tolerance, max error {np.abs(got - want).max():.3e}"
+
+
+SHAPES = [(4, 4, 64), (8, 2, 128), (65, 5, 64), (3, 3, 128), (16, 1, 128), (16, 1, 64)]
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("H,Hkv,hd", SHAPES)
+def test_attention_shapes_and_types(ops, H, Hkv, hd, io):
+    rng = np.random.default_rng(H * 100 + hd)
+    check_attention(ops, rng, H, Hkv, hd, io, [0, 1, 15, 16, 17, 130, 47], [1] * 7)
+    check_attention(ops, rng, H, Hkv, hd, io, [0, 3, 14, 40], [2, 1, 5, 3], strided=True)
+    check_attention(ops, rng, H, Hkv, hd, io, [0, 37, 90], [33, 1, 20])
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("lens,rows", [([0], [1]), ([0], [2]), ([15], [1]), ([15], [2]), ([16], [1]), ([31], [16]), ([32], [33]),
+                                       ([0], [200]), ([63, 64, 65], [16, 17, 33]), ([0, 500], [130, 1]), ([40] * 128, [1] * 128),
+                                       ([3000], [1]), ([9000, 3], [2, 1]), ([2000, 0], [70, 260])])
+def test_attention_lengths_and_splits(ops, io, lens, rows):
+    """One position to many KV splits; single tokens, chunks of all sizes; the largest batch; a two-layer cache's second layer."""
+    rng = np.random.default_rng(7)
+    check_attention(ops, rng, 4, 2, 64, io, lens, rows, layers=2, layer=1)
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("H,Hkv,hd,rows", [(16, 2, 128, 64), (16, 2, 64, 70), (32, 2, 128, 5), (4, 4, 128, 33), (8, 8, 64, 20), (2, 2, 128, 150)])
+def test_attention_of_chunks_over_long_contexts(ops, H, Hkv, hd, rows, io):
+    """Several column groups and KV splits at once, whole steps of either parity, beside a short request."""
+    rng = np.random.default_rng(hd + rows)
+    for lens in ([1700, 5], [1683, 40]):
+        check_attention(ops, rng, H, Hkv, hd, io, lens, [rows, 3], tag="chunks")
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+def test_attention_scores_of_all_sizes(ops, io):
+    """A few positions take nearly all weight, early or late ones: maxima that rise and fall; and values of many scales."""
+    rng = np.random.default_rng(21)
+    for rows, at in ((1, (5, 1900)), (40, (0, 700)), (130, (1000, 1990))):
+        lens, slots = [2000], [0]
+        cache = filled(rng, 1, 0, 1, 128, slots, lens, [rows])
+        q, qx = rounded(0.2 * rng.standard_normal((rows, 2, 128)), io)
+        k = 0.2 * rng.standard_normal((2000 + rows, 1, 128))
+        v = rng.standard_normal((2000 + rows, 1, 128)) * 2.0 ** rng.integers(-18, 15, (2000 + rows, 1, 1))
+        for p in at:
+            k[p] = qx[0, 0] * 60
+        cache.append(0, 0, 0, k, v)
+        want = ref.attention(cache, 0, slots, lens, [rows], qx)
+        got = ops.attention(cache.device(), 0, CacheBatch(slots, lens, [rows]), q).double().cpu().numpy()
+        tol = tolerance(cache, 0, slots, lens, [rows], qx, io, want)
+        assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("scale", [2.0 ** -60, 2.0 ** -20, 2.0 ** 20, 2.0 ** 90])
+def test_attention_of_values_far_from_one(ops, io, scale):
+    """Values of any scale give outputs of it, to the same relative tolerance."""
+    rng = np.random.default_rng(30)
+    for rows in (1, 90):
+        cache = filled(rng, 1, 0, 2, 128, [0], [300], [rows])
+        q, qx = rounded(rng.standard_normal((rows, 4, 128)), io)
+        v = rng.standard_normal((300 + rows, 2, 128))
+        k = rng.standard_normal((300 + rows, 2, 128))
+        cache.append(0, 0, 0, k, v)
+        want = ref.attention(cache, 0, [0], [300], [rows], qx)
+        tol = tolerance(cache, 0, [0], [300], [rows], qx, io, want)
+        cache.append(0, 0, 0, k, v * scale)
+        got = ops.attention(cache.device(), 0, CacheBatch([0], [300], [rows]), q).double().cpu().numpy() / scale
+        assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("hd,rows", [(64, 5), (128, 5), (64, 50), (128, 50), (128, 200)])
+def test_attention_nan_reaches_the_rows_that_see_it(ops, hd, rows, io):
+    """A NaN group of a value reaches its 32 dimensions of the rows that see its position, one of a key reaches those rows
+    whole, and no other row changes."""
+    rng = np.random.default_rng(hd + rows)
+    length, H, Hkv = 37, 4, 2
+    q, qx = rounded(rng.standard_normal((rows, H, hd)), io)
+    for pos, key in ((length + rows // 2, False), (length + rows // 2, True), (length - 2, False), (length + rows - 1, True),
+                     (length + 1, False)):
+        cache = filled(rng, 1, 0, Hkv, hd, [0], [length], [rows])
+        want = ref.attention(cache, 0, [0], [length], [rows], qx)
+        tol = np.broadcast_to(tolerance(cache, 0, [0], [length], [rows], qx, io, want), want.shape)
+        _, _, kso, vso, _, _ = ref.offsets(hd)
+        cache.data[0, cache.table[0, pos // 16], 1, (kso if key else vso)[pos % 16, 32]] = 255  # KV head 1, second group
+        got = ops.attention(cache.device(), 0, CacheBatch([0], [length], [rows]), q).double().cpu().numpy()
+        hit = np.zeros(want.shape, bool)
+        first = max(0, pos - length)
+        hit[first:, 2:, slice(None) if key else slice(32, 64)] = True
+        assert np.isnan(got[hit]).all(), (pos, key)
+        assert (np.abs(got - want)[~hit] <= tol[~hit]).all(), (pos, key)
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+def test_attention_queries_that_are_no_numbers(ops, io):
+    """They spoil their own row and head."""
+    rng = np.random.default_rng(2)
+    for rows in (3, 60):
+        cache = filled(rng, 1, 0, 2, 128, [0], [40], [rows])
+        q, qx = rounded(rng.standard_normal((rows, 4, 128)), io)
+        want = ref.attention(cache, 0, [0], [40], [rows], qx)
+        tol = np.broadcast_to(tolerance(cache, 0, [0], [40], [rows], qx, io, want), want.shape)
+        q[1, 2, 77], q[rows - 1, 0, 3] = float("nan"), float("inf")
+        got = ops.attention(cache.device(), 0, CacheBatch([0], [40], [rows]), q).double().cpu().numpy()
+        bad = np.zeros(want.shape, bool)
+        bad[1, 2] = bad[rows - 1, 0] = True
+        assert np.isnan(got[bad]).all() and (np.abs(got - want)[~bad] <= tol[~bad]).all()
+
+
+@pytest.mark.parametrize("rows", [1, 70])
+def test_attention_far_into_a_large_pool(ops, rows):
+    """Blocks behind byte 2^32 of the pool and of the layer."""
+    rng = np.random.default_rng(5)
+    small = filled(rng, 1, 0, 8, 128, [0], [200], [rows])
+    q, qx = rounded(rng.standard_normal((rows, 8, 128)), BF16)
+    want = ref.attention(small, 0, [0], [200], [rows], qx)
+    n = small.data.shape[1]
+    blocks = 2 ** 32 // (8 * 17 * 128) + 100
+    data = torch.zeros(2, blocks, 8, 17 * 128, dtype=torch.uint8, device="cuda")
+    data[1, blocks - n:] = torch.from_numpy(small.data[0]).cuda()
+    view = KV4View(data, torch.from_numpy(small.table + blocks - n).cuda())
+    got = ops.attention(view, 1, CacheBatch([0], [200], [rows]), q).double().cpu().numpy()
+    assert (np.abs(got - want) <= tolerance(small, 0, [0], [200], [rows], qx, BF16, want)).all()
+    x, xx = rounded(rng.standard_normal((1, 8, 128)), F32)
+    b = CacheBatch([0], [199], [1])
+    ops.append(view, 1, b, x, x)
+    assert np.array_equal(ops.read(view, 1, b)[1].double().cpu().numpy(), ref.values(*ref.quantise(xx)))
+    last = blocks - 1
+    ops.move(view, [last - 5], [3])
+    assert torch.equal(data[:, 3], data[:, last - 5])
+
+
+# ------------------------------------------------------------------------------------------------ pages
+
+
+def any_cache(rng, kind, layers, blocks, Hkv, hd, slots, mb):
+    table = torch.from_numpy(rng.integers(0, blocks, (slots, mb)).astype(np.int32)).cuda()
+    if kind == "mx4":
+        return KV4View(torch.from_numpy(rng.integers(0, 256, (layers, blocks, Hkv, 17 * hd), dtype=np.uint8)).cuda(), table)
+    k, v = (torch.from_numpy(rng.standard_normal((layers, blocks, Hkv, 16 * hd))).to(kind).cuda() for _ in range(2))
+    return KVView(k, v, table)
+
+
+def pools(view):
+    return [view.data] if isinstance(view, KV4View) else [view.k, view.v]
+
+
+@pytest.mark.parametrize("kind", ["mx4", F32, BF16])
+@pytest.mark.parametrize("layers,Hkv,hd", [(1, 1, 64), (3, 5, 64), (2, 8, 128), (2, 40, 128)])
+def test_fork(ops, kind, layers, Hkv, hd):
+    rng = np.random.default_rng(Hkv + hd)
+    for trial in range(6):
+        slots, mb, blocks, n = 12, 6, 90, int(rng.integers(1, 9))
+        view = any_cache(rng, kind, layers, blocks, Hkv, hd, slots, mb)
+        ids = rng.permutation(blocks)
+        at = rng.permutation(slots)
+        target, sources = at[:n], at[9:]
+        source = rng.choice(sources[:1 + trial % 3], n)
+        table = view.block_table.cpu().numpy()
+        table[sources] = ids[20:20 + 3 * mb].reshape(3, mb)
+        view.block_table.copy_(torch.from_numpy(table))
+        lens = rng.choice([0, 1, 15, 16, 17, 33, 80, 95, 96], n)
+        fresh = np.where(lens % 16 == 0, -5, ids[:n])
+        before = [p.clone() for p in pools(view)]
+        say(f"fork: {kind} layers {layers} Hkv {Hkv} hd {hd} source {source} lens {lens}")
+        ops.fork(view, source, target, lens, fresh)
+        torch.cuda.synchronize()
+        for s, t, x, f in zip(source, target, lens, fresh):
+            table[t, :x // 16] = table[s, :x // 16]
+            if x % 16:
+                for p in before:
+                    p[:, int(f)] = p[:, int(table[s, x // 16])]
+                table[t, x // 16] = f
+        assert np.array_equal(view.block_table.cpu().numpy(), table)
+        assert all(torch.equal(a, b) for a, b in zip(pools(view), before))
+
+
+def test_fork_of_the_largest_batch(ops):
+    rng = np.random.default_rng(3)
+    view = any_cache(rng, "mx4", 2, 400, 4, 64, 140, 4)
+    table = view.block_table.cpu().numpy()
+    table[:3] = np.arange(12).reshape(3, 4)
+    view.block_table.copy_(torch.from_numpy(table))
+    before = view.data.clone()
+    source, fresh = np.arange(128) % 3, 20 + rng.permutation(128)
+    ops.fork(view, source, 5 + np.arange(128), [39] * 128, fresh)
+    for i in range(128):
+        table[5 + i, :2] = table[source[i], :2]
+        table[5 + i, 2] = fresh[i]
+        before[:, int(fresh[i])] = before[:, int(table[source[i], 2])]
+    assert np.array_equal(view.block_table.cpu().numpy(), table) and torch.equal(view.data, before)
+
+
+@pytest.mark.parametrize("what", ["outside", "negative", "fresh"])
+def test_fork_of_a_source_that_is_not_there(what):
+    """Nothing is copied, and the handle's next call says so."""
+    o = CacheOps()
+    rng = np.random.default_rng(3)
+    view = any_cache(rng, BF16, 2, 20, 2, 64, 3, 2)
+    view.block_table[0] = torch.tensor([1, {"outside": 20, "negative": -3, "fresh": 7}[what]], dtype=torch.int32)
+    before = [p.clone() for p in pools(view)]
+    o.fork(view, [0, 0], [1, 2], [20, 5], [7, 8])
+    torch.cuda.synchronize()
+    for p, b in zip(pools(view), before):
+        b[:, 8] = b[:, 1]
+        assert torch.equal(p, b)
+    with pytest.raises(SproutError, match="fresh block" if what == "fresh" else "block id") as e:
+        o.move(view, [1], [2])
+    assert e.value.status == binding.SPR_ERR_DEVICE_CHECK
+    o.close()
+
+
+@pytest.mark.parametrize("kind", ["mx4", F32, BF16])
+@pytest.mark.parametrize("layers,Hkv,hd,blocks,n,slots,mb", [(1, 1, 64, 2, 1, 1, 1), (3, 5, 64, 60, 20, 7, 9), (2, 8, 128, 40, 13, 300, 21),
+                                                          (1, 1, 64, 1500, 750, 40, 60)])
+def test_move(ops, kind, layers, Hkv, hd, blocks, n, slots, mb):
+    """One pair to more than a launch takes; tables of one entry to many, with blocks that several entries share."""
+    rng = np.random.default_rng(n)
+    view = any_cache(rng, kind, layers, blocks, Hkv, hd, slots, mb)
+    ids = rng.permutation(blocks)
+    src, dst = ids[:n], ids[n:2 * n]
+    table, before = view.block_table.cpu().numpy(), [p.clone() for p in pools(view)]
+    say(f"move: {kind} layers {layers} Hkv {Hkv} hd {hd} blocks {blocks} moved {n}")
+    ops.move(view, src, dst)
+    torch.cuda.synchronize()
+    now = np.arange(blocks)
+    now[src] = dst
+    for p, b in zip(pools(view), before):
+        b[:, torch.from_numpy(dst).cuda()] = b[:, torch.from_numpy(src).cuda()]
+        assert torch.equal(p, b)
+    assert np.array_equal(view.block_table.cpu().numpy(), now[table])
+
+
+def test_pages_refusals(ops):
+    rng = np.random.default_rng(3)
+    view = any_cache(rng, "mx4", 1, 20, 2, 64, 3, 2)
+    before = (view.data.clone(), view.block_table.clone())
+    for call, what in ((lambda: ops.fork(view, [0], [0], [5], [3]), "also a source"), (lambda: ops.fork(view, [0], [1], [33], [3]), "lens"),
+                       (lambda: ops.fork(view, [], [], [], []), "n must"), (lambda: ops.move(view, [], []), "n must"),
+                       (lambda: ops.move(view, [3], [20]), "out of range"), (lambda: ops.move(view, [3, 4], [4, 5]), "also a src")):
+        with pytest.raises(SproutError, match=what) as e:
+            call()
+        assert e.value.status == binding.SPR_ERR_INVALID_ARG
+    assert torch.equal(view.data, before[0]) and torch.equal(view.block_table, before[1])
+
+
+# ------------------------------------------------------------------------------------------------ together
+
+
+class Serving:
+    """Requests of a small model's one layer over a 4-bit cache on the device, with the plain forms beside it."""
+
+    def __init__(self, rng, io, H=4, Hkv=2, hd=64, blocks=80, slots=8, mb=8):
+        self.rng, self.io, self.H, self.Hkv, self.hd = rng, io, H, Hkv, hd
+        self.cache = ref.Cache(rng, 1, Hkv, hd, [0] * slots, extra_blocks=blocks)
+        self.cache.mb = mb
+        self.cache.table = np.zeros((slots, mb), np.int32)
+        self.free = self.cache.free
+        self.view = self.cache.device()
+        self.turn = dict(dims=48, layout="pairs", base=5e5, factor=4.0, original=64, low=1.0, high=32.0, amplitude=1.1)
+        self.rotary = Rotary(**self.turn)
+        self.length = [0] * slots
+
+    def sync(self):
+        self.view.block_table.copy_(torch.from_numpy(self.cache.table))
+
+    def step(self, ops, slots, rows):
+        """A projection's rows through rotary, append and attention; the same beside it; returns both outputs."""
+        lens = [self.length[s] for s in slots]
+        for s, n in zip(slots, rows):
+            for b in range((self.length[s] + 15) // 16, (self.length[s] + n + 15) // 16):
+                self.cache.table[s, b] = self.free.pop()
+        self.sync()
+        x, xx = rounded(self.rng.standard_normal((sum(rows), self.H + 2 * self.Hkv, self.hd)), self.io)
+        pos = np.concatenate([length + np.arange(n) for length, n in zip(lens, rows)])
+        H, e = self.H, self.H + self.Hkv
+        batch = CacheBatch(slots, lens, rows)
+        p = torch.from_numpy(pos.astype(np.int32)).cuda()
+        ops.append(self.view, 0, batch, x[:, H:e], x[:, e:], rotary=self.rotary)
+        q = ops.rotary(self.rotary, x[:, :H], p)
+        out = ops.attention(self.view, 0, batch, q)
+        r0 = 0
+        for s, length, n in zip(slots, lens, rows):
+            self.cache.append(0, s, length, ref.turn(xx[r0:r0 + n, H:e], pos[r0:r0 + n], **self.turn), xx[r0:r0 + n, e:])
+            self.length[s] += n
+            r0 += n
+        qx = q.double().cpu().numpy()
+        want = ref.attention(self.cache, 0, slots, lens, rows, qx)
+        tol = tolerance(self.cache, 0, slots, lens, rows, qx, self.io, want)
+        assert (np.abs(out.double().cpu().numpy() - want) <= tol).all()
+        return out
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+def test_a_serving_loop(ops, io):
+    """Prompts, decode steps, a prompt's continuations by forking, requests that leave, compaction; the cache byte by byte."""
+    rng = np.random.default_rng(40)
+    s = Serving(rng, io)
+    s.step(ops, [0, 3], [37, 16])                 # two prompts
+    s.step(ops, [3, 0], [1, 1])
+    fresh = [s.free.pop() for _ in range(2)]      # 38 positions: two full blocks and six positions; and 32 of them alone
+    ops.fork(s.view, [0, 0, 0], [1, 2, 5], [38, 38, 32], fresh + [-1])
+    for t, f in ((1, fresh[0]), (2, fresh[1])):
+        s.cache.table[t, :2] = s.cache.table[0, :2]
+        s.cache.table[t, 2] = f
+        s.cache.data[:, f] = s.cache.data[:, s.cache.table[0, 2]]
+        s.length[t] = 38
+    s.cache.table[5, :2] = s.cache.table[0, :2]
+    s.length[5] = 32
+    assert np.array_equal(s.view.block_table.cpu().numpy(), s.cache.table)
+    for _ in range(12):                           # each goes its own way
+        s.step(ops, [0, 1, 2, 5, 3], [1] * 5)
+    s.step(ops, [1], [40])                        # a second turn's prompt
+    s.length[2] = 0                               # request 2 has left; its blocks but the shared ones are free
+    used = sorted({int(b) for t in (0, 1, 3, 5) for b in s.cache.table[t, :(s.length[t] + 15) // 16]})
+    holes = [b for b in range(len(used)) if b not in used]
+    src = [b for b in used if b >= len(used)]
+    ops.move(s.view, src, holes)
+    now = np.arange(s.cache.data.shape[1])
+    now[src] = holes
+    s.cache.data[:, holes] = s.cache.data[:, src]
+    s.cache.table = now[s.cache.table].astype(np.int32)
+    s.free[:] = [b for b in range(s.cache.data.shape[1]) if b >= len(used)]
+    assert np.array_equal(s.view.block_table.cpu().numpy(), s.cache.table)
+    for rows in (1, 3):
+        s.step(ops, [5, 0, 1, 3], [rows] * 4)
+    assert np.array_equal(s.view.data.cpu().numpy(), s.cache.data)
+
+
+def test_a_captured_step_replays(ops):
+    """A graph of append, rotary, attention and read with eager work between its replays, on the same handle."""
+    rng = np.random.default_rng(41)
+    io, H, Hkv, hd = BF16, 8, 2, 128
+    for lens, rows in (([700, 20], [1, 1]), ([300, 64], [40, 9])):
+        cache = filled(rng, 1, 0, Hkv, hd, [0, 1], lens, rows)
+        view, batch, r = cache.device(), CacheBatch([0, 1], lens, rows), Rotary(128)
+        x = torch.zeros(sum(rows), H + 2 * Hkv, hd, dtype=io, device="cuda")
+        pos = torch.from_numpy(np.concatenate([a + np.arange(n) for a, n in zip(lens, rows)]).astype(np.int32)).cuda()
+
+        def step():
+            ops.append(view, 0, batch, x[:, H:H + Hkv], x[:, H + Hkv:], rotary=r)
+            return ops.attention(view, 0, batch, ops.rotary(r, x[:, :H], pos)), ops.read(view, 0, batch, dtype=io)
+
+        step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got, (gk, gv) = step()
+        for trial in range(4):
+            x.copy_(torch.from_numpy(rng.standard_normal(tuple(x.shape))).to(io))
+            want, (wk, wv) = step()
+            want, wk, wv = want.clone(), wk.clone(), wv.clone()
+            view.data[..., -1] ^= 0  # eager work of the program's own
+            x2 = x.clone()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(got, want) and torch.equal(gk, wk) and torch.equal(gv, wv) and torch.equal(x, x2)
+
+
+def test_captured_pages_replay(ops):
+    """A captured fork and move keep the numbers they were given."""
+    rng = np.random.default_rng(42)
+    view = any_cache(rng, "mx4", 2, 30, 2, 64, 4, 3)
+    ops.fork(view, [0], [1], [20], [9])
+    view.block_table[0] = torch.tensor([4, 5, 6], dtype=torch.int32)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    fresh = np.array([7, 8], dtype=np.int32)
+    with torch.cuda.graph(graph):
+        ops.fork(view, [0, 0], [1, 2], [20, 37], fresh)
+        ops.move(view, [5], [2])
+    fresh[:] = 0
+    for trial in range(3):
+        view.block_table[0] = torch.tensor([4, 5, 6], dtype=torch.int32)
+        view.data.copy_(torch.from_numpy(rng.integers(0, 256, tuple(view.data.shape), dtype=np.uint8)))
+        want = view.data.clone()
+        want[:, 7], want[:, 8], want[:, 2] = want[:, 5], want[:, 6], want[:, 5]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(view.data, want)
+        assert view.block_table[:3].tolist()[0] == [4, 2, 6] and view.block_table[1, :2].tolist() == [4, 7]
+        assert view.block_table[2].tolist() == [4, 2, 8]
+
+
+def test_streams_take_turns_and_handles_run_beside_each_other():
+    """Calls of one handle on two streams in turn; two handles on two streams at once: the results of calls alone."""
+    rng = np.random.default_rng(43)
+    a, b = CacheOps(), CacheOps()
+    lens, rows = [3000, 100, 7], [1, 2, 1]
+    cache = filled(rng, 1, 0, 2, 128, [0, 1, 2], lens, rows)
+    view, batch = cache.device(), CacheBatch([0, 1, 2], lens, rows)
+    q = [torch.from_numpy(rng.standard_normal((4, 16, 128))).float().cuda() for _ in range(6)]
+    want = [a.attention(view, 0, batch, x) for x in q]
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for i, x in enumerate(q):
+        with torch.cuda.stream((s1, s2)[i % 2]):
+            got.append(a.attention(view, 0, batch, x))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    got = []
+    for i, x in enumerate(q):
+        with torch.cuda.stream((s1, s2)[i % 2]):
+            got.append((a, b)[i % 2].attention(view, 0, batch, x))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    a.close(), b.close()
+
+
+def test_results_do_not_change_from_call_to_call(ops):
+    """Splits are merged in a fixed order, whichever arrives last."""
+    rng = np.random.default_rng(44)
+    for lens, rows, io in (([9000, 300], [1, 1], F32), ([4000], [70], BF16)):
+        cache = filled(rng, 1, 0, 2, 64, list(range(len(lens))), lens, rows)
+        view, batch = cache.device(), CacheBatch(list(range(len(lens))), lens, rows)
+        q = torch.from_numpy(rng.standard_normal((sum(rows), 8, 64))).to(io).cuda()
+        want = ops.attention(view, 0, batch, q)
+        for _ in range(5):
+            assert torch.equal(ops.attention(view, 0, batch, q), want)
