@@ -6,6 +6,7 @@
 
 #include "cache_rule.h"
 #include "device_common.h"
+#include "op_handle.h"
 
 namespace sprk {
 

@@ -226,7 +226,6 @@ constexpr int kErrTokenRange = 1;  // a fed token id outside [0, V)
 constexpr int kErrLogits = 2;      // a logits row with a NaN or no finite maximum
 constexpr int kErrBlockId = 4;     // a block id outside the pool
 constexpr int kErrPath = 8;        // a malformed path of tree nodes
-constexpr int kErrFresh = 16;      // a fork's fresh block that is also copied from
 
 // Sets bit `bit` of the flag.  The flag lives in host memory, so this is a
 // plain load and store (no read-modify-write atomic over the host link); two

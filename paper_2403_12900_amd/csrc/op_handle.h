@@ -26,6 +26,10 @@ constexpr size_t kOpPartBytes = size_t{32} << 20;
 constexpr int kOpCounters = 65536;
 constexpr size_t kOpWorkspaceBytes = kOpPartBytes + kOpCounters * sizeof(int32_t);
 
+// A bit of the device check flag beside those of device_common.h: a fork's fresh
+// block that another of its forks copies from.
+constexpr int kErrFresh = 16;
+
 struct OpHandle {
   char* ws = nullptr;
   hipStream_t st = nullptr;
