@@ -7,9 +7,12 @@
 namespace sprk {
 namespace {
 
+// CW columns per work-group: up to 32 on k_cache_attn, 64 and more on
+// k_cache_attn_wide.
 template <class IO, int HD, int CW>
 constexpr auto kernel() {
-  return &k_cache_attn<IO, HD, CW / 16>;
+  if constexpr (CW <= 32) return &k_cache_attn<IO, HD, CW / 16>;
+  else return &k_cache_attn_wide<IO, HD, CW / 64>;
 }
 
 // Work-groups of the kernel that a CU holds at once.
@@ -47,7 +50,7 @@ hipError_t launch(const CacheAttnCall& c) {
   a.qscale = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(HD)));
   const size_t floats = std::min(c.part_floats, size_t{1} << 28);
   a.part_bytes = static_cast<uint32_t>(floats * 4);
-  const CacheSplit sp = cache_split(t, a.G, a.Hkv, HD, CW, 8, groups_per_cu<IO, HD, CW>() * c.n_cu, floats, c.n_cnt);
+  const CacheSplit sp = cache_split(t, a.G, a.Hkv, HD, CW, CW <= 32 ? 8 : 2, groups_per_cu<IO, HD, CW>() * c.n_cu, floats, c.n_cnt);
   a.bps = sp.bps;
   for (int r = 0; r < t.n; ++r) {
     const int i = sp.order[r];
@@ -60,13 +63,27 @@ hipError_t launch(const CacheAttnCall& c) {
   }
   a.item0[t.n] = sp.item0[t.n];
   kernel<IO, HD, CW>()<<<static_cast<unsigned>(sp.item0[t.n]) * a.Hkv, 256, 0, c.st>>>(a);
-  return hipGetLastError();
+  hipError_t e = hipGetLastError();
+  if constexpr (CW > 32)
+    if (e == hipSuccess && sp.split) {
+      k_cache_merge<IO, HD, CW><<<static_cast<unsigned>(sp.groups) * a.Hkv * (CW / kMergeWide), 256, 0, c.st>>>(a);
+      e = hipGetLastError();
+    }
+  return e;
 }
 
 template <class IO, int HD>
 hipError_t by_columns(const CacheAttnCall& c) {
-  if (cache_cols_per_group(*c.batch, c.H / c.kv.n_kv_heads, 32) == 16) return launch<IO, HD, 16>(c);
-  return launch<IO, HD, 32>(c);
+  constexpr int most = IO::kRaw ? 128 : 64;  // three-part queries leave no registers for more
+  switch (cache_cols_per_group(*c.batch, c.H / c.kv.n_kv_heads, most)) {
+    case 16: return launch<IO, HD, 16>(c);
+    case 32: return launch<IO, HD, 32>(c);
+    case 64: return launch<IO, HD, 64>(c);
+    case 128:
+      if constexpr (most == 128) return launch<IO, HD, 128>(c);
+      break;
+  }
+  return hipErrorInvalidValue;  // not reached: no more than `most`
 }
 
 template <class IO>
