@@ -211,6 +211,66 @@ __device__ __forceinline__ void query_operand(const CacheAttnArgs& a, const Tree
   query_parts<BF16, IO>(p, out);
 }
 
+// One step of a wave whose keys and values lie in registers: 16 NT columns, the
+// blocks at i and i + 1 (< hi).  q(jt, c, part): a piece of the queries; all,
+// some: positions that every column of the group sees, and that one of them
+// does; seen: that this lane's columns do.
+template <class IO, int HD, int NT, class Queries>
+__device__ __forceinline__ void cache_step(const CacheAttnArgs& a, CacheStep<HD>& B, int i, int hi, int all, int some,
+                                           const int* seen, const Queries& q, float* m, float* l,
+                                           f32x4_t (*O)[HD / 16], int lane) {
+  using Parts = CacheParts<IO>;
+  constexpr int P = HD / 32, NE = HD / 16;
+  const int g = lane >> 4;
+  f32x4_t S[NT][2];
+#pragma unroll
+  for (int jt = 0; jt < NT; ++jt)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) S[jt][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < P; ++c)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const uint4 x = B.key(b, c);
+#pragma unroll
+      for (int jt = 0; jt < NT; ++jt)
+#pragma unroll
+        for (int k = 0; k < Parts::q; ++k) S[jt][b] = BF16::mma(S[jt][b], x, q(jt, c, k));
+    }
+  // A step that reaches past what all columns see, or past hi, is masked.
+  const bool tail = 16 * (i + 2) > all || i + 2 > hi;
+  uint32_t sees[NT][2], odd[2][P];
+  bool any = false;
+  if (tail) {
+    uint32_t live[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int pos = 16 * (i + b) + 4 * g;
+      live[b] = i + b < hi ? live_bits(pos, some) : 0u;
+#pragma unroll
+      for (int jt = 0; jt < NT; ++jt) {
+        sees[jt][b] = live[b] & live_bits(pos, seen[jt]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[jt][b][r] = sees[jt][b] >> r & 1 ? S[jt][b][r] : -INFINITY;
+      }
+    }
+    any = __ballot(B.mask_values(live, odd)) != 0;
+  }
+#pragma unroll
+  for (int jt = 0; jt < NT; ++jt) {
+    float p[2][4];
+    softmax_step<2, NE>(S[jt], a.qscale, m[jt], l[jt], O[jt], p);
+    float v[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) v[r] = p[r / 4][r % 4];
+    uint4 x[Parts::p];
+#pragma unroll
+    for (int k = 0; k < Parts::p; ++k) x[k] = next_part<BF16>(v);
+    B.template pv<Parts::p>(O[jt], x);
+    if (any) add_nan_values<P>(O[jt], odd, sees[jt]);
+  }
+}
+
 // Up to 32 columns: the four waves of a work-group take runs of the split's
 // blocks, K and V go straight into registers, and the waves' results are merged
 // through LDS, the splits' by the one that arrives last.
@@ -218,7 +278,7 @@ template <class IO, int HD, int NT>
 __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
   using Step = CacheStep<HD>;
   using Parts = CacheParts<IO>;
-  constexpr int NF = HD / 32, NE = HD / 16, EPW = NE / 4, CW = 16 * NT, P = Step::P;
+  constexpr int NF = HD / 32, NE = HD / 16, EPW = NE / 4, CW = 16 * NT;
   __shared__ CacheSmem<IO, HD, NT> sm;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -242,9 +302,9 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
 #pragma unroll
     for (int q = 0; q < Parts::q; ++q) sm.q[jt][c][q][lane] = x[q];
   }
-  int end[NT];  // positions that this lane's columns see
+  int seen[NT];  // positions that this lane's columns see
 #pragma unroll
-  for (int jt = 0; jt < NT; ++jt) end[jt] = t.len + 1 + min(c0 + 16 * jt + h, t.cols - 1) / a.G;
+  for (int jt = 0; jt < NT; ++jt) seen[jt] = t.len + 1 + min(c0 + 16 * jt + h, t.cols - 1) / a.G;
   const int all = t.len + 1 + c0 / a.G;       // positions that every column sees
   const int some = t.len + 1 + (min(t.cols, c0 + CW) - 1) / a.G;
   __syncthreads();
@@ -268,54 +328,9 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
     const size_t tile[2] = {tile_of(i), tile_of(i + 1 < hi ? i + 1 : i)};
     B.load(a.pool, tile, lane);
   };
+  const auto queries = [&](int jt, int c, int k) { return sm.q[jt][c][k][lane]; };
   const auto compute = [&](Step& B, int i) {
-    f32x4_t S[NT][2];
-#pragma unroll
-    for (int jt = 0; jt < NT; ++jt)
-#pragma unroll
-      for (int b = 0; b < 2; ++b) S[jt][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < NF; ++c)
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const uint4 x = B.key(b, c);
-#pragma unroll
-        for (int jt = 0; jt < NT; ++jt)
-#pragma unroll
-          for (int q = 0; q < Parts::q; ++q) S[jt][b] = BF16::mma(S[jt][b], x, sm.q[jt][c][q][lane]);
-      }
-    // A step that reaches past what all columns see, or past the run, is masked.
-    const bool tail = 16 * (i + 2) > all || i + 2 > hi;
-    uint32_t sees[NT][2], odd[2][P];
-    bool any = false;
-    if (tail) {
-      uint32_t live[2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int pos = 16 * (i + b) + 4 * g;
-        live[b] = i + b < hi ? live_bits(pos, some) : 0u;
-#pragma unroll
-        for (int jt = 0; jt < NT; ++jt) {
-          sees[jt][b] = live[b] & live_bits(pos, end[jt]);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) S[jt][b][r] = sees[jt][b] >> r & 1 ? S[jt][b][r] : -INFINITY;
-        }
-      }
-      any = __ballot(B.mask_values(live, odd)) != 0;
-    }
-#pragma unroll
-    for (int jt = 0; jt < NT; ++jt) {
-      float p[2][4];
-      softmax_step<2, NE>(S[jt], a.qscale, m[jt], l[jt], O[jt], p);
-      float v[8];
-#pragma unroll
-      for (int r = 0; r < 8; ++r) v[r] = p[r / 4][r % 4];
-      uint4 x[Parts::p];
-#pragma unroll
-      for (int q = 0; q < Parts::p; ++q) x[q] = next_part<BF16>(v);
-      B.template pv<Parts::p>(O[jt], x);
-      if (any) add_nan_values<P>(O[jt], odd, sees[jt]);
-    }
+    cache_step<IO, HD, NT>(a, B, i, hi, all, some, seen, queries, m, l, O, lane);
   };
   Step A, B;
   if (lo < hi) fetch(A, lo);
@@ -394,7 +409,7 @@ __device__ __forceinline__ void value_halves_f16(uint32_t w, uint32_t scales, ui
 // lowest such byte has no borrow from below) with codes that are not zero, or a
 // NaN.
 __device__ __forceinline__ bool beyond_f16(uint32_t w, uint32_t scales) {
-  return ((scales - 0x6D6D6D6Du) & 0xE0E0E0E0u) != 0 && ((w & 0x77777777u) != 0 || nan_bytes(scales) != 0);
+  return (((scales - 0x6D6D6D6Du) & 0xE0E0E0E0u) != 0) & (((w & 0x77777777u) | nan_bytes(scales)) != 0);
 }
 
 // The eight probabilities of a step, rounded to fp16, as one operand part; taken
@@ -416,37 +431,80 @@ __device__ __forceinline__ f32x4_t mma_f16(f32x4_t acc, uint4 a, uint4 b) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), acc, 0, 0, 0);
 }
 
-// More than 32 columns.  Work-group: a request's column group of 64 NT columns
-// (16 NT per wave) over the blocks of one split.  Its waves share every block
-// through LDS: keys as codes, which each wave expands to bf16 in registers,
-// values expanded to fp16 by the thread that fetched them.  While a step is
-// computed from LDS, the next one's codes lie in registers or arrive there, and
-// the one's after it are asked for; after the step the next one goes to the
-// other LDS buffer: one barrier per step.
+// More than 32 columns.  Work-group: a request's column group of 16 NT columns
+// for each of its waves, over the blocks of one split.  The waves share every
+// block through LDS: keys as codes, which each wave expands to bf16 in
+// registers, values expanded to fp16 by the thread that fetched them.  While a
+// step is computed from LDS, the next one goes to the other buffer and the one
+// after it is fetched: one barrier per step.
 //
 // Probabilities enter their product in fp16: 2^-12 of themselves for bf16
 // outputs (whose own rounding is 2^-8), 2^-23 in two parts for fp32 ones.  Held
 // 2^7 above the running maximum's place they keep those bits down to 2^-21 of
-// the largest.  A step with a value that fp16 does not hold exactly, or a NaN
-// that not all columns see, takes its values from memory once more, as the
-// other kernel does.
+// the largest.  Their sum is one more product, with ones.  Where a step meets a
+// value that fp16 does not hold exactly, or a NaN that not all columns see, the
+// work-group starts over, its waves reading the blocks themselves as the other
+// kernel's do.
 template <class IO>
 struct WideParts {
   static constexpr int p = IO::kRaw ? 1 : 2;
 };
 constexpr int kWideLift = 7;
 
-template <class IO, int HD, int NT>
-__global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
+// Online softmax of a wave's column tiles as softmax_step, without the sum:
+// scores S to probabilities p.
+template <int NT, int NE>
+__device__ __forceinline__ void wide_softmax(const f32x4_t (*S)[2], float qscale, float* m, f32x4_t* l, f32x4_t (*O)[NE],
+                                             float (*p)[8]) {
+  const auto highest = [](const float* x) {
+    return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+  };
+  bool over = false;
+#pragma unroll
+  for (int jt = 0; jt < NT; ++jt) {
+#pragma unroll
+    for (int r = 0; r < 8; ++r) p[jt][r] = fmaf(S[jt][r / 4][r % 4], qscale, -m[jt]);
+    over |= highest(p[jt]) > kWideLift + kRaise;
+  }
+  if (__ballot(over) != 0) {
+#pragma unroll
+    for (int jt = 0; jt < NT; ++jt) {
+#pragma unroll
+      for (int r = 0; r < 8; ++r) p[jt][r] = S[jt][r / 4][r % 4] * qscale;
+      float mx = highest(p[jt]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float up = fmaxf(m[jt], mx - kWideLift);
+      const float alpha = __builtin_amdgcn_exp2f(m[jt] - up);
+      m[jt] = up;
+      l[jt] *= alpha;
+#pragma unroll
+      for (int e = 0; e < NE; ++e) O[jt][e] *= alpha;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) p[jt][r] = fmaf(S[jt][r / 4][r % 4], qscale, -up);
+    }
+  }
+#pragma unroll
+  for (int jt = 0; jt < NT; ++jt)
+#pragma unroll
+    for (int r = 0; r < 8; ++r) p[jt][r] = __builtin_amdgcn_exp2f(p[jt][r]);
+}
+
+template <class IO, int HD, int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_cache_attn_wide(CacheAttnArgs a) {
   using F = Mx4<HD>;
   using Parts = CacheParts<IO>;
-  constexpr int NF = HD / 32, NE = HD / 16, P = F::P, CW = 64 * NT;
-  constexpr int W = HD / 64;                       // words of a thread, keys or values
-  constexpr int kKeys = 2 * 8 * HD / 4;            // words of a step's key codes
-  constexpr int kScales = HD / 4;                  // and key scales
-  __shared__ uint4 vals[2][NE * 64];               // operands: lane's 8 bytes of block 0, of block 1
-  __shared__ __attribute__((aligned(16))) uint32_t keys[2][kKeys + kScales];
-  __shared__ int slow_s[2];
+  constexpr int NF = HD / 32, NE = HD / 16, P = F::P, CW = 16 * NT * WAVES;
+  constexpr int kKeys = 4 * HD;                             // words of a step's key codes; as many of its values
+  constexpr int kScales = HD / 4;                           // words of its key scales
+  constexpr int W = kKeys / (64 * WAVES) >= 1 ? kKeys / (64 * WAVES) : 1;  // words of a thread, keys or values
+  constexpr int kHalf = kKeys / W / 2;                      // threads that fetch one block
+  struct Keys {
+    uint32_t code[kKeys], scale[kScales];
+  };
+  __shared__ uint4 vals[2][NE * 64];  // operands: a lane's 8 bytes of block 0, of block 1
+  __shared__ __attribute__((aligned(16))) Keys keys[2];
+  __shared__ int slow_s;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane & 15, g = lane >> 4;
@@ -457,16 +515,15 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
   const bool busy = c0 < t.cols;  // this wave has columns
   const int all = t.len + 1 + CW * t.cg / a.G;  // positions that every column of the group sees
   const int some = t.len + 1 + (min(t.cols, CW * (t.cg + 1)) - 1) / a.G;
+  if (tid == 0) slow_s = 0;
 
-  // Block ids are asked for one step before the blocks they name; past the
-  // split's end they are its last one's (a missing second block re-reads the
-  // first, masked).
-  int ids[2];
-  const auto ask = [&](int i) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b) ids[b] = t.btrow[min(i + b, end - 1)];
-  };
-  ask(t.first);
+  // Steps are numbered from the split's start; past its end their blocks are its
+  // last one (a missing second block re-reads the first, masked).  A wave fetches
+  // from one block of a step.  Ids are held 64 at a time, a lane each, and asked
+  // for as many ahead.
+  const int steps = (t.count + 1) / 2;
+  const auto ask = [&](int i) { return pool_id(a, t.btrow[min(t.first + i + lane, end - 1)]); };
+  int ids = ask(0), ids_next = ask(64);
 
   uint4 Q[NT][NF][Parts::q];
   int seen[NT];  // positions that this lane's columns see
@@ -478,23 +535,13 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
 #pragma unroll
     for (int k = 0; k < NF; ++k) query_operand<IO, HD>(a, col, k, g, Q[jt][k]);
   }
-  f32x4_t O[NT][NE];
-  float m[NT], l[NT];
-#pragma unroll
-  for (int jt = 0; jt < NT; ++jt) {
-    m[jt] = kTreeFloor;
-    l[jt] = 0.f;
-#pragma unroll
-    for (int e = 0; e < NE; ++e) O[jt][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
 
-  // This thread's share of a step: W words of block tid / 128's key codes, and W
-  // value words (groups vp on) of its lane vl, whose positions are 4 (vl / 16) on.
-  const int fb = tid >> 7, at = (tid & 127) * W;
-  const int vl = at / P, vp = at % P;
-  struct Next {
-    uint32_t k[W], v[W], vs[W], ks;
-  } next[2];  // of even and odd steps
+  // This thread's share of a step: W words of block fb's key codes, and W value
+  // words (groups vp on) of its lane vl, whose positions are 4 (vl / 16) on.
+  constexpr bool kAll = kHalf * 2 == 64 * WAVES;
+  const bool mine = kAll || tid < kHalf * 2;
+  const int fb = wave / (kHalf / 64) & 1, ft = tid % kHalf;
+  const int at = ft * W, vl = at / P, vp = at % P;
   const auto words = [](const uint8_t* p, uint32_t* w) {
     if constexpr (W == 2) {
       const uint2 x = *reinterpret_cast<const uint2*>(p);
@@ -503,163 +550,212 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
       w[0] = *reinterpret_cast<const uint32_t*>(p);
     }
   };
-  const auto fetch = [&](int then, auto parity) {
-    Next& x = next[decltype(parity)::value];
-    const uint8_t* tile[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-      tile[b] = a.pool + (static_cast<size_t>(__builtin_amdgcn_readfirstlane(pool_id(a, ids[b]))) * a.Hkv + kvh) * F::kTile;
-    ask(then);
-    const uint8_t* mine = fb ? tile[1] : tile[0];
-    words(mine + at * 4, x.k);
-    words(mine + F::kV + at * 4, x.v);
-    words(mine + F::value_scales(vl / 16, vp), x.vs);
-    // Key scales of both blocks: HD / 8 words each, by the first threads.
-    if (tid < kScales)
-      x.ks = *reinterpret_cast<const uint32_t*>((tid < kScales / 2 ? tile[0] : tile[1]) + F::kKs + tid % (kScales / 2) * 4);
+  uint32_t nk[W] = {}, ns = 0, nv[W] = {}, nvs[W] = {};  // on their way into LDS
+  // This wave's tile of a step; called for each step in order.
+  const auto tile_of = [&](int step) {
+    const int i = min(2 * step + fb, t.count - 1);
+    if ((step & 31) == 0 && step > 0) {
+      ids = ids_next;
+      ids_next = ask(2 * step + 64);
+    }
+    return a.pool + (static_cast<size_t>(__builtin_amdgcn_readlane(ids, i & 63)) * a.Hkv + kvh) * F::kTile;
   };
-  const auto put = [&](int i, auto parity, auto tail) {
-    constexpr int to = decltype(parity)::value;
-    Next& x = next[to];
-    uint32_t* k = keys[to] + fb * (kKeys / 2) + at;
+  const auto fetch_keys = [&](const uint8_t* tile) {
+    if (mine) words(tile + at * 4, nk);
+    if (ft < kScales / 2) ns = *reinterpret_cast<const uint32_t*>(tile + F::kKs + ft * 4);
+  };
+  const auto fetch_values = [&](const uint8_t* tile) {
+    if (mine) {
+      words(tile + F::kV + at * 4, nv);
+      words(tile + F::value_scales(vl / 16, vp), nvs);
+    }
+  };
+  // Whether a step reaches past what all columns see, or past the split.
+  const auto is_tail = [&](int step) { return 16 * (t.first + 2 * step + 2) > all || t.first + 2 * step + 2 > end; };
+  const auto put_keys = [&](Keys& to) {
+    if (mine) {
 #pragma unroll
-    for (int w = 0; w < W; ++w) k[w] = x.k[w];
-    if (tid < kScales) keys[to][kKeys + tid] = x.ks;
-    uint32_t live = 15;
-    if constexpr (decltype(tail)::value) live = i + fb < end ? live_bits(16 * (i + fb) + 4 * (vl / 16), some) : 0u;
+      for (int w = 0; w < W; ++w) to.code[fb * (kKeys / 2) + at + w] = nk[w];
+    }
+    if (mine && ft < kScales / 2) to.scale[fb * (kScales / 2) + ft] = ns;
+  };
+  const auto put_values = [&](int step, uint4* to, auto tail) {
+    if (!mine) return;
     bool beyond = false;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      uint32_t v = x.v[w], s = x.vs[w];
+      uint32_t v = nv[w], x = nvs[w];
       if constexpr (decltype(tail)::value) {
-        const uint32_t keep = byte_mask(live);
+        const int b = t.first + 2 * step + fb;
+        const uint32_t keep = byte_mask(b < end ? live_bits(16 * b + 4 * (vl / 16), some) : 0u);
         v &= keep;
-        s = (s & keep) | (0x7F7F7F7Fu & ~keep);
+        x = (x & keep) | (0x7F7F7F7Fu & ~keep);
       }
-      beyond |= beyond_f16(v, s);
+      beyond |= beyond_f16(v, x);
       uint2 lo, hi;
-      value_halves_f16(v, s, lo, hi);
-      uint2* op = reinterpret_cast<uint2*>(vals[to] + 2 * (vp + w) * 64 + vl) + fb;
+      value_halves_f16(v, x, lo, hi);
+      uint2* op = reinterpret_cast<uint2*>(to + 2 * (vp + w) * 64 + vl) + fb;
       op[0] = lo;
       op[128] = hi;
     }
-    if (__ballot(beyond) != 0 && lane == 0) slow_s[to] = i + 1;
+    if (beyond) slow_s = 1;
   };
-  const auto is_tail = [&](int i) { return 16 * (i + 2) > all || i + 2 > end; };
-  const auto compute = [&](int i, auto parity, auto tail) {
-    constexpr int from = decltype(parity)::value;
-    f32x4_t S[NT][2];
+
+  f32x4_t O[NT][NE], l[NT];  // l: the sum, in every register
+  float m[NT];
+  const auto reset = [&] {
+#pragma unroll
+    for (int jt = 0; jt < NT; ++jt) {
+      m[jt] = kTreeFloor;
+      l[jt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < NE; ++e) O[jt][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  struct Scores {
+    f32x4_t x[NT][2];
+  };
+  const auto scores = [&](int step, const Keys& from, Scores& S, auto tail) {
 #pragma unroll
     for (int jt = 0; jt < NT; ++jt)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) S[jt][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int b = 0; b < 2; ++b) S.x[jt][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    uint32_t kw[2][P];
+    float ks[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const uint8_t* kb = reinterpret_cast<const uint8_t*>(keys[from]) + b * (kKeys * 2);
-      uint32_t kw[P];
+      const uint8_t* kb = reinterpret_cast<const uint8_t*>(from.code) + b * (kKeys * 2) + F::key_code(h, HD / 4 * g);
       if constexpr (P == 4) {
-        const uint4 x = *reinterpret_cast<const uint4*>(kb + F::key_code(h, HD / 4 * g));
-        kw[0] = x.x, kw[1] = x.y, kw[2] = x.z, kw[3] = x.w;
+        const uint4 x = *reinterpret_cast<const uint4*>(kb);
+        kw[b][0] = x.x, kw[b][1] = x.y, kw[b][2] = x.z, kw[b][3] = x.w;
       } else {
-        const uint2 x = *reinterpret_cast<const uint2*>(kb + F::key_code(h, HD / 4 * g));
-        kw[0] = x.x, kw[1] = x.y;
+        const uint2 x = *reinterpret_cast<const uint2*>(kb);
+        kw[b][0] = x.x, kw[b][1] = x.y;
       }
-      const uint8_t* sb = reinterpret_cast<const uint8_t*>(keys[from] + kKeys) + b * (HD / 2);
-      const float ks = scale_of<0>(sb[HD / 4 * g / 32 * 16 + h]);
+      ks[b] = scale_of<0>((reinterpret_cast<const uint8_t*>(from.scale) + b * (HD / 2))[HD / 4 * g / 32 * 16 + h]);
+    }
 #pragma unroll
-      for (int c = 0; c < NF; ++c) {
-        const uint4 x = make_uint4(codes_to_bf16<0>(kw[c], ks), codes_to_bf16<1>(kw[c], ks), codes_to_bf16<2>(kw[c], ks),
-                                   codes_to_bf16<3>(kw[c], ks));
+    for (int c = 0; c < NF; ++c)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const uint4 x = make_uint4(codes_to_bf16<0>(kw[b][c], ks[b]), codes_to_bf16<1>(kw[b][c], ks[b]),
+                                   codes_to_bf16<2>(kw[b][c], ks[b]), codes_to_bf16<3>(kw[b][c], ks[b]));
 #pragma unroll
         for (int q = 0; q < Parts::q; ++q)
 #pragma unroll
-          for (int jt = 0; jt < NT; ++jt) S[jt][b] = BF16::mma(S[jt][b], x, Q[jt][c][q]);
+          for (int jt = 0; jt < NT; ++jt) S.x[jt][b] = BF16::mma(S.x[jt][b], x, Q[jt][c][q]);
       }
-    }
-    uint32_t live[2], sees[NT][2];
     if constexpr (decltype(tail)::value) {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const int pos = 16 * (i + b) + 4 * g;
-        live[b] = i + b < end ? live_bits(pos, some) : 0u;
+        const int block = t.first + 2 * step + b, pos = 16 * block + 4 * g;
 #pragma unroll
         for (int jt = 0; jt < NT; ++jt) {
-          sees[jt][b] = live[b] & live_bits(pos, seen[jt]);
+          const uint32_t sees = block < end ? live_bits(pos, seen[jt]) : 0u;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) S[jt][b][r] = sees[jt][b] >> r & 1 ? S[jt][b][r] : -INFINITY;
+          for (int r = 0; r < 4; ++r) S.x[jt][b][r] = sees >> r & 1 ? S.x[jt][b][r] : -INFINITY;
         }
       }
     }
-    float p[NT][2][4];
-#pragma unroll
-    for (int jt = 0; jt < NT; ++jt) softmax_step<2, NE, kWideLift>(S[jt], a.qscale, m[jt], l[jt], O[jt], p[jt]);
-    if (slow_s[from] == i + 1) {
-      CacheStep<HD> B;
-      const size_t tile[2] = {static_cast<size_t>(pool_id(a, t.btrow[i])) * a.Hkv + kvh,
-                              static_cast<size_t>(pool_id(a, t.btrow[min(i + 1, end - 1)])) * a.Hkv + kvh};
-      B.load(a.pool, tile, lane);
-      uint32_t odd[2][P];
-      bool any = false;
-      if constexpr (decltype(tail)::value) any = __ballot(B.mask_values(live, odd)) != 0;
-#pragma unroll
-      for (int jt = 0; jt < NT; ++jt) {
-        float v[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) v[r] = p[jt][r / 4][r % 4];
-        uint4 x[Parts::p];
-#pragma unroll
-        for (int q = 0; q < Parts::p; ++q) x[q] = next_part<BF16>(v);
-        B.template pv<Parts::p>(O[jt], x);
-        if constexpr (decltype(tail)::value)
-          if (any) add_nan_values<P>(O[jt], odd, sees[jt]);
-      }
-      return;
-    }
+  };
+  const auto outputs = [&](const Scores& S, const uint4* from) {
+    float p[NT][8];
+    wide_softmax<NT, NE>(S.x, a.qscale, m, l, O, p);
     uint4 pp[NT][WideParts<IO>::p];
 #pragma unroll
-    for (int jt = 0; jt < NT; ++jt) {
-      float v[8];
+    for (int jt = 0; jt < NT; ++jt)
 #pragma unroll
-      for (int r = 0; r < 8; ++r) v[r] = p[jt][r / 4][r % 4];
-#pragma unroll
-      for (int q = 0; q < WideParts<IO>::p; ++q) pp[jt][q] = next_part_f16(v);
-    }
+      for (int q = 0; q < WideParts<IO>::p; ++q) {
+        pp[jt][q] = next_part_f16(p[jt]);
+        l[jt] = mma_f16(l[jt], make_uint4(0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u), pp[jt][q]);
+      }
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
-      const uint4 x = vals[from][e * 64 + lane];
+      const uint4 x = from[e * 64 + lane];
 #pragma unroll
       for (int q = 0; q < WideParts<IO>::p; ++q)
 #pragma unroll
         for (int jt = 0; jt < NT; ++jt) O[jt][e] = mma_f16(O[jt][e], x, pp[jt][q]);
     }
+    // Schedule: four operands ahead of the exponentials, the others between the
+    // products, so that none is waited for (295 us without, 285 with; see above
+    // for the case).
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+    __builtin_amdgcn_sched_group_barrier(0x402, NT * 12, 0);
+    const auto group = [](auto) {
+      __builtin_amdgcn_sched_group_barrier(0x8, NT * WideParts<IO>::p, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    };
+    static_for<NE>(group);
   };
-  constexpr std::false_type kPlain{};
-  constexpr std::true_type kTail{};
-  constexpr std::integral_constant<int, 0> kEven{};
-  constexpr std::integral_constant<int, 1> kOdd{};
-  // One step: fetch the one after the next, compute, put the next.  Whole steps
-  // do so without a condition.
-  const auto step = [&](int i, auto parity, auto other, auto tail) {
-    constexpr bool whole = !decltype(tail)::value;
-    __syncthreads();  // this step is in its buffer; the other buffer has been read
-    if (whole || i + 4 < end) fetch(i + 6, parity);
-    if (busy) compute(i, parity, tail);
-    if (whole || i + 2 < end) put(i + 2, other, tail);
+
+  // Step s: the keys of step s + 2 and the values of s + 1 go to LDS, the ones
+  // after those are fetched, the scores of s + 1 are computed, whose products run
+  // while s's scores become probabilities, and s's outputs.
+  const auto walk = [&](auto busy_wave) {
+    constexpr bool kBusy = decltype(busy_wave)::value;
+    constexpr std::integral_constant<int, 0> kEven{};
+    constexpr std::integral_constant<int, 1> kOdd{};
+    Scores S[2];
+    const uint8_t* next;  // tile of step s + 2, whose keys were fetched in the step before
+    const auto step = [&](int s, auto parity, auto tail) {
+      constexpr int now = decltype(parity)::value;
+      __syncthreads();  // keys of s + 1 and values of s are there; keys of s and values of s - 1 have been read
+      put_keys(keys[now]);
+      put_values(s + 1, vals[now ^ 1], tail);
+      fetch_values(next);
+      next = tile_of(s + 3);
+      fetch_keys(next);
+      if constexpr (kBusy) {
+        scores(s + 1, keys[now ^ 1], S[now ^ 1], tail);
+        outputs(S[now], vals[now]);
+      }
+    };
+    next = tile_of(0);
+    fetch_keys(next);
+    fetch_values(next);
+    put_keys(keys[0]);
+    put_values(0, vals[0], std::true_type{});
+    next = tile_of(1);
+    fetch_keys(next);
+    fetch_values(next);
+    put_keys(keys[1]);
+    next = tile_of(2);
+    fetch_keys(next);
+    __syncthreads();
+    if constexpr (kBusy) scores(0, keys[0], S[0], std::true_type{});
+    int s = 0;
+    for (; s + 2 < steps && !is_tail(s + 2); s += 2) {
+      step(s, kEven, std::false_type{});
+      step(s + 1, kOdd, std::false_type{});
+    }
+    for (; s < steps; s += 2) {
+      step(s, kEven, std::true_type{});
+      if (s + 1 < steps) step(s + 1, kOdd, std::true_type{});
+    }
   };
-  if (tid < 2) slow_s[tid] = 0;
+  // Two walks, not a condition in one: where some steps leave the accumulators as
+  // they are, the compiler copies them all after each step's products.
+  reset();
+  if (busy) walk(std::true_type{});
+  else walk(std::false_type{});
   __syncthreads();
-  int i = t.first;
-  fetch(i + 2, kEven);
-  fetch(i + 4, kOdd);
-  if (is_tail(i)) put(i, kEven, kTail);
-  else put(i, kEven, kPlain);
-  for (; i + 6 < end && !is_tail(i + 4); i += 4) {  // two steps and the one after them are whole
-    step(i, kEven, kOdd, kPlain);
-    step(i + 2, kOdd, kEven, kPlain);
-  }
-  for (; i < end; i += 4) {
-    step(i, kEven, kOdd, kTail);
-    if (i + 2 < end) step(i + 2, kOdd, kEven, kTail);
+  if (slow_s) {
+    reset();
+    float sum[NT] = {};
+    const auto queries = [&](int jt, int c, int k) { return Q[jt][c][k]; };
+    for (int i = t.first; i < end && busy; i += 2) {
+      const size_t tile[2] = {static_cast<size_t>(pool_id(a, t.btrow[i])) * a.Hkv + kvh,
+                              static_cast<size_t>(pool_id(a, t.btrow[min(i + 1, end - 1)])) * a.Hkv + kvh};
+      CacheStep<HD> B;
+      B.load(a.pool, tile, lane);
+      cache_step<IO, HD, NT>(a, B, i, end, all, some, seen, queries, m, sum, O, lane);
+    }
+#pragma unroll
+    for (int jt = 0; jt < NT; ++jt) {
+      sum[jt] += __shfl_xor(sum[jt], 16);
+      l[jt][0] = sum[jt] + __shfl_xor(sum[jt], 32);
+    }
   }
 
   const CoherentBuffer pb(a.part, a.part_bytes);
@@ -667,20 +763,17 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
   if (!busy) return;
 #pragma unroll
   for (int jt = 0; jt < NT; ++jt) {
-    float L = l[jt];
-    L += __shfl_xor(L, 16);
-    L += __shfl_xor(L, 32);
     const int c = 16 * (NT * wave + jt) + h;  // within the group
     if (CW * t.cg + c >= t.cols) continue;
     const TreeColumn col = tree_column(a, t.row0, kvh, CW * t.cg + c);
-    const float inv = 1.f / L;
+    const float inv = 1.f / l[jt][0];
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
       const int d0 = 16 * e + 4 * g;
       if (t.nsplit == 1) IO::store4(a, col.row, col.hq * HD + d0, O[jt][e] * inv);
       else pb.store4(item + (c * (HD + 4) + 4 + d0) * 4, O[jt][e]);
     }
-    if (t.nsplit > 1 && g == 0) pb.store4(item + c * (HD + 4) * 4, f32x4_t{m[jt], L, 0.f, 0.f});
+    if (t.nsplit > 1 && g == 0) pb.store4(item + c * (HD + 4) * 4, f32x4_t{m[jt], l[jt][0], 0.f, 0.f});
   }
 }
 

@@ -406,9 +406,7 @@ __device__ __forceinline__ void query_parts(const QueryPiece& p, uint4* out) {
 // probabilities, adds them to l, and raises the running maximum first where a
 // score exceeds it by more than kRaise.  (The test runs on the exponents, which
 // are needed anyway.)
-// kLift: the maximum is held so much lower, and the largest exponents lie so
-// much higher (a fp16 probability then has its 11 bits further down).
-template <int BP, int NE, int kLift = 0>
+template <int BP, int NE>
 __device__ __forceinline__ void softmax_step(const f32x4_t* S, float qscale, float& m, float& l, f32x4_t* O, float (*p)[4]) {
   const auto highest = [](const float (*x)[4]) {
     float v = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3]));
@@ -420,7 +418,7 @@ __device__ __forceinline__ void softmax_step(const f32x4_t* S, float qscale, flo
   for (int b = 0; b < BP; ++b)
 #pragma unroll
     for (int r = 0; r < 4; ++r) p[b][r] = fmaf(S[b][r], qscale, -m);
-  if (__ballot(highest(p) > kRaise + kLift) != 0) {
+  if (__ballot(highest(p) > kRaise) != 0) {
 #pragma unroll
     for (int b = 0; b < BP; ++b)
 #pragma unroll
@@ -428,7 +426,7 @@ __device__ __forceinline__ void softmax_step(const f32x4_t* S, float qscale, flo
     float mx = highest(p);
     mx = fmaxf(mx, __shfl_xor(mx, 16));
     mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float up = fmaxf(m, mx - kLift);
+    const float up = fmaxf(m, mx);
     const float alpha = __builtin_amdgcn_exp2f(m - up);
     l *= alpha;
     m = up;
