@@ -502,8 +502,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cache_attn_wide(CacheAttnArgs
   struct Keys {
     uint32_t code[kKeys], scale[kScales];
   };
-  __shared__ uint4 vals[2][NE * 64];  // operands: a lane's 8 bytes of block 0, of block 1
-  __shared__ __attribute__((aligned(16))) Keys keys[2];
+  __shared__ uint4 vals[4][NE * 64];  // of a step: operands: a lane's 8 bytes of block 0, of block 1
+  __shared__ __attribute__((aligned(16))) Keys keys[4];
   __shared__ int slow_s;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -550,7 +550,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cache_attn_wide(CacheAttnArgs
       w[0] = *reinterpret_cast<const uint32_t*>(p);
     }
   };
-  uint32_t nk[W] = {}, ns = 0, nv[W] = {}, nvs[W] = {};  // on their way into LDS
   // This wave's tile of a step; called for each step in order.
   const auto tile_of = [&](int step) {
     const int i = min(2 * step + fb, t.count - 1);
@@ -560,31 +559,34 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cache_attn_wide(CacheAttnArgs
     }
     return a.pool + (static_cast<size_t>(__builtin_amdgcn_readlane(ids, i & 63)) * a.Hkv + kvh) * F::kTile;
   };
-  const auto fetch_keys = [&](const uint8_t* tile) {
-    if (mine) words(tile + at * 4, nk);
-    if (ft < kScales / 2) ns = *reinterpret_cast<const uint32_t*>(tile + F::kKs + ft * 4);
+  struct {
+    uint32_t k[W], ks, v[W], vs[W];
+  } next[2] = {};  // two steps on their way into LDS
+  const auto fetch_keys = [&](int n, const uint8_t* tile) {
+    if (mine) words(tile + at * 4, next[n].k);
+    if (ft < kScales / 2) next[n].ks = *reinterpret_cast<const uint32_t*>(tile + F::kKs + ft * 4);
   };
-  const auto fetch_values = [&](const uint8_t* tile) {
+  const auto fetch_values = [&](int n, const uint8_t* tile) {
     if (mine) {
-      words(tile + F::kV + at * 4, nv);
-      words(tile + F::value_scales(vl / 16, vp), nvs);
+      words(tile + F::kV + at * 4, next[n].v);
+      words(tile + F::value_scales(vl / 16, vp), next[n].vs);
     }
   };
   // Whether a step reaches past what all columns see, or past the split.
   const auto is_tail = [&](int step) { return 16 * (t.first + 2 * step + 2) > all || t.first + 2 * step + 2 > end; };
-  const auto put_keys = [&](Keys& to) {
+  const auto put_keys = [&](int n, Keys& to) {
     if (mine) {
 #pragma unroll
-      for (int w = 0; w < W; ++w) to.code[fb * (kKeys / 2) + at + w] = nk[w];
+      for (int w = 0; w < W; ++w) to.code[fb * (kKeys / 2) + at + w] = next[n].k[w];
     }
-    if (mine && ft < kScales / 2) to.scale[fb * (kScales / 2) + ft] = ns;
+    if (mine && ft < kScales / 2) to.scale[fb * (kScales / 2) + ft] = next[n].ks;
   };
-  const auto put_values = [&](int step, uint4* to, auto tail) {
+  const auto put_values = [&](int n, int step, uint4* to, auto tail) {
     if (!mine) return;
     bool beyond = false;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      uint32_t v = nv[w], x = nvs[w];
+      uint32_t v = next[n].v[w], x = next[n].vs[w];
       if constexpr (decltype(tail)::value) {
         const int b = t.first + 2 * step + fb;
         const uint32_t keep = byte_mask(b < end ? live_bits(16 * b + 4 * (vl / 16), some) : 0u);
@@ -689,49 +691,62 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cache_attn_wide(CacheAttnArgs
     static_for<NE>(group);
   };
 
-  // Step s: the keys of step s + 2 and the values of s + 1 go to LDS, the ones
-  // after those are fetched, the scores of s + 1 are computed, whose products run
-  // while s's scores become probabilities, and s's outputs.
+  // Pair q of steps, 2q and 2q + 1.  While it is computed the next pair's values
+  // and the keys of the two steps from 2q + 3 on go to LDS, and what follows them
+  // is fetched; scores run a step ahead of the outputs, so that their products run
+  // while scores become probabilities.  One barrier per pair.
   const auto walk = [&](auto busy_wave) {
     constexpr bool kBusy = decltype(busy_wave)::value;
     constexpr std::integral_constant<int, 0> kEven{};
     constexpr std::integral_constant<int, 1> kOdd{};
     Scores S[2];
-    const uint8_t* next;  // tile of step s + 2, whose keys were fetched in the step before
-    const auto step = [&](int s, auto parity, auto tail) {
-      constexpr int now = decltype(parity)::value;
-      __syncthreads();  // keys of s + 1 and values of s are there; keys of s and values of s - 1 have been read
-      put_keys(keys[now]);
-      put_values(s + 1, vals[now ^ 1], tail);
-      fetch_values(next);
-      next = tile_of(s + 3);
-      fetch_keys(next);
+    const uint8_t* first;  // tile of the first step whose values are fetched next
+    int asked = 1;         // step whose keys are
+    const auto fetch = [&] {
+      const uint8_t *t0 = tile_of(asked), *t1 = tile_of(asked + 1);
+      fetch_keys(0, t0);
+      fetch_keys(1, t1);
+      fetch_values(0, first);
+      fetch_values(1, t0);
+      first = t1;
+      asked += 2;
+    };
+    const auto put = [&](int q, auto parity, auto tail) {
+      constexpr int to = 2 * decltype(parity)::value;
+      put_keys(0, keys[to + 1]);
+      put_keys(1, keys[(to + 2) & 3]);
+      put_values(0, 2 * q, vals[to], tail);
+      put_values(1, 2 * q + 1, vals[to + 1], tail);
+    };
+    const auto pair = [&](int q, auto parity, auto other, auto tail) {
+      constexpr int from = 2 * decltype(parity)::value;
+      __syncthreads();
+      put(q + 1, other, tail);
+      fetch();
       if constexpr (kBusy) {
-        scores(s + 1, keys[now ^ 1], S[now ^ 1], tail);
-        outputs(S[now], vals[now]);
+        scores(2 * q + 1, keys[from + 1], S[1], tail);
+        outputs(S[0], vals[from]);
+        scores(2 * q + 2, keys[(from + 2) & 3], S[0], tail);
+        outputs(S[1], vals[from + 1]);
       }
     };
-    next = tile_of(0);
-    fetch_keys(next);
-    fetch_values(next);
-    put_keys(keys[0]);
-    put_values(0, vals[0], std::true_type{});
-    next = tile_of(1);
-    fetch_keys(next);
-    fetch_values(next);
-    put_keys(keys[1]);
-    next = tile_of(2);
-    fetch_keys(next);
+    first = tile_of(0);
+    fetch_keys(0, first);
+    put_keys(0, keys[0]);
+    fetch();
+    put(0, kEven, std::true_type{});
+    fetch();
     __syncthreads();
     if constexpr (kBusy) scores(0, keys[0], S[0], std::true_type{});
-    int s = 0;
-    for (; s + 2 < steps && !is_tail(s + 2); s += 2) {
-      step(s, kEven, std::false_type{});
-      step(s + 1, kOdd, std::false_type{});
+    const int pairs = (steps + 1) / 2;
+    int q = 0;
+    for (; q + 1 < pairs && !is_tail(2 * q + 5); q += 2) {
+      pair(q, kEven, kOdd, std::false_type{});
+      pair(q + 1, kOdd, kEven, std::false_type{});
     }
-    for (; s < steps; s += 2) {
-      step(s, kEven, std::true_type{});
-      if (s + 1 < steps) step(s + 1, kOdd, std::true_type{});
+    for (; q < pairs; q += 2) {
+      pair(q, kEven, kOdd, std::true_type{});
+      if (q + 1 < pairs) pair(q + 1, kOdd, kEven, std::true_type{});
     }
   };
   // Two walks, not a condition in one: where some steps leave the accumulators as
