@@ -7,25 +7,20 @@
 namespace sprk {
 namespace {
 
-// CW columns per work-group: up to 32 on k_cache_attn, more on
-// k_cache_attn_wide, 32 a wave (fp32 queries in three parts: 16).
+// CW columns per work-group: up to 32 on k_cache_attn, 64 and more on
+// k_cache_attn_wide.
 template <class IO, int HD, int CW>
 constexpr auto kernel() {
   if constexpr (CW <= 32) return &k_cache_attn<IO, HD, CW / 16>;
-  else if constexpr (CW == 64) return &k_cache_attn_wide<IO, HD, 1, 4>;
-  else if constexpr (IO::kRaw) return &k_cache_attn_wide<IO, HD, 2, CW / 32>;
-  else return &k_cache_attn_wide<IO, HD, 1, CW / 16>;
+  else return &k_cache_attn_wide<IO, HD, CW / 64>;
 }
-template <class IO, int CW>
-constexpr int kThreads = CW <= 64 ? 256 : IO::kRaw ? 2 * CW : 4 * CW;
 
 // Work-groups of the kernel that a CU holds at once.
 template <class IO, int HD, int CW>
 int groups_per_cu() {
   static const int n = [] {
     int o = 0;
-    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&o, reinterpret_cast<const void*>(kernel<IO, HD, CW>()),
-                                                     kThreads<IO, CW>, 0) !=
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&o, reinterpret_cast<const void*>(kernel<IO, HD, CW>()), 256, 0) !=
             hipSuccess || o < 1)
       o = 1;
     return o;
@@ -67,7 +62,7 @@ hipError_t launch(const CacheAttnCall& c) {
     a.item0[r] = sp.item0[r];
   }
   a.item0[t.n] = sp.item0[t.n];
-  kernel<IO, HD, CW>()<<<static_cast<unsigned>(sp.item0[t.n]) * a.Hkv, kThreads<IO, CW>, 0, c.st>>>(a);
+  kernel<IO, HD, CW>()<<<static_cast<unsigned>(sp.item0[t.n]) * a.Hkv, 256, 0, c.st>>>(a);
   hipError_t e = hipGetLastError();
   if constexpr (CW > 32)
     if (e == hipSuccess && sp.split) {
@@ -79,14 +74,13 @@ hipError_t launch(const CacheAttnCall& c) {
 
 template <class IO, int HD>
 hipError_t by_columns(const CacheAttnCall& c) {
-  constexpr int most = IO::kRaw ? 256 : 128;
+  constexpr int most = IO::kRaw ? 128 : 64;  // three-part queries leave no registers for more
   switch (cache_cols_per_group(*c.batch, c.H / c.kv.n_kv_heads, most)) {
     case 16: return launch<IO, HD, 16>(c);
     case 32: return launch<IO, HD, 32>(c);
     case 64: return launch<IO, HD, 64>(c);
-    case 128: return launch<IO, HD, 128>(c);
-    case 256:
-      if constexpr (most == 256) return launch<IO, HD, 256>(c);
+    case 128:
+      if constexpr (most == 128) return launch<IO, HD, 128>(c);
       break;
   }
   return hipErrorInvalidValue;  // not reached: no more than `most`

@@ -42,6 +42,7 @@ static_assert(sizeof(CacheAttnArgs) <= 3584, "kernel arguments");
 // What a work item is: its request, column group and blocks.
 struct CacheItem {
   int cg, cg0, nsplit, ncg, item0;
+  int item;                   // of its partial result
   int len, nblk, row0, cols;  // nblk: blocks that the column group's rows see
   int first, count;           // blocks of the split (count < 1: nothing to do)
   const int32_t* btrow;
@@ -60,8 +61,12 @@ __device__ __forceinline__ CacheItem cache_item(const CacheAttnArgs& a, int f) {
   t.row0 = a.row0[r];
   t.cols = a.rows[r] * a.G;
   t.ncg = (t.cols + CW - 1) / CW;
-  const int w = f - t.item0, s = w / t.ncg;
-  t.cg = w - s * t.ncg;  // column groups of one split run side by side and share its blocks
+  // Column groups of one split run side by side and share its blocks.  Later rows
+  // see more: the groups go down from the last one, and the second half of them
+  // up from the first, so that two of a CU are together as long everywhere.
+  const int w = f - t.item0, s = w / t.ncg, j = w - s * t.ncg, down = t.ncg - t.ncg / 2;
+  t.cg = j < down ? t.ncg - 1 - j : j - down;
+  t.item = t.item0 + s * t.ncg + t.cg;
   const int last = (min(t.cols, (t.cg + 1) * CW) - 1) / a.G;  // row
   t.nblk = (t.len + last + 16) >> 4;
   t.nsplit = (t.nblk + a.bps - 1) / a.bps;
@@ -351,7 +356,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
     if (g == 0) sm.sml[wave][jt][h] = make_float2(m[jt], l[jt]);
   }
   const CoherentBuffer pb(a.part, a.part_bytes);
-  const uint32_t item = (static_cast<uint32_t>(f) * a.Hkv + kvh) * CW * (HD + 4) * 4;
+  const uint32_t item = (static_cast<uint32_t>(t.item) * a.Hkv + kvh) * CW * (HD + 4) * 4;
 #pragma unroll
   for (int jt = 0; jt < NT; ++jt) {
     __syncthreads();  // Q (and the previous tile's outputs) have been read
@@ -431,8 +436,8 @@ __device__ __forceinline__ f32x4_t mma_f16(f32x4_t acc, uint4 a, uint4 b) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), acc, 0, 0, 0);
 }
 
-// More than 32 columns.  Work-group: a request's column group of 16 NT columns
-// for each of its waves, over the blocks of one split.  The waves share every
+// More than 32 columns.  Work-group: a request's column group of 64 NT columns
+// (16 NT per wave) over the blocks of one split.  The waves share every
 // block through LDS: keys as codes, which each wave expands to bf16 in
 // registers, values expanded to fp16 by the thread that fetched them.  While a
 // step is computed from LDS, the next one goes to the other buffer and the one
@@ -490,15 +495,14 @@ __device__ __forceinline__ void wide_softmax(const f32x4_t (*S)[2], float qscale
     for (int r = 0; r < 8; ++r) p[jt][r] = __builtin_amdgcn_exp2f(p[jt][r]);
 }
 
-template <class IO, int HD, int NT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_cache_attn_wide(CacheAttnArgs a) {
+template <class IO, int HD, int NT>
+__global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
   using F = Mx4<HD>;
   using Parts = CacheParts<IO>;
-  constexpr int NF = HD / 32, NE = HD / 16, P = F::P, CW = 16 * NT * WAVES;
+  constexpr int NF = HD / 32, NE = HD / 16, P = F::P, CW = 64 * NT;
   constexpr int kKeys = 4 * HD;                             // words of a step's key codes; as many of its values
   constexpr int kScales = HD / 4;                           // words of its key scales
-  constexpr int W = kKeys / (64 * WAVES) >= 1 ? kKeys / (64 * WAVES) : 1;  // words of a thread, keys or values
-  constexpr int kHalf = kKeys / W / 2;                      // threads that fetch one block
+  constexpr int W = kKeys / 256;                            // words of a thread, keys or values
   struct Keys {
     uint32_t code[kKeys], scale[kScales];
   };
@@ -538,9 +542,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cache_attn_wide(CacheAttnArgs
 
   // This thread's share of a step: W words of block fb's key codes, and W value
   // words (groups vp on) of its lane vl, whose positions are 4 (vl / 16) on.
-  constexpr bool kAll = kHalf * 2 == 64 * WAVES;
-  const bool mine = kAll || tid < kHalf * 2;
-  const int fb = wave / (kHalf / 64) & 1, ft = tid % kHalf;
+  const int fb = wave >> 1, ft = tid & 127;
   const int at = ft * W, vl = at / P, vp = at % P;
   const auto words = [](const uint8_t* p, uint32_t* w) {
     if constexpr (W == 2) {
@@ -563,26 +565,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cache_attn_wide(CacheAttnArgs
     uint32_t k[W], ks, v[W], vs[W];
   } next[2] = {};  // two steps on their way into LDS
   const auto fetch_keys = [&](int n, const uint8_t* tile) {
-    if (mine) words(tile + at * 4, next[n].k);
+    words(tile + at * 4, next[n].k);
     if (ft < kScales / 2) next[n].ks = *reinterpret_cast<const uint32_t*>(tile + F::kKs + ft * 4);
   };
   const auto fetch_values = [&](int n, const uint8_t* tile) {
-    if (mine) {
-      words(tile + F::kV + at * 4, next[n].v);
-      words(tile + F::value_scales(vl / 16, vp), next[n].vs);
-    }
+    words(tile + F::kV + at * 4, next[n].v);
+    words(tile + F::value_scales(vl / 16, vp), next[n].vs);
   };
   // Whether a step reaches past what all columns see, or past the split.
   const auto is_tail = [&](int step) { return 16 * (t.first + 2 * step + 2) > all || t.first + 2 * step + 2 > end; };
   const auto put_keys = [&](int n, Keys& to) {
-    if (mine) {
 #pragma unroll
-      for (int w = 0; w < W; ++w) to.code[fb * (kKeys / 2) + at + w] = next[n].k[w];
-    }
-    if (mine && ft < kScales / 2) to.scale[fb * (kScales / 2) + ft] = next[n].ks;
+    for (int w = 0; w < W; ++w) to.code[fb * (kKeys / 2) + at + w] = next[n].k[w];
+    if (ft < kScales / 2) to.scale[fb * (kScales / 2) + ft] = next[n].ks;
   };
   const auto put_values = [&](int n, int step, uint4* to, auto tail) {
-    if (!mine) return;
     bool beyond = false;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
@@ -774,7 +771,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_cache_attn_wide(CacheAttnArgs
   }
 
   const CoherentBuffer pb(a.part, a.part_bytes);
-  const uint32_t item = (static_cast<uint32_t>(f) * a.Hkv + kvh) * CW * (HD + 4) * 4;
+  const uint32_t item = (static_cast<uint32_t>(t.item) * a.Hkv + kvh) * CW * (HD + 4) * 4;
   if (!busy) return;
 #pragma unroll
   for (int jt = 0; jt < NT; ++jt) {
