@@ -121,16 +121,27 @@ struct CacheStep {
   }
   // Lane r + 16 g: keys of position r, dimensions HD / 4 g on.
   static __device__ __forceinline__ int key_at(int r, int g) { return F::key_code(r, HD / 4 * g); }
-  __device__ __forceinline__ void load(const uint8_t* pool, const size_t* tile, int lane) {
+  __device__ __forceinline__ void load_keys(const uint8_t* pool, const size_t* tile, int lane) {
     const int r = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const uint8_t* t = pool + tile[b] * F::kTile;
       words<P>(t + key_at(r, g), k[b]);
       ks[b] = t[F::key_scale(r, HD / 4 * g / 32)];
+    }
+  }
+  __device__ __forceinline__ void load_values(const uint8_t* pool, const size_t* tile, int lane) {
+    const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const uint8_t* t = pool + tile[b] * F::kTile;
       words<P>(t + F::value_word(g, r, 0), v[b]);
       words<P>(t + F::value_scales(g, 0), vs[b]);
     }
+  }
+  __device__ __forceinline__ void load(const uint8_t* pool, const size_t* tile, int lane) {
+    load_keys(pool, tile, lane);
+    load_values(pool, tile, lane);
   }
   // Part c of block b's keys as an operand.
   __device__ __forceinline__ uint4 key(int b, int c) const {
@@ -193,6 +204,88 @@ struct CacheParts {
   static constexpr int p = IO::kRaw ? 2 : 3;
 };
 
+// Positions 0 .. 3 of dimensions e (low nibbles) and e + 16 of a word, in fp16.
+__device__ __forceinline__ void value_halves_f16(uint32_t w, uint32_t scales, uint2& lo, uint2& hi) {
+  const uint32_t x0 = codes_to_f16<0>(w, scale_of<0>(scales)), x1 = codes_to_f16<1>(w, scale_of<1>(scales));
+  const uint32_t x2 = codes_to_f16<2>(w, scale_of<2>(scales)), x3 = codes_to_f16<3>(w, scale_of<3>(scales));
+  lo = make_uint2(__builtin_amdgcn_perm(x1, x0, 0x05040100u), __builtin_amdgcn_perm(x3, x2, 0x05040100u));
+  hi = make_uint2(__builtin_amdgcn_perm(x1, x0, 0x07060302u), __builtin_amdgcn_perm(x3, x2, 0x07060302u));
+}
+
+// Whether a word's values are not all exact in fp16: a scale outside 2^-18 ..
+// 2^13 (bytes 109 .. 140: a byte out of that range leaves a top bit, and the
+// lowest such byte has no borrow from below) with codes that are not zero, or a
+// NaN.
+__device__ __forceinline__ bool beyond_f16(uint32_t w, uint32_t scales) {
+  return (((scales - 0x6D6D6D6Du) & 0xE0E0E0E0u) != 0) & (((w & 0x77777777u) | nan_bytes(scales)) != 0);
+}
+
+// The eight probabilities of a step, rounded to fp16, as one operand part; taken
+// from v.
+__device__ __forceinline__ uint4 next_part_f16(float* v) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const f16x2_t x = __builtin_convertvector((f32x2_t{v[2 * j], v[2 * j + 1]}), f16x2_t);
+    w[j] = __builtin_bit_cast(uint32_t, x);
+    v[2 * j] -= static_cast<float>(x.x);
+    v[2 * j + 1] -= static_cast<float>(x.y);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ f32x4_t mma_f16(f32x4_t acc, uint4 a, uint4 b) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), acc, 0, 0, 0);
+}
+
+constexpr uint4 kHalfOnes{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};  // eight fp16 ones
+
+template <class IO>
+struct HalfParts {
+  static constexpr int p = IO::kRaw ? 1 : 2;
+};
+constexpr int kLift = 7;
+
+// Online softmax of a wave's column tiles as softmax_step, without the sum:
+// scores S to probabilities p.
+template <int NT, int NE>
+__device__ __forceinline__ void lifted_softmax(const f32x4_t (*S)[2], float qscale, float* m, f32x4_t* l, f32x4_t (*O)[NE],
+                                             float (*p)[8]) {
+  const auto highest = [](const float* x) {
+    return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+  };
+  bool over = false;
+#pragma unroll
+  for (int jt = 0; jt < NT; ++jt) {
+#pragma unroll
+    for (int r = 0; r < 8; ++r) p[jt][r] = fmaf(S[jt][r / 4][r % 4], qscale, -m[jt]);
+    over |= highest(p[jt]) > kLift + kRaise;
+  }
+  if (__ballot(over) != 0) {
+#pragma unroll
+    for (int jt = 0; jt < NT; ++jt) {
+#pragma unroll
+      for (int r = 0; r < 8; ++r) p[jt][r] = S[jt][r / 4][r % 4] * qscale;
+      float mx = highest(p[jt]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float up = fmaxf(m[jt], mx - kLift);
+      const float alpha = __builtin_amdgcn_exp2f(m[jt] - up);
+      m[jt] = up;
+      l[jt] *= alpha;
+#pragma unroll
+      for (int e = 0; e < NE; ++e) O[jt][e] *= alpha;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) p[jt][r] = fmaf(S[jt][r / 4][r % 4], qscale, -up);
+    }
+  }
+#pragma unroll
+  for (int jt = 0; jt < NT; ++jt)
+#pragma unroll
+    for (int r = 0; r < 8; ++r) p[jt][r] = __builtin_amdgcn_exp2f(p[jt][r]);
+}
+
 template <class IO, int HD, int NT>
 struct CacheSmem {
   union {
@@ -216,9 +309,28 @@ __device__ __forceinline__ void query_operand(const CacheAttnArgs& a, const Tree
   query_parts<BF16, IO>(p, out);
 }
 
+// Scores of a step whose keys lie in registers, before their scale.  q(jt, c,
+// part): a piece of the queries.
+template <class IO, int HD, int NT, class Queries>
+__device__ __forceinline__ void key_products(const CacheStep<HD>& B, const Queries& q, f32x4_t (*S)[2]) {
+#pragma unroll
+  for (int jt = 0; jt < NT; ++jt)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) S[jt][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < HD / 32; ++c)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const uint4 x = B.key(b, c);
+#pragma unroll
+      for (int jt = 0; jt < NT; ++jt)
+#pragma unroll
+        for (int k = 0; k < CacheParts<IO>::q; ++k) S[jt][b] = BF16::mma(S[jt][b], x, q(jt, c, k));
+    }
+}
+
 // One step of a wave whose keys and values lie in registers: 16 NT columns, the
-// blocks at i and i + 1 (< hi).  q(jt, c, part): a piece of the queries; all,
-// some: positions that every column of the group sees, and that one of them
+// blocks at i and i + 1 (< hi).  all, some: positions that every column of the group sees, and that one of them
 // does; seen: that this lane's columns do.
 template <class IO, int HD, int NT, class Queries>
 __device__ __forceinline__ void cache_step(const CacheAttnArgs& a, CacheStep<HD>& B, int i, int hi, int all, int some,
@@ -228,20 +340,7 @@ __device__ __forceinline__ void cache_step(const CacheAttnArgs& a, CacheStep<HD>
   constexpr int P = HD / 32, NE = HD / 16;
   const int g = lane >> 4;
   f32x4_t S[NT][2];
-#pragma unroll
-  for (int jt = 0; jt < NT; ++jt)
-#pragma unroll
-    for (int b = 0; b < 2; ++b) S[jt][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int c = 0; c < P; ++c)
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const uint4 x = B.key(b, c);
-#pragma unroll
-      for (int jt = 0; jt < NT; ++jt)
-#pragma unroll
-        for (int k = 0; k < Parts::q; ++k) S[jt][b] = BF16::mma(S[jt][b], x, q(jt, c, k));
-    }
+  key_products<IO, HD, NT>(B, q, S);
   // A step that reaches past what all columns see, or past hi, is masked.
   const bool tail = 16 * (i + 2) > all || i + 2 > hi;
   uint32_t sees[NT][2], odd[2][P];
@@ -278,12 +377,14 @@ __device__ __forceinline__ void cache_step(const CacheAttnArgs& a, CacheStep<HD>
 
 // Up to 32 columns: the four waves of a work-group take runs of the split's
 // blocks, K and V go straight into registers, and the waves' results are merged
-// through LDS, the splits' by the one that arrives last.
+// through LDS, the splits' by the one that arrives last.  A wave that meets a
+// value that fp16 does not hold exactly, or a NaN that not all columns see,
+// starts its run over with cache_step.
 template <class IO, int HD, int NT>
-__global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
+__global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_cache_attn(CacheAttnArgs a) {
   using Step = CacheStep<HD>;
   using Parts = CacheParts<IO>;
-  constexpr int NF = HD / 32, NE = HD / 16, EPW = NE / 4, CW = 16 * NT;
+  constexpr int NF = HD / 32, NE = HD / 16, EPW = NE / 4, CW = 16 * NT, P = Step::P;
   __shared__ CacheSmem<IO, HD, NT> sm;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -314,47 +415,128 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
   const int some = t.len + 1 + (min(t.cols, c0 + CW) - 1) / a.G;
   __syncthreads();
 
-  f32x4_t O[NT][NE];
-  float m[NT], l[NT];
+  f32x4_t O[NT][NE], l[NT];  // l: the sum, in every register
+  float m[NT];
+  const auto reset = [&] {
 #pragma unroll
-  for (int jt = 0; jt < NT; ++jt) {
-    m[jt] = kTreeFloor;
-    l[jt] = 0.f;
+    for (int jt = 0; jt < NT; ++jt) {
+      m[jt] = kTreeFloor;
+      l[jt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < NE; ++e) O[jt][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
-
+      for (int e = 0; e < NE; ++e) O[jt][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+  };
   const auto tile_of = [&](int i) {
     return static_cast<size_t>(__builtin_amdgcn_readlane(ids, (i - lo) & 63)) * a.Hkv + kvh;
   };
   // The blocks of the step at i; a missing second one re-reads the first, masked.
-  const auto fetch = [&](Step& B, int i) {
+  size_t tile[2] = {};
+  const auto find = [&](int i) {
     if (((i - lo) & 63) == 0 && i != lo) ids = ask(i + lane);
-    const size_t tile[2] = {tile_of(i), tile_of(i + 1 < hi ? i + 1 : i)};
-    B.load(a.pool, tile, lane);
+    tile[0] = tile_of(i);
+    tile[1] = tile_of(i + 1 < hi ? i + 1 : i);
   };
   const auto queries = [&](int jt, int c, int k) { return sm.q[jt][c][k][lane]; };
-  const auto compute = [&](Step& B, int i) {
-    cache_step<IO, HD, NT>(a, B, i, hi, all, some, seen, queries, m, l, O, lane);
+  bool beyond = false;  // (uniform)
+  // A step's key registers take the next step's keys as soon as its scores are
+  // there, the value registers the next values after its outputs.
+  Step B;
+  const auto compute = [&](int i, bool more, auto tail) {
+    f32x4_t S[NT][2];
+    key_products<IO, HD, NT>(B, queries, S);
+    if (more) {
+      find(i + 2);
+      B.load_keys(a.pool, tile, lane);
+    }
+    if constexpr (decltype(tail)::value) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int pos = 16 * (i + b) + 4 * g;
+        const uint32_t keep = byte_mask(i + b < hi ? live_bits(pos, some) : 0u);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          B.v[b][p] &= keep;
+          B.vs[b][p] = (B.vs[b][p] & keep) | (0x7F7F7F7Fu & ~keep);
+        }
+#pragma unroll
+        for (int jt = 0; jt < NT; ++jt) {
+          const uint32_t sees = i + b < hi ? live_bits(pos, seen[jt]) : 0u;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) S[jt][b][r] = sees >> r & 1 ? S[jt][b][r] : -INFINITY;
+        }
+      }
+    }
+    uint32_t out = 0;  // scales that may not do: see beyond_f16
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int p = 0; p < P; ++p) out |= (B.vs[b][p] - 0x6D6D6D6Du) & 0xE0E0E0E0u;
+    if (__ballot(out != 0) != 0) {
+      asm volatile("");  // (keeps what follows behind the branch)
+      bool x = false;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int p = 0; p < P; ++p) x |= beyond_f16(B.v[b][p], B.vs[b][p]);
+      beyond |= __ballot(x) != 0;
+    }
+    float p[NT][8];
+    lifted_softmax<NT, NE>(S, a.qscale, m, l, O, p);
+    uint4 pp[NT][HalfParts<IO>::p];
+#pragma unroll
+    for (int jt = 0; jt < NT; ++jt)
+#pragma unroll
+      for (int q = 0; q < HalfParts<IO>::p; ++q) {
+        pp[jt][q] = next_part_f16(p[jt]);
+        l[jt] = mma_f16(l[jt], kHalfOnes, pp[jt][q]);
+      }
+#pragma unroll
+    for (int w = 0; w < P; ++w) {
+      uint2 lo2[2], hi2[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) value_halves_f16(B.v[b][w], B.vs[b][w], lo2[b], hi2[b]);
+      const uint4 x0 = make_uint4(lo2[0].x, lo2[0].y, lo2[1].x, lo2[1].y), x1 = make_uint4(hi2[0].x, hi2[0].y, hi2[1].x, hi2[1].y);
+#pragma unroll
+      for (int q = 0; q < HalfParts<IO>::p; ++q)
+#pragma unroll
+        for (int jt = 0; jt < NT; ++jt) {
+          O[jt][2 * w] = mma_f16(O[jt][2 * w], x0, pp[jt][q]);
+          O[jt][2 * w + 1] = mma_f16(O[jt][2 * w + 1], x1, pp[jt][q]);
+        }
+    }
+    if (more) B.load_values(a.pool, tile, lane);
   };
-  Step A, B;
-  if (lo < hi) fetch(A, lo);
-  for (int i = lo; i < hi; i += 4) {
-    if (i + 2 < hi) fetch(B, i + 2);
-    compute(A, i);
-    if (i + 2 >= hi) break;
-    if (i + 4 < hi) fetch(A, i + 4);
-    compute(B, i + 2);
+  reset();
+  // Whole steps without a mask, then the rest with one.
+  const int whole = lo + max(0, min(hi, all / 16) - lo) / 2 * 2;
+  if (lo < hi) {
+    find(lo);
+    B.load(a.pool, tile, lane);
+  }
+  int i = lo;
+  for (; i < whole; i += 2) compute(i, i + 2 < hi, std::false_type{});
+  for (; i < hi; i += 2) compute(i, i + 2 < hi, std::true_type{});
+  if (beyond) {
+    reset();
+    float sum[NT] = {};
+    ids = ask(lo + lane);
+    for (i = lo; i < hi; i += 2) {
+      find(i);
+      B.load(a.pool, tile, lane);
+      cache_step<IO, HD, NT>(a, B, i, hi, all, some, seen, queries, m, sum, O, lane);
+    }
+#pragma unroll
+    for (int jt = 0; jt < NT; ++jt) {
+      sum[jt] += __shfl_xor(sum[jt], 16);
+      l[jt][0] = sum[jt] + __shfl_xor(sum[jt], 32);
+    }
   }
 
   // Merge of the four waves, column tile by column tile; wave w combines and
   // stores output operands [w EPW, (w + 1) EPW).
 #pragma unroll
-  for (int jt = 0; jt < NT; ++jt) {
-    l[jt] += __shfl_xor(l[jt], 16);
-    l[jt] += __shfl_xor(l[jt], 32);
-    if (g == 0) sm.sml[wave][jt][h] = make_float2(m[jt], l[jt]);
-  }
+  for (int jt = 0; jt < NT; ++jt)
+    if (g == 0) sm.sml[wave][jt][h] = make_float2(m[jt], l[jt][0]);
   const CoherentBuffer pb(a.part, a.part_bytes);
   const uint32_t item = (static_cast<uint32_t>(t.item) * a.Hkv + kvh) * CW * (HD + 4) * 4;
 #pragma unroll
@@ -401,41 +583,6 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn(CacheAttnArgs a) {
 
 // ---------------------------------------------------------------------------
 
-// Positions 0 .. 3 of dimensions e (low nibbles) and e + 16 of a word, in fp16.
-__device__ __forceinline__ void value_halves_f16(uint32_t w, uint32_t scales, uint2& lo, uint2& hi) {
-  const uint32_t x0 = codes_to_f16<0>(w, scale_of<0>(scales)), x1 = codes_to_f16<1>(w, scale_of<1>(scales));
-  const uint32_t x2 = codes_to_f16<2>(w, scale_of<2>(scales)), x3 = codes_to_f16<3>(w, scale_of<3>(scales));
-  lo = make_uint2(__builtin_amdgcn_perm(x1, x0, 0x05040100u), __builtin_amdgcn_perm(x3, x2, 0x05040100u));
-  hi = make_uint2(__builtin_amdgcn_perm(x1, x0, 0x07060302u), __builtin_amdgcn_perm(x3, x2, 0x07060302u));
-}
-
-// Whether a word's values are not all exact in fp16: a scale outside 2^-18 ..
-// 2^13 (bytes 109 .. 140: a byte out of that range leaves a top bit, and the
-// lowest such byte has no borrow from below) with codes that are not zero, or a
-// NaN.
-__device__ __forceinline__ bool beyond_f16(uint32_t w, uint32_t scales) {
-  return (((scales - 0x6D6D6D6Du) & 0xE0E0E0E0u) != 0) & (((w & 0x77777777u) | nan_bytes(scales)) != 0);
-}
-
-// The eight probabilities of a step, rounded to fp16, as one operand part; taken
-// from v.
-__device__ __forceinline__ uint4 next_part_f16(float* v) {
-  uint32_t w[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const f16x2_t x = __builtin_convertvector((f32x2_t{v[2 * j], v[2 * j + 1]}), f16x2_t);
-    w[j] = __builtin_bit_cast(uint32_t, x);
-    v[2 * j] -= static_cast<float>(x.x);
-    v[2 * j + 1] -= static_cast<float>(x.y);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
-__device__ __forceinline__ f32x4_t mma_f16(f32x4_t acc, uint4 a, uint4 b) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), acc, 0, 0, 0);
-}
-
 // More than 32 columns.  Work-group: a request's column group of 64 NT columns
 // (16 NT per wave) over the blocks of one split.  The waves share every
 // block through LDS: keys as codes, which each wave expands to bf16 in
@@ -450,51 +597,6 @@ __device__ __forceinline__ f32x4_t mma_f16(f32x4_t acc, uint4 a, uint4 b) {
 // value that fp16 does not hold exactly, or a NaN that not all columns see, the
 // work-group starts over, its waves reading the blocks themselves as the other
 // kernel's do.
-template <class IO>
-struct WideParts {
-  static constexpr int p = IO::kRaw ? 1 : 2;
-};
-constexpr int kWideLift = 7;
-
-// Online softmax of a wave's column tiles as softmax_step, without the sum:
-// scores S to probabilities p.
-template <int NT, int NE>
-__device__ __forceinline__ void wide_softmax(const f32x4_t (*S)[2], float qscale, float* m, f32x4_t* l, f32x4_t (*O)[NE],
-                                             float (*p)[8]) {
-  const auto highest = [](const float* x) {
-    return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-  };
-  bool over = false;
-#pragma unroll
-  for (int jt = 0; jt < NT; ++jt) {
-#pragma unroll
-    for (int r = 0; r < 8; ++r) p[jt][r] = fmaf(S[jt][r / 4][r % 4], qscale, -m[jt]);
-    over |= highest(p[jt]) > kWideLift + kRaise;
-  }
-  if (__ballot(over) != 0) {
-#pragma unroll
-    for (int jt = 0; jt < NT; ++jt) {
-#pragma unroll
-      for (int r = 0; r < 8; ++r) p[jt][r] = S[jt][r / 4][r % 4] * qscale;
-      float mx = highest(p[jt]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float up = fmaxf(m[jt], mx - kWideLift);
-      const float alpha = __builtin_amdgcn_exp2f(m[jt] - up);
-      m[jt] = up;
-      l[jt] *= alpha;
-#pragma unroll
-      for (int e = 0; e < NE; ++e) O[jt][e] *= alpha;
-#pragma unroll
-      for (int r = 0; r < 8; ++r) p[jt][r] = fmaf(S[jt][r / 4][r % 4], qscale, -up);
-    }
-  }
-#pragma unroll
-  for (int jt = 0; jt < NT; ++jt)
-#pragma unroll
-    for (int r = 0; r < 8; ++r) p[jt][r] = __builtin_amdgcn_exp2f(p[jt][r]);
-}
-
 template <class IO, int HD, int NT>
 __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
   using F = Mx4<HD>;
@@ -659,20 +761,20 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
   };
   const auto outputs = [&](const Scores& S, const uint4* from) {
     float p[NT][8];
-    wide_softmax<NT, NE>(S.x, a.qscale, m, l, O, p);
-    uint4 pp[NT][WideParts<IO>::p];
+    lifted_softmax<NT, NE>(S.x, a.qscale, m, l, O, p);
+    uint4 pp[NT][HalfParts<IO>::p];
 #pragma unroll
     for (int jt = 0; jt < NT; ++jt)
 #pragma unroll
-      for (int q = 0; q < WideParts<IO>::p; ++q) {
+      for (int q = 0; q < HalfParts<IO>::p; ++q) {
         pp[jt][q] = next_part_f16(p[jt]);
-        l[jt] = mma_f16(l[jt], make_uint4(0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u), pp[jt][q]);
+        l[jt] = mma_f16(l[jt], kHalfOnes, pp[jt][q]);
       }
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
       const uint4 x = from[e * 64 + lane];
 #pragma unroll
-      for (int q = 0; q < WideParts<IO>::p; ++q)
+      for (int q = 0; q < HalfParts<IO>::p; ++q)
 #pragma unroll
         for (int jt = 0; jt < NT; ++jt) O[jt][e] = mma_f16(O[jt][e], x, pp[jt][q]);
     }
@@ -682,7 +784,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
     __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
     __builtin_amdgcn_sched_group_barrier(0x402, NT * 12, 0);
     const auto group = [](auto) {
-      __builtin_amdgcn_sched_group_barrier(0x8, NT * WideParts<IO>::p, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, NT * HalfParts<IO>::p, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     };
     static_for<NE>(group);
