@@ -50,16 +50,25 @@ struct CacheItem {
 template <int CW>
 __device__ __forceinline__ CacheItem cache_item(const CacheAttnArgs& a, int f) {
   const int lane = threadIdx.x & 63;
-  int rank = 0;
-  for (int k = 0; k < a.n; k += 64)
-    rank += __popcll(__ballot(k + lane < a.n && a.item0[min(k + lane, a.n - 1) + 1] <= f));
-  const int r = __builtin_amdgcn_readfirstlane(rank);
   CacheItem t;
-  t.item0 = a.item0[r];
-  t.cg0 = a.cg0[r];
-  t.len = a.len[r];
-  t.row0 = a.row0[r];
-  t.cols = a.rows[r] * a.G;
+  int slot;
+  // Lane = request, 64 at a time and all of them at once: one trip to memory.
+  for (int k = 0;; k += 64) {
+    const int r = min(k + lane, a.n - 1);
+    const int item0 = a.item0[r], item1 = a.item0[r + 1], cg0 = a.cg0[r], len = a.len[r], row0 = a.row0[r];
+    const int rows = a.rows[r], slots = a.slot[r];
+    // Request: the number of requests whose items all precede f.
+    const int before = __popcll(__ballot(k + lane < a.n && item1 <= f));
+    if (before == 64 && k + 64 < a.n) continue;
+    const auto mine = [&](int v) { return __builtin_amdgcn_readlane(v, before); };
+    t.item0 = mine(item0);
+    t.cg0 = mine(cg0);
+    t.len = mine(len);
+    t.row0 = mine(row0);
+    t.cols = mine(rows) * a.G;
+    slot = mine(slots);
+    break;
+  }
   t.ncg = (t.cols + CW - 1) / CW;
   // Column groups of one split run side by side and share its blocks.  Later rows
   // see more: the groups go down from the last one, and the second half of them
@@ -72,7 +81,7 @@ __device__ __forceinline__ CacheItem cache_item(const CacheAttnArgs& a, int f) {
   t.nsplit = (t.nblk + a.bps - 1) / a.bps;
   t.first = a.bps * s;
   t.count = min(t.nblk - t.first, a.bps);
-  t.btrow = a.bt + static_cast<size_t>(a.slot[r]) * a.mb;
+  t.btrow = a.bt + static_cast<size_t>(slot) * a.mb;
   return t;
 }
 __device__ __forceinline__ int pool_id(const CacheAttnArgs& a, int id) {
@@ -381,7 +390,7 @@ __device__ __forceinline__ void cache_step(const CacheAttnArgs& a, CacheStep<HD>
 // value that fp16 does not hold exactly, or a NaN that not all columns see,
 // starts its run over with cache_step.
 template <class IO, int HD, int NT>
-__global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_cache_attn(CacheAttnArgs a) {
+__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_cache_attn(CacheAttnArgs a) {
   using Step = CacheStep<HD>;
   using Parts = CacheParts<IO>;
   constexpr int NF = HD / 32, NE = HD / 16, EPW = NE / 4, CW = 16 * NT, P = Step::P;
@@ -397,6 +406,28 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_cache_attn(CacheAttnAr
   const int lo = t.first + min(t.count, wave * run), hi = t.first + min(t.count, (wave + 1) * run);
   const auto ask = [&](int i) { return pool_id(a, i < hi ? t.btrow[i] : 0); };
   int ids = ask(lo + lane);  // of the next 64 blocks of the run
+
+  const auto tile_of = [&](int i) {
+    return static_cast<size_t>(__builtin_amdgcn_readlane(ids, (i - lo) & 63)) * a.Hkv + kvh;
+  };
+  // The blocks of the step at i; a missing second one re-reads the first, masked.
+  size_t tile[2] = {};
+  const auto find = [&](int i) {
+    if (((i - lo) & 63) == 0 && i != lo) ids = ask(i + lane);
+    tile[0] = tile_of(i);
+    tile[1] = tile_of(i + 1 < hi ? i + 1 : i);
+  };
+  // A step's key registers take the next but one's keys as soon as its scores are
+  // there, the value registers the values after its outputs.
+  Step X, Y;
+  if (lo < hi) {
+    find(lo);
+    X.load(a.pool, tile, lane);
+  }
+  if (lo + 2 < hi) {
+    find(lo + 2);
+    Y.load(a.pool, tile, lane);
+  }
 
   const int c0 = CW * t.cg;
 #pragma unroll
@@ -426,26 +457,13 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_cache_attn(CacheAttnAr
       for (int e = 0; e < NE; ++e) O[jt][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
   };
-  const auto tile_of = [&](int i) {
-    return static_cast<size_t>(__builtin_amdgcn_readlane(ids, (i - lo) & 63)) * a.Hkv + kvh;
-  };
-  // The blocks of the step at i; a missing second one re-reads the first, masked.
-  size_t tile[2] = {};
-  const auto find = [&](int i) {
-    if (((i - lo) & 63) == 0 && i != lo) ids = ask(i + lane);
-    tile[0] = tile_of(i);
-    tile[1] = tile_of(i + 1 < hi ? i + 1 : i);
-  };
   const auto queries = [&](int jt, int c, int k) { return sm.q[jt][c][k][lane]; };
   bool beyond = false;  // (uniform)
-  // A step's key registers take the next step's keys as soon as its scores are
-  // there, the value registers the next values after its outputs.
-  Step B;
-  const auto compute = [&](int i, bool more, auto tail) {
+  const auto compute = [&](Step& B, int i, bool more, auto tail) {
     f32x4_t S[NT][2];
     key_products<IO, HD, NT>(B, queries, S);
     if (more) {
-      find(i + 2);
+      find(i + 4);
       B.load_keys(a.pool, tile, lane);
     }
     if constexpr (decltype(tail)::value) {
@@ -509,21 +527,23 @@ __global__ __launch_bounds__(256, NT == 1 ? 4 : 2) void k_cache_attn(CacheAttnAr
   reset();
   // Whole steps without a mask, then the rest with one.
   const int whole = lo + max(0, min(hi, all / 16) - lo) / 2 * 2;
-  if (lo < hi) {
-    find(lo);
-    B.load(a.pool, tile, lane);
-  }
   int i = lo;
-  for (; i < whole; i += 2) compute(i, i + 2 < hi, std::false_type{});
-  for (; i < hi; i += 2) compute(i, i + 2 < hi, std::true_type{});
+  for (; i + 2 < whole; i += 4) {
+    compute(X, i, i + 4 < hi, std::false_type{});
+    compute(Y, i + 2, i + 6 < hi, std::false_type{});
+  }
+  for (; i < hi; i += 4) {
+    compute(X, i, i + 4 < hi, std::true_type{});
+    if (i + 2 < hi) compute(Y, i + 2, i + 6 < hi, std::true_type{});
+  }
   if (beyond) {
     reset();
     float sum[NT] = {};
     ids = ask(lo + lane);
     for (i = lo; i < hi; i += 2) {
       find(i);
-      B.load(a.pool, tile, lane);
-      cache_step<IO, HD, NT>(a, B, i, hi, all, some, seen, queries, m, sum, O, lane);
+      X.load(a.pool, tile, lane);
+      cache_step<IO, HD, NT>(a, X, i, hi, all, some, seen, queries, m, sum, O, lane);
     }
 #pragma unroll
     for (int jt = 0; jt < NT; ++jt) {

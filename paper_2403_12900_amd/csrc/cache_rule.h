@@ -249,7 +249,10 @@ constexpr int kCacheSplits = 64;
 // Splits hold `least` blocks (a step of every wave that walks blocks) until
 // the launch has more than `slots` resident work-groups take at once; they
 // grow further while the partials exceed `floats` or a request has more than
-// kCacheSplits.  No splits where the column groups alone exceed `counters`.
+// kCacheSplits.  No splits where the column groups alone are as many, unless one
+// request is far longer than a slot's share (32 requests of 32 heads, 80 to 1450
+// positions: 21.5 us, with splits 22.5; one of 20000 among them would alone take
+// that many steps), nor where there are more of them than `counters`.
 inline CacheSplit cache_split(const CacheInfo& t, int G, int Hkv, int hd, int cw, int least, int slots, size_t floats,
                               int counters) {
   CacheSplit s;
@@ -266,8 +269,9 @@ inline CacheSplit cache_split(const CacheInfo& t, int G, int Hkv, int hd, int cw
   }
   s.groups = static_cast<int>(cg);
   const int64_t per = static_cast<int64_t>(Hkv) * cw * (hd + 4);
-  const bool whole = cg * Hkv > counters || cg * Hkv >= slots;
-  int64_t bps = whole ? blocks_of(s.order[0]) : std::max<int64_t>(1, (blocks * Hkv + slots - 1) / slots);
+  const int64_t share = std::max<int64_t>(1, (blocks * Hkv + slots - 1) / slots), longest = blocks_of(s.order[0]);
+  const bool whole = cg * Hkv > counters || (cg * Hkv >= slots && longest <= 4 * share);
+  int64_t bps = whole ? longest : share;
   // Rounding every request up to whole splits can leave more work-groups than
   // stay resident; splits up to twice as long that fit them into one round are
   // taken, but not longer ones.
