@@ -159,8 +159,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                        ("spr_cache_append", [vp, kv4, i32, rows, rotary, i32, vp, i64, vp, i64]),
                        ("spr_cache_read", [vp, kv4, i32, rows, i32, vp, i64, vp, i64]),
                        ("spr_cache_attention", [vp, kv4, i32, rows, i32, i32, vp, i64, vp, i64]),
-                       ("spr_cache_fork", [vp, pages, i32, _I32P, _I32P, _I32P, _I32P]),
-                       ("spr_cache_move", [vp, pages, i32, _I32P, _I32P])):
+                       ("spr_cache_fork", [vp, pages, i32, vp, vp, vp, vp]),
+                       ("spr_cache_move", [vp, pages, i32, vp, vp])):
         getattr(L, name).restype = ctypes.c_int
         getattr(L, name).argtypes = args
     L.spr_release.restype = ctypes.c_int

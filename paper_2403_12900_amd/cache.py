@@ -12,8 +12,12 @@ from typing import Optional, Sequence, Union
 import numpy as np
 import torch
 
-from .binding import SprCacheBatch, SprKv4View, SprPages, SprRotary, _check, _ptr, load_library
+from .binding import SPR_OK, SprCacheBatch, SprKv4View, SprPages, SprRotary, _check, _ptr, load_library
 from .tree import _DTYPES, KVView, OpHandle, _int32, _refuse
+
+
+def _address(a: np.ndarray) -> int:
+    return a.__array_interface__["data"][0]
 
 
 class KV4View:
@@ -81,55 +85,61 @@ class CacheOps(OpHandle):
     def rotary(self, rotary: Rotary, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None):
         """Rotary positions (spr_cache_rotary): x [rows, heads, head_dim], fp32 or bf16, rows at any stride, positions int32
         [rows]; returns out like it (which may be x itself)."""
-        if x.dim() != 3 or x.dtype not in _DTYPES:
+        dtype = _DTYPES.get(x.dtype)
+        if x.dim() != 3 or dtype is None:
             _refuse("cache rotary: x must be [rows, heads, head_dim], fp32 or bf16")
         self._no_grad("cache rotary", x)
         rows, heads, hd = x.shape
         p_positions = self._vector("cache rotary: positions", positions, torch.int32, rows)
-        out = self._out("cache rotary", x, out)
-        xs, os = self._row_stride("cache rotary", x, heads, hd), self._row_stride("cache rotary", out, heads, hd)
+        xs = self._row_stride("cache rotary", x, heads, hd)
+        out, os = self._out("cache rotary", x, out, heads, hd)
         self._enter()
-        _check(self.lib.spr_cache_rotary(self.h, rotary.ref, rows, heads, hd, _DTYPES[x.dtype], p_positions, x.data_ptr(), xs,
-                                         out.data_ptr(), os))
+        self._done(self.lib.spr_cache_rotary(self.h, rotary.ref, rows, heads, hd, dtype, p_positions, x.data_ptr(), xs,
+                                             out.data_ptr(), os))
         return out
 
     def append(self, kv: KV4View, layer: int, batch: CacheBatch, k: torch.Tensor, v: torch.Tensor, rotary: Optional[Rotary] = None):
         """Writes the rows' keys and values (spr_cache_append): k and v [rows, KV heads, head_dim], fp32 or bf16, rows at any
         stride; keys are turned at their cache positions first where rotary is given."""
-        shape = (batch.rows, kv.n_kv_heads, kv.head_dim)
-        if k.shape != shape or v.shape != shape or k.dtype not in _DTYPES or v.dtype != k.dtype:
+        shape, dtype = (batch.rows, kv.n_kv_heads, kv.head_dim), _DTYPES.get(k.dtype)
+        if k.shape != shape or v.shape != shape or dtype is None or v.dtype != k.dtype:
             _refuse("cache append: k and v must be [rows, kv_heads, head_dim] of one type, fp32 or bf16")
-        self._no_grad("cache append", k, v)
-        ks, vs = (self._row_stride("cache append", t, *shape[1:]) for t in (k, v))
+        self._no_grad("cache append", k)
+        self._no_grad("cache append", v)
+        ks = self._row_stride("cache append", k, shape[1], shape[2])
+        vs = self._row_stride("cache append", v, shape[1], shape[2])
         self._same_device("cache append", kv)
         self._enter()
-        _check(self.lib.spr_cache_append(self.h, kv.ref, layer, batch.ref, None if rotary is None else rotary.ref,
-                                         _DTYPES[k.dtype], k.data_ptr(), ks, v.data_ptr(), vs))
+        self._done(self.lib.spr_cache_append(self.h, kv.ref, layer, batch.ref, None if rotary is None else rotary.ref, dtype,
+                                             k.data_ptr(), ks, v.data_ptr(), vs))
 
     def read(self, kv: KV4View, layer: int, batch: CacheBatch, dtype: torch.dtype = torch.float32):
         """The values that the cache holds at the rows (spr_cache_read): k and v [rows, KV heads, head_dim]."""
-        if dtype not in _DTYPES:
+        code = _DTYPES.get(dtype)
+        if code is None:
             _refuse("cache read: dtype must be fp32 or bf16")
         self._same_device("cache read", kv)
-        width = kv.n_kv_heads * kv.head_dim
-        k, v = (torch.empty(batch.rows, kv.n_kv_heads, kv.head_dim, dtype=dtype, device=kv.data.device) for _ in range(2))
+        heads, hd = kv.n_kv_heads, kv.head_dim
+        k, v = torch.empty((2, batch.rows, heads, hd), dtype=dtype, device=kv.data.device).unbind(0)
         self._enter()
-        _check(self.lib.spr_cache_read(self.h, kv.ref, layer, batch.ref, _DTYPES[dtype], k.data_ptr(), width, v.data_ptr(), width))
+        self._done(self.lib.spr_cache_read(self.h, kv.ref, layer, batch.ref, code, k.data_ptr(), heads * hd, v.data_ptr(),
+                                           heads * hd))
         return k, v
 
     def attention(self, kv: KV4View, layer: int, batch: CacheBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None):
         """Attention of the rows over the cache (spr_cache_attention): q [rows, heads, head_dim], fp32 or bf16, rows at any
         stride; returns out like it."""
-        if q.dim() != 3 or q.shape[0] != batch.rows or q.shape[2] != kv.head_dim or q.dtype not in _DTYPES:
+        hd, dtype = kv.head_dim, _DTYPES.get(q.dtype)
+        if q.dim() != 3 or q.shape[0] != batch.rows or q.shape[2] != hd or dtype is None:
             _refuse("cache attention: q must be [rows, heads, head_dim], fp32 or bf16")
         self._no_grad("cache attention", q)
-        _, heads, hd = q.shape
-        out = self._out("cache attention", q, out)
-        qs, os = self._row_stride("cache attention", q, heads, hd), self._row_stride("cache attention", out, heads, hd)
+        heads = q.shape[1]
+        qs = self._row_stride("cache attention", q, heads, hd)
+        out, os = self._out("cache attention", q, out, heads, hd)
         self._same_device("cache attention", kv)
         self._enter()
-        _check(self.lib.spr_cache_attention(self.h, kv.ref, layer, batch.ref, heads, _DTYPES[q.dtype], q.data_ptr(), qs,
-                                            out.data_ptr(), os))
+        self._done(self.lib.spr_cache_attention(self.h, kv.ref, layer, batch.ref, heads, dtype, q.data_ptr(), qs,
+                                                out.data_ptr(), os))
         return out
 
     def fork(self, kv: Union[KV4View, KVView], source: Sequence[int], target: Sequence[int], lens: Sequence[int],
@@ -142,7 +152,7 @@ class CacheOps(OpHandle):
             _refuse("cache fork: source, target, lens and fresh must be of one length")
         pages = self._pages("cache fork", kv)
         self._enter()
-        _check(self.lib.spr_cache_fork(self.h, pages, len(a[0]), *(_ptr(x) for x in a)))
+        self._done(self.lib.spr_cache_fork(self.h, pages, len(a[0]), *map(_address, a)))
 
     def move(self, kv: Union[KV4View, KVView], src: Sequence[int], dst: Sequence[int]):
         """Moves blocks src[i] to dst[i] in every layer, and the table's entries with them (spr_cache_move).  Any paged cache."""
@@ -151,29 +161,38 @@ class CacheOps(OpHandle):
             _refuse("cache move: src and dst must be of one length")
         pages = self._pages("cache move", kv)
         self._enter()
-        _check(self.lib.spr_cache_move(self.h, pages, len(a[0]), *(_ptr(x) for x in a)))
+        self._done(self.lib.spr_cache_move(self.h, pages, len(a[0]), *map(_address, a)))
 
     def _pages(self, what, kv):
         self._same_device(what, kv)
-        k, v = (kv.data, None) if isinstance(kv, KV4View) else (kv.k, kv.v)
-        layers, blocks, heads, tile = k.shape
-        return ctypes.byref(SprPages(k.data_ptr(), None if v is None else v.data_ptr(), heads * tile * k.element_size(), layers,
-                                     blocks, kv.block_table.data_ptr(), *kv.block_table.shape))
+        ref = getattr(kv, "_pages", None)
+        if ref is None:  # as lasting as the view's own record
+            k, v = (kv.data, None) if isinstance(kv, KV4View) else (kv.k, kv.v)
+            layers, blocks, heads, tile = k.shape
+            ref = kv._pages = ctypes.byref(SprPages(k.data_ptr(), None if v is None else v.data_ptr(),
+                                                    heads * tile * k.element_size(), layers, blocks, kv.block_table.data_ptr(),
+                                                    *kv.block_table.shape))
+        return ref
+
+    def _done(self, status):
+        if status != SPR_OK:
+            _check(status)
 
     def _same_device(self, what, kv):
         if kv.index != self.index:
             _refuse(f"{what}: the cache must be on {self.device}")
 
-    def _no_grad(self, what, *tensors):
-        if torch.is_grad_enabled() and any(t.requires_grad for t in tensors):
+    def _no_grad(self, what, x):
+        if x.requires_grad and torch.is_grad_enabled():
             _refuse(f"{what}: it has no gradient; detach its inputs, or call it under torch.no_grad()")
 
-    def _out(self, what, x, out):
+    def _out(self, what, x, out, heads, hd):
+        """The output, a new one like x if none is given, and its row stride."""
         if out is None:
-            return x.new_empty(x.shape)
+            return x.new_empty(x.shape), heads * hd
         if out.shape != x.shape or out.dtype != x.dtype:
             _refuse(f"{what}: out must be like its input")
-        return out
+        return out, self._row_stride(what, out, heads, hd)
 
     def _row_stride(self, what, t, heads, hd):
         row, head, one = t.stride()

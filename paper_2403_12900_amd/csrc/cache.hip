@@ -77,23 +77,29 @@ spr_status rows_call(spr_cache_ops* o, const char* what, const spr_kv4_view* kv,
     a.turned = 1;
     a.r = rotary_args(*rotary);
   }
+  const bool single = t.max_rows == 1;
   int tiles = 0;
   for (int i = 0; i < t.n; ++i) {
     a.slot[i] = t.slot[i];
     a.len[i] = t.len[i];
+    a.rows[i] = t.n_rows[i];
     a.row0[i] = t.row0[i];
     a.tile0[i] = tiles;
-    tiles += (t.len[i] + t.n_rows[i] - 1) / 16 - t.len[i] / 16 + 1;
+    tiles += single ? 1 : (t.len[i] + t.n_rows[i] - 1) / 16 - t.len[i] / 16 + 1;
   }
-  a.row0[t.n] = t.rows;
   a.tile0[t.n] = tiles;
-  const int at_once = 4 * (128 / kv->head_dim);
+  const int at_once = (single ? 16 : 1) * (128 / kv->head_dim);
   a.per = heads_per_group(tiles, a.Hkv, at_once, o->n_cu);
   const dim3 grid(tiles, (a.Hkv + a.per - 1) / a.per);
+  const auto launch = [&](auto n, auto hd, auto rg) {
+    constexpr int N = decltype(n)::value, HD = decltype(hd)::value, RG = decltype(rg)::value;
+    static_assert(kRowHeads<RG, HD> == (RG == 1 ? 16 : 1) * (128 / HD), "at_once");
+    if (append) k_cache_append<N, HD, RG><<<grid, 256, 0, o->st>>>(a);
+    else k_cache_read<N, HD, RG><<<grid, 256, 0, o->st>>>(a);
+  };
   const auto run = [&](auto n, auto hd) {
-    constexpr int N = decltype(n)::value, HD = decltype(hd)::value;
-    if (append) k_cache_append<N, HD><<<grid, 256, 0, o->st>>>(a);
-    else k_cache_read<N, HD><<<grid, 256, 0, o->st>>>(a);
+    if (single) launch(n, hd, std::integral_constant<int, 1>{});
+    else launch(n, hd, std::integral_constant<int, kRowsOfBlock>{});
   };
   using std::integral_constant;
   if (kv->head_dim == 128) {

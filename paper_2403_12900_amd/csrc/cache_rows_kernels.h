@@ -139,7 +139,10 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryCall a) {
 
 // ---------------------------------------------------------------------------
 
-// The blocks that a batch's rows lie in: tile0[i] counts those of the requests
+// Rows of keys and values.  A thread takes eight dimensions of a row and KV
+// head.  A work-group's 256 threads are either the 16 positions of one block for
+// a head (HD = 64: two) at a time, or, where every request has a single row, that
+// row for 16 (32) heads.  tile0[i] counts the blocks, or rows, of the requests
 // before i.
 struct CacheRowsArgs {
   const int32_t* bt;
@@ -150,44 +153,71 @@ struct CacheRowsArgs {
   int n, Hkv, mb, nb, per;  // per: KV heads of a work-group
   int turned;
   RotaryArgs r;
-  int slot[kCacheReqs], len[kCacheReqs], row0[kCacheReqs + 1];
+  int slot[kCacheReqs], len[kCacheReqs], row0[kCacheReqs];
   int tile0[kCacheReqs + 1];
+  int rows[kCacheReqs];
 };
 static_assert(sizeof(CacheRowsArgs) <= 3584, "kernel arguments");
 
+// Positions of a block that a work-group takes (1: a single row's).
+constexpr int kRowsOfBlock = 16;
+template <int RG, int HD>
+constexpr int kRowHeads = 256 / (RG * (HD / 8));  // heads at a time
+
 struct CacheTile {
-  int first, end;  // positions 16 b + [first, end) of block b
-  int base;        // row of position 16 b (before the request's first row where first > 0)
-  int pos;         // 16 b
+  int pos, first, end;  // positions pos + [first, end) of the block at pos
+  int base;             // row of position pos (before the request's first row where first > 0)
   int id;
 };
+template <int RG>
 __device__ __forceinline__ CacheTile cache_tile(const CacheRowsArgs& a, int f) {
   const int lane = threadIdx.x & 63;
-  int rank = 0;
-  for (int k = 0; k < a.n; k += 64)
-    rank += __popcll(__ballot(k + lane < a.n && a.tile0[min(k + lane, a.n - 1) + 1] <= f));
-  const int i = __builtin_amdgcn_readfirstlane(rank);
-  const int len = a.len[i], total = len + a.row0[i + 1] - a.row0[i];
-  const int b = len / 16 + f - a.tile0[i];
-  CacheTile t;
-  t.pos = 16 * b;
-  t.first = max(len - t.pos, 0);
-  t.end = min(total - t.pos, 16);
-  t.base = a.row0[i] + t.pos - len;
-  t.id = a.bt[static_cast<size_t>(a.slot[i]) * a.mb + b];
-  return t;
+  // Lane = request, 64 at a time and all of them at once: one trip to memory.
+  for (int k = 0;; k += 64) {
+    const int r = min(k + lane, a.n - 1);
+    const int tile0 = a.tile0[r], tile1 = a.tile0[r + 1], lens = a.len[r], row0 = a.row0[r], rows = a.rows[r];
+    const int slot = a.slot[r];
+    // Request: the number of requests whose tiles all precede f.
+    const int before = __popcll(__ballot(k + lane < a.n && tile1 <= f));
+    if (before == 64 && k + 64 < a.n) continue;
+    const auto mine = [&](int v) { return __builtin_amdgcn_readlane(v, before); };
+    const int len = mine(lens), total = len + mine(rows), w = f - mine(tile0);
+    CacheTile t;
+    if constexpr (RG == 1) {
+      t.pos = (len + w) & ~15;
+      t.first = (len + w) & 15;
+      t.end = t.first + 1;
+    } else {
+      t.pos = 16 * (len / 16 + w);
+      t.first = max(len - t.pos, 0);
+      t.end = min(total - t.pos, 16);
+    }
+    t.base = mine(row0) + t.pos - len;
+    t.id = a.bt[static_cast<size_t>(mine(slot)) * a.mb + t.pos / 16];
+    return t;
+  }
 }
 
-// Lane of a wave: KV head `head` of the wave's 128 / HD, positions 4 g .. 4 g +
-// 3 of the tile and eight dimensions from 8 m on.
-template <int HD>
-struct RowLane {
-  int head, g, m;
-  __device__ __forceinline__ RowLane() {
-    const int lane = threadIdx.x & 63;
-    m = lane % (HD / 8);
-    g = lane / (HD / 8) & 3;
-    head = lane / (HD / 2);
+// A thread's place: position t of the block, head `head` of those at a time,
+// eight dimensions from 8 m on (group p of 32, quarter q of it).
+template <int RG, int HD>
+struct RowThread {
+  int t, head, m, p, q;
+  bool live;
+  __device__ __forceinline__ RowThread(const CacheTile& tile) {
+    const int tid = threadIdx.x;
+    m = tid % (HD / 8);
+    p = m / 4;
+    q = m % 4;
+    if constexpr (RG == 1) {
+      t = tile.first;
+      head = tid / (HD / 8);
+      live = true;
+    } else {
+      t = tid / (HD / 8) % 16;
+      head = tid / (2 * HD);
+      live = t >= tile.first && t < tile.end;
+    }
   }
 };
 
@@ -213,149 +243,138 @@ __device__ __forceinline__ uint32_t quantise(const float* x, uint32_t& byte) {
   return byte == 255 ? 0u : to_codes(x, __uint_as_float(byte << 23));
 }
 
-// Append: a work-group takes a tile's rows of `per` KV heads, a wave 128 / HD
-// of them at a time.  Keys: a lane's eight codes are a word of the tile.
-// Values: it trades half its codes with the lane 16 dimensions on, and has four
-// bytes of each of its four positions, stored as four words where the call
-// writes all four positions, else byte by byte.
-template <int N, int HD>
+// Eight turned values of a lane in fp32.  What decides a code or a scale is on
+// which side of a border a value lies, and borders have three significant bits:
+// rounding to nearest can only mislead where it ends on such a number, and there
+// the values are rounded to odd instead.
+// turned: how many of the eight are (the rest are exact).
+template <class Turn>
+__device__ __forceinline__ void turn_lane(float* x, int turned, const Turn& turn) {
+  double z[8];
+  bool near = false;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    z[j] = turn(j);
+    x[j] = static_cast<float>(z[j]);
+    const uint32_t u = __float_as_uint(x[j]);
+    near |= (j < turned) & (((u & 0xFFFFFu) == 0) | ((u & 0x7F800000u) == 0x7F800000u));
+  }
+  if (__ballot(near) != 0) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = odd_f32(z[j]);
+  }
+}
+
+// Append.  Keys: a thread's eight codes are a word of the tile.  Values: it
+// trades half its codes with the thread 16 dimensions on, and stores four bytes.
+// (A lane's position is the same for all heads, and so are its sines.)
+template <int N, int HD, int RG>
 __global__ __launch_bounds__(256) void k_cache_append(CacheRowsArgs a) {
   using F = Mx4<HD>;
   using E = typename RowPiece<N>::elem;
-  constexpr int kHeads = 4 * (128 / HD);  // at a time
-  __shared__ double2 cs[16][HD / 2];
-  const CacheTile t = cache_tile(a, blockIdx.x);
+  constexpr int kHeads = kRowHeads<RG, HD>;
+  __shared__ double2 cs[RG][HD / 2];
+  const CacheTile t = cache_tile<RG>(a, blockIdx.x);
+  const RowThread<RG, HD> l(t);
+  const int h1 = min(static_cast<int>(blockIdx.y + 1) * a.per, a.Hkv);
+  const int64_t row = t.base + (l.live ? l.t : t.first);
+  const E* k = static_cast<const E*>(a.k) + row * a.ks;
+  const E* v = static_cast<const E*>(a.v) + row * a.vs;
+  float x[8], y[8] = {}, w[8];
+  const auto load = [&](int h0) {
+    const int at = min(h0 + l.head, h1 - 1) * HD;
+    load8<N>(k + at + 8 * l.m, x);
+    if (a.turned && !a.r.pairs) {
+#pragma unroll
+      for (int j = 0; j < 8; j += N) load_partners<N>(k + at, 8 * l.m + j, a.r.dims, y + j);
+    }
+    load8<N>(v + at + 8 * l.m, w);
+  };
+  int h0 = blockIdx.y * a.per;
+  load(h0);
+  if (a.turned) {
+    const int half = a.r.dims / 2, n = (t.end - t.first) * half;
+    for (int i = threadIdx.x; i < n; i += 256) {
+      const int at = i / half, d = i - at * half;
+      cs[RG == 1 ? 0 : t.first + at][d] = rotary_turn(a.r, t.pos + t.first + at, d);
+    }
+    __syncthreads();
+  }
   if (static_cast<unsigned>(t.id) >= static_cast<unsigned>(a.nb)) {
     if (threadIdx.x == 0) raise_check(a.err, kErrBlockId);
     return;
   }
-  if (a.turned) {
-    const int half = a.r.dims / 2, n = (t.end - t.first) * half;
-    for (int x = threadIdx.x; x < n; x += 256) {
-      const int p = x / half, k = x - p * half;
-      cs[t.first + p][k] = rotary_turn(a.r, t.pos + t.first + p, k);
-    }
-    __syncthreads();
-  }
-  const RowLane<HD> l;
-  const int wave = threadIdx.x >> 6;
-  const int h1 = min(static_cast<int>(blockIdx.y + 1) * a.per, a.Hkv);
-  for (int h0 = blockIdx.y * a.per; h0 < h1; h0 += kHeads) {
-    const int head = h0 + wave * (128 / HD) + l.head;
-    const bool mine = head < h1;  // the lanes of a head agree
+  const double2* table = cs[RG == 1 ? 0 : l.live ? l.t : t.first];
+  for (;;) {
+    const int head = h0 + l.head;
     uint8_t* tile = a.pool + (static_cast<size_t>(t.id) * a.Hkv + min(head, h1 - 1)) * F::kTile;
-    const int p = l.m / 4, q = l.m % 4;
-    const auto live = [&](int r) { return mine && 4 * l.g + r >= t.first && 4 * l.g + r < t.end; };
-    const auto row_of = [&](int r) { return static_cast<int64_t>(t.base + min(max(4 * l.g + r, t.first), t.end - 1)); };
-    const int at = min(head, h1 - 1) * HD;
-    float x[4][8], y[4][8] = {}, v[4][8];
+    if (a.turned) {
+      float z[8];
+      turn_lane(z, a.r.dims - 8 * l.m, [&](int j) { return turn_element<8>(x, y, j, 8 * l.m, a.r.dims, a.r.pairs, table); });
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const E* k = static_cast<const E*>(a.k) + row_of(r) * a.ks + at;
-      load8<N>(k + 8 * l.m, x[r]);
-      if (a.turned && !a.r.pairs) {
-#pragma unroll
-        for (int j = 0; j < 8; j += N) load_partners<N>(k, 8 * l.m + j, a.r.dims, y[r] + j);
-      }
-      load8<N>(static_cast<const E*>(a.v) + row_of(r) * a.vs + at + 8 * l.m, v[r]);
+      for (int j = 0; j < 8; ++j) x[j] = z[j];
     }
-    uint32_t words[4] = {0, 0, 0, 0}, scales = 0;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int pos = 4 * l.g + r;
-      if (a.turned) {
-        float z[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          z[j] = odd_f32(turn_element<8>(x[r], y[r], j, 8 * l.m, a.r.dims, a.r.pairs, cs[min(max(pos, t.first), t.end - 1)]));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[r][j] = z[j];
-      }
-      uint32_t byte;
-      const uint32_t kw = quantise(x[r], byte);
-      if (live(r)) {
-        *reinterpret_cast<uint32_t*>(tile + F::key_code(pos, 8 * l.m)) = kw;
-        if (q == 0) tile[F::key_scale(pos, p)] = static_cast<uint8_t>(byte);
-      }
-      const uint32_t vw = quantise(v[r], byte);
-      const uint32_t ow = __shfl_xor(static_cast<int>(vw), 2);
-      // Dimensions 32 p + e and 32 p + 16 + e, four e of this lane's eight.
-      const uint32_t lo = q < 2 ? vw : ow >> 16, hi = q < 2 ? ow : vw >> 16;
+    uint32_t kb, vb;
+    const uint32_t kw = quantise(x, kb), vw = quantise(w, vb);
+    const uint32_t ow = __shfl_xor(static_cast<int>(vw), 2);
+    // Dimensions 32 p + e and 32 p + 16 + e, four e of this thread's eight.
+    const uint32_t lo = l.q < 2 ? vw : ow >> 16, hi = l.q < 2 ? ow : vw >> 16;
+    const int e0 = l.q < 2 ? 8 * l.q : 8 * (l.q - 2) + 4;
+    if (l.live && head < h1) {
+      *reinterpret_cast<uint32_t*>(tile + F::key_code(l.t, 8 * l.m)) = kw;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        words[e] |= ((lo >> 4 * e & 15u) | (hi >> 4 * e & 15u) << 4) << 8 * r;
-      scales |= byte << 8 * r;
-    }
-    const int e0 = q < 2 ? 8 * q : 8 * (q - 2) + 4;
-    if (live(0) && live(3)) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(tile + F::value_word(l.g, e0 + e, p)) = words[e];
-      if (q == 0) *reinterpret_cast<uint32_t*>(tile + F::value_scales(l.g, p)) = scales;
-    } else {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if (!live(r)) continue;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) tile[F::value_word(l.g, e0 + e, p) + r] = static_cast<uint8_t>(words[e] >> 8 * r);
-        if (q == 0) tile[F::value_scales(l.g, p) + r] = static_cast<uint8_t>(scales >> 8 * r);
+        tile[F::value_word(l.t / 4, e0 + e, l.p) + l.t % 4] = static_cast<uint8_t>((lo >> 4 * e & 15u) | (hi >> 4 * e & 15u) << 4);
+      if (l.q == 0) {
+        tile[F::key_scale(l.t, l.p)] = static_cast<uint8_t>(kb);
+        tile[F::value_scales(l.t / 4, l.p) + l.t % 4] = static_cast<uint8_t>(vb);
       }
     }
+    h0 += kHeads;
+    if (h0 >= h1) break;
+    load(h0);
   }
 }
 
-// Read: the same lanes the other way.
-template <int N, int HD>
+// Read: the same threads the other way.
+template <int N, int HD, int RG>
 __global__ __launch_bounds__(256) void k_cache_read(CacheRowsArgs a) {
   using F = Mx4<HD>;
   using E = typename RowPiece<N>::elem;
-  constexpr int kHeads = 4 * (128 / HD);
-  CacheTile t = cache_tile(a, blockIdx.x);
+  CacheTile t = cache_tile<RG>(a, blockIdx.x);
   if (static_cast<unsigned>(t.id) >= static_cast<unsigned>(a.nb)) {
     if (threadIdx.x == 0) raise_check(a.err, kErrBlockId);
     t.id = 0;
   }
-  const RowLane<HD> l;
-  const int wave = threadIdx.x >> 6;
+  const RowThread<RG, HD> l(t);
+  if (!l.live) return;
   const int h1 = min(static_cast<int>(blockIdx.y + 1) * a.per, a.Hkv);
-  for (int h0 = blockIdx.y * a.per; h0 < h1; h0 += kHeads) {
-    const int head = h0 + wave * (128 / HD) + l.head;
-    if (head >= h1) continue;
+  const int64_t row = t.base + l.t;
+  E* k = static_cast<E*>(const_cast<void*>(a.k)) + row * a.ks + 8 * l.m;
+  E* v = static_cast<E*>(const_cast<void*>(a.v)) + row * a.vs + 8 * l.m;
+  for (int head = blockIdx.y * a.per + l.head; head < h1; head += kRowHeads<RG, HD>) {
     const uint8_t* tile = a.pool + (static_cast<size_t>(t.id) * a.Hkv + head) * F::kTile;
-    const int p = l.m / 4, q = l.m % 4;
-    uint32_t kw[4], kb[4], vw[8];
+    const uint32_t kw = *reinterpret_cast<const uint32_t*>(tile + F::key_code(l.t, 8 * l.m));
+    const float ks = __uint_as_float(static_cast<uint32_t>(tile[F::key_scale(l.t, l.p)]) << 23);
+    const float vs = __uint_as_float(static_cast<uint32_t>(tile[F::value_scales(l.t / 4, l.p) + l.t % 4]) << 23);
+    uint32_t vw[8];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      kw[r] = *reinterpret_cast<const uint32_t*>(tile + F::key_code(4 * l.g + r, 8 * l.m));
-      kb[r] = tile[F::key_scale(4 * l.g + r, p)];
+    for (int e = 0; e < 8; ++e) vw[e] = tile[F::value_word(l.t / 4, 8 * (l.q % 2) + e, l.p) + l.t % 4];
+    float x[8];
+    const auto pair = [&](int j, f32x2_t z) { x[j] = z.x, x[j + 1] = z.y; };
+    pair(0, codes_to_f32<0>(kw, ks));
+    pair(2, codes_to_f32<1>(kw, ks));
+    pair(4, codes_to_f32<2>(kw, ks));
+    pair(6, codes_to_f32<3>(kw, ks));
+#pragma unroll
+    for (int j = 0; j < 8; j += N) RowPiece<N>::store(k + head * HD + j, x + j);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const f32x2_t z = codes_to_f32<0>(vw[e], vs);
+      x[e] = l.q < 2 ? z.x : z.y;
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) vw[e] = *reinterpret_cast<const uint32_t*>(tile + F::value_word(l.g, 8 * (q % 2) + e, p));
-    const uint32_t vb = *reinterpret_cast<const uint32_t*>(tile + F::value_scales(l.g, p));
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int pos = 4 * l.g + r;
-      if (pos < t.first || pos >= t.end) continue;
-      const int64_t row = t.base + pos;
-      float x[8];
-      const float ks = __uint_as_float(kb[r] << 23);
-      const auto pair = [&](int j, f32x2_t v) { x[j] = v.x, x[j + 1] = v.y; };
-      pair(0, codes_to_f32<0>(kw[r], ks));
-      pair(2, codes_to_f32<1>(kw[r], ks));
-      pair(4, codes_to_f32<2>(kw[r], ks));
-      pair(6, codes_to_f32<3>(kw[r], ks));
-      E* dk = static_cast<E*>(const_cast<void*>(a.k)) + row * a.ks + head * HD + 8 * l.m;
-#pragma unroll
-      for (int j = 0; j < 8; j += N) RowPiece<N>::store(dk + j, x + j);
-      const float vs = __uint_as_float((vb >> 8 * r & 255u) << 23);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const f32x2_t v = codes_to_f32<0>(vw[e] >> 8 * r, vs);
-        x[e] = q < 2 ? v.x : v.y;
-      }
-      E* dv = static_cast<E*>(const_cast<void*>(a.v)) + row * a.vs + head * HD + 8 * l.m;
-#pragma unroll
-      for (int j = 0; j < 8; j += N) RowPiece<N>::store(dv + j, x + j);
-    }
+    for (int j = 0; j < 8; j += N) RowPiece<N>::store(v + head * HD + j, x + j);
   }
 }
 

@@ -25,6 +25,8 @@ def _refuse(msg: str):
 
 def _int32(x, name, what="tree batch"):
     """x as a vector of int32 of its own, each entry with its value."""
+    if type(x) is np.ndarray and x.dtype == np.int32 and x.ndim == 1:
+        return x.copy()
     try:
         if isinstance(x, (list, tuple)) and len(x):
             return np.frombuffer(array("i", x), dtype=np.int32)  # whole numbers of any type; OverflowError past 32 bits
