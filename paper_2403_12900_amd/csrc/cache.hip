@@ -32,11 +32,11 @@ bool overlap(const void* a, int64_t as, const void* b, int64_t bs, int64_t width
 
 int size_of(int dtype) { return dtype == SPR_F32 ? 4 : 2; }
 
-// KV heads of a work-group: as many as leave the chip enough work-groups (8
-// per CU), in whole rounds of its waves.
-int heads_per_group(int tiles, int heads, int at_once, int n_cu) {
+// Heads of a work-group: as many as leave the chip `groups` of them, in whole
+// rounds of its threads.
+int heads_per_group(int tiles, int heads, int at_once, int groups) {
   int per = at_once;
-  while (per < heads && static_cast<int64_t>(tiles) * ((heads + 2 * per - 1) / (2 * per)) >= 8 * n_cu) per *= 2;
+  while (per < heads && static_cast<int64_t>(tiles) * ((heads + 2 * per - 1) / (2 * per)) >= groups) per *= 2;
   return per;
 }
 
@@ -89,7 +89,9 @@ spr_status rows_call(spr_cache_ops* o, const char* what, const spr_kv4_view* kv,
   }
   a.tile0[t.n] = tiles;
   const int at_once = (single ? 16 : 1) * (128 / kv->head_dim);
-  a.per = heads_per_group(tiles, a.Hkv, at_once, o->n_cu);
+  // Appending, a work-group's sines serve all its heads (5600 rows of 8 heads: 14.5
+  // us with 2 work-groups a CU, with 8 of them 18); reading has no such table.
+  a.per = heads_per_group(tiles, a.Hkv, at_once, (append ? 2 : 8) * o->n_cu);
   const dim3 grid(tiles, (a.Hkv + a.per - 1) / a.per);
   const auto launch = [&](auto n, auto hd, auto rg) {
     constexpr int N = decltype(n)::value, HD = decltype(hd)::value, RG = decltype(rg)::value;
@@ -113,15 +115,15 @@ spr_status rows_call(spr_cache_ops* o, const char* what, const spr_kv4_view* kv,
   return e == hipSuccess ? SPR_OK : hip_failed(o, what, e);
 }
 
-// Chunks of 16 KB and what a launch has to know of the pools.
-PageCopy page_copy(const spr_pages& p) {
+// What a launch has to know of the pools; deep: 16-byte pieces of a thread.
+PageCopy page_copy(const spr_pages& p, int deep) {
   PageCopy c{};
   c.pool[0] = static_cast<char*>(p.k);
   c.pool[1] = static_cast<char*>(p.v);
   c.pools = p.v != nullptr ? 2 : 1;
   c.layers = p.n_layers;
   c.pieces = static_cast<int>(p.block_bytes / 16);
-  c.chunks = (c.pieces + 256 * kPageDeep - 1) / (256 * kPageDeep);
+  c.chunks = (c.pieces + 256 * deep - 1) / (256 * deep);
   c.chunk = (c.pieces + c.chunks - 1) / c.chunks;
   c.block_bytes = p.block_bytes;
   c.layer_bytes = p.block_bytes * p.n_blocks;
@@ -189,7 +191,7 @@ spr_status spr_cache_rotary(spr_cache_ops* o, const spr_rotary* rotary, int32_t 
     a.os = out_stride;
     a.heads = n_heads;
     const int at_once = 256 / (head_dim * size / 16);
-    a.per = heads_per_group(rows, n_heads, at_once, o->n_cu);
+    a.per = heads_per_group(rows, n_heads, at_once, 8 * o->n_cu);
     const dim3 grid(rows, (n_heads + a.per - 1) / a.per);
     if (head_dim == 128) {
       if (dtype == SPR_F32) k_rotary<4, 128><<<grid, 256, 0, o->st>>>(a);
@@ -268,7 +270,7 @@ spr_status spr_cache_fork(spr_cache_ops* o, const spr_pages* pages, int32_t n, c
     DeviceGuard dev(o->dev);
     if (dev.e != hipSuccess) return hip_failed(o, "cache_fork", dev.e);
     ForkArgs a{};
-    a.c = page_copy(*pages);
+    a.c = page_copy(*pages, kForkDeep);
     a.bt = pages->block_table;
     a.err = o->err_dev;
     a.mb = pages->max_blocks;
@@ -297,7 +299,7 @@ spr_status spr_cache_move(spr_cache_ops* o, const spr_pages* pages, int32_t n, c
     std::vector<std::pair<int32_t, int32_t>> moves;
     if ((s = plan_move(pages, n, src, dst, &moves, &err)) != SPR_OK) return set_error(s, err);
     MoveArgs a{};
-    a.c = page_copy(*pages);
+    a.c = page_copy(*pages, kMoveDeep);
     a.bt = pages->block_table;
     a.entries = static_cast<int64_t>(pages->n_slots) * pages->max_blocks;
     const int64_t items = static_cast<int64_t>(a.c.pools) * a.c.layers * a.c.chunks;

@@ -357,9 +357,13 @@ __global__ __launch_bounds__(256) void k_cache_read(CacheRowsArgs a) {
     const uint32_t kw = *reinterpret_cast<const uint32_t*>(tile + F::key_code(l.t, 8 * l.m));
     const float ks = __uint_as_float(static_cast<uint32_t>(tile[F::key_scale(l.t, l.p)]) << 23);
     const float vs = __uint_as_float(static_cast<uint32_t>(tile[F::value_scales(l.t / 4, l.p) + l.t % 4]) << 23);
-    uint32_t vw[8];
+    // Four value bytes, and the four of the thread 16 dimensions on.
+    const int e0 = l.q < 2 ? 8 * l.q : 8 * (l.q - 2) + 4;
+    uint32_t own = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) vw[e] = tile[F::value_word(l.t / 4, 8 * (l.q % 2) + e, l.p) + l.t % 4];
+    for (int e = 0; e < 4; ++e) own |= static_cast<uint32_t>(tile[F::value_word(l.t / 4, e0 + e, l.p) + l.t % 4]) << 8 * e;
+    const uint32_t other = __shfl_xor(static_cast<int>(own), 2);
+    const uint32_t v0 = l.q < 2 ? own : other, v1 = l.q < 2 ? other : own;
     float x[8];
     const auto pair = [&](int j, f32x2_t z) { x[j] = z.x, x[j + 1] = z.y; };
     pair(0, codes_to_f32<0>(kw, ks));
@@ -370,7 +374,7 @@ __global__ __launch_bounds__(256) void k_cache_read(CacheRowsArgs a) {
     for (int j = 0; j < 8; j += N) RowPiece<N>::store(k + head * HD + j, x + j);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const f32x2_t z = codes_to_f32<0>(vw[e], vs);
+      const f32x2_t z = codes_to_f32<0>((e < 4 ? v0 : v1) >> 8 * (e % 4), vs);
       x[e] = l.q < 2 ? z.x : z.y;
     }
 #pragma unroll
