@@ -16,10 +16,6 @@ from .binding import SPR_OK, SprCacheBatch, SprKv4View, SprPages, SprRotary, _ch
 from .tree import _DTYPES, KVView, OpHandle, _int32, _refuse
 
 
-def _address(a: np.ndarray) -> int:
-    return a.__array_interface__["data"][0]
-
-
 class KV4View:
     """A paged KV cache in 4 bits (spr_kv4_view): data [layers, blocks, KV heads, 17 * head_dim] bytes in the tile order that
     the header gives, and the int32 block table [slots, blocks per slot], contiguous on one device.  A fresh cache may hold
@@ -120,7 +116,8 @@ class CacheOps(OpHandle):
             _refuse("cache read: dtype must be fp32 or bf16")
         self._same_device("cache read", kv)
         heads, hd = kv.n_kv_heads, kv.head_dim
-        k, v = torch.empty((2, batch.rows, heads, hd), dtype=dtype, device=kv.data.device).unbind(0)
+        k = torch.empty(batch.rows, heads, hd, dtype=dtype, device=kv.data.device)
+        v = torch.empty_like(k)
         self._enter()
         self._done(self.lib.spr_cache_read(self.h, kv.ref, layer, batch.ref, code, k.data_ptr(), heads * hd, v.data_ptr(),
                                            heads * hd))
@@ -146,22 +143,34 @@ class CacheOps(OpHandle):
              fresh: Sequence[int]):
         """Forks requests (spr_cache_fork): slot target[i] continues the first lens[i] positions of slot source[i], whose full
         blocks it shares; fresh[i] takes a copy of the last, partly filled one.  Any paged cache."""
-        a = [_int32(x, name, "cache fork") for x, name in
-             ((source, "source"), (target, "target"), (lens, "lens"), (fresh, "fresh"))]
-        if any(len(x) != len(a[0]) for x in a):
-            _refuse("cache fork: source, target, lens and fresh must be of one length")
+        n, at = self._lists("cache fork", source=source, target=target, lens=lens, fresh=fresh)
         pages = self._pages("cache fork", kv)
         self._enter()
-        self._done(self.lib.spr_cache_fork(self.h, pages, len(a[0]), *map(_address, a)))
+        self._done(self.lib.spr_cache_fork(self.h, pages, n, at, at + 4 * n, at + 8 * n, at + 12 * n))
 
     def move(self, kv: Union[KV4View, KVView], src: Sequence[int], dst: Sequence[int]):
         """Moves blocks src[i] to dst[i] in every layer, and the table's entries with them (spr_cache_move).  Any paged cache."""
-        a = [_int32(src, "src", "cache move"), _int32(dst, "dst", "cache move")]
-        if len(a[0]) != len(a[1]):
-            _refuse("cache move: src and dst must be of one length")
+        n, at = self._lists("cache move", src=src, dst=dst)
         pages = self._pages("cache move", kv)
         self._enter()
-        self._done(self.lib.spr_cache_move(self.h, pages, len(a[0]), *map(_address, a)))
+        self._done(self.lib.spr_cache_move(self.h, pages, n, at, at + 4 * n))
+
+    _staged: Optional[np.ndarray] = None  # a call's lists, one after the other
+
+    def _lists(self, what, **lists):
+        """The lists' common length, and the address at which they stand one after the other for the call."""
+        a = [x if type(x) is np.ndarray and x.dtype == np.int32 and x.ndim == 1 else _int32(x, name, what)
+             for name, x in lists.items()]
+        n = len(a[0])
+        for x in a:
+            if len(x) != n:
+                _refuse(f"{what}: {', '.join(lists)} must be of one length")
+        if self._staged is None or len(self._staged) < n * len(a):
+            self._staged = np.empty(max(512, n * len(a)), dtype=np.int32)
+            self._staged_at = self._staged.ctypes.data
+        for i, x in enumerate(a):
+            self._staged[i * n:(i + 1) * n] = x
+        return n, self._staged_at
 
     def _pages(self, what, kv):
         self._same_device(what, kv)
@@ -189,7 +198,7 @@ class CacheOps(OpHandle):
     def _out(self, what, x, out, heads, hd):
         """The output, a new one like x if none is given, and its row stride."""
         if out is None:
-            return x.new_empty(x.shape), heads * hd
+            return torch.empty_like(x, memory_format=torch.contiguous_format), heads * hd
         if out.shape != x.shape or out.dtype != x.dtype:
             _refuse(f"{what}: out must be like its input")
         return out, self._row_stride(what, out, heads, hd)
