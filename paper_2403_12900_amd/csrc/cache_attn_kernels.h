@@ -221,12 +221,14 @@ __device__ __forceinline__ void value_halves_f16(uint32_t w, uint32_t scales, ui
   hi = make_uint2(__builtin_amdgcn_perm(x1, x0, 0x07060302u), __builtin_amdgcn_perm(x3, x2, 0x07060302u));
 }
 
-// Whether a word's values are not all exact in fp16: a scale outside 2^-18 ..
-// 2^13 (bytes 109 .. 140: a byte out of that range leaves a top bit, and the
-// lowest such byte has no borrow from below) with codes that are not zero, or a
-// NaN.
+// Not 0: one of a word's scales is outside 2^-18 .. 2^13 (bytes 109 .. 140: a byte
+// out of that range leaves a top bit, and the lowest such byte has no borrow from
+// below).
+__device__ __forceinline__ uint32_t odd_scales(uint32_t scales) { return (scales - 0x6D6D6D6Du) & 0xE0E0E0E0u; }
+// Whether a word's values are not all exact in fp16: such a scale with codes that
+// are not zero, or a NaN.
 __device__ __forceinline__ bool beyond_f16(uint32_t w, uint32_t scales) {
-  return (((scales - 0x6D6D6D6Du) & 0xE0E0E0E0u) != 0) & (((w & 0x77777777u) | nan_bytes(scales)) != 0);
+  return (odd_scales(scales) != 0) & (((w & 0x77777777u) | nan_bytes(scales)) != 0);
 }
 
 // The eight probabilities of a step, rounded to fp16, as one operand part; taken
@@ -484,11 +486,11 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_cache_attn(CacheAttnAr
         }
       }
     }
-    uint32_t out = 0;  // scales that may not do: see beyond_f16
+    uint32_t out = 0;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int p = 0; p < P; ++p) out |= (B.vs[b][p] - 0x6D6D6D6Du) & 0xE0E0E0E0u;
+      for (int p = 0; p < P; ++p) out |= odd_scales(B.vs[b][p]);
     if (__ballot(out != 0) != 0) {
       asm volatile("");  // (keeps what follows behind the branch)
       bool x = false;
@@ -630,7 +632,6 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
   };
   __shared__ uint4 vals[4][NE * 64];  // of a step: operands: a lane's 8 bytes of block 0, of block 1
   __shared__ __attribute__((aligned(16))) Keys keys[4];
-  __shared__ int slow_s;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane & 15, g = lane >> 4;
@@ -641,7 +642,6 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
   const bool busy = c0 < t.cols;  // this wave has columns
   const int all = t.len + 1 + CW * t.cg / a.G;  // positions that every column of the group sees
   const int some = t.len + 1 + (min(t.cols, CW * (t.cg + 1)) - 1) / a.G;
-  if (tid == 0) slow_s = 0;
 
   // Steps are numbered from the split's start; past its end their blocks are its
   // last one (a missing second block re-reads the first, masked).  A wave fetches
@@ -701,25 +701,33 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
     for (int w = 0; w < W; ++w) to.code[fb * (kKeys / 2) + at + w] = next[n].k[w];
     if (ft < kScales / 2) to.scale[fb * (kScales / 2) + ft] = next[n].ks;
   };
+  uint32_t beyond = 0;  // not 0: this thread met a value that fp16 does not hold, or a NaN
   const auto put_values = [&](int n, int step, uint4* to, auto tail) {
-    bool beyond = false;
+    uint32_t v[W], x[W], out = 0;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      uint32_t v = next[n].v[w], x = next[n].vs[w];
+      v[w] = next[n].v[w], x[w] = next[n].vs[w];
       if constexpr (decltype(tail)::value) {
         const int b = t.first + 2 * step + fb;
         const uint32_t keep = byte_mask(b < end ? live_bits(16 * b + 4 * (vl / 16), some) : 0u);
-        v &= keep;
-        x = (x & keep) | (0x7F7F7F7Fu & ~keep);
+        v[w] &= keep;
+        x[w] = (x[w] & keep) | (0x7F7F7F7Fu & ~keep);
       }
-      beyond |= beyond_f16(v, x);
+      out |= odd_scales(x[w]);
+    }
+    if (__ballot(out != 0) != 0) {
+      asm volatile("");  // (keeps what follows behind the branch: 255 us without, 247.5 with)
+#pragma unroll
+      for (int w = 0; w < W; ++w) beyond |= beyond_f16(v[w], x[w]) ? 1u : 0u;
+    }
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
       uint2 lo, hi;
-      value_halves_f16(v, x, lo, hi);
+      value_halves_f16(v[w], x[w], lo, hi);
       uint2* op = reinterpret_cast<uint2*>(to + 2 * (vp + w) * 64 + vl) + fb;
       op[0] = lo;
       op[128] = hi;
     }
-    if (beyond) slow_s = 1;
   };
 
   f32x4_t O[NT][NE], l[NT];  // l: the sum, in every register
@@ -798,10 +806,10 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
 #pragma unroll
         for (int jt = 0; jt < NT; ++jt) O[jt][e] = mma_f16(O[jt][e], x, pp[jt][q]);
     }
-    // Schedule: four operands ahead of the exponentials, the others between the
+    // Schedule: three operands ahead of the exponentials, the others between the
     // products, so that none is waited for (295 us without, 285 with; see above
     // for the case).
-    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
     __builtin_amdgcn_sched_group_barrier(0x402, NT * 12, 0);
     const auto group = [](auto) {
       __builtin_amdgcn_sched_group_barrier(0x8, NT * HalfParts<IO>::p, 0);
@@ -873,8 +881,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
   reset();
   if (busy) walk(std::true_type{});
   else walk(std::false_type{});
-  __syncthreads();
-  if (slow_s) {
+  if (__syncthreads_or(static_cast<int>(beyond))) {
     reset();
     float sum[NT] = {};
     const auto queries = [&](int jt, int c, int k) { return Q[jt][c][k]; };

@@ -389,6 +389,24 @@ def test_attention_of_values_far_from_one(ops, io, scale):
 
 
 @pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("hd,rows", [(64, 3), (128, 3), (64, 40), (128, 40), (128, 130)])
+def test_attention_of_one_large_value(ops, hd, rows, io):
+    """One group of one position, of the first blocks or of others, far above the rest: whoever reads it first."""
+    rng = np.random.default_rng(hd + rows)
+    q, qx = rounded(rng.standard_normal((rows, 2, hd)), io)
+    k, v = (rng.standard_normal((200 + rows, 1, hd)) for _ in range(2))
+    for pos in (0, 6, 9, 15, 17, 20, 27, 30, 33, 61, 100, 199):
+        cache = filled(rng, 1, 0, 1, hd, [0], [200], [rows])
+        big = v.copy()
+        big[pos, 0, 32:64] *= 2.0 ** 40
+        cache.append(0, 0, 0, k, big)
+        want = ref.attention(cache, 0, [0], [200], [rows], qx)
+        got = ops.attention(cache.device(), 0, CacheBatch([0], [200], [rows]), q).double().cpu().numpy()
+        tol = np.broadcast_to(tolerance(cache, 0, [0], [200], [rows], qx, io, want), want.shape)
+        assert (np.abs(got - want) <= tol).all(), (pos, (np.abs(got - want) / tol).max())
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
 @pytest.mark.parametrize("hd,rows", [(64, 5), (128, 5), (64, 50), (128, 50), (128, 200)])
 def test_attention_nan_reaches_the_rows_that_see_it(ops, hd, rows, io):
     """A NaN group of a value reaches its 32 dimensions of the rows that see its position, one of a key reaches those rows
