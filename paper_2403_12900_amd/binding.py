@@ -273,8 +273,10 @@ class DecodeModel:
             return self.ws[at:at + n].view(dtype).view(*shape)
 
         pool = (v.n_layers, v.n_blocks, v.n_kv_heads, 16 * v.head_dim)
-        return KVView(part(v.k, dt, *pool), part(v.v, dt, *pool),
+        view = KVView(part(v.k, dt, *pool), part(v.v, dt, *pool),
                       part(v.block_table, torch.int32, v.n_slots, v.max_blocks))
+        view.of_model = True
+        return view
 
     def tree_step(self, batch, tokens, tok, temperature=None, accept=None, sample=None, draft_probs=None):
         """One decode step over drafted trees (spr_tree_step).

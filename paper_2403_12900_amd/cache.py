@@ -174,6 +174,8 @@ class CacheOps(OpHandle):
 
     def _pages(self, what, kv):
         self._same_device(what, kv)
+        if not isinstance(kv, KV4View) and kv.of_model:
+            _refuse(f"{what}: a model's own cache: its slots own its blocks")
         ref = getattr(kv, "_pages", None)
         if ref is None:  # as lasting as the view's own record
             k, v = (kv.data, None) if isinstance(kv, KV4View) else (kv.k, kv.v)

@@ -51,6 +51,8 @@ class KVView:
     """A paged KV cache (spr_kv_view): k and v [layers, blocks, KV heads, 16 * head_dim] in the tile order that the header
     gives, fp32 or bf16, and the int32 block table [slots, blocks per slot], all contiguous on one device."""
 
+    of_model = False  # a model's own cache, whose slots own its blocks
+
     def __init__(self, k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor):
         if k.dim() != 4 or k.shape != v.shape or k.dtype not in _DTYPES or v.dtype != k.dtype:
             _refuse("kv view: k and v must be [layers, blocks, kv_heads, 16 * head_dim] of one type, fp32 or bf16")

@@ -352,6 +352,15 @@ def test_attention_of_chunks_over_long_contexts(ops, H, Hkv, hd, rows, io):
 
 
 @pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("lens,rows", [([20, 12000] + [33] * 30, [1] * 32), ([0, 6000, 9, 40], [300, 1, 1, 70]),
+                                       ([1030] + list(range(60)), [1] + [2] * 60)])
+def test_attention_of_mixed_batches(ops, lens, rows, io):
+    """One request far longer than the rest; prompts beside single tokens."""
+    rng = np.random.default_rng(len(lens))
+    check_attention(ops, rng, 8, 4, 128, io, lens, rows, tag="mixed")
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
 def test_attention_scores_of_all_sizes(ops, io):
     """A few positions take nearly all weight, early or late ones: maxima that rise and fall; and values of many scales."""
     rng = np.random.default_rng(21)
@@ -582,6 +591,22 @@ def test_pages_refusals(ops):
     assert torch.equal(view.data, before[0]) and torch.equal(view.block_table, before[1])
 
 
+def test_a_models_own_cache_is_not_forked_or_moved(ops):
+    from paper_2403_12900_amd.binding import DecodeModel
+    from paper_2403_12900_amd.configs import ModelConfig
+    dm = DecodeModel(ModelConfig(n_layers=1, d_model=64, n_heads=1, n_kv_heads=1, head_dim=64, d_ff=64, vocab=300), 5,
+                     max_slots=2, max_ctx=40)
+    view = dm.kv_view()
+    parts = [t.view(torch.uint8) for t in (view.k, view.v, view.block_table)]  # (a fresh cache may hold NaN)
+    before = [t.clone() for t in parts]
+    for call in (lambda: ops.fork(view, [0], [1], [16], [-1]), lambda: ops.move(view, [0], [1])):
+        with pytest.raises(SproutError, match="model's own") as e:
+            call()
+        assert e.value.status == binding.SPR_ERR_INVALID_ARG
+    assert all(torch.equal(t, b) for t, b in zip(parts, before))
+    dm.close()
+
+
 # ------------------------------------------------------------------------------------------------ together
 
 
@@ -720,6 +745,30 @@ def test_captured_pages_replay(ops):
         assert torch.equal(view.data, want)
         assert view.block_table[:3].tolist()[0] == [4, 2, 6] and view.block_table[1, :2].tolist() == [4, 7]
         assert view.block_table[2].tolist() == [4, 2, 8]
+
+
+def test_graphs_of_one_handle_take_turns(ops):
+    """Two captured calls that share the handle's partial results and counters, one after the other, and eager ones between."""
+    rng = np.random.default_rng(46)
+    calls = []
+    for lens, rows, io in (([5000, 30], [1, 2], F32), ([2100, 9], [90, 1], BF16)):
+        cache = filled(rng, 1, 0, 2, 128, [0, 1], lens, rows)
+        view, batch = cache.device(), CacheBatch([0, 1], lens, rows)
+        q = torch.from_numpy(rng.standard_normal((sum(rows), 8, 128))).to(io).cuda()
+        want = ops.attention(view, 0, batch, q).clone()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = ops.attention(view, 0, batch, q)
+        calls.append((graph, out, want, (view, 0, batch, q)))
+    for trial in range(4):
+        for graph, out, want, _ in calls:
+            out.zero_()
+            graph.replay()
+        eager = [ops.attention(*args) for _, _, _, args in calls[::-1]]
+        torch.cuda.synchronize()
+        for (_, out, want, _), e in zip(calls, eager[::-1]):
+            assert torch.equal(out, want) and torch.equal(e, want)
 
 
 def test_streams_take_turns_and_handles_run_beside_each_other():
