@@ -74,8 +74,8 @@ hipError_t launch(const CacheAttnCall& c) {
 
 template <class IO, int HD>
 hipError_t by_columns(const CacheAttnCall& c) {
-  constexpr int most = IO::kRaw ? 128 : 64;  // three-part queries leave no registers for more
-  switch (cache_cols_per_group(*c.batch, c.H / c.kv.n_kv_heads, most)) {
+  constexpr int most = IO::kRaw ? 128 : 64;  // three-part queries leave too few registers for more
+  switch (cache_cols_per_group(*c.batch, c.H / c.kv.n_kv_heads, c.kv.n_kv_heads, c.n_cu, most)) {
     case 16: return launch<IO, HD, 16>(c);
     case 32: return launch<IO, HD, 32>(c);
     case 64: return launch<IO, HD, 64>(c);

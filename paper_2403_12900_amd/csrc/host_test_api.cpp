@@ -174,12 +174,12 @@ int sprh_cache_parse(const spr_cache_batch* b, int n_slots, int max_blocks, int3
 int sprh_kv4_view(const spr_kv4_view* v, int layer) { return sprk::check_kv4_view(v, layer, "view", &g_err); }
 
 // out = {columns per group, blocks per split, groups, any split}, then item0[0..n], order[n], ncg[n] and cg0[n].
-int sprh_cache_split(const spr_cache_batch* b, int G, int Hkv, int hd, int most, int least, int slots, size_t floats,
-                     int counters, int32_t* out) {
+int sprh_cache_split(const spr_cache_batch* b, int G, int Hkv, int hd, int n_cu, int most, int least, int slots,
+                     size_t floats, int counters, int32_t* out) {
   sprk::CacheInfo t;
   const spr_status st = sprk::parse_cache(b, 1 << 20, 1 << 27, "split", &t, &g_err);
   if (st != SPR_OK) return st;
-  const int cw = sprk::cache_cols_per_group(t, G, most);
+  const int cw = sprk::cache_cols_per_group(t, G, Hkv, n_cu, most);
   const sprk::CacheSplit s = sprk::cache_split(t, G, Hkv, hd, cw, least, slots, floats, counters);
   int32_t* o = out;
   for (int v : {cw, s.bps, s.groups, static_cast<int>(s.split)}) *o++ = v;

@@ -131,6 +131,11 @@ def attention(cache: Cache, layer, slots, lens, rows, q: np.ndarray) -> np.ndarr
         k, v = cache.rows(layer, slot, length + n)
         for h in range(H):
             kh, vh = k[:, h // G], v[:, h // G]
+            if np.isfinite(kh).all() and np.isfinite(vh).all():  # all rows at once: nothing masked is infinite or NaN
+                s = np.where(np.arange(length + n) <= length + np.arange(n)[:, None], q[r0:r0 + n, h] @ kh.T / np.sqrt(hd), -np.inf)
+                p = np.exp(s - s.max(-1, keepdims=True))
+                out[r0:r0 + n, h] = (p @ vh) / p.sum(-1, keepdims=True)
+                continue
             for j in range(n):
                 see = length + j + 1
                 s = kh[:see] @ q[r0 + j, h] / np.sqrt(hd)

@@ -23,7 +23,7 @@ F64 = ctypes.c_double
 def host():
     L = ctypes.CDLL(HOST_LIB)
     L.sprh_last_error.restype = ctypes.c_char_p
-    L.sprh_cache_split.argtypes = [ctypes.c_void_p] + [ctypes.c_int] * 6 + [ctypes.c_size_t, ctypes.c_int, I32]
+    L.sprh_cache_split.argtypes = [ctypes.c_void_p] + [ctypes.c_int] * 7 + [ctypes.c_size_t, ctypes.c_int, I32]
     L.sprh_rotary.argtypes = [ctypes.c_int] * 2 + [F64] * 6 + [ctypes.c_void_p, ctypes.c_int]
     return L
 
@@ -282,13 +282,14 @@ def test_work_items_of_an_attention_launch():
         lens = np.minimum(np.exp(rng.uniform(0, 13 if trial % 9 == 0 else 8, n)), 2 ** 20).astype(np.int32) - 1
         rows = np.ones(n, np.int32) if trial % 3 else np.exp(rng.uniform(0, 8, n)).astype(np.int32)
         G, Hkv, hd = int(rng.integers(1, 17)), int(rng.choice([1, 4, 8, 40, 512])), int(rng.choice([64, 128]))
-        least, slots, floats, counters = int(rng.choice([2, 8])), int(rng.choice([256, 768, 1024])), 1 << 23, 65536
+        n_cu, least, slots, floats, counters = 256, int(rng.choice([2, 8])), int(rng.choice([256, 768, 1024])), 1 << 23, 65536
         b = raw_batch(n, np.arange(n), lens, rows)
         out = np.zeros(5 + 4 * n, np.int32)
-        assert L.sprh_cache_split(ctypes.byref(b), G, Hkv, hd, 128, least, slots, floats, counters, p32(out)) == 0
+        assert L.sprh_cache_split(ctypes.byref(b), G, Hkv, hd, n_cu, 128, least, slots, floats, counters, p32(out)) == 0
         cw, bps, groups, split = (int(x) for x in out[:4])
         item0, order, ncg, cg0 = out[4:5 + n], out[5 + n:5 + 2 * n], out[5 + 2 * n:5 + 3 * n], out[5 + 3 * n:]
-        assert cw in (16, 32, 64, 128) and (cw == 128 or cw >= rows.max() * G) and (cw == 16 or cw < 2 * rows.max() * G)
+        cols, every = int(rows.max()) * G, int(rows.sum()) * G * Hkv
+        assert cw == (16 if cols <= 16 else 32 if cols <= 32 or every <= 64 * n_cu else 64 if cols <= 64 or every <= 192 * n_cu else 128)
         assert sorted(order) == list(range(n)) and bps % least == 0 and item0[0] == 0
         blocks = (lens.astype(np.int64) + rows + 15) // 16
         assert (np.diff(blocks[order]) <= 0).all()

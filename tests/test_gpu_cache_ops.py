@@ -361,17 +361,42 @@ def test_attention_of_mixed_batches(ops, lens, rows, io):
 
 
 @pytest.mark.parametrize("io", [F32, BF16])
-def test_attention_scores_of_all_sizes(ops, io):
+@pytest.mark.parametrize("H,Hkv,hd", [(512, 32, 128), (512, 32, 64), (1000, 200, 64), (260, 260, 128)])
+@pytest.mark.parametrize("lens,rows", [([0], [35]), ([37, 0, 90], [33, 1, 70]), ([15, 3], [200, 2]), ([129], [97])])
+def test_attention_of_many_rows_and_heads(ops, H, Hkv, hd, lens, rows, io):
+    """Enough of them that work-groups take 64 and 128 columns."""
+    rng = np.random.default_rng(H + hd + rows[0])
+    check_attention(ops, rng, H, Hkv, hd, io, lens, rows, strided=rows[0] == 97, tag="many")
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("H,Hkv,hd,rows", [(512, 32, 128, 34), (512, 32, 64, 34), (512, 32, 128, 100), (512, 32, 64, 100), (600, 40, 64, 85)])
+def test_attention_of_many_rows_and_heads_over_long_contexts(ops, H, Hkv, hd, rows, io):
+    """Those with KV splits, of either parity of whole steps."""
+    rng = np.random.default_rng(hd + rows)
+    for length in (700, 683):
+        check_attention(ops, rng, H, Hkv, hd, io, [length], [rows], tag="many, long")
+
+
+# Heads and KV heads of the tests below: few, whose rows' columns work-groups share 16 or 32 at a time, and so many that from
+# 33 rows on they take 64 and from 97 on, in bf16, 128.
+HEADS = pytest.mark.parametrize("H,Hkv", [(4, 2), (512, 32)])
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
+@HEADS
+def test_attention_scores_of_all_sizes(ops, H, Hkv, io):
     """A few positions take nearly all weight, early or late ones: maxima that rise and fall; and values of many scales."""
     rng = np.random.default_rng(21)
-    for rows, at in ((1, (5, 1900)), (40, (0, 700)), (130, (1000, 1990))):
-        lens, slots = [2000], [0]
-        cache = filled(rng, 1, 0, 1, 128, slots, lens, [rows])
-        q, qx = rounded(0.2 * rng.standard_normal((rows, 2, 128)), io)
-        k = 0.2 * rng.standard_normal((2000 + rows, 1, 128))
-        v = rng.standard_normal((2000 + rows, 1, 128)) * 2.0 ** rng.integers(-18, 15, (2000 + rows, 1, 1))
+    n = 2000 if Hkv == 2 else 200
+    for rows, at in ((1, (5, n - 100)), (40, (0, n // 3)), (130, (n // 2, n - 10))):
+        lens, slots = [n], [0]
+        cache = filled(rng, 1, 0, Hkv, 128, slots, lens, [rows])
+        q, qx = rounded(0.2 * rng.standard_normal((rows, H, 128)), io)
+        k = 0.2 * rng.standard_normal((n + rows, Hkv, 128))
+        v = rng.standard_normal((n + rows, Hkv, 128)) * 2.0 ** rng.integers(-18, 15, (n + rows, 1, 1))
         for p in at:
-            k[p] = qx[0, 0] * 60
+            k[p] = qx[0, ::H // Hkv] * 60
         cache.append(0, 0, 0, k, v)
         want = ref.attention(cache, 0, slots, lens, [rows], qx)
         got = ops.attention(cache.device(), 0, CacheBatch(slots, lens, [rows]), q).double().cpu().numpy()
@@ -381,47 +406,52 @@ def test_attention_scores_of_all_sizes(ops, io):
 
 @pytest.mark.parametrize("io", [F32, BF16])
 @pytest.mark.parametrize("scale", [2.0 ** -60, 2.0 ** -20, 2.0 ** 20, 2.0 ** 90])
-def test_attention_of_values_far_from_one(ops, io, scale):
+@HEADS
+def test_attention_of_values_far_from_one(ops, H, Hkv, io, scale):
     """Values of any scale give outputs of it, to the same relative tolerance."""
     rng = np.random.default_rng(30)
-    for rows in (1, 90):
-        cache = filled(rng, 1, 0, 2, 128, [0], [300], [rows])
-        q, qx = rounded(rng.standard_normal((rows, 4, 128)), io)
-        v = rng.standard_normal((300 + rows, 2, 128))
-        k = rng.standard_normal((300 + rows, 2, 128))
+    n = 300 if Hkv == 2 else 60
+    for rows in (1, 50, 100):
+        cache = filled(rng, 1, 0, Hkv, 128, [0], [n], [rows])
+        q, qx = rounded(rng.standard_normal((rows, H, 128)), io)
+        v = rng.standard_normal((n + rows, Hkv, 128))
+        k = rng.standard_normal((n + rows, Hkv, 128))
         cache.append(0, 0, 0, k, v)
-        want = ref.attention(cache, 0, [0], [300], [rows], qx)
-        tol = tolerance(cache, 0, [0], [300], [rows], qx, io, want)
+        want = ref.attention(cache, 0, [0], [n], [rows], qx)
+        tol = tolerance(cache, 0, [0], [n], [rows], qx, io, want)
         cache.append(0, 0, 0, k, v * scale)
-        got = ops.attention(cache.device(), 0, CacheBatch([0], [300], [rows]), q).double().cpu().numpy() / scale
+        got = ops.attention(cache.device(), 0, CacheBatch([0], [n], [rows]), q).double().cpu().numpy() / scale
         assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
 
 
 @pytest.mark.parametrize("io", [F32, BF16])
 @pytest.mark.parametrize("hd,rows", [(64, 3), (128, 3), (64, 40), (128, 40), (128, 130)])
-def test_attention_of_one_large_value(ops, hd, rows, io):
+@HEADS
+def test_attention_of_one_large_value(ops, H, Hkv, hd, rows, io):
     """One group of one position, of the first blocks or of others, far above the rest: whoever reads it first."""
     rng = np.random.default_rng(hd + rows)
-    q, qx = rounded(rng.standard_normal((rows, 2, hd)), io)
-    k, v = (rng.standard_normal((200 + rows, 1, hd)) for _ in range(2))
-    for pos in (0, 6, 9, 15, 17, 20, 27, 30, 33, 61, 100, 199):
-        cache = filled(rng, 1, 0, 1, hd, [0], [200], [rows])
+    q, qx = rounded(rng.standard_normal((rows, H, hd)), io)
+    n = 200 if Hkv == 2 else 70
+    k, v = (rng.standard_normal((n + rows, Hkv, hd)) for _ in range(2))
+    cache = filled(rng, 1, 0, Hkv, hd, [0], [n], [rows])
+    for pos in (0, 6, 9, 15, 17, 20, 27, 30, 33, 61, n // 2, n - 1) if Hkv == 2 else (0, 9, 20, 27, n - 1):
         big = v.copy()
-        big[pos, 0, 32:64] *= 2.0 ** 40
+        big[pos, Hkv - 1, 32:64] *= 2.0 ** 40
         cache.append(0, 0, 0, k, big)
-        want = ref.attention(cache, 0, [0], [200], [rows], qx)
-        got = ops.attention(cache.device(), 0, CacheBatch([0], [200], [rows]), q).double().cpu().numpy()
-        tol = np.broadcast_to(tolerance(cache, 0, [0], [200], [rows], qx, io, want), want.shape)
+        want = ref.attention(cache, 0, [0], [n], [rows], qx)
+        got = ops.attention(cache.device(), 0, CacheBatch([0], [n], [rows]), q).double().cpu().numpy()
+        tol = np.broadcast_to(tolerance(cache, 0, [0], [n], [rows], qx, io, want), want.shape)
         assert (np.abs(got - want) <= tol).all(), (pos, (np.abs(got - want) / tol).max())
 
 
 @pytest.mark.parametrize("io", [F32, BF16])
 @pytest.mark.parametrize("hd,rows", [(64, 5), (128, 5), (64, 50), (128, 50), (128, 200)])
-def test_attention_nan_reaches_the_rows_that_see_it(ops, hd, rows, io):
+@HEADS
+def test_attention_nan_reaches_the_rows_that_see_it(ops, H, Hkv, hd, rows, io):
     """A NaN group of a value reaches its 32 dimensions of the rows that see its position, one of a key reaches those rows
     whole, and no other row changes."""
     rng = np.random.default_rng(hd + rows)
-    length, H, Hkv = 37, 4, 2
+    length, G = 37, H // Hkv
     q, qx = rounded(rng.standard_normal((rows, H, hd)), io)
     for pos, key in ((length + rows // 2, False), (length + rows // 2, True), (length - 2, False), (length + rows - 1, True),
                      (length + 1, False)):
@@ -433,18 +463,19 @@ def test_attention_nan_reaches_the_rows_that_see_it(ops, hd, rows, io):
         got = ops.attention(cache.device(), 0, CacheBatch([0], [length], [rows]), q).double().cpu().numpy()
         hit = np.zeros(want.shape, bool)
         first = max(0, pos - length)
-        hit[first:, 2:, slice(None) if key else slice(32, 64)] = True
+        hit[first:, G:2 * G, slice(None) if key else slice(32, 64)] = True
         assert np.isnan(got[hit]).all(), (pos, key)
         assert (np.abs(got - want)[~hit] <= tol[~hit]).all(), (pos, key)
 
 
 @pytest.mark.parametrize("io", [F32, BF16])
-def test_attention_queries_that_are_no_numbers(ops, io):
+@HEADS
+def test_attention_queries_that_are_no_numbers(ops, H, Hkv, io):
     """They spoil their own row and head."""
     rng = np.random.default_rng(2)
-    for rows in (3, 60):
-        cache = filled(rng, 1, 0, 2, 128, [0], [40], [rows])
-        q, qx = rounded(rng.standard_normal((rows, 4, 128)), io)
+    for rows in (3, 60, 110):
+        cache = filled(rng, 1, 0, Hkv, 128, [0], [40], [rows])
+        q, qx = rounded(rng.standard_normal((rows, H, 128)), io)
         want = ref.attention(cache, 0, [0], [40], [rows], qx)
         tol = np.broadcast_to(tolerance(cache, 0, [0], [40], [rows], qx, io, want), want.shape)
         q[1, 2, 77], q[rows - 1, 0, 3] = float("nan"), float("inf")
@@ -454,7 +485,7 @@ def test_attention_queries_that_are_no_numbers(ops, io):
         assert np.isnan(got[bad]).all() and (np.abs(got - want)[~bad] <= tol[~bad]).all()
 
 
-@pytest.mark.parametrize("rows", [1, 70])
+@pytest.mark.parametrize("rows", [1, 70, 2100])
 def test_attention_far_into_a_large_pool(ops, rows):
     """Blocks behind byte 2^32 of the pool and of the layer."""
     rng = np.random.default_rng(5)
@@ -694,7 +725,7 @@ def test_a_captured_step_replays(ops):
     """A graph of append, rotary, attention and read with eager work between its replays, on the same handle."""
     rng = np.random.default_rng(41)
     io, H, Hkv, hd = BF16, 8, 2, 128
-    for lens, rows in (([700, 20], [1, 1]), ([300, 64], [40, 9])):
+    for lens, rows in (([700, 20], [1, 1]), ([300, 64], [40, 9]), ([300, 1], [2100, 3])):
         cache = filled(rng, 1, 0, Hkv, hd, [0, 1], lens, rows)
         view, batch, r = cache.device(), CacheBatch([0, 1], lens, rows), Rotary(128)
         x = torch.zeros(sum(rows), H + 2 * Hkv, hd, dtype=io, device="cuda")
@@ -751,7 +782,7 @@ def test_graphs_of_one_handle_take_turns(ops):
     """Two captured calls that share the handle's partial results and counters, one after the other, and eager ones between."""
     rng = np.random.default_rng(46)
     calls = []
-    for lens, rows, io in (([5000, 30], [1, 2], F32), ([2100, 9], [90, 1], BF16)):
+    for lens, rows, io in (([5000, 30], [1, 2], F32), ([2100, 9], [90, 1], BF16), ([700, 20], [2100, 5], BF16)):
         cache = filled(rng, 1, 0, 2, 128, [0, 1], lens, rows)
         view, batch = cache.device(), CacheBatch([0, 1], lens, rows)
         q = torch.from_numpy(rng.standard_normal((sum(rows), 8, 128))).to(io).cuda()
@@ -800,7 +831,7 @@ def test_streams_take_turns_and_handles_run_beside_each_other():
 def test_results_do_not_change_from_call_to_call(ops):
     """Splits are merged in a fixed order, whichever arrives last."""
     rng = np.random.default_rng(44)
-    for lens, rows, io in (([9000, 300], [1, 1], F32), ([4000], [70], BF16)):
+    for lens, rows, io in (([9000, 300], [1, 1], F32), ([4000], [70], BF16), ([4000], [2100], BF16), ([4000], [2100], F32)):
         cache = filled(rng, 1, 0, 2, 64, list(range(len(lens))), lens, rows)
         view, batch = cache.device(), CacheBatch(list(range(len(lens))), lens, rows)
         q = torch.from_numpy(rng.standard_normal((sum(rows), 8, 64))).to(io).cuda()
