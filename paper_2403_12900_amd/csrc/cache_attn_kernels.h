@@ -7,11 +7,13 @@
 //   S[t][c]   = K_tile(16 x hd) . Q^T(hd x 16)
 //   O^T[e][c] += V^T_tile(16 dims x positions) . P(positions x 16)
 // with P the S accumulator re-used in place as the B operand; two blocks make
-// one 16x16x32 product.
+// one 16x16x32 product.  One pass, with a running maximum m and sum l.
 //
-// Codes times their scales are exact in bf16, and so are the products of
-// fp32 queries in three bf16 parts; the probabilities enter their product in
-// three parts for fp32 outputs (24 bits) and in two for bf16 ones (16 bits).
+// Codes times their scales are exact in bf16, and so are the products of fp32
+// queries in three bf16 parts.  Probabilities and values meet in fp16, whose 11
+// bits of a probability bf16 would take two parts for, where fp16 holds the
+// values exactly (any code at scales 2^-18 .. 2^13); else in bf16, the
+// probabilities in two parts (bf16 outputs, 16 bits) or three (fp32, 24).
 #pragma once
 
 #include <type_traits>
@@ -391,6 +393,14 @@ __device__ __forceinline__ void cache_step(const CacheAttnArgs& a, CacheStep<HD>
 // through LDS, the splits' by the one that arrives last.  A wave that meets a
 // value that fp16 does not hold exactly, or a NaN that not all columns see,
 // starts its run over with cache_step.
+//
+// Bound by memory in long caches: 8 requests of about 24000 positions, 64 heads on
+// 8, bf16 (228 MB): 46.5 us, 4.9 TB/s with launch, prologue and merge (the same
+// loads alone: 45); by the trips to memory of a run's few steps in short ones: 32
+// requests of about 400 positions, 32 heads, fp32 (67 MB): 21.3 us, the loads alone
+// 17.5.  Two steps on their way in registers: three measured 22.8 / 47.2 (short /
+// long), four work-groups on a CU with fewer registers 23.3 / 50.3, loads that stay
+// in the cache 20.5 / 52, work-groups of two waves 32 (short).
 template <class IO, int HD, int NT>
 __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_cache_attn(CacheAttnArgs a) {
   using Step = CacheStep<HD>;
@@ -606,11 +616,9 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_cache_attn(CacheAttnAr
 // ---------------------------------------------------------------------------
 
 // More than 32 columns.  Work-group: a request's column group of 64 NT columns
-// (16 NT per wave) over the blocks of one split.  The waves share every
-// block through LDS: keys as codes, which each wave expands to bf16 in
-// registers, values expanded to fp16 by the thread that fetched them.  While a
-// step is computed from LDS, the next one goes to the other buffer and the one
-// after it is fetched: one barrier per step.
+// (16 NT per wave) over the blocks of one split.  The waves share every block
+// through LDS: the thread that fetched a word of codes expands it, keys to bf16
+// and values to fp16, and puts it there as a piece of an operand.
 //
 // Probabilities enter their product in fp16: 2^-12 of themselves for bf16
 // outputs (whose own rounding is 2^-8), 2^-23 in two parts for fp32 ones.  Held
@@ -619,16 +627,24 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_cache_attn(CacheAttnAr
 // value that fp16 does not hold exactly, or a NaN that not all columns see, the
 // work-group starts over, its waves reading the blocks themselves as the other
 // kernel's do.
+//
+// Bound by the vector unit's issue (softmax and expansion) beside the products:
+// 2048 rows of 32 heads behind 5100 positions, bf16, 230 us, 1050 TFLOP/s of the
+// 1359 that a library product of 16384^3 reaches.  Expanded keys in each wave
+// instead of once 241; a barrier per step instead of every other, and scores in
+// the outputs' own step, 274; 32x32 products no faster; 256 columns 276.
 template <class IO, int HD, int NT>
 __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
   using F = Mx4<HD>;
   using Parts = CacheParts<IO>;
   constexpr int NF = HD / 32, NE = HD / 16, P = F::P, CW = 64 * NT;
   constexpr int kKeys = 4 * HD;                             // words of a step's key codes; as many of its values
-  constexpr int kScales = HD / 4;                           // words of its key scales
   constexpr int W = kKeys / 256;                            // words of a thread, keys or values
+  // Operands of a step's keys: piece c of block b at [(2 c + b) * 64 + lane], the
+  // second half of the pieces moved by 64 bytes (a thread writes pieces of either).
   struct Keys {
-    uint32_t code[kKeys], scale[kScales];
+    uint4 op[NF * 2 * 64 + 4];
+    static __device__ __forceinline__ int at(int c, int b) { return (2 * c + b) * 64 + c / 2 * 4; }
   };
   __shared__ uint4 vals[4][NE * 64];  // of a step: operands: a lane's 8 bytes of block 0, of block 1
   __shared__ __attribute__((aligned(16))) Keys keys[4];
@@ -688,7 +704,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
   } next[2] = {};  // two steps on their way into LDS
   const auto fetch_keys = [&](int n, const uint8_t* tile) {
     words(tile + at * 4, next[n].k);
-    if (ft < kScales / 2) next[n].ks = *reinterpret_cast<const uint32_t*>(tile + F::kKs + ft * 4);
+    next[n].ks = tile[F::kKs + at / 4];
   };
   const auto fetch_values = [&](int n, const uint8_t* tile) {
     words(tile + F::kV + at * 4, next[n].v);
@@ -697,9 +713,14 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
   // Whether a step reaches past what all columns see, or past the split.
   const auto is_tail = [&](int step) { return 16 * (t.first + 2 * step + 2) > all || t.first + 2 * step + 2 > end; };
   const auto put_keys = [&](int n, Keys& to) {
+    const float s = scale_of<0>(next[n].ks);
 #pragma unroll
-    for (int w = 0; w < W; ++w) to.code[fb * (kKeys / 2) + at + w] = next[n].k[w];
-    if (ft < kScales / 2) to.scale[fb * (kScales / 2) + ft] = next[n].ks;
+    for (int w = 0; w < W; ++w) {
+      const uint32_t x = next[n].k[w];
+      const int d0 = at / 64 * 32 + at % 4 * 8 + 8 * w, kg = d0 / (HD / 4), c = d0 % (HD / 4) / 8;
+      to.op[Keys::at(c, fb) + at / 4 % 16 + 16 * kg] =
+          make_uint4(codes_to_bf16<0>(x, s), codes_to_bf16<1>(x, s), codes_to_bf16<2>(x, s), codes_to_bf16<3>(x, s));
+    }
   };
   uint32_t beyond = 0;  // not 0: this thread met a value that fp16 does not hold, or a NaN
   const auto put_values = [&](int n, int step, uint4* to, auto tail) {
@@ -716,7 +737,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
       out |= odd_scales(x[w]);
     }
     if (__ballot(out != 0) != 0) {
-      asm volatile("");  // (keeps what follows behind the branch: 255 us without, 247.5 with)
+      asm volatile("");  // (keeps what follows behind the branch: 247 us where checking every word took 255)
 #pragma unroll
       for (int w = 0; w < W; ++w) beyond |= beyond_f16(v[w], x[w]) ? 1u : 0u;
     }
@@ -749,26 +770,11 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
     for (int jt = 0; jt < NT; ++jt)
 #pragma unroll
       for (int b = 0; b < 2; ++b) S.x[jt][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    uint32_t kw[2][P];
-    float ks[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const uint8_t* kb = reinterpret_cast<const uint8_t*>(from.code) + b * (kKeys * 2) + F::key_code(h, HD / 4 * g);
-      if constexpr (P == 4) {
-        const uint4 x = *reinterpret_cast<const uint4*>(kb);
-        kw[b][0] = x.x, kw[b][1] = x.y, kw[b][2] = x.z, kw[b][3] = x.w;
-      } else {
-        const uint2 x = *reinterpret_cast<const uint2*>(kb);
-        kw[b][0] = x.x, kw[b][1] = x.y;
-      }
-      ks[b] = scale_of<0>((reinterpret_cast<const uint8_t*>(from.scale) + b * (HD / 2))[HD / 4 * g / 32 * 16 + h]);
-    }
 #pragma unroll
     for (int c = 0; c < NF; ++c)
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const uint4 x = make_uint4(codes_to_bf16<0>(kw[b][c], ks[b]), codes_to_bf16<1>(kw[b][c], ks[b]),
-                                   codes_to_bf16<2>(kw[b][c], ks[b]), codes_to_bf16<3>(kw[b][c], ks[b]));
+        const uint4 x = from.op[Keys::at(c, b) + lane];
 #pragma unroll
         for (int q = 0; q < Parts::q; ++q)
 #pragma unroll
@@ -807,8 +813,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
         for (int jt = 0; jt < NT; ++jt) O[jt][e] = mma_f16(O[jt][e], x, pp[jt][q]);
     }
     // Schedule: three operands ahead of the exponentials, the others between the
-    // products, so that none is waited for (295 us without, 285 with; see above
-    // for the case).
+    // products, so that none is waited for (236 us without).
     __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
     __builtin_amdgcn_sched_group_barrier(0x402, NT * 12, 0);
     const auto group = [](auto) {
@@ -920,6 +925,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
 
 // Merge of the wide kernel's splits in a launch of its own, whose work-groups
 // share out all outputs: 16 columns of one (column group of CW, KV head) each.
+// (One last arrival would have 64 or 128 columns of up to 64 splits to itself.)
 constexpr int kMergeWide = 16;
 template <class IO, int HD, int CW>
 __global__ __launch_bounds__(256) void k_cache_merge(CacheAttnArgs a) {

@@ -227,18 +227,18 @@ inline spr_status plan_move(const spr_pages* p, int n, const int32_t* src, const
 // Columns that one attention work-group takes: up to 32, whose four waves share
 // out the blocks, or 64 or 128 (no more than `most`), whose waves share out the
 // columns.  More columns read the cache less often; fewer make more work-groups
-// of shorter steps, which counts as long as a CU gets no more than two of 32 or one
-// and a half of 128.  On 256 CUs, 32 heads, bf16, in us with 32 / 64 / 128 columns:
-//   1 x 512 rows at position 0    12 / 24 / 27     16 x 64 rows at position 500   34 / 27 / 28
-//   1 x 256 rows at 2000          28 / 36 / 42      1 x 1024 rows at 500          42 / 38 / 52
-//   1 x 512 rows at 8000         109 / 111 / 121    1 x 2048 rows at 2000        176 / 158 / 129
-// (over 330 shapes of 0 to 8000 positions 0.7% behind the best of the three on
-// average, with the widest that fit 25%; fp32, which has no 128, 2% and 21%.)
+// of shorter steps, which counts as long as a CU gets no more than two of 32 or
+// one of 128.  On 256 CUs, 32 heads, bf16, in us with 32 / 64 / 128 columns:
+//   1 x 512 rows at position 0    11 / 22 / 27     16 x 64 rows at position 500   34 / 27 / 26
+//   1 x 256 rows at 2000          28 / 33 / 40      1 x 1024 rows at 500          41 / 37 / 50
+//   1 x 512 rows at 8000         109 / 113 / 113    1 x 2048 rows at 2000        175 / 164 / 121
+// (over 264 shapes of 0 to 8000 positions 0.6% behind the best of the three on
+// average, with the widest that fit 22%; fp32, which has no 128, 0.7% and 16%.)
 inline int cache_cols_per_group(const CacheInfo& t, int G, int Hkv, int n_cu, int most) {
   const int64_t cols = static_cast<int64_t>(t.max_rows) * G, all = static_cast<int64_t>(t.rows) * G * Hkv;
   if (cols <= 16) return 16;
   if (cols <= 32 || all <= int64_t{64} * n_cu) return 32;
-  return cols <= 64 || all <= int64_t{192} * n_cu ? 64 : most;
+  return cols <= 64 || all <= int64_t{128} * n_cu ? 64 : most;
 }
 
 // Work items of one attention launch: per request its column groups, each in

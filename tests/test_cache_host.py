@@ -289,7 +289,7 @@ def test_work_items_of_an_attention_launch():
         cw, bps, groups, split = (int(x) for x in out[:4])
         item0, order, ncg, cg0 = out[4:5 + n], out[5 + n:5 + 2 * n], out[5 + 2 * n:5 + 3 * n], out[5 + 3 * n:]
         cols, every = int(rows.max()) * G, int(rows.sum()) * G * Hkv
-        assert cw == (16 if cols <= 16 else 32 if cols <= 32 or every <= 64 * n_cu else 64 if cols <= 64 or every <= 192 * n_cu else 128)
+        assert cw == (16 if cols <= 16 else 32 if cols <= 32 or every <= 64 * n_cu else 64 if cols <= 64 or every <= 128 * n_cu else 128)
         assert sorted(order) == list(range(n)) and bps % least == 0 and item0[0] == 0
         blocks = (lens.astype(np.int64) + rows + 15) // 16
         assert (np.diff(blocks[order]) <= 0).all()

@@ -379,7 +379,7 @@ def test_attention_of_many_rows_and_heads_over_long_contexts(ops, H, Hkv, hd, ro
 
 
 # Heads and KV heads of the tests below: few, whose rows' columns work-groups share 16 or 32 at a time, and so many that from
-# 33 rows on they take 64 and from 97 on, in bf16, 128.
+# 33 rows on they take 64 and from 65 on, in bf16, 128.
 HEADS = pytest.mark.parametrize("H,Hkv", [(4, 2), (512, 32)])
 
 
