@@ -629,7 +629,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_cache_attn(CacheAttnAr
 // kernel's do.
 //
 // Bound by the vector unit's issue (softmax and expansion) beside the products:
-// 2048 rows of 32 heads behind 5100 positions, bf16, 230 us, 1050 TFLOP/s of the
+// 2048 rows of 32 heads behind 6150 positions, bf16, 230 us, 1050 TFLOP/s of the
 // 1359 that a library product of 16384^3 reaches.  Expanded keys in each wave
 // instead of once 241; a barrier per step instead of every other, and scores in
 // the outputs' own step, 274; 32x32 products no faster; 256 columns 276.
