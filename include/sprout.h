@@ -655,6 +655,7 @@ spr_status spr_cache_attention(spr_cache_ops* ops, const spr_kv4_view* kv, int32
  * is not NULL (a 4-bit cache has one pool: data as k).  block_bytes is a
  * multiple of 16, the pools are 16-byte aligned.  Views of a model's own cache
  * are not for spr_cache_fork and spr_cache_move: its slots own its blocks.
+ * Calls that would copy from more than 64 GiB of blocks are refused.
  */
 typedef struct {
   void* k; /* device */

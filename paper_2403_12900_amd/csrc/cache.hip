@@ -115,6 +115,9 @@ spr_status rows_call(spr_cache_ops* o, const char* what, const spr_kv4_view* kv,
   return e == hipSuccess ? SPR_OK : hip_failed(o, what, e);
 }
 
+// Work-groups of a launch: its threads are counted in 32 bits.
+constexpr int64_t kMostGroups = (int64_t{1} << 24) - 1;
+
 // What a launch has to know of the pools; deep: 16-byte pieces of a thread.
 PageCopy page_copy(const spr_pages& p, int deep) {
   PageCopy c{};
@@ -283,7 +286,7 @@ spr_status spr_cache_fork(spr_cache_ops* o, const spr_pages* pages, int32_t n, c
     std::memcpy(a.fresh, f.fresh, sizeof(int) * f.n);
     std::memcpy(a.first, f.first, sizeof(int) * (f.groups + 1));
     const int64_t items = static_cast<int64_t>(a.c.pools) * a.c.layers * a.c.chunks;
-    if (f.n + f.groups * items > INT32_MAX) return bad_arg("cache_fork: more than 2^31 pieces of work");
+    if (f.n + f.groups * items > kMostGroups) return bad_arg("cache_fork: the blocks are too large for one call");
     k_cache_fork<<<static_cast<unsigned>(f.n + f.groups * items), 256, 0, o->st>>>(a);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SPR_OK : hip_failed(o, "cache_fork", e);
@@ -304,7 +307,7 @@ spr_status spr_cache_move(spr_cache_ops* o, const spr_pages* pages, int32_t n, c
     a.entries = static_cast<int64_t>(pages->n_slots) * pages->max_blocks;
     const int64_t items = static_cast<int64_t>(a.c.pools) * a.c.layers * a.c.chunks;
     const int64_t groups = (a.entries + kTableEntries - 1) / kTableEntries;
-    if (groups + kMoves * items > INT32_MAX) return bad_arg("cache_move: more than 2^31 pieces of work");
+    if (groups + std::min(n, kMoves) * items > kMostGroups) return bad_arg("cache_move: the blocks or the table are too large for one call");
     a.table_groups = static_cast<int>(groups);
     DeviceGuard dev(o->dev);
     if (dev.e != hipSuccess) return hip_failed(o, "cache_move", dev.e);

@@ -15,6 +15,8 @@ Tolerances of the rest, derived (eps = 2^-24, half a step of fp32; half a step o
     - fp32 outputs: probabilities enter their product to 2^-22 of themselves, which moves the mean by at most 2^-22 max|v|;
     - bf16 outputs: probabilities enter it to 2^-12 of themselves, and the output's own rounding is 2^-8 of it.
 """
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -619,6 +621,15 @@ def test_pages_refusals(ops):
         with pytest.raises(SproutError, match=what) as e:
             call()
         assert e.value.status == binding.SPR_ERR_INVALID_ARG
+    # Pools of a size that a launch has too many work-groups for (refused before anything is touched).
+    huge = binding.SprPages(view.data.data_ptr(), None, 1 << 30, 1000, 20, view.block_table.data_ptr(), 3, 2)
+    one = [np.array([x], dtype=np.int32) for x in (0, 1, 20, 3)]
+    at = [x.ctypes.data for x in one]
+    for status in (ops.lib.spr_cache_fork(ops.h, ctypes.byref(huge), 1, *at),
+                   ops.lib.spr_cache_move(ops.h, ctypes.byref(huge), 1, at[0], at[1])):
+        assert status == binding.SPR_ERR_INVALID_ARG
+    huge = binding.SprPages(view.data.data_ptr(), None, 1 << 10, 1, 20, view.block_table.data_ptr(), 1 << 20, 1 << 20)
+    assert ops.lib.spr_cache_move(ops.h, ctypes.byref(huge), 1, at[0], at[1]) == binding.SPR_ERR_INVALID_ARG
     assert torch.equal(view.data, before[0]) and torch.equal(view.block_table, before[1])
 
 
