@@ -640,8 +640,10 @@ spr_status spr_cache_read(spr_cache_ops* ops, const spr_kv4_view* kv, int32_t la
  * in the cache behind a row's last position does not reach its output,
  * whatever it holds.
  *   n_heads  a multiple of n_kv_heads, n_heads / n_kv_heads <= 16
- *   dtype    of q and out; scores, sums and products are held in fp32, the
- *            probabilities of bf16 outputs to 2^-12
+ *   dtype    of q and out; scores and sums are held in fp32.  Probabilities enter
+ *            their product with the values to 2^-11 of themselves for bf16
+ *            outputs and to 2^-22 for fp32 ones, small ones to 2^-32 and 2^-36
+ *            of the row's largest
  *   q, out   device [rows] x [n_heads * head_dim], aligned as in
  *            spr_cache_rotary.  out must not overlap q.
  */

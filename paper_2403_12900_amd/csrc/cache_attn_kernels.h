@@ -254,15 +254,21 @@ __device__ __forceinline__ f32x4_t mma_f16(f32x4_t acc, uint4 a, uint4 b) {
 
 constexpr uint4 kHalfOnes{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};  // eight fp16 ones
 
+// Parts of a probability in fp16, and how far it is lifted: a row's largest one so
+// far lies in [2^lift, 2^limit], below fp16's largest number, so that fp16's last
+// step, 2^-24, is 2^-31 (bf16 outputs) or 2^-35 (fp32) of it: one part's 2^-11 holds
+// down to 2^-21 of the largest, two parts' 2^-22 down to 2^-14.  More lift raises the
+// maximum more often (4 x 1024 first rows of 32 heads, lift 7 / 10 / 11 / 12: fp32
+// 115 / 116 / 116 / 119 us; bf16 74 with 7, 81 with 12).
 template <class IO>
 struct HalfParts {
   static constexpr int p = IO::kRaw ? 1 : 2;
+  static constexpr float lift = IO::kRaw ? 7.f : 11.f, limit = IO::kRaw ? 15.f : 15.9f;
 };
-constexpr int kLift = 7;
 
 // Online softmax of a wave's column tiles as softmax_step, without the sum:
-// scores S to probabilities p.
-template <int NT, int NE>
+// scores S to probabilities p, lifted as above.
+template <class IO, int NT, int NE>
 __device__ __forceinline__ void lifted_softmax(const f32x4_t (*S)[2], float qscale, float* m, f32x4_t* l, f32x4_t (*O)[NE],
                                              float (*p)[8]) {
   const auto highest = [](const float* x) {
@@ -273,7 +279,7 @@ __device__ __forceinline__ void lifted_softmax(const f32x4_t (*S)[2], float qsca
   for (int jt = 0; jt < NT; ++jt) {
 #pragma unroll
     for (int r = 0; r < 8; ++r) p[jt][r] = fmaf(S[jt][r / 4][r % 4], qscale, -m[jt]);
-    over |= highest(p[jt]) > kLift + kRaise;
+    over |= highest(p[jt]) > HalfParts<IO>::limit;
   }
   if (__ballot(over) != 0) {
 #pragma unroll
@@ -283,7 +289,7 @@ __device__ __forceinline__ void lifted_softmax(const f32x4_t (*S)[2], float qsca
       float mx = highest(p[jt]);
       mx = fmaxf(mx, __shfl_xor(mx, 16));
       mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float up = fmaxf(m[jt], mx - kLift);
+      const float up = fmaxf(m[jt], mx - HalfParts<IO>::lift);
       const float alpha = __builtin_amdgcn_exp2f(m[jt] - up);
       m[jt] = up;
       l[jt] *= alpha;
@@ -511,7 +517,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_cache_attn(CacheAttnAr
       beyond |= __ballot(x) != 0;
     }
     float p[NT][8];
-    lifted_softmax<NT, NE>(S, a.qscale, m, l, O, p);
+    lifted_softmax<IO, NT, NE>(S, a.qscale, m, l, O, p);
     uint4 pp[NT][HalfParts<IO>::p];
 #pragma unroll
     for (int jt = 0; jt < NT; ++jt)
@@ -620,10 +626,12 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void k_cache_attn(CacheAttnAr
 // through LDS: the thread that fetched a word of codes expands it, keys to bf16
 // and values to fp16, and puts it there as a piece of an operand.
 //
-// Probabilities enter their product in fp16: 2^-12 of themselves for bf16
-// outputs (whose own rounding is 2^-8), 2^-23 in two parts for fp32 ones.  Held
-// 2^7 above the running maximum's place they keep those bits down to 2^-21 of
-// the largest.  Their sum is one more product, with ones.  Where a step meets a
+// Probabilities enter their product in fp16: to 2^-11 of themselves for bf16
+// outputs (whose own rounding is 2^-8; two parts: 313 us where one takes 235, and
+// outputs 0.00166 of their norm from 64 bits instead of 0.00167), to 2^-22 in two
+// parts for fp32 ones; small ones to 2^-32 and 2^-36 of the row's largest (half of
+// fp16's last step, see HalfParts).  The sums in fp32 round by more: a step's 32
+// positions move them by 2^-24.  Their sum is one more product, with ones.  Where a step meets a
 // value that fp16 does not hold exactly, or a NaN that not all columns see, the
 // work-group starts over, its waves reading the blocks themselves as the other
 // kernel's do.
@@ -795,7 +803,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_attn_wide(CacheAttnArgs a) {
   };
   const auto outputs = [&](const Scores& S, const uint4* from) {
     float p[NT][8];
-    lifted_softmax<NT, NE>(S.x, a.qscale, m, l, O, p);
+    lifted_softmax<IO, NT, NE>(S.x, a.qscale, m, l, O, p);
     uint4 pp[NT][HalfParts<IO>::p];
 #pragma unroll
     for (int jt = 0; jt < NT; ++jt)

@@ -406,6 +406,35 @@ def test_attention_scores_of_all_sizes(ops, H, Hkv, io):
         assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
 
 
+@HEADS
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("rows", [1, 40, 100])
+def test_attention_of_fp32_small_probabilities(ops, H, Hkv, hd, rows):
+    """Every 16th position takes nearly all weight and has the value 0 but in one dimension of each group, the others have p =
+    2^-20 of its weight and the value 1: an output is about 15 p, to what p is held to.
+
+    A score is one exact product (dimension 0) or 0.  p is off by 2^-36 of the largest from its parts (2^-22 of itself is less),
+    by 20 * 2^-24 ln 2 < 2^-20 of itself from the factor of the scores (a difference of 20 between two), by 2^-20 from the
+    exponent's argument (below 16 in magnitude: half a step is 2^-21) and 2^-23 from exp2; the two sums, one addition for each 16
+    positions at most, by (T / 16 + 8) eps each, merges and the output's own rounding among them."""
+    rng = np.random.default_rng(hd + rows)
+    length = 500
+    T = length + rows
+    q = rng.standard_normal((rows, H, hd))
+    q[..., 0] = rng.uniform(19.5, 20.5, (rows, H)) * np.log(2) * np.sqrt(hd)
+    q, qx = rounded(q, F32)
+    k, v = np.zeros((T, Hkv, hd)), np.ones((T, Hkv, hd))
+    k[::16, :, 0], v[::16] = 1, np.arange(hd) % 32 == 0
+    cache = ref.Cache(rng, 1, Hkv, hd, [T])
+    cache.append(0, 0, 0, k, v)
+    want = ref.attention(cache, 0, [0], [length], [rows], qx)
+    got = ops.attention(cache.device(), 0, CacheBatch([0], [length], [rows]), q).double().cpu().numpy()
+    p = np.exp(-qx[..., :1] / np.sqrt(hd))
+    tol = 2.0 ** -36 / p + 2.0 ** -22 + 2 * 2.0 ** -20 + 2.0 ** -23 + 2 * (T / 16 + 8) * EPS
+    worst = (np.abs(got - want) / (tol * want))[..., np.arange(hd) % 32 > 0].max()
+    assert worst <= 1, f"{worst} of the tolerance"
+
+
 @pytest.mark.parametrize("io", [F32, BF16])
 @pytest.mark.parametrize("scale", [2.0 ** -60, 2.0 ** -20, 2.0 ** 20, 2.0 ** 90])
 @HEADS
