@@ -678,7 +678,10 @@ typedef struct {
  *   lens    host [n]: 0 .. max_blocks * 16
  *   fresh   host [n]: distinct free blocks (not read where lens[i] % 16 == 0)
  * A source entry outside the pool, or one that is a fresh block of the call,
- * is not copied and fails the handle's next call.
+ * is not copied to the target's row, nor is its block, and fails the handle's
+ * next call.  No fork writes to a block that another of the call copies from;
+ * a fresh block that is one of the sources' full blocks is written all the
+ * same (that fresh blocks are free is the caller's to see to).
  */
 spr_status spr_cache_fork(spr_cache_ops* ops, const spr_pages* pages, int32_t n, const int32_t* source,
                           const int32_t* target, const int32_t* lens, const int32_t* fresh);

@@ -283,8 +283,10 @@ spr_status spr_cache_fork(spr_cache_ops* o, const spr_pages* pages, int32_t n, c
     std::memcpy(a.source, f.source, sizeof(int) * f.n);
     std::memcpy(a.target, f.target, sizeof(int) * f.n);
     std::memcpy(a.len, f.len, sizeof(int) * f.n);
-    std::memcpy(a.fresh, f.fresh, sizeof(int) * f.n);
-    std::memcpy(a.first, f.first, sizeof(int) * (f.groups + 1));
+    std::fill(std::copy(f.fresh, f.fresh + f.n, a.fresh), a.fresh + kCacheReqs, -1);
+    for (int g = 0; g <= f.groups; ++g) a.first[g] = static_cast<uint8_t>(f.first[g]);
+    for (int g = 0; g < f.groups; ++g)
+      a.part[g] = static_cast<int64_t>(f.source[f.first[g]]) * a.mb + f.len[f.first[g]] / spr::kKvBlock;
     const int64_t items = static_cast<int64_t>(a.c.pools) * a.c.layers * a.c.chunks;
     if (f.n + f.groups * items > kMostGroups) return bad_arg("cache_fork: the blocks are too large for one call");
     k_cache_fork<<<static_cast<unsigned>(f.n + f.groups * items), 256, 0, o->st>>>(a);

@@ -41,43 +41,82 @@ struct ForkArgs {
   int32_t* bt;
   int* err;
   int mb, nb, n, groups;
-  int source[kCacheReqs], target[kCacheReqs], len[kCacheReqs], fresh[kCacheReqs];
-  int first[kCacheReqs + 1];
+  int source[kCacheReqs], target[kCacheReqs], len[kCacheReqs];
+  int fresh[kCacheReqs];           // -1 from first[groups] on
+  int64_t part[kCacheReqs];        // table entry of each group's block
+  uint8_t first[kCacheReqs + 1];
 };
 static_assert(sizeof(ForkArgs) <= 3584, "kernel arguments");
+static_assert(kCacheReqs <= 255 && kCacheReqs % 8 == 0, "first's type, and fresh in eights");
+
+// What keeps the forks f0 .. f1 - 1 from taking a copy of block id (0: nothing): id
+// outside the pool, or a fresh block of the call that another of its forks copies
+// from, be it id or one of their own.  The same for all threads of a work-group.
+__device__ __forceinline__ int fork_fault(const ForkArgs& a, int f0, int f1, int id) {
+  const int tid = threadIdx.x;
+  bool fresh = false;
+  for (int i = tid; i < a.first[a.groups]; i += 256) fresh |= a.fresh[i] == id;
+  for (int i = tid; i < a.groups * (f1 - f0); i += 256) {  // (block that is copied, fresh block of these)
+    const int f = i / a.groups;
+    fresh |= a.fresh[f0 + f] == a.bt[a.part[i - f * a.groups]];
+  }
+  if (__syncthreads_or(fresh)) return kErrFresh;
+  return static_cast<unsigned>(id) >= static_cast<unsigned>(a.nb) ? kErrBlockId : 0;
+}
 
 // Work-groups: n for the table rows, then the chunks of each group of forks
 // that copy one block: it is read once and written to all of their blocks.
 // Bound by the writes: 60 forks of 3 blocks, 40 layers of 40 heads in bf16 (524
 // MB): 98 us, 5.6 TB/s of the 6.9 that a fill of 4 GiB reaches.  Stores that stay
 // in the cache: 112 us with chunks of 16 KB, 107 without them; chunks of 8 KB 103,
-// of 4 KB 98.
+// of 4 KB 98.  Looking the forks over takes less than 1 us of these, beside the
+// block's read.
 __global__ __launch_bounds__(256) void k_cache_fork(ForkArgs a) {
   const int tid = threadIdx.x;
   if (static_cast<int>(blockIdx.x) < a.n) {
     const int i = blockIdx.x, full = a.len[i] / 16;
     const int32_t* from = a.bt + static_cast<size_t>(a.source[i]) * a.mb;
     int32_t* to = a.bt + static_cast<size_t>(a.target[i]) * a.mb;
-    for (int e = tid; e < full; e += 256) to[e] = from[e];
-    if (tid == 0 && a.fresh[i] >= 0) to[full] = a.fresh[i];
+    const int copies = a.first[a.groups];
+    constexpr int kDeep = 8;  // entries of a thread in flight
+    for (int e0 = tid; e0 < full; e0 += 256 * kDeep) {
+      int id[kDeep], fault = 0;
+      uint32_t fresh = 0;
+#pragma unroll
+      for (int k = 0; k < kDeep; ++k) id[k] = from[min(e0 + 256 * k, full - 1)];
+      for (int f = 0; f < copies; f += 8)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int k = 0; k < kDeep; ++k) fresh |= id[k] == a.fresh[f + j] ? 1u << k : 0u;
+#pragma unroll
+      for (int k = 0; k < kDeep; ++k) {
+        if (e0 + 256 * k >= full) break;
+        const bool lost = static_cast<unsigned>(id[k]) >= static_cast<unsigned>(a.nb);
+        if (lost || fresh >> k & 1) fault = lost ? kErrBlockId : kErrFresh;
+        else to[e0 + 256 * k] = id[k];
+      }
+      if (fault) raise_check(a.err, fault);
+    }
+    if (i >= copies) return;
+    const int group = __syncthreads_count(tid < a.groups && a.first[tid] <= i) - 1;
+    if (fork_fault(a, a.first[group], a.first[group + 1], from[full]) == 0 && tid == 0) to[full] = a.fresh[i];
     return;
   }
   const int items = a.c.pools * a.c.layers * a.c.chunks;
   const int w = blockIdx.x - a.n, group = w / items;
   const int f0 = a.first[group], f1 = a.first[group + 1];
-  const int id = a.bt[static_cast<size_t>(a.source[f0]) * a.mb + a.len[f0] / 16];
-  bool fresh = false;
-  for (int i = tid; i < a.first[a.groups]; i += 256) fresh |= a.fresh[i] == id;
-  const bool lost = static_cast<unsigned>(id) >= static_cast<unsigned>(a.nb);
-  if (__syncthreads_or(fresh) || lost) {
-    if (tid == 0) raise_check(a.err, lost ? kErrBlockId : kErrFresh);
+  const int id = a.bt[a.part[group]];
+  const PageItem it = page_item(a.c, w - group * items);
+  const int x = it.first + tid;
+  // Read while the forks are looked over (block 0 where there is no such block).
+  const int at = static_cast<unsigned>(id) < static_cast<unsigned>(a.nb) ? id : 0;
+  const page_piece_t v = reinterpret_cast<const page_piece_t*>(it.base + at * a.c.block_bytes)[min(x, it.end - 1)];
+  if (const int fault = fork_fault(a, f0, f1, id)) {
+    if (tid == 0) raise_check(a.err, fault);
     return;
   }
-  const PageItem it = page_item(a.c, w - group * items);
-  const page_piece_t* src = reinterpret_cast<const page_piece_t*>(it.base + id * a.c.block_bytes);
-  const int x = it.first + tid;
   if (x >= it.end) return;
-  const page_piece_t v = src[x];
   for (int f = f0; f < f1; ++f)
     __builtin_nontemporal_store(v, reinterpret_cast<page_piece_t*>(it.base + a.fresh[f] * a.c.block_bytes) + x);
 }

@@ -619,6 +619,50 @@ def test_fork_of_a_source_that_is_not_there(what):
     o.close()
 
 
+def check_faulty_fork(source_rows, target, source, lens, fresh, want_rows, copied, match):
+    """A fork over sources with these table rows, its targets' rows afterwards, the blocks that were copied, the next call."""
+    o = CacheOps()
+    view = any_cache(np.random.default_rng(3), BF16, 2, 30, 2, 64, 6, 3)
+    for s, row in source_rows.items():
+        view.block_table[s] = torch.tensor(row, dtype=torch.int32)
+    for t in target:
+        view.block_table[t] = 29  # (what was there)
+    table, before = view.block_table.clone(), [p.clone() for p in pools(view)]
+    o.fork(view, source, target, lens, fresh)
+    torch.cuda.synchronize()
+    for t, row in want_rows.items():
+        table[t] = torch.tensor(row, dtype=torch.int32)
+    assert torch.equal(view.block_table, table)
+    for p, b in zip(pools(view), before):
+        for src, dst in copied:
+            b[:, dst] = b[:, src]
+        assert torch.equal(p, b)
+    with pytest.raises(SproutError, match=match) as e:
+        o.move(view, [1], [2])
+    assert e.value.status == binding.SPR_ERR_DEVICE_CHECK
+    o.close()
+
+
+@pytest.mark.parametrize("bad", [-1, 30, 2 ** 31 - 1])
+@pytest.mark.parametrize("partly", [False, True])
+def test_fork_of_a_source_whose_entry_is_outside_the_pool(bad, partly):
+    """A full block's, and a partly filled one's: the target's row takes all entries but that one."""
+    if partly:
+        check_faulty_fork({0: [4, 5, bad]}, [3, 4], [0, 0], [37, 20], [7, 8], {3: [4, 5, 29], 4: [4, 8, 29]}, [(5, 8)], "block id")
+    else:
+        check_faulty_fork({0: [4, bad, 6]}, [3, 4], [0, 0], [37, 48], [7, -1], {3: [4, 29, 7], 4: [4, 29, 6]}, [(6, 7)], "block id")
+
+
+def test_fork_of_a_full_block_that_is_fresh():
+    check_faulty_fork({0: [4, 5, 6], 1: [8, 9, 10]}, [3, 4], [0, 1], [32, 20], [-1, 5], {3: [4, 29, 29], 4: [8, 5, 29]}, [(9, 5)], "fresh block")
+
+
+def test_fork_onto_a_block_that_another_fork_copies_from():
+    """Neither fork is carried out, whose source would change under the other, nor the first's second target; the third is."""
+    check_faulty_fork({0: [4, 5, 6], 1: [8, 9, 10]}, [3, 4, 5, 2], [0, 1, 1, 0], [20, 35, 33, 7], [7, 5, 11, 12],
+                      {3: [4, 29, 29], 4: [8, 9, 29], 5: [8, 9, 29], 2: [12, 29, 29]}, [(4, 12)], "fresh block")
+
+
 @pytest.mark.parametrize("kind", ["mx4", F32, BF16])
 @pytest.mark.parametrize("layers,Hkv,hd,blocks,n,slots,mb", [(1, 1, 64, 2, 1, 1, 1), (3, 5, 64, 60, 20, 7, 9), (2, 8, 128, 40, 13, 300, 21),
                                                           (1, 1, 64, 1500, 750, 40, 60)])
