@@ -836,6 +836,41 @@ def test_a_captured_step_replays(ops):
             assert torch.equal(got, want) and torch.equal(gk, wk) and torch.equal(gv, wv) and torch.equal(x, x2)
 
 
+@pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("lens,rows", [([700, 20], [1, 1]), ([300, 64], [40, 9]), ([300, 1], [2100, 3])])
+def test_a_captured_step_writes_its_rows(ops, lens, rows, io):
+    """Replays over positions that an eager append has just filled with other values; the same step, eager, on a cache of its
+    own that never held them: outputs, what is read back, and the caches whole."""
+    rng = np.random.default_rng(47)
+    H, Hkv, hd = 8, 2, 128
+    cache = filled(rng, 1, 0, Hkv, hd, [0, 1], lens, rows)
+    view, beside, batch, r = cache.device(), cache.device(), CacheBatch([0, 1], lens, rows), Rotary(128)
+    x = torch.zeros(sum(rows), H + 2 * Hkv, hd, dtype=io, device="cuda")
+    pos = torch.from_numpy(np.concatenate([a + np.arange(n) for a, n in zip(lens, rows)]).astype(np.int32)).cuda()
+
+    def step(v):
+        ops.append(v, 0, batch, x[:, H:H + Hkv], x[:, H + Hkv:], rotary=r)
+        return (ops.attention(v, 0, batch, ops.rotary(r, x[:, :H], pos)), *ops.read(v, 0, batch, dtype=io))
+
+    step(view)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(view)
+    for trial in range(3):
+        x.copy_(torch.from_numpy(rng.standard_normal(tuple(x.shape))).to(io))
+        other = torch.from_numpy(rng.standard_normal((sum(rows), Hkv, hd))).to(io).cuda()
+        ops.append(view, 0, batch, other, other)
+        for g in got:
+            g.fill_(trial)
+        want = step(beside)
+        torch.cuda.synchronize()
+        assert not torch.equal(view.data, beside.data)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, w) for g, w in zip(got, want)) and torch.equal(view.data, beside.data)
+
+
 def test_captured_pages_replay(ops):
     """A captured fork and move keep the numbers they were given."""
     rng = np.random.default_rng(42)
