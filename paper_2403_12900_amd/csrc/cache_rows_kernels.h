@@ -133,6 +133,8 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryCall a) {
     float v[N], y[N] = {}, r[N];
     Piece::load(x + h * HD + d0, v);
     if (!a.r.pairs) load_partners<N>(x + h * HD, d0, a.r.dims, y);
+    // (To bf16 in one rounding: the compiler takes this conversion and the store's as
+    // one, through a rounding to odd.)
 #pragma unroll
     for (int j = 0; j < N; ++j) r[j] = static_cast<float>(turn_element<N>(v, y, j, d0, a.r.dims, a.r.pairs, cs));
     Piece::store(out + h * HD + d0, r);

@@ -105,6 +105,36 @@ def test_rotary_strides_and_in_place(ops, hd, dims, io):
             check_rotary(ops, rng, 21, hd, dims, layout, io, rng.integers(0, 5000, 37), strided=strided, in_place=in_place)
 
 
+def nearest_bf16(z):
+    """z in 64 bits (normal bf16 numbers), rounded once to bf16, and whether it is not too near a border of two to tell."""
+    u = np.ascontiguousarray(z).view(np.int64)
+    step, low = 1 << 45, u & ((1 << 45) - 1)
+    up = (u + (step // 2 - 1) + (u >> 45 & 1)) & ~np.int64(step - 1)
+    return up.view(np.float64), np.abs(low - step // 2) > 1 << 16  # (2^-36 of z)
+
+
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("hd,dims", [(64, 64), (128, 128), (64, 46)])
+def test_rotary_rounds_bf16_once(ops, hd, dims, layout):
+    """Results that lie 2^-40 of themselves beside the middle of two bf16 numbers (fp32 would put them onto it), and so many
+    others that some dozen of them do by chance."""
+    rng = np.random.default_rng(hd + dims)
+    x, want = rounded(rng.choice([-1, 1], (5, 3, hd)) * 2.0 ** rng.integers(-60, 60, (5, 3, hd)), BF16)
+    at0 = torch.zeros(5, dtype=torch.int32, device="cuda")
+    for odd in (1, 3):  # 1 + odd / 256: a tie, which goes down, and up
+        for beside in (-1, 0, 1):
+            got = ops.rotary(Rotary(dims, layout=layout, amplitude=1 + odd / 256 + beside * 2.0 ** -40), x, at0).double().cpu().numpy()
+            to = 1 + (odd + (beside if beside else 1 if odd == 3 else -1)) / 256
+            assert np.array_equal(got[..., :dims], to * want[..., :dims]), (odd, beside)
+    rows = 2000
+    x, want = rounded(rng.standard_normal((rows, 8, hd)), BF16)
+    positions = rng.integers(0, 5000, rows)
+    got = ops.rotary(Rotary(dims, layout=layout), x, torch.from_numpy(positions.astype(np.int32)).cuda()).double().cpu().numpy()
+    to, sure = nearest_bf16(ref.turn(want, positions, dims, layout))
+    sure[..., dims:] = True
+    assert sure.mean() > 0.999 and np.array_equal(got[sure], to[sure]), (got != to)[sure].sum()
+
+
 def test_rotary_of_many_rows_and_heads(ops):
     rng = np.random.default_rng(4)
     check_rotary(ops, rng, 64, 64, 64, "half", BF16, np.arange(700) + 5)
