@@ -657,7 +657,11 @@ spr_status spr_cache_attention(spr_cache_ops* ops, const spr_kv4_view* kv, int32
  * is not NULL (a 4-bit cache has one pool: data as k).  block_bytes is a
  * multiple of 16, the pools are 16-byte aligned.  Views of a model's own cache
  * are not for spr_cache_fork and spr_cache_move: its slots own its blocks.
- * Calls that would copy from more than 64 GiB of blocks are refused.
+ * A launch has fewer than 2^24 work-groups, and calls that would need more are
+ * refused: a fork one for each of the n table rows and, for every block it
+ * copies (once for all its forks), one for each started 4 KiB in each layer of
+ * k and v; a move one for each started 1024 table entries and, for up to 384 of
+ * its blocks (more take further launches), one for each started 16 KiB likewise.
  */
 typedef struct {
   void* k; /* device */

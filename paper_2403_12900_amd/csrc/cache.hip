@@ -115,9 +115,6 @@ spr_status rows_call(spr_cache_ops* o, const char* what, const spr_kv4_view* kv,
   return e == hipSuccess ? SPR_OK : hip_failed(o, what, e);
 }
 
-// Work-groups of a launch: its threads are counted in 32 bits.
-constexpr int64_t kMostGroups = (int64_t{1} << 24) - 1;
-
 // What a launch has to know of the pools; deep: 16-byte pieces of a thread.
 PageCopy page_copy(const spr_pages& p, int deep) {
   PageCopy c{};
@@ -287,9 +284,7 @@ spr_status spr_cache_fork(spr_cache_ops* o, const spr_pages* pages, int32_t n, c
     for (int g = 0; g <= f.groups; ++g) a.first[g] = static_cast<uint8_t>(f.first[g]);
     for (int g = 0; g < f.groups; ++g)
       a.part[g] = static_cast<int64_t>(f.source[f.first[g]]) * a.mb + f.len[f.first[g]] / spr::kKvBlock;
-    const int64_t items = static_cast<int64_t>(a.c.pools) * a.c.layers * a.c.chunks;
-    if (f.n + f.groups * items > kMostGroups) return bad_arg("cache_fork: the blocks are too large for one call");
-    k_cache_fork<<<static_cast<unsigned>(f.n + f.groups * items), 256, 0, o->st>>>(a);
+    k_cache_fork<<<static_cast<unsigned>(f.n + f.groups * page_items(*pages, kForkDeep)), 256, 0, o->st>>>(a);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SPR_OK : hip_failed(o, "cache_fork", e);
   });
@@ -307,9 +302,7 @@ spr_status spr_cache_move(spr_cache_ops* o, const spr_pages* pages, int32_t n, c
     a.c = page_copy(*pages, kMoveDeep);
     a.bt = pages->block_table;
     a.entries = static_cast<int64_t>(pages->n_slots) * pages->max_blocks;
-    const int64_t items = static_cast<int64_t>(a.c.pools) * a.c.layers * a.c.chunks;
-    const int64_t groups = (a.entries + kTableEntries - 1) / kTableEntries;
-    if (groups + std::min(n, kMoves) * items > kMostGroups) return bad_arg("cache_move: the blocks or the table are too large for one call");
+    const int64_t items = page_items(*pages, kMoveDeep), groups = table_groups(*pages);
     a.table_groups = static_cast<int>(groups);
     DeviceGuard dev(o->dev);
     if (dev.e != hipSuccess) return hip_failed(o, "cache_move", dev.e);

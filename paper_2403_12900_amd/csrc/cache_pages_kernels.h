@@ -20,8 +20,6 @@ struct PageCopy {
   int64_t block_bytes, layer_bytes;
 };
 
-constexpr int kForkDeep = 1, kMoveDeep = 4;  // pieces of a thread, all in flight; a chunk has 256 times as many
-
 // Work item w of a block: its chunk in some layer of some pool.
 struct PageItem {
   char* base;  // of block 0 of the layer
@@ -121,7 +119,6 @@ __global__ __launch_bounds__(256) void k_cache_fork(ForkArgs a) {
     __builtin_nontemporal_store(v, reinterpret_cast<page_piece_t*>(it.base + a.fresh[f] * a.c.block_bytes) + x);
 }
 
-constexpr int kMoves = 384;  // of one launch
 struct MoveArgs {
   PageCopy c;
   int32_t* bt;
@@ -130,8 +127,6 @@ struct MoveArgs {
   int src[kMoves], dst[kMoves];  // src ascending
 };
 static_assert(sizeof(MoveArgs) <= 3584, "kernel arguments");
-
-constexpr int kTableEntries = 1024;  // of one work-group
 
 // Work-groups: table_groups for the table's entries (each looked up among the
 // moved blocks), then the chunks of each moved block.  Bound by memory, at the

@@ -147,6 +147,22 @@ inline spr_status check_pages(const spr_pages* p, const char* what, std::string*
   return SPR_OK;
 }
 
+// Pieces of 16 bytes that a thread of a fork or a move copies, all in flight (a
+// work-group has 256 times as many, of one block in one layer of one pool), moves of
+// one launch, and table entries of one of its work-groups.
+constexpr int kForkDeep = 1, kMoveDeep = 4, kMoves = 384, kTableEntries = 1024;
+// Work-groups of a launch: its threads are counted in 32 bits.
+constexpr int64_t kMostGroups = (int64_t{1} << 24) - 1;
+
+// Work-groups that copy one block in every layer.
+inline int64_t page_items(const spr_pages& p, int deep) {
+  return (p.v != nullptr ? 2 : 1) * int64_t{p.n_layers} * ((p.block_bytes / 16 + 256 * deep - 1) / (256 * deep));
+}
+// Work-groups that look through the block table.
+inline int64_t table_groups(const spr_pages& p) {
+  return (static_cast<int64_t>(p.n_slots) * p.max_blocks + kTableEntries - 1) / kTableEntries;
+}
+
 // The forks of one call, those that copy the same block side by side.
 struct ForkPlan {
   int n = 0, groups = 0;
@@ -195,6 +211,7 @@ inline spr_status plan_fork(const spr_pages* p, int n, const int32_t* source, co
     f->fresh[k] = lens[i] % spr::kKvBlock == 0 ? -1 : fresh[i];
   }
   f->first[f->groups] = copies;
+  if (n + f->groups * page_items(*p, kForkDeep) > kMostGroups) return bad("the blocks are too large for one call");
   return SPR_OK;
 }
 
@@ -207,6 +224,8 @@ inline spr_status plan_move(const spr_pages* p, int n, const int32_t* src, const
   };
   if (src == nullptr || dst == nullptr) return bad("src and dst must not be null");
   if (n < 1 || n > p->n_blocks) return bad("n must be in [1, n_blocks]");
+  if (table_groups(*p) + std::min(n, kMoves) * page_items(*p, kMoveDeep) > kMostGroups)
+    return bad("the blocks or the table are too large for one call");
   moves->resize(n);
   std::vector<int32_t> d(dst, dst + n);
   for (int i = 0; i < n; ++i) {

@@ -254,6 +254,33 @@ def test_forks_of_one_block_are_grouped():
         assert len(set(keys)) == groups
 
 
+@pytest.mark.parametrize("both", [False, True])
+def test_work_groups_of_a_launch_are_limited(both):
+    """The largest calls that the header allows, and the next ones: a fork's pieces of 4 KiB, a move's of 16 and its table."""
+    L, most = host(), 2 ** 24 - 1
+    out, v = np.zeros(2000, np.int32), 8192 if both else None
+    fork = lambda p, n, lens: L.sprh_fork(ctypes.byref(p), n, p32(a32([0] * n)), p32(a32(range(1, n + 1))), p32(a32(lens)), p32(a32(range(n))), p32(out))  # noqa: E731
+    move = lambda p, n: L.sprh_move(ctypes.byref(p), n, p32(a32(range(n))), p32(a32(range(n, 2 * n))), p32(out))  # noqa: E731
+    pools = 2 if both else 1
+    for size, pieces in ((4096, 1), (4112, 2), (1088, 1), (2 ** 30, 2 ** 18)):
+        layers = (most - 1) // (pools * pieces)  # beside the one table row
+        assert fork(pages(v=v, block_bytes=size, n_layers=layers), 1, [5]) == 0
+        assert fork(pages(v=v, block_bytes=size, n_layers=layers + 1), 1, [16]) == 0  # nothing to copy
+        refused(L, fork(pages(v=v, block_bytes=size, n_layers=layers + 1), 1, [5]), "too large")
+    layers = (most - 3) // (2 * pools)
+    assert fork(pages(v=v, block_bytes=4096, n_layers=layers), 3, [5, 6, 17]) == 0  # three forks of two blocks
+    refused(L, fork(pages(v=v, block_bytes=4096, n_layers=layers + 1), 3, [5, 6, 17]), "too large")
+    for size, pieces in ((16384, 1), (16400, 2), (1088, 1), (2 ** 30, 2 ** 16)):
+        layers = (most - 1) // (pools * pieces)  # beside the table of 40 entries
+        assert move(pages(v=v, block_bytes=size, n_layers=layers), 1) == 0
+        refused(L, move(pages(v=v, block_bytes=size, n_layers=layers + 1), 1), "too large")
+    layers = (most - 1) // (384 * pools)
+    assert move(pages(v=v, block_bytes=1024, n_layers=layers, n_blocks=2000), 900) == 0
+    refused(L, move(pages(v=v, block_bytes=1024, n_layers=layers + 1, n_blocks=2000), 900), "too large")
+    assert move(pages(v=v, n_slots=1024, max_blocks=most - 2 * pools), 1) == 0
+    refused(L, move(pages(v=v, n_slots=1024, max_blocks=most - 2 * pools + 1), 1), "too large")
+
+
 @pytest.mark.parametrize("n,src,dst,what", [
     (0, [0], [1], "n must"), (41, list(range(41)), [0] * 41, "n must"), (1, None, [1], "null"), (1, [0], None, "null"),
     (1, [40], [1], "out of range"), (1, [-1], [1], "out of range"), (1, [0], [40], "out of range"), (1, [0], [-7], "out of range"),
