@@ -8,6 +8,7 @@
 #include "cache_rule.h"
 #include "host_state.h"
 #include "launch_rule.h"
+#include "cache_bits.h"
 #include "tree_exp.h"
 #include "tree_rule.h"
 
@@ -221,6 +222,16 @@ int sprh_move(const spr_pages* p, int n, const int32_t* src, const int32_t* dst,
     out[n + i] = m[i].second;
   }
   return SPR_OK;
+}
+
+// out[i] = {bytes of the four bits masks[i], NaN bits of scales[i], odd_scales, beyond_f16}.
+void sprh_cache_bits(const uint32_t* words, const uint32_t* scales, const uint32_t* masks, uint32_t* out, int n) {
+  for (int i = 0; i < n; ++i, out += 4) {
+    out[0] = sprk::byte_mask(masks[i]);
+    out[1] = sprk::nan_bits(scales[i]);
+    out[2] = sprk::odd_scales(scales[i]);
+    out[3] = sprk::beyond_f16(words[i], scales[i]);
+  }
 }
 
 void sprh_exp_neg(const double* x, double* y, int n) {

@@ -328,6 +328,30 @@ def test_work_items_of_an_attention_launch():
             assert ns.max() <= 64 and int(item0[-1]) * Hkv * cw * (hd + 4) <= floats and groups * Hkv <= counters
 
 
+def test_masks_of_code_and_scale_bytes():
+    """Position by position.  Values are not exact in fp16 where a position's scale is out of 2^-18 .. 2^13 and one of its two
+    codes is not zero, or where it is NaN: a position of zeros (scale 2^-120) beside others is."""
+    rng = np.random.default_rng(11)
+    L, n = host(), 200000
+    scales = rng.choice([0, 7, 108, 109, 110, 127, 140, 141, 252, 255], (n, 4), p=[.05, .2, .05, .1, .1, .1, .1, .1, .1, .1]).astype(np.uint8)
+    scales[:n // 4] = rng.integers(0, 256, (n // 4, 4))
+    scales[-n // 4:][rng.random((n // 4, 4)) < 0.8] = 120
+    words = rng.choice([0x00, 0x80, 0x08, 0x88, 0x01, 0x10, 0x7F, 0xF7, 0x40], (n, 4)).astype(np.uint8)
+    words[scales == 7] &= 0x88
+    bits = rng.integers(0, 16, n).astype(np.uint32)
+    out = np.zeros((n, 4), np.uint32)
+    u = lambda a: ctypes.c_void_p(np.ascontiguousarray(a).ctypes.data)  # noqa: E731
+    w, s = (np.ascontiguousarray(x).view("<u4").reshape(-1) for x in (words, scales))
+    L.sprh_cache_bits(u(w), u(s), u(bits), u(out), n)
+    assert np.array_equal(out[:, 0], ((bits[:, None] >> np.arange(4) & 1) * 255 << 8 * np.arange(4)).sum(1))
+    assert np.array_equal(out[:, 1], ((scales == 255) << np.arange(4)).sum(1))
+    odd = (scales < 109) | (scales > 140)
+    assert np.array_equal(out[:, 2] != 0, odd.any(1))
+    assert np.array_equal(out[:, 3] != 0, (odd & (words & 0x77 != 0) | (scales == 255)).any(1))
+    zero = (scales == 7).any(1) & ~(odd & (scales != 7)).any(1)
+    assert zero.sum() > 1000 and not out[zero, 3].any()
+
+
 # ------------------------------------------------------------------------------------------------ the Python surface
 
 

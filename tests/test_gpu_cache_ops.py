@@ -466,6 +466,26 @@ def test_attention_of_fp32_small_probabilities(ops, H, Hkv, hd, rows):
 
 
 @pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("hd", [64, 128])
+@HEADS
+def test_attention_of_values_that_are_zero(ops, H, Hkv, hd, io):
+    """Positions, and groups of some, whose values are zeros (of the lowest scale), whole blocks of them too."""
+    rng = np.random.default_rng(hd)
+    n = 300 if Hkv == 2 else 60
+    for rows in (1, 50, 100):
+        cache = filled(rng, 1, 0, Hkv, hd, [0], [n], [rows])
+        q, qx = rounded(rng.standard_normal((rows, H, hd)), io)
+        k, v = (rng.standard_normal((n + rows, Hkv, hd)) for _ in range(2))
+        v[rng.random(n + rows) < 0.3] = 0
+        v[16:48], v[::3, :, 32:64] = 0, -0.0
+        cache.append(0, 0, 0, k, v)
+        want = ref.attention(cache, 0, [0], [n], [rows], qx)
+        got = ops.attention(cache.device(), 0, CacheBatch([0], [n], [rows]), q).double().cpu().numpy()
+        tol = tolerance(cache, 0, [0], [n], [rows], qx, io, want)
+        assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
+
+
+@pytest.mark.parametrize("io", [F32, BF16])
 @pytest.mark.parametrize("scale", [2.0 ** -60, 2.0 ** -20, 2.0 ** 20, 2.0 ** 90])
 @HEADS
 def test_attention_of_values_far_from_one(ops, H, Hkv, io, scale):
