@@ -2,7 +2,7 @@
 spr_cache_attention, spr_cache_fork and spr_cache_move.
 
 Argument marshalling only, as in tree.py: shapes, types and devices are checked here, all other checks are the library's.
-Inference only: inputs that want gradients are refused.
+Inference only: tensors that want gradients or carry tangents are refused.
 """
 from __future__ import annotations
 
@@ -84,7 +84,7 @@ class CacheOps(OpHandle):
         dtype = _DTYPES.get(x.dtype)
         if x.dim() != 3 or dtype is None:
             _refuse("cache rotary: x must be [rows, heads, head_dim], fp32 or bf16")
-        self._no_grad("cache rotary", x)
+        self._no_grad("cache rotary", x, x if out is None else out)
         rows, heads, hd = x.shape
         p_positions = self._vector("cache rotary: positions", positions, torch.int32, rows)
         xs = self._row_stride("cache rotary", x, heads, hd)
@@ -100,8 +100,7 @@ class CacheOps(OpHandle):
         shape, dtype = (batch.rows, kv.n_kv_heads, kv.head_dim), _DTYPES.get(k.dtype)
         if k.shape != shape or v.shape != shape or dtype is None or v.dtype != k.dtype:
             _refuse("cache append: k and v must be [rows, kv_heads, head_dim] of one type, fp32 or bf16")
-        self._no_grad("cache append", k)
-        self._no_grad("cache append", v)
+        self._no_grad("cache append", k, v)
         ks = self._row_stride("cache append", k, shape[1], shape[2])
         vs = self._row_stride("cache append", v, shape[1], shape[2])
         self._same_device("cache append", kv)
@@ -129,7 +128,7 @@ class CacheOps(OpHandle):
         hd, dtype = kv.head_dim, _DTYPES.get(q.dtype)
         if q.dim() != 3 or q.shape[0] != batch.rows or q.shape[2] != hd or dtype is None:
             _refuse("cache attention: q must be [rows, heads, head_dim], fp32 or bf16")
-        self._no_grad("cache attention", q)
+        self._no_grad("cache attention", q, q if out is None else out)
         heads = q.shape[1]
         qs = self._row_stride("cache attention", q, heads, hd)
         out, os = self._out("cache attention", q, out, heads, hd)
@@ -174,8 +173,10 @@ class CacheOps(OpHandle):
 
     def _pages(self, what, kv):
         self._same_device(what, kv)
-        if not isinstance(kv, KV4View) and kv.of_model:
-            _refuse(f"{what}: a model's own cache: its slots own its blocks")
+        if not isinstance(kv, KV4View):
+            self._no_grad(what, kv.k, kv.v)
+            if kv.of_model:
+                _refuse(f"{what}: a model's own cache: its slots own its blocks")
         ref = getattr(kv, "_pages", None)
         if ref is None:  # as lasting as the view's own record
             k, v = (kv.data, None) if isinstance(kv, KV4View) else (kv.k, kv.v)
@@ -192,10 +193,6 @@ class CacheOps(OpHandle):
     def _same_device(self, what, kv):
         if kv.index != self.index:
             _refuse(f"{what}: the cache must be on {self.device}")
-
-    def _no_grad(self, what, x):
-        if x.requires_grad and torch.is_grad_enabled():
-            _refuse(f"{what}: it has no gradient; detach its inputs, or call it under torch.no_grad()")
 
     def _out(self, what, x, out, heads, hd):
         """The output, a new one like x if none is given, and its row stride."""

@@ -12,6 +12,7 @@ from typing import Optional, Sequence
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 from .binding import (KV_BLOCK, SPR_BF16, SPR_ERR_INVALID_ARG, SPR_F32, SproutError, SprKvView, SprTreeBatch, _check, _ptr,
                       load_library)
@@ -149,6 +150,14 @@ class OpHandle:
             _refuse(f"{what} must be a contiguous {dtype} tensor of {n} elements on {self.device}")
         return t.data_ptr()
 
+    def _no_grad(self, what, *tensors):
+        """Refuses what autograd would follow: tensors that want gradients, or carry a tangent."""
+        if forward_ad._current_level >= 0 and any(forward_ad.unpack_dual(x).tangent is not None for x in tensors):
+            _refuse(f"{what}: it has no gradient; detach its inputs, which carry a tangent")
+        for x in tensors:
+            if x.requires_grad and torch.is_grad_enabled():
+                _refuse(f"{what}: it has no gradient; detach its inputs, or call it under torch.no_grad()")
+
     def close(self):
         if getattr(self, "h", None) is not None and self.h.value:
             self._entry("release")(self.h)
@@ -174,8 +183,7 @@ class TreeOps(OpHandle):
         if q.dim() != 3 or q.shape[0] != batch.rows or q.shape[2] != hd or q.dtype not in _DTYPES:
             _refuse("tree attention: q must be [rows, heads, head_dim], fp32 or bf16")
         rows, heads, _ = q.shape
-        if (q.requires_grad or kv.k.requires_grad or kv.v.requires_grad) and torch.is_grad_enabled():
-            _refuse("tree attention: it has no gradient; detach its inputs, or call it under torch.no_grad()")
+        self._no_grad("tree attention", q, kv.k, kv.v, q if out is None else out)
         if out is None:
             out = q.new_empty(rows, heads, hd)
         elif out.shape != q.shape or out.dtype != q.dtype:

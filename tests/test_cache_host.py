@@ -452,6 +452,40 @@ def test_tensors_that_do_not_fit_are_refused():
     assert o.lib.calls == 4
 
 
+def test_tensors_that_autograd_follows_are_refused():
+    """None of the operators has a derivative: tangents of its inputs, and gradients of what it writes to, would be lost in
+    silence."""
+    import torch.autograd.forward_ad as fw
+    o, b, v, r = host_ops(), CacheBatch([0], [5], [3]), cpu_view(), Rotary(64)
+    q, k, pos = torch.zeros(3, 4, 64), torch.zeros(3, 2, 64), torch.zeros(3, dtype=torch.int32)
+    pool, table = torch.zeros(1, 4, 2, 1024), torch.zeros(2, 2, dtype=torch.int32)
+    lists = ([0], [1], [5], [2])
+    over = [(lambda x: o.attention(v, 0, b, x), q), (lambda x: o.attention(v, 0, b, q, out=x), q), (lambda x: o.rotary(r, x, pos), q),
+            (lambda x: o.rotary(r, q, pos, out=x), q), (lambda x: o.append(v, 0, b, x, k), k), (lambda x: o.append(v, 0, b, k, x), k),
+            (lambda x: o.fork(KVView(x, pool, table), *lists), pool), (lambda x: o.fork(KVView(pool, x, table), *lists), pool),
+            (lambda x: o.move(KVView(x, pool, table), [0], [1]), pool), (lambda x: o.move(KVView(pool, x, table), [0], [1]), pool)]
+    for i, (call, x) in enumerate(over):
+        calls = o.lib.calls
+        leaf = x.clone().requires_grad_()
+        with pytest.raises(SproutError, match="gradient") as e:
+            call(leaf)
+        assert e.value.status == binding.SPR_ERR_INVALID_ARG
+        with pytest.raises(SproutError, match="gradient"):
+            call(leaf * 2)
+        with fw.dual_level():
+            dual = fw.make_dual(x.clone(), torch.ones_like(x))
+            for t in (dual, dual * 2):
+                with pytest.raises(SproutError, match="tangent"):
+                    call(t)
+            assert o.lib.calls == calls
+            call(dual.detach()), call(x)
+        with torch.no_grad():
+            call(leaf)
+        assert o.lib.calls == calls + 3
+    with pytest.raises(Exception):
+        torch.func.jvp(lambda x: o.rotary(r, x, pos), (q,), (torch.ones_like(q),))
+
+
 def test_any_paged_cache_can_be_forked_and_moved():
     o = host_ops()
     table = torch.zeros(2, 2, dtype=torch.int32)

@@ -72,6 +72,25 @@ def test_attention_refuses_tensors_that_want_gradients():
     assert o.lib.calls == 2 + len(calls)
 
 
+def test_attention_refuses_tangents_and_outputs_that_want_gradients():
+    from torch.autograd import forward_ad
+
+    from paper_2403_12900_amd.tree import KVView
+    k, table = torch.zeros(1, 2, 2, 1024), torch.zeros(1, 2, dtype=torch.int32)
+    b, q, o = TreeBatch([0], [4], [2], [-1, 0]), torch.zeros(2, 4, 64), host_ops()
+    with pytest.raises(SproutError, match="gradient"):
+        o.attention(KVView(k, k, table), 0, b, q, out=q.clone().requires_grad_())
+    with forward_ad.dual_level():
+        dual = lambda t: forward_ad.make_dual(t.clone(), torch.ones_like(t))  # noqa: E731
+        for call in (lambda: o.attention(KVView(k, k, table), 0, b, dual(q)), lambda: o.attention(KVView(dual(k), k, table), 0, b, q),
+                     lambda: o.attention(KVView(k, dual(k), table), 0, b, q), lambda: o.attention(KVView(k, k, table), 0, b, q, out=dual(q))):
+            with pytest.raises(SproutError, match="tangent"):
+                call()
+        assert o.lib.calls == 0
+        o.attention(KVView(k, k, table), 0, b, dual(q).detach())
+    assert o.lib.calls == 1
+
+
 def test_rows_that_overlap():
     """The rule that attention's q and out go by, against the sets of bytes themselves."""
     import ctypes
