@@ -96,6 +96,20 @@ def test_rotary_far_positions_and_long_contexts(ops, layout):
             check_rotary(ops, rng, 5, hd, dims, layout, F32, positions, scaling)
 
 
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+def test_rotary_positions_of_31_bits(ops, layout):
+    """The angle is off by its stored frequency's and its product's roundings, (8 * 2^-52 + 2^-53) of it, which turns a pair
+    by as much; then the output rounds once."""
+    rng = np.random.default_rng(13)
+    positions = np.concatenate([[2 ** 31 - 1, -2 ** 31, 10 ** 9, 2 ** 30], rng.integers(2 ** 21, 2 ** 31, 20)])
+    for hd, dims, scaling in ((128, 128, {}), (64, 40, dict(base=500000.0, factor=8.0, original=8192, low=1.0, high=4.0))):
+        x, want = rounded(rng.standard_normal((len(positions), 3, hd)), F32)
+        exact = ref.turn(want, positions, dims, layout, **scaling)
+        got = ops.rotary(Rotary(dims, layout=layout, **scaling), x, torch.from_numpy(positions.astype(np.int32)).cuda())
+        angle = np.abs(positions)[:, None, None] * 17 * 2.0 ** -53  # (the quickest frequency is 1)
+        assert (np.abs(got.double().cpu().numpy() - exact) <= EPS * np.abs(exact) + angle * 1.5 * np.abs(want).max()).all()
+
+
 @pytest.mark.parametrize("io", [F32, BF16])
 @pytest.mark.parametrize("hd,dims", [(64, 64), (128, 90), (128, 128), (64, 6)])
 def test_rotary_strides_and_in_place(ops, hd, dims, io):
