@@ -303,10 +303,24 @@ template <class IO, int HD>
 __device__ __forceinline__ void query_operand(const CacheAttnArgs& a, const TreeColumn& col, int c, int g, uint4* out) {
   const typename IO::elem* src =
       static_cast<const typename IO::elem*>(a.q) + col.row * a.qs + col.hq * HD + HD / 4 * g + 8 * c;
-  QueryPiece p{};
-  p.x = *reinterpret_cast<const uint4*>(src);
-  if constexpr (!IO::kRaw) p.y = *reinterpret_cast<const uint4*>(src + 4);
-  query_parts<BF16, IO>(p, out);
+  const uint4 x = *reinterpret_cast<const uint4*>(src);
+  if constexpr (IO::kRaw) {
+    out[0] = x;
+  } else {
+    // The first part is cut, not rounded (which would take the largest numbers to
+    // infinity): 16 bits are left, of which the second takes 8 and the third the rest.
+    const uint4 y = *reinterpret_cast<const uint4*>(src + 4);
+    const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    uint32_t first[4];
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) first[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], 0x07060302u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]) - __uint_as_float(w[j] & 0xFFFF0000u);
+    out[0] = make_uint4(first[0], first[1], first[2], first[3]);
+#pragma unroll
+    for (int q = 1; q < CacheParts<IO>::q; ++q) out[q] = next_part<BF16>(v);
+  }
 }
 
 // Scores of a step whose keys lie in registers, before their scale.  q(jt, c,

@@ -580,6 +580,33 @@ def test_attention_queries_that_are_no_numbers(ops, H, Hkv, io):
         assert np.isnan(got[bad]).all() and (np.abs(got - want)[~bad] <= tol[~bad]).all()
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@HEADS
+def test_attention_of_the_largest_queries(ops, H, Hkv, hd):
+    """Finite fp32 queries beyond bf16's largest number, whose scores are ordinary: their keys have the lowest scale.
+
+    A score's roundings are below (hd + 4) eps of the sum of its products' magnitudes."""
+    rng = np.random.default_rng(hd)
+    top = float(np.finfo(np.float32).max)
+    n = 300 if Hkv == 2 else 60
+    for rows in (1, 50, 100):
+        T = n + rows
+        q = rng.standard_normal((rows, H, hd))
+        q[..., 0] = rng.choice([-1, 1], (rows, H)) * top * rng.choice([1, 1 - 2.0 ** -23, 0.999, 0.9], (rows, H))
+        k, v = (rng.standard_normal((T, Hkv, hd)) for _ in range(2))
+        k[..., :32] = 0
+        k[..., 0] = rng.integers(-2, 3, (T, Hkv)) * 2.0 ** -121
+        q, qx = rounded(q, F32)
+        cache = ref.Cache(rng, 1, Hkv, hd, [T])
+        cache.append(0, 0, 0, k, v)
+        want = ref.attention(cache, 0, [0], [n], [rows], qx)
+        got = ops.attention(cache.device(), 0, CacheBatch([0], [n], [rows]), q).double().cpu().numpy()
+        kx, vx = cache.rows(0, 0, T)
+        size = (np.abs(qx).max((0, 1)) * np.abs(kx).max((0, 1))).sum() / np.sqrt(hd)
+        tol = (2 * (hd + 4) * EPS * size + (2 * size + 26 + 8 * np.sqrt(T)) * EPS + 2.0 ** -22) * np.abs(vx).max()
+        assert (np.abs(got - want) <= tol).all(), np.abs(got - want).max() / tol
+
+
 @pytest.mark.parametrize("rows", [1, 70, 2100])
 def test_attention_far_into_a_large_pool(ops, rows):
     """Blocks behind byte 2^32 of the pool and of the layer."""
