@@ -643,7 +643,8 @@ spr_status spr_cache_read(spr_cache_ops* ops, const spr_kv4_view* kv, int32_t la
  *   dtype    of q and out; scores and sums are held in fp32.  Probabilities enter
  *            their product with the values to 2^-11 of themselves for bf16
  *            outputs and to 2^-22 for fp32 ones, small ones to 2^-32 and 2^-36
- *            of the row's largest
+ *            of the row's largest.  The sums are up to 2^8 times their values:
+ *            values beyond 2^120 over the number of positions may overflow
  *   q, out   device [rows] x [n_heads * head_dim], aligned as in
  *            spr_cache_rotary.  out must not overlap q.
  */
@@ -694,7 +695,8 @@ spr_status spr_cache_fork(spr_cache_ops* ops, const spr_pages* pages, int32_t n,
  * Moves block src[i] to dst[i] in every layer, and every table entry that is
  * src[i] to dst[i] (compaction, say).  What src[i] holds stays there.
  *   n         1..n_blocks
- *   src, dst  host [n]: blocks of the pool, distinct, and no dst is a src
+ *   src, dst  host [n]: blocks of the pool, distinct, and no dst is a src (what
+ *             dst[i] holds is lost: that it is free is the caller's to see to)
  */
 spr_status spr_cache_move(spr_cache_ops* ops, const spr_pages* pages, int32_t n, const int32_t* src, const int32_t* dst);
 

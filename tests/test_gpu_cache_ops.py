@@ -580,6 +580,23 @@ def test_attention_queries_that_are_no_numbers(ops, H, Hkv, io):
         assert np.isnan(got[bad]).all() and (np.abs(got - want)[~bad] <= tol[~bad]).all()
 
 
+@pytest.mark.parametrize("io", [F32, BF16])
+@pytest.mark.parametrize("lens,rows", [([20, 0], [1, 3]), ([3000], [2]), ([30], [40]), ([700], [100])])
+@HEADS
+def test_attention_into_columns_of_a_wider_tensor(ops, H, Hkv, lens, rows, io):
+    """The same bits as into a tensor of its own, and nothing beside them, in rows before and behind either."""
+    rng = np.random.default_rng(sum(lens))
+    cache = filled(rng, 1, 0, Hkv, 64, list(range(len(lens))), lens, rows)
+    q, _ = rounded(rng.standard_normal((sum(rows), H, 64)), io)
+    view, batch, R = cache.device(), CacheBatch(list(range(len(lens))), lens, rows), sum(rows)
+    want = ops.attention(view, 0, batch, q)
+    wide = torch.full((R + 4, H + 3, 64), 7.0, dtype=io, device="cuda")
+    out = wide[2:2 + R, 1:1 + H]
+    assert ops.attention(view, 0, batch, q, out=out) is out and torch.equal(out, want)
+    out.fill_(7.0)
+    assert (wide == 7.0).all()
+
+
 @pytest.mark.parametrize("hd", [64, 128])
 @HEADS
 def test_attention_of_the_largest_queries(ops, H, Hkv, hd):
