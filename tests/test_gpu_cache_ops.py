@@ -12,8 +12,10 @@ Tolerances of the rest, derived (eps = 2^-24, half a step of fp32; half a step o
       a change of at most ds in every score changes the weighted mean of v by at most 2 ds max|v|;
     - exp2 (1 ulp, and its argument's rounding: |s log2 e| <= 2^5 here, 2^5 eps ln 2 < 24 eps), the sums over T positions
       (4 sqrt(T) eps, on numerator and denominator) and the merges add (26 + 8 sqrt(T)) eps max|v|;
-    - fp32 outputs: probabilities enter their product to 2^-22 of themselves, which moves the mean by at most 2^-22 max|v|;
-    - bf16 outputs: probabilities enter it to 2^-12 of themselves, and the output's own rounding is 2^-8 of it.
+    - fp32 outputs: probabilities enter their product, and their sum, to 2^-22 of themselves, which moves the mean by at most
+      2^-22 of the mean distance of v from it, no more than max|v|;
+    - bf16 outputs: they enter it to 2^-11 of themselves (2 * 2^-12 below), and the output's own rounding is 2^-8 of it;
+    - small probabilities are off by 2^-36 (fp32) or 2^-32 (bf16) of the largest: all T of them below the sums' 8 sqrt(T) eps.
 """
 import ctypes
 
